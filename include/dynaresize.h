@@ -525,6 +525,93 @@ int dr_shard_range(uint64_t flat_elems, uint32_t world, uint32_t rank, uint64_t*
                    uint64_t* shard_elems);
 
 /*
+ * Computing with the rollout arena: the linear layers a rollout (or training) GPU runs on the weights that
+ * dr_reshard has just written (the paper has no counterpart; it hands the weights to a rollout engine).
+ *
+ * dr_quant_rows -- activations to fp8 e4m3 with one fp32 scale per row and 128 columns, by the rule of the
+ * weights' block scaling above: per row and block of 128 columns amax = max |v| (NaNs skipped), stored
+ * scale = amax / 448 held inside [2^-126, FLT_MAX], code = e4m3(v / scale): one fp32 division rounded to
+ * nearest, then nearest even onto the e4m3 grid, saturating at 448, NaN -> 0x7F.
+ *   x_dev     : DR_BF16 or DR_F32, row r at x + r * ldx elements
+ *   form      : DR_ROWS_PLAIN   v = x[r, c]                       (a row of x has cols elements)
+ *               DR_ROWS_SWIGLU  v = silu(x[r, c]) * x[r, cols + c] (2 * cols elements: gate, then up; the order of the
+ *                               rows of gate_up and w13), computed in fp32 and rounded nowhere else
+ *   row_index : NULL: output row r is source row r.  Otherwise rows int64 indices (device): output row r is
+ *               source row row_index[r] (the dispatch of tokens to experts); an index outside [0, src_rows)
+ *               gives a row of zeros
+ *   codes_dev : rows x cols bytes, row r at codes + r * ld_codes
+ *   scales_dev: fp32, scale of row r and column block b at scales[b * ld_scales + r] (ld_scales >= rows:
+ *               the scales of one column block lie side by side, as dr_linear_forward reads them)
+ * Asynchronous on cuda_stream, allocates nothing, may be captured.  rows = 0 does nothing.
+ * Errors (before launch): DR_ERR_INVALID, DR_ERR_UNSUPPORTED (x_dtype, form, dimension above 2^31 - 1),
+ * DR_ERR_ALIGN (a pointer off its element size), DR_ERR_CUDA.  16-byte aligned bases and rows take the vector path,
+ * others an element-wise one, same result.
+ */
+enum { DR_ROWS_PLAIN = 0, DR_ROWS_SWIGLU = 1 };
+int dr_quant_rows(const void* x_dev, uint32_t x_dtype, uint64_t ldx, uint64_t src_rows, const int64_t* row_index_dev,
+                  uint32_t form, uint64_t rows, uint64_t cols, void* codes_dev, uint64_t ld_codes, float* scales_dev,
+                  uint64_t ld_scales, void* cuda_stream);
+
+/*
+ * A linear weight on the device, in the form a rollout arena holds it: n_groups matrices [out_features,
+ * in_features] stacked into one [n_groups * out_features, in_features], row-major, row r at
+ * weight + r * weight_ld elements.  n_groups = 1: a dense layer (qkv, o, gate_up, down); n_groups = E: the
+ * experts of w13 or w2.  dtype DR_BF16, or DR_FP8_E4M3_B128 with the block scales of the stacked matrix:
+ * scale of element (r, c) at scale[(r / 128) * scale_ld + c / 128] (a block may span two experts' rows).
+ * The handle keeps pointers: it owns no weight, and the arena may be rewritten (dr_reshard) behind it.
+ */
+typedef struct dr_linear_desc {
+    uint32_t struct_size, dtype;         /* sizeof(dr_linear_desc); DR_BF16 or DR_FP8_E4M3_B128            */
+    uint32_t n_groups, pad;              /* >= 1                                                           */
+    uint64_t out_features, in_features;  /* of one group                                                   */
+    const void* weight_dev;
+    uint64_t weight_bytes, weight_ld;    /* bytes behind weight_dev; elements between rows, 0: in_features */
+    const float* scale_dev;              /* fp8: block scales; NULL for bf16                               */
+    uint64_t scale_bytes, scale_ld;      /* floats between scale rows, 0: ceil(in_features / 128)          */
+} dr_linear_desc;
+typedef struct dr_linear dr_linear;
+
+/* Checks the descriptor and records it for the current device.  Errors: DR_ERR_INVALID, DR_ERR_UNSUPPORTED
+ * (dtype; a dimension above 2^31 - 1), DR_ERR_SIZE (weight_bytes / scale_bytes too small), DR_ERR_ALIGN (a pointer off its
+ * element size), DR_ERR_NOMEM, DR_ERR_CUDA. */
+int dr_linear_create(const dr_linear_desc* desc, dr_linear** out);
+int dr_linear_destroy(dr_linear* lin); /* NULL is accepted; launches already enqueued may still run */
+
+/*
+ * dr_linear_forward -- y[r, n] = sum_k x[r, k] W_e[n, k] for every row r of group e.
+ *   rows, offsets_dev : offsets_dev holds n_groups + 1 int32 on the device, ascending: group e owns rows
+ *               [offsets[e], offsets[e + 1]) of x and y, none where the two are equal.  Rows that no group owns
+ *               are neither read nor written.  Values are clamped to [0, rows] and a descending pair is an empty group,
+ *               so no offsets lead outside the buffers; groups that overlap leave the shared rows unspecified.
+ *               n_groups = 1: offsets_dev may be NULL (all rows).
+ *   bf16 layer: x is bf16, x_scale_dev NULL; fp32 accumulation over the whole contraction.
+ *   fp8 layer : x and x_scale are dr_quant_rows' codes and scales (ld_scale floats between column blocks):
+ *               y[r, n] = sum over blocks b of 128 columns of fl32(xs[b, r] * ws[n / 128, b]) * (sum over the block of
+ *               value(xq) * value(wq)), products exact, sums in fp32.
+ *   y_dtype   : DR_BF16 (one rounding to nearest even) or DR_F32; row r at y + r * ldy elements.
+ * dr_linear_dgrad -- dx[r, k] = sum_n dy[r, n] W_e[n, k]; bf16 layers only, dy bf16, dx DR_BF16 or DR_F32.
+ * dr_linear_wgrad -- dW_e[n, k] = sum over rows r of group e of dy[r, n] x[r, k], fp32, laid out as the weight
+ *               ([n_groups * out_features] rows of lddw floats: the positions of the same tensor in the arena of a DR_F32
+ *               plan, from where dr_reshard_inverse takes it to the flat gradient buffer).  accumulate = 0: dW is written,
+ *               zeros for a group without rows; 1: the sum is added to it.  bf16 layers only.
+ * Rows of other groups never enter a sum, whatever they hold (infinities and NaNs included).  Sums are taken in a fixed order:
+ * the same call gives the same bits.  The calls only enqueue kernels on cuda_stream, allocate nothing, read no
+ * device value on the host, and leave the handle unmodified: concurrent calls on different streams are allowed, and
+ * (after one ordinary call has loaded the module) they may be captured into a CUDA graph.  rows = 0 does
+ * nothing (dr_linear_wgrad without accumulate: writes zeros).
+ * Errors (before launch): DR_ERR_INVALID (NULL, a leading dimension below the row's length, missing offsets or
+ * scales, scales for a bf16 layer), DR_ERR_UNSUPPORTED (dtype, fp8 gradients, dimensions above 2^31 - 1), DR_ERR_ALIGN (a
+ * pointer off its element size), DR_ERR_STATE (another current device), DR_ERR_CUDA.
+ */
+int dr_linear_forward(const dr_linear* lin, const void* x_dev, uint64_t ldx, const float* x_scale_dev, uint64_t ld_scale,
+                      uint64_t rows, const int32_t* offsets_dev, void* y_dev, uint64_t ldy, uint32_t y_dtype,
+                      void* cuda_stream);
+int dr_linear_dgrad(const dr_linear* lin, const void* dy_dev, uint64_t lddy, uint64_t rows, const int32_t* offsets_dev,
+                    void* dx_dev, uint64_t lddx, uint32_t dx_dtype, void* cuda_stream);
+int dr_linear_wgrad(const dr_linear* lin, const void* x_dev, uint64_t ldx, const void* dy_dev, uint64_t lddy, uint64_t rows,
+                    const int32_t* offsets_dev, float* dw_dev, uint64_t lddw, uint32_t accumulate, void* cuda_stream);
+
+/*
  * Hysteresis-guided reconfiguration (Sec. 3.4; host only, no CUDA).  The controller only decides WHEN to
  * move between pre-specified topologies, listed from most-Training to most-Rollout (e.g. 6:2, 5:3, 4:4).
  * Per step: imbalance = (t_rollout - t_train) / max(t_rollout, t_train).  A step signals "towards

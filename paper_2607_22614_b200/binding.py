@@ -22,7 +22,8 @@ DR_STAGE_DIR_OUT, DR_STAGE_DIR_IN = 0, 1
 
 EXPORTS = ["dr_plan_create", "dr_plan_create_host", "dr_plan_window_host", "dr_plan_query", "dr_plan_tensor", "dr_plan_segment",
            "dr_reshard", "dr_reshard_inverse", "dr_plan_group", "dr_reshard_groups", "dr_reshard_static", "dr_plan_ranges", "dr_reshard_push", "dr_reshard_stream", "dr_shard_range", "dr_stage_out", "dr_stage_in", "dr_stage_begin", "dr_stage_wait_buffer", "dr_stage_poll", "dr_stage_end", "dr_plan_destroy", "dr_strerror",
-           "dr_last_error", "dr_probe_stream", "dr_host_copy", "dr_diag_bulk_wait_failures", "dr_diag_bulk_starve", "dr_ctl_create", "dr_ctl_observe", "dr_ctl_break_even", "dr_ctl_destroy"]
+           "dr_last_error", "dr_probe_stream", "dr_host_copy", "dr_diag_bulk_wait_failures", "dr_diag_bulk_starve", "dr_ctl_create", "dr_ctl_observe", "dr_ctl_break_even", "dr_ctl_destroy",
+           "dr_quant_rows", "dr_linear_create", "dr_linear_destroy", "dr_linear_forward", "dr_linear_dgrad", "dr_linear_wgrad"]
 
 u8, u32, u64, i64, vp = C.c_uint8, C.c_uint32, C.c_uint64, C.c_int64, C.c_void_p
 
@@ -99,6 +100,12 @@ class dr_ctl_config(C.Structure):
                 ("cooldown_steps", u32), ("enter_threshold", C.c_double), ("exit_threshold", C.c_double)]
 
 
+class dr_linear_desc(C.Structure):
+    _fields_ = [("struct_size", u32), ("dtype", u32), ("n_groups", u32), ("pad", u32), ("out_features", u64),
+                ("in_features", u64), ("weight_dev", vp), ("weight_bytes", u64), ("weight_ld", u64), ("scale_dev", vp),
+                ("scale_bytes", u64), ("scale_ld", u64)]
+
+
 class DrError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -147,6 +154,12 @@ def lib() -> C.CDLL:
         L.dr_ctl_observe.argtypes = [vp, C.c_double, C.c_double, P(C.c_int32), P(u32)]
         L.dr_ctl_break_even.argtypes = [C.c_double, C.c_double, C.c_double, P(C.c_double)]
         L.dr_ctl_destroy.argtypes = [vp]
+        L.dr_quant_rows.argtypes = [vp, u32, u64, u64, vp, u32, u64, u64, vp, u64, vp, u64, vp]
+        L.dr_linear_create.argtypes = [P(dr_linear_desc), P(vp)]
+        L.dr_linear_destroy.argtypes = [vp]
+        L.dr_linear_forward.argtypes = [vp, vp, u64, vp, u64, u64, vp, vp, u64, u32, vp]
+        L.dr_linear_dgrad.argtypes = [vp, vp, u64, u64, vp, vp, u64, u32, vp]
+        L.dr_linear_wgrad.argtypes = [vp, vp, u64, vp, u64, u64, vp, vp, u64, u32, vp]
         for n in EXPORTS:
             getattr(L, n).restype = C.c_int
         L.dr_strerror.argtypes = [C.c_int]
@@ -390,6 +403,36 @@ def dr_ctl_destroy(ctl):
     return lib().dr_ctl_destroy(ctl)
 
 
+DR_ROWS_PLAIN, DR_ROWS_SWIGLU = 0, 1
+
+
+def dr_quant_rows(x_dev, x_dtype, ldx, src_rows, row_index_dev, form, rows, cols, codes_dev, ld_codes, scales_dev, ld_scales,
+                  cuda_stream):
+    return lib().dr_quant_rows(x_dev, x_dtype, ldx, src_rows, row_index_dev, form, rows, cols, codes_dev, ld_codes,
+                               scales_dev, ld_scales, cuda_stream)
+
+
+def dr_linear_create(desc):
+    h = vp()
+    return lib().dr_linear_create(C.byref(desc), C.byref(h)), h
+
+
+def dr_linear_destroy(lin):
+    return lib().dr_linear_destroy(lin)
+
+
+def dr_linear_forward(lin, x_dev, ldx, x_scale_dev, ld_scale, rows, offsets_dev, y_dev, ldy, y_dtype, cuda_stream):
+    return lib().dr_linear_forward(lin, x_dev, ldx, x_scale_dev, ld_scale, rows, offsets_dev, y_dev, ldy, y_dtype, cuda_stream)
+
+
+def dr_linear_dgrad(lin, dy_dev, lddy, rows, offsets_dev, dx_dev, lddx, dx_dtype, cuda_stream):
+    return lib().dr_linear_dgrad(lin, dy_dev, lddy, rows, offsets_dev, dx_dev, lddx, dx_dtype, cuda_stream)
+
+
+def dr_linear_wgrad(lin, x_dev, ldx, dy_dev, lddy, rows, offsets_dev, dw_dev, lddw, accumulate, cuda_stream):
+    return lib().dr_linear_wgrad(lin, x_dev, ldx, dy_dev, lddy, rows, offsets_dev, dw_dev, lddw, accumulate, cuda_stream)
+
+
 def dr_plan_destroy(plan):
     return lib().dr_plan_destroy(plan)
 
@@ -449,6 +492,7 @@ class Plan:
         rc, self.info = dr_plan_query(self.handle)
         if rc:
             raise DrError(rc, "dr_plan_query")
+        self.experts = spec.get("n_experts", 0) // max(1, moe_ep)  # held by this rank
 
     def window(self, src_elem_lo, src_elem_hi):
         """Host-only plan for the source window [lo, hi) (what one chunk of the streamed repack covers)."""
@@ -457,6 +501,7 @@ class Plan:
             raise DrError(rc, "dr_plan_window_host")
         w = Plan.__new__(Plan)
         w.handle = h
+        w.experts = self.experts
         rc, w.info = dr_plan_query(h)
         return w
 
@@ -486,6 +531,25 @@ class Plan:
         return out
 
     _stream = staticmethod(_current_stream)
+
+    def linear(self, arena, name, n_groups=None):
+        """The Linear layer over rollout tensor `name` ("layers.0.qkv", "layers.3.w13", ...) of `arena` (a uint8 CUDA
+        tensor that dr_reshard writes).  n_groups: experts stacked in w13 / w2; taken from the plan when it is None."""
+        import torch
+        t = next((t for t in self.tensors() if t.name.decode() == name), None)
+        if t is None:
+            raise KeyError(f"the plan has no rollout tensor {name!r}")
+        if t.elem_size == 4:
+            raise TypeError("a linear layer needs bf16 or fp8 weights")
+        if n_groups is None:
+            n_groups = max(1, self.experts) if name.rsplit(".", 1)[-1] in ("w13", "w2") else 1
+
+        def part(off, rows, cols, dtype, size):
+            return arena[off:off + rows * cols * size].view(dtype).view(rows, cols)
+
+        w = part(t.arena_off, t.rows, t.cols, torch.float8_e4m3fn if t.quantised else torch.bfloat16, t.elem_size)
+        s = part(t.scale_off, t.scale_rows, t.scale_cols, torch.float32, 4) if t.quantised else None
+        return Linear(w, s, n_groups=n_groups)
 
     def reshard(self, src, dst, stream=None):
         """src: CUDA tensor holding the flat fp32 buffer; dst: CUDA tensor holding the rollout arena."""
@@ -551,3 +615,171 @@ class Plan:
         if rc:
             raise DrError(rc, "dr_stage_begin")
         return StageJob(job, desc)
+
+
+def _matrix(t, what):
+    if t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] > 1):
+        raise ValueError(f"{what} must be a matrix with contiguous rows")
+    if not t.is_cuda:
+        raise ValueError(f"{what} must be a CUDA tensor")
+    return t
+
+
+def _ld(t):
+    """Elements between rows (torch gives any stride to a matrix of one row)."""
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def _code_of(t, what):
+    import torch
+    code = {torch.bfloat16: DR_BF16, torch.float32: DR_F32}.get(t.dtype)
+    if code is None:
+        raise TypeError(f"{what} must be bfloat16 or float32, not {t.dtype}")
+    return code
+
+
+def quant_rows(x, codes=None, scales=None, *, row_index=None, swiglu=False, stream=None):
+    """dr_quant_rows: x [source rows, cols] (2 * cols with swiglu: gate, then up; bf16 or fp32) -> (codes [rows, cols],
+    scales [ceil(cols / 128), rows]).  row_index (int64) gathers rows.  Outputs that are not given are allocated."""
+    import torch
+    _matrix(x, "x")
+    cols = x.shape[1] // 2 if swiglu else x.shape[1]
+    if swiglu and x.shape[1] % 2:
+        raise ValueError("x holds gate and up side by side: its column count must be even")
+    if row_index is None:
+        rows = x.shape[0]
+    else:
+        if row_index.dtype != torch.int64 or row_index.dim() != 1 or not row_index.is_contiguous() or not row_index.is_cuda:
+            raise ValueError("row_index must be a contiguous int64 CUDA vector")
+        rows = row_index.shape[0]
+    if codes is None:
+        codes = torch.empty(rows, cols, dtype=torch.float8_e4m3fn, device=x.device)
+    if scales is None:
+        scales = torch.empty(-(-cols // 128), rows, dtype=torch.float32, device=x.device)
+    _matrix(codes, "codes")
+    _matrix(scales, "scales")
+    if codes.element_size() != 1 or codes.shape[0] != rows or codes.shape[1] != cols:
+        raise ValueError(f"codes must be {rows} x {cols} bytes")
+    if scales.dtype != torch.float32 or scales.shape[0] != -(-cols // 128) or scales.shape[1] != rows:
+        raise ValueError(f"scales must be fp32, {-(-cols // 128)} x {rows}")
+    rc = dr_quant_rows(x.data_ptr(), _code_of(x, "x"), _ld(x), x.shape[0], None if row_index is None else row_index.data_ptr(),
+                       DR_ROWS_SWIGLU if swiglu else DR_ROWS_PLAIN, rows, cols, codes.data_ptr(), _ld(codes),
+                       scales.data_ptr(), _ld(scales), _current_stream(stream))
+    if rc:
+        raise DrError(rc, "dr_quant_rows")
+    return codes, scales
+
+
+class Linear:
+    """Owns one ``dr_linear``: a weight [n_groups * out, in] (bf16, or e4m3 codes with `scale`, one fp32 per 128 x 128
+    block of the stacked matrix), its products and, for bf16, its gradients.  Keeps references to both tensors."""
+
+    def __init__(self, weight, scale=None, n_groups=1):
+        import torch
+        _matrix(weight, "weight")
+        fp8 = weight.element_size() == 1
+        if not fp8 and weight.dtype != torch.bfloat16:
+            raise TypeError(f"weight must be bfloat16 or e4m3 codes, not {weight.dtype}")
+        if n_groups < 1 or weight.shape[0] % n_groups:
+            raise ValueError("n_groups must divide the weight's rows")
+        if scale is not None:
+            _matrix(scale, "scale")
+            if scale.dtype != torch.float32 or scale.shape[0] != -(-weight.shape[0] // 128) or \
+                    scale.shape[1] != -(-weight.shape[1] // 128):
+                raise ValueError("scale must be fp32 with one value for each 128 x 128 block of the weight")
+        self.weight, self.scale, self.n_groups, self.fp8 = weight, scale, n_groups, fp8
+        self.out_features, self.in_features = weight.shape[0] // n_groups, weight.shape[1]
+
+        def span(t):
+            return ((t.shape[0] - 1) * _ld(t) + t.shape[1]) * t.element_size()
+
+        desc = dr_linear_desc(struct_size=C.sizeof(dr_linear_desc), dtype=DR_FP8_E4M3_B128 if fp8 else DR_BF16,
+                              n_groups=n_groups, out_features=self.out_features, in_features=self.in_features,
+                              weight_dev=weight.data_ptr(), weight_bytes=span(weight), weight_ld=_ld(weight),
+                              scale_dev=None if scale is None else scale.data_ptr(),
+                              scale_bytes=0 if scale is None else span(scale), scale_ld=0 if scale is None else _ld(scale))
+        rc, self.handle = dr_linear_create(desc)
+        if rc:
+            self.handle = None
+            raise DrError(rc, "dr_linear_create")
+
+    def close(self):
+        if getattr(self, "handle", None):
+            dr_linear_destroy(self.handle)
+            self.handle = None
+
+    __del__ = close
+
+    def _operand(self, t, cols, what, fp8=False):
+        import torch
+        _matrix(t, what)
+        if t.shape[1] != cols:
+            raise ValueError(f"{what} must have {cols} columns")
+        if t.element_size() != 1 if fp8 else t.dtype != torch.bfloat16:
+            raise TypeError(f"{what} has the wrong type: {t.dtype}")
+        return t
+
+    def _offsets(self, offsets):
+        import torch
+        if offsets is None:
+            return None
+        if offsets.dtype != torch.int32 or not offsets.is_contiguous() or offsets.numel() != self.n_groups + 1 or \
+                not offsets.is_cuda:
+            raise ValueError(f"offsets must be {self.n_groups + 1} int32 on the GPU")
+        return offsets.data_ptr()
+
+    def _out(self, out, rows, cols, dtype, device, what):
+        import torch
+        if out is None:
+            return torch.empty(rows, cols, dtype=dtype or torch.bfloat16, device=device)
+        _matrix(out, what)
+        if out.shape[0] != rows or out.shape[1] != cols:
+            raise ValueError(f"{what} must be {rows} x {cols}")
+        return out
+
+    def forward(self, x, x_scale=None, offsets=None, out=None, out_dtype=None, stream=None):
+        """dr_linear_forward: y = x W^T, for rows sorted by group where `offsets` (n_groups + 1, int32) is given.  An fp8
+        layer takes quant_rows' codes and scales.  Rows of an allocated output that no group owns are not initialised."""
+        self._operand(x, self.in_features, "x", self.fp8)
+        y = self._out(out, x.shape[0], self.out_features, out_dtype, x.device, "out")
+        ps = lds = None
+        if x_scale is not None:
+            _matrix(x_scale, "x_scale")
+            if x_scale.element_size() != 4 or x_scale.shape[0] != -(-self.in_features // 128) or x_scale.shape[1] < x.shape[0]:
+                raise ValueError("x_scale must be fp32, one row for each block of 128 columns, one column for each row of x")
+            ps, lds = x_scale.data_ptr(), _ld(x_scale)
+        rc = dr_linear_forward(self.handle, x.data_ptr(), _ld(x), ps, lds or 0, x.shape[0], self._offsets(offsets),
+                               y.data_ptr(), _ld(y), _code_of(y, "out"), _current_stream(stream))
+        if rc:
+            raise DrError(rc, "dr_linear_forward")
+        return y
+
+    __call__ = forward
+
+    def dgrad(self, dy, offsets=None, out=None, out_dtype=None, stream=None):
+        """dr_linear_dgrad: the gradient of x, dy W."""
+        self._operand(dy, self.out_features, "dy")
+        dx = self._out(out, dy.shape[0], self.in_features, out_dtype, dy.device, "out")
+        rc = dr_linear_dgrad(self.handle, dy.data_ptr(), _ld(dy), dy.shape[0], self._offsets(offsets), dx.data_ptr(), _ld(dx),
+                             _code_of(dx, "out"), _current_stream(stream))
+        if rc:
+            raise DrError(rc, "dr_linear_dgrad")
+        return dx
+
+    def wgrad(self, x, dy, offsets=None, out=None, accumulate=False, stream=None):
+        """dr_linear_wgrad: the gradient of the weight in fp32, dy^T x group by group; accumulate adds it to `out`."""
+        import torch
+        self._operand(x, self.in_features, "x")
+        self._operand(dy, self.out_features, "dy")
+        if x.shape[0] != dy.shape[0]:
+            raise ValueError("x and dy must have the same rows")
+        if accumulate and out is None:
+            raise ValueError("accumulate adds to `out`: give one")
+        dw = self._out(out, self.weight.shape[0], self.in_features, torch.float32, x.device, "out")
+        if dw.dtype != torch.float32:
+            raise TypeError("the gradient of the weight is fp32")
+        rc = dr_linear_wgrad(self.handle, x.data_ptr(), _ld(x), dy.data_ptr(), _ld(dy), x.shape[0], self._offsets(offsets),
+                             dw.data_ptr(), _ld(dw), int(accumulate), _current_stream(stream))
+        if rc:
+            raise DrError(rc, "dr_linear_wgrad")
+        return dw

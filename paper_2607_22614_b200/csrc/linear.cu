@@ -1,0 +1,204 @@
+// Entry points of the linear layers: argument checks, the handle, choice of kernel.
+#include "linear.h"
+
+#include <new>
+
+using namespace dr;
+
+namespace {
+
+constexpr uint64_t kMaxDim = 0x7FFFFFFFull;
+
+int check_layer(const dr_linear* lin)
+{
+    if (!lin) {
+        set_error("NULL layer");
+        return DR_ERR_INVALID;
+    }
+    int dev = -1;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev != lin->device) {
+        set_error("current device differs from the layer's device");
+        return DR_ERR_STATE;
+    }
+    return DR_OK;
+}
+
+// Rows, offsets, and the two row-major operands every product has.
+int check_rows(const dr_linear* lin, uint64_t rows, const int32_t* offsets, const void* p, uint64_t ldp, uint64_t p_cols,
+               uint32_t p_es, const void* q, uint64_t ldq, uint64_t q_cols, uint32_t q_es)
+{
+    if (rows > kMaxDim) {
+        set_error("more than 2^31 - 1 rows");
+        return DR_ERR_UNSUPPORTED;
+    }
+    if (!offsets && lin->d.n_groups != 1) {
+        set_error("a layer of %u groups needs offsets", lin->d.n_groups);
+        return DR_ERR_INVALID;
+    }
+    if (rows && (!p || !q)) {
+        set_error("NULL buffer");
+        return DR_ERR_INVALID;
+    }
+    if (ldp < p_cols || ldq < q_cols) {
+        set_error("leading dimension below the row's length");
+        return DR_ERR_INVALID;
+    }
+    if ((uintptr_t)p % p_es || (uintptr_t)q % q_es || (uintptr_t)offsets % 4) {
+        set_error("a pointer is not aligned to its element size");
+        return DR_ERR_ALIGN;
+    }
+    return DR_OK;
+}
+
+int check_out_dtype(uint32_t dtype)
+{
+    if (dtype != DR_BF16 && dtype != DR_F32) {
+        set_error("output must be DR_BF16 or DR_F32");
+        return DR_ERR_UNSUPPORTED;
+    }
+    return DR_OK;
+}
+
+int check_gradient(const dr_linear* lin)
+{
+    if (lin->fp8) {
+        set_error("gradients need a bf16 layer");
+        return DR_ERR_UNSUPPORTED;
+    }
+    return DR_OK;
+}
+
+int launch(const LinearCall& c) { return launch_linear_simt(c); }
+
+}  // namespace
+
+extern "C" {
+
+int dr_linear_create(const dr_linear_desc* desc, dr_linear** out)
+{
+    if (!out) {
+        set_error("NULL out");
+        return DR_ERR_INVALID;
+    }
+    *out = nullptr;
+    if (!desc || desc->struct_size != sizeof(dr_linear_desc)) {
+        set_error("NULL descriptor or struct_size mismatch");
+        return DR_ERR_INVALID;
+    }
+    if (desc->dtype != DR_BF16 && desc->dtype != DR_FP8_E4M3_B128) {
+        set_error("a layer's weight is DR_BF16 or DR_FP8_E4M3_B128");
+        return DR_ERR_UNSUPPORTED;
+    }
+    dr_linear_desc d = *desc;
+    const bool fp8 = d.dtype == DR_FP8_E4M3_B128;
+    if (!d.n_groups || !d.out_features || !d.in_features) {
+        set_error("zero layer dimension");
+        return DR_ERR_INVALID;
+    }
+    if (d.out_features > kMaxDim || d.in_features > kMaxDim || d.n_groups > kMaxDim || d.out_features * d.n_groups > kMaxDim) {
+        set_error("layer dimension above 2^31 - 1");
+        return DR_ERR_UNSUPPORTED;
+    }
+    const uint64_t rows = d.out_features * d.n_groups, sr = (rows + 127) / 128, sc = (d.in_features + 127) / 128;
+    if (!d.weight_ld) d.weight_ld = d.in_features;
+    if (!d.scale_ld) d.scale_ld = sc;
+    if (!d.weight_dev || (fp8 && !d.scale_dev) || (!fp8 && d.scale_dev)) {
+        set_error("NULL weight, fp8 without scales or bf16 with them");
+        return DR_ERR_INVALID;
+    }
+    if (d.weight_ld < d.in_features || (fp8 && d.scale_ld < sc) || d.weight_ld > (1ull << 40) || d.scale_ld > (1ull << 40)) {
+        set_error("leading dimension out of range");
+        return DR_ERR_INVALID;
+    }
+    const uint32_t es = fp8 ? 1 : 2;
+    if ((uintptr_t)d.weight_dev % es || (uintptr_t)d.scale_dev % 4) {
+        set_error("a pointer is not aligned to its element size");
+        return DR_ERR_ALIGN;
+    }
+    if (d.weight_bytes < ((rows - 1) * d.weight_ld + d.in_features) * es ||
+        (fp8 && d.scale_bytes < ((sr - 1) * d.scale_ld + sc) * 4)) {
+        set_error("weight or scales smaller than the layer");
+        return DR_ERR_SIZE;
+    }
+    int dev = -1;
+    DR_CUDA(cudaGetDevice(&dev));
+    dr_linear* lin = new (std::nothrow) dr_linear();
+    if (!lin) return DR_ERR_NOMEM;
+    lin->d = d;
+    lin->device = dev;
+    lin->fp8 = fp8;
+    *out = lin;
+    return DR_OK;
+}
+
+int dr_linear_destroy(dr_linear* lin)
+{
+    delete lin;
+    return DR_OK;
+}
+
+int dr_linear_forward(const dr_linear* lin, const void* x_dev, uint64_t ldx, const float* x_scale_dev, uint64_t ld_scale,
+                      uint64_t rows, const int32_t* offsets_dev, void* y_dev, uint64_t ldy, uint32_t y_dtype,
+                      void* cuda_stream)
+{
+    int rc = check_layer(lin);
+    if (rc == DR_OK) rc = check_out_dtype(y_dtype);
+    if (rc) return rc;
+    const dr_linear_desc& d = lin->d;
+    rc = check_rows(lin, rows, offsets_dev, x_dev, ldx, d.in_features, lin->fp8 ? 1 : 2, y_dev, ldy, d.out_features,
+                    y_dtype == DR_F32 ? 4 : 2);
+    if (rc) return rc;
+    if (lin->fp8 ? rows && (!x_scale_dev || ld_scale < rows) : x_scale_dev != nullptr) {
+        set_error("an fp8 layer needs x's scales (ld_scale >= rows), a bf16 layer takes none");
+        return DR_ERR_INVALID;
+    }
+    if ((uintptr_t)x_scale_dev % 4) {
+        set_error("a pointer is not aligned to its element size");
+        return DR_ERR_ALIGN;
+    }
+    if (rows == 0) return DR_OK;
+    LinearCall c{lin,  kForward, x_dev, d.weight_dev, ldx, d.weight_ld, x_scale_dev, ld_scale, (uint32_t)rows,
+                 offsets_dev, y_dev, ldy, y_dtype == DR_F32, false, (cudaStream_t)cuda_stream};
+    return launch(c);
+}
+
+int dr_linear_dgrad(const dr_linear* lin, const void* dy_dev, uint64_t lddy, uint64_t rows, const int32_t* offsets_dev,
+                    void* dx_dev, uint64_t lddx, uint32_t dx_dtype, void* cuda_stream)
+{
+    int rc = check_layer(lin);
+    if (rc == DR_OK) rc = check_gradient(lin);
+    if (rc == DR_OK) rc = check_out_dtype(dx_dtype);
+    if (rc) return rc;
+    const dr_linear_desc& d = lin->d;
+    rc = check_rows(lin, rows, offsets_dev, dy_dev, lddy, d.out_features, 2, dx_dev, lddx, d.in_features,
+                    dx_dtype == DR_F32 ? 4 : 2);
+    if (rc || rows == 0) return rc;
+    LinearCall c{lin,  kDgrad, dy_dev, d.weight_dev, lddy, d.weight_ld, nullptr, 0, (uint32_t)rows,
+                 offsets_dev, dx_dev, lddx, dx_dtype == DR_F32, false, (cudaStream_t)cuda_stream};
+    return launch(c);
+}
+
+int dr_linear_wgrad(const dr_linear* lin, const void* x_dev, uint64_t ldx, const void* dy_dev, uint64_t lddy, uint64_t rows,
+                    const int32_t* offsets_dev, float* dw_dev, uint64_t lddw, uint32_t accumulate, void* cuda_stream)
+{
+    int rc = check_layer(lin);
+    if (rc == DR_OK) rc = check_gradient(lin);
+    if (rc) return rc;
+    const dr_linear_desc& d = lin->d;
+    rc = check_rows(lin, rows, offsets_dev, x_dev, ldx, d.in_features, 2, dy_dev, lddy, d.out_features, 2);
+    if (rc) return rc;
+    if (!dw_dev || lddw < d.in_features || accumulate > 1) {
+        set_error("NULL dw, leading dimension below the row's length, or accumulate not 0 / 1");
+        return DR_ERR_INVALID;
+    }
+    if ((uintptr_t)dw_dev % 4) {
+        set_error("a pointer is not aligned to its element size");
+        return DR_ERR_ALIGN;
+    }
+    if (rows == 0 && accumulate) return DR_OK;
+    LinearCall c{lin,  kWgrad, dy_dev, x_dev, lddy, ldx, nullptr, 0, (uint32_t)rows,
+                 offsets_dev, dw_dev, lddw, true, accumulate != 0, (cudaStream_t)cuda_stream};
+    return launch(c);
+}
+
+}  // extern "C"
