@@ -612,6 +612,13 @@ int dr_linear_wgrad(const dr_linear* lin, const void* x_dev, uint64_t ldx, const
                     const int32_t* offsets_dev, float* dw_dev, uint64_t lddw, uint32_t accumulate, void* cuda_stream);
 
 /*
+ * dr_diag_linear_wait_failures -- diagnostic: the tensor-core kernels of the linear layers wait for their copies and products
+ * with a limit (2 s); a wait that runs out ends the kernel with its output incomplete and counts here.  *count = such
+ * events on the current device since the library was loaded; expected 0.  Synchronous.  DR_ERR_INVALID, DR_ERR_CUDA.
+ */
+int dr_diag_linear_wait_failures(uint64_t* count);
+
+/*
  * Hysteresis-guided reconfiguration (Sec. 3.4; host only, no CUDA).  The controller only decides WHEN to
  * move between pre-specified topologies, listed from most-Training to most-Rollout (e.g. 6:2, 5:3, 4:4).
  * Per step: imbalance = (t_rollout - t_train) / max(t_rollout, t_train).  A step signals "towards

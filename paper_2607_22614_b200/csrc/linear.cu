@@ -68,7 +68,12 @@ int check_gradient(const dr_linear* lin)
     return DR_OK;
 }
 
-int launch(const LinearCall& c) { return launch_linear_simt(c); }
+int launch(const LinearCall& c)
+{
+    // wgrad without rows only writes zeros, which needs no operand a tensor map could describe
+    if (c.rows && linear_tc_takes(c)) return launch_linear_tc(c);
+    return launch_linear_simt(c);
+}
 
 }  // namespace
 
@@ -121,14 +126,28 @@ int dr_linear_create(const dr_linear_desc* desc, dr_linear** out)
         return DR_ERR_SIZE;
     }
     int dev = -1;
+    int sms = 0;
     DR_CUDA(cudaGetDevice(&dev));
+    DR_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
+    const int rc = prepare_linear_tc();
+    if (rc) return rc;
     dr_linear* lin = new (std::nothrow) dr_linear();
     if (!lin) return DR_ERR_NOMEM;
     lin->d = d;
     lin->device = dev;
+    lin->sms = sms;
     lin->fp8 = fp8;
     *out = lin;
     return DR_OK;
+}
+
+int dr_diag_linear_wait_failures(uint64_t* count)
+{
+    if (!count) {
+        set_error("NULL argument");
+        return DR_ERR_INVALID;
+    }
+    return linear_wait_failures(count);
 }
 
 int dr_linear_destroy(dr_linear* lin)

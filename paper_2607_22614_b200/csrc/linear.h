@@ -7,6 +7,7 @@
 struct dr_linear {
     dr_linear_desc d{};  // strides filled in
     int device = -1;
+    int sms = 0;
     bool fp8 = false;
 };
 
@@ -33,6 +34,13 @@ struct LinearCall {
 };
 
 int launch_linear_simt(const LinearCall& c);  // linear_simt.cu: every stride and alignment
+
+// linear_tc.cu: tensor cores, for operands that tensor maps can read
+constexpr uint32_t kMaxTcGroups = 1024;     // groups whose tile counts fit a CTA's table
+bool linear_tc_takes(const LinearCall& c);
+int launch_linear_tc(const LinearCall& c);
+int prepare_linear_tc();                    // once per device
+int linear_wait_failures(uint64_t* out);    // bounded waits that ran out (expected: 0)
 
 // Rows [lo, hi) of group e, held inside [0, rows] and never descending, whatever the offsets hold.
 __device__ __forceinline__ void group_rows(const int32_t* offsets, uint32_t e, uint32_t rows, uint32_t& lo, uint32_t& hi)

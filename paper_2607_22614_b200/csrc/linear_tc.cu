@@ -1,0 +1,652 @@
+// Linear layers on the tensor cores: pairs of CTAs, 256 x 256 tiles, tcgen05 products fed by tensor-map copies.
+//
+// Every product is taken transposed: the weight's features (wgrad: the rows of dW) are the M side of the product, 128 to
+// each CTA of a pair, and the tokens its N side.  N is an operand of the instruction, so a ragged group costs 32-row
+// steps and not whole tiles: a group's rows are cut into equal tiles of at most 256.
+//
+//   forward  D[n, r] = sum_k W[n, k] x[r, k]      both operands contiguous along the contraction
+//   dgrad    D[k, r] = sum_n W[n, k] dy[r, n]     W contiguous along its outputs (MN-major)
+//   wgrad    D[n, k] = sum_r dy[r, n] x[r, k]     both MN-major, the contraction runs over a group's rows
+//
+// Roles of a CTA's 12 warps: 0 issues the copies of its half of the operands into a ring of six 32 KB stages; 1 (of the pair's
+// first CTA) issues the products of the pair; 2 multiplies the scales (fp8) or clears the rows of other groups from the last
+// stage (wgrad); 4-11 read the accumulators.  Accumulators take half of tensor memory each, two in turn, so that a tile is
+// written out while the next is computed.
+//
+// fp8: one product covers exactly one block of 128 of the contraction, after which its partial sums are scaled by
+// xs[b, r] * ws[n / 128, b] and added to fp32 sums in registers (128 a thread).  A CTA's 128 features are one scale block, so
+// ws is one number per block, and the products of the two scales, one per token, come through shared memory.  The accumulators are
+// read in the fragment layout of 8 x 8 blocks (a thread holds two tokens of four features): a thread then needs the
+// scales of a quarter of the tokens only, which keeps the shared-memory port free for the tensor cores, and two multiply-adds
+// share an instruction.
+//
+// Outputs leave through a 640-byte transpose per warp: eight tokens of 32 features, 64 contiguous bytes a row.
+#include <cudaTypedefs.h>
+
+#include "linear.h"
+#include "tc_ptx.cuh"
+
+namespace dr {
+namespace {
+
+using namespace tc;
+
+__device__ unsigned long long g_wait_failures;
+
+constexpr uint32_t kStages = 6, kStageBytes = 32768, kOperandBytes = 16384;
+constexpr uint32_t kThreads = 384, kEpilogueWarps = 8;
+constexpr uint32_t kTile = 256;          // features and tokens of a pair's tile
+constexpr uint32_t kScaleSlots = 4;
+constexpr uint32_t kScratchPitch = 80;   // bytes between tokens of the transpose: 16-byte units of eight rows fall on different banks
+constexpr uint32_t kBand = 16;           // token tiles a band of a large group holds
+
+struct Shared {
+    alignas(1024) uint8_t stage[kStages][kStageBytes];
+    alignas(16) uint8_t scratch[kEpilogueWarps][8 * kScratchPitch];
+    alignas(16) float scale[kScaleSlots][kTile];
+    uint64_t full[kStages], empty[kStages], landed[kStages];
+    uint64_t acc_full[2], acc_empty[2];
+    uint64_t scale_full[kScaleSlots], scale_empty[kScaleSlots];
+    uint32_t tmem, stop;
+    uint32_t tiles_before[kMaxTcGroups + 1];  // token tiles of the groups before
+};
+
+struct TcArgs {
+    const int32_t* offsets;
+    const float* a_scale;  // tokens' scales
+    const float* b_scale;  // the weight's
+    void* c;
+    uint64_t ld_as, ld_bs, ldc;
+    uint32_t rows, n_groups, n, k;
+    uint32_t feature_tiles, column_tiles;  // column_tiles: wgrad's tiles of in_features
+    uint32_t c_f32, accumulate, vector;
+};
+
+// One tile of a pair.
+struct Tile {
+    uint32_t e, row0, row_end;  // tokens [row0, row_end); wgrad: the group's rows
+    uint32_t feature;           // first of the pair's 256 outputs on the M side (forward: row of the stacked weight)
+    uint32_t col0;              // wgrad: first of its columns
+    uint32_t nt;                // N of the product, a multiple of 32
+    uint32_t steps;             // stages of the contraction
+};
+
+template <int OP, bool FP8>
+struct Walk {
+    static constexpr uint32_t kStep = FP8 ? 128 : 64;
+    uint32_t e = 0;
+
+    // Tile t of all, ascending t; false past the last.  A tile without features (fp8 groups that are not whole scale blocks
+    // have one tile fewer here and there) comes back with nt = 0.
+    __device__ __forceinline__ bool get(const TcArgs& a, const Shared& s, uint32_t t, Tile& o)
+    {
+        if constexpr (OP == kWgrad) {
+            const uint32_t per = a.feature_tiles * a.column_tiles;
+            o.e = t / per;
+            if (o.e >= a.n_groups) return false;
+            const uint32_t i = t - o.e * per;
+            group_rows(a.offsets, o.e, a.rows, o.row0, o.row_end);
+            o.feature = (i / a.column_tiles) * kTile;
+            o.col0 = (i % a.column_tiles) * kTile;
+            o.nt = min(kTile, (a.k - o.col0 + 31) / 32 * 32);
+            o.steps = (o.row_end - o.row0 + kStep - 1) / kStep;
+            return true;
+        } else {
+            while (e < a.n_groups && t >= s.tiles_before[e + 1] * a.feature_tiles) ++e;
+            if (e >= a.n_groups) return false;
+            uint32_t lo, hi;
+            group_rows(a.offsets, e, a.rows, lo, hi);
+            const uint32_t tiles = s.tiles_before[e + 1] - s.tiles_before[e];
+            uint32_t i = t - s.tiles_before[e] * a.feature_tiles;
+            // bands of kBand token tiles, all feature tiles of a band before the next, token tiles innermost
+            const uint32_t band = i / (kBand * a.feature_tiles);
+            const uint32_t in_band = min(kBand, tiles - band * kBand);
+            i -= band * kBand * a.feature_tiles;
+            const uint32_t f = i / in_band, m = band * kBand + i % in_band;
+            o.e = e;
+            o.nt = ((hi - lo + tiles - 1) / tiles + 31) / 32 * 32;
+            o.row0 = lo + m * o.nt;
+            o.row_end = min(hi, o.row0 + o.nt);
+            o.col0 = 0;
+            if (OP == kForward) {
+                const uint32_t first = e * a.n;
+                o.feature = (FP8 ? first / 128 * 128 : first) + f * kTile;
+                o.steps = (a.k + kStep - 1) / kStep;
+                if (o.feature >= first + a.n) o.nt = 0;
+            } else {
+                o.feature = f * kTile;
+                o.steps = (a.n + kStep - 1) / kStep;
+            }
+            if (o.row0 >= o.row_end) o.nt = 0;  // 32-row steps can leave a last tile without rows
+            return true;
+        }
+    }
+};
+
+// Eight tokens (columns c .. c + 7 of the tile) of the warp's 32 features: v[g][i] = token 2 (t % 4) + i of feature t / 4 + 8 g.
+// `f` is the warp's first feature among the outputs of a row of c, valid from f_lo to f_hi.
+__device__ __forceinline__ void store_tokens(const TcArgs& a, uint32_t scratch, uint32_t row, uint32_t row_end, int f, int f_hi,
+                                             const float (&v)[4][2])
+{
+    const uint32_t lane = threadIdx.x & 31;
+    if (a.vector) {
+        __syncwarp();
+        store_transposed(scratch + (lane & 7) * kScratchPitch + (lane >> 3) * 16, pack_bf16(v[0][0], v[0][1]),
+                         pack_bf16(v[1][0], v[1][1]), pack_bf16(v[2][0], v[2][1]), pack_bf16(v[3][0], v[3][1]));
+        __syncwarp();
+        const uint32_t r = row + (lane >> 2);
+        const int ff = f + (int)(lane & 3) * 8;
+        uint32_t w[4];
+        asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];"
+                     : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3])
+                     : "r"(scratch + (lane >> 2) * kScratchPitch + (lane & 3) * 16));
+        if (r < row_end && ff >= 0 && ff < f_hi)  // the outputs of a row are a multiple of eight here
+            *(uint4*)((uint16_t*)a.c + (uint64_t)r * a.ldc + ff) = make_uint4(w[0], w[1], w[2], w[3]);
+        return;
+    }
+#pragma unroll
+    for (int g = 0; g < 4; ++g)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const uint32_t r = row + 2 * (lane & 3) + i;
+            const int ff = f + (int)(lane >> 2) + 8 * g;
+            if (r >= row_end || ff < 0 || ff >= f_hi) continue;
+            if (a.c_f32)
+                ((float*)a.c)[(uint64_t)r * a.ldc + ff] = v[g][i];
+            else
+                ((uint16_t*)a.c)[(uint64_t)r * a.ldc + ff] = (uint16_t)pack_bf16(v[g][i], 0.0f);
+        }
+}
+
+// The same eight columns of dW: rows are the warp's 32 features.
+__device__ __forceinline__ void store_dw(const TcArgs& a, uint64_t row, uint32_t rows_left, uint32_t col, const float (&v)[4][2])
+{
+    const uint32_t lane = threadIdx.x & 31, c = col + 2 * (lane & 3);
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+        const uint32_t r = (lane >> 2) + 8 * g;
+        if (r >= rows_left || c >= a.k) continue;
+        float* p = (float*)a.c + (row + r) * a.ldc + c;
+        if (a.vector) {
+            float2 w = make_float2(v[g][0], v[g][1]);
+            if (a.accumulate) {
+                const float2 was = *(float2*)p;
+                w.x += was.x;
+                w.y += was.y;
+            }
+            *(float2*)p = w;
+        } else {
+            p[0] = a.accumulate ? p[0] + v[g][0] : v[g][0];
+            if (c + 1 < a.k) p[1] = a.accumulate ? p[1] + v[g][1] : v[g][1];
+        }
+    }
+}
+
+template <int OP, bool FP8>
+__device__ __forceinline__ void produce(const TcArgs& a, Shared& s, const CUtensorMap* map_a, const CUtensorMap* map_b)
+{
+    constexpr uint32_t kStep = Walk<OP, FP8>::kStep;
+    const uint32_t rank = cta_rank(), stages = smem_u32(s.stage), empty = smem_u32(s.empty);
+    // copies signal the first CTA of the pair, which issues the products; in wgrad their own CTA, which may have rows to clear
+    const uint32_t full = OP == kWgrad ? smem_u32(s.landed) : in_cta(smem_u32(s.full), 0);
+    uint32_t n = 0;
+    bool ok = true;
+    Walk<OP, FP8> walk;
+    Tile t;
+    for (uint32_t i = blockIdx.x >> 1; ok && walk.get(a, s, i, t); i += gridDim.x >> 1) {
+        if (t.nt == 0) continue;
+        const uint32_t half = t.nt / 2, feature = t.feature + rank * 128;
+        const uint32_t boxes = OP == kWgrad ? (half + 63) / 64 : (half + 31) / 32, box_bytes = OP == kWgrad ? 8192 : 4096;
+        const uint32_t bytes = kOperandBytes + boxes * box_bytes;
+        for (uint32_t l = 0; l < t.steps; ++l, ++n) {
+            const uint32_t st = n % kStages;
+            ok = bar_wait(empty + 8 * st, (n / kStages & 1) ^ 1, &s.stop, &g_wait_failures);
+            if (!ok) break;
+            const uint32_t at = stages + st * kStageBytes, bar = full + 8 * st;
+            if (OP == kWgrad)
+                bar_expect(bar, bytes);
+            else if (rank == 0)
+                bar_expect(smem_u32(s.full) + 8 * st, 2 * bytes);
+            if (OP == kForward) {
+                load_2d<true>(at, map_a, bar, l * kStep, feature);
+            } else if (OP == kDgrad) {
+                load_3d<true>(at, map_a, bar, feature, l * kStep, t.e);
+                load_3d<true>(at + 8192, map_a, bar, feature + 64, l * kStep, t.e);
+            } else {
+                load_2d<false>(at, map_a, bar, feature, t.row0 + l * kStep);
+                load_2d<false>(at + 8192, map_a, bar, feature + 64, t.row0 + l * kStep);
+            }
+            for (uint32_t b = 0; b < boxes; ++b) {
+                const uint32_t to = at + kOperandBytes + b * box_bytes;
+                if (OP == kWgrad)
+                    load_2d<false>(to, map_b, bar, t.col0 + rank * half + b * 64, t.row0 + l * kStep);
+                else
+                    load_2d<true>(to, map_b, bar, l * kStep, t.row0 + rank * half + b * 32);
+            }
+        }
+    }
+    // every stage given back before this CTA may end: no commit of the pair is still on its way here
+    for (uint32_t q = 0; q < kStages && q < n; ++q) {
+        const uint32_t m = n - 1 - q;
+        if (!bar_wait(empty + 8 * (m % kStages), m / kStages & 1, &s.stop, &g_wait_failures)) break;
+    }
+}
+
+template <int OP, bool FP8>
+__device__ __forceinline__ void multiply(const TcArgs& a, Shared& s)
+{
+    const uint32_t stages = smem_u32(s.stage), full = smem_u32(s.full), empty = smem_u32(s.empty);
+    const uint32_t acc_full = smem_u32(s.acc_full), acc_empty = smem_u32(s.acc_empty), tmem = s.tmem;
+    constexpr bool a_mn = OP != kForward, b_mn = OP == kWgrad;
+    uint32_t n = 0, acc = 0;
+    bool ok = true;
+    Walk<OP, FP8> walk;
+    Tile t;
+    for (uint32_t i = blockIdx.x >> 1; ok && walk.get(a, s, i, t); i += gridDim.x >> 1) {
+        if (t.nt == 0 || t.steps == 0) continue;
+        const uint32_t shape = shape_of(FP8, a_mn, b_mn, 256, t.nt);
+        for (uint32_t l = 0; l < t.steps; ++l, ++n) {
+            if (FP8 || l == 0) {
+                ok = bar_wait(acc_empty + 8 * (acc & 1), (acc >> 1 & 1) ^ 1, &s.stop, &g_wait_failures);
+                if (!ok) return;
+            }
+            const uint32_t st = n % kStages;
+            ok = bar_wait(full + 8 * st, n / kStages & 1, &s.stop, &g_wait_failures);
+            if (!ok) return;
+            fence_after();
+            const uint32_t at = stages + st * kStageBytes, d = tmem + (acc & 1) * kTile;
+#pragma unroll
+            for (uint32_t q = 0; q < 4; ++q) {
+                const uint64_t da = operand(at + q * (a_mn ? 2048 : 32), 8192);
+                const uint64_t db = operand(at + kOperandBytes + q * (b_mn ? 2048 : 32), 8192);
+                mma<2, FP8>(d, da, db, shape, FP8 ? q != 0 : (l | q) != 0);
+            }
+            commit<2>(empty + 8 * st);
+            if (FP8 || l + 1 == t.steps) commit<2>(acc_full + 8 * (acc++ & 1));
+        }
+    }
+}
+
+// fp8: the product of the two scales for every token of the tile, one block of the contraction after the other.
+__device__ __forceinline__ void scale_tokens(const TcArgs& a, Shared& s)
+{
+    const uint32_t lane = threadIdx.x & 31, rank = cta_rank();
+    const uint32_t full = smem_u32(s.scale_full), empty = smem_u32(s.scale_empty);
+    const uint32_t scale_rows = (a.n_groups * a.n + 127) / 128;
+    uint32_t n = 0;
+    Walk<kForward, true> walk;
+    Tile t;
+    for (uint32_t i = blockIdx.x >> 1; walk.get(a, s, i, t); i += gridDim.x >> 1) {
+        if (t.nt == 0) continue;
+        const uint32_t wr = min((t.feature + rank * 128) / 128, scale_rows - 1);
+        const float* ws = a.b_scale + (uint64_t)wr * a.ld_bs;
+        const float* xs = a.a_scale + t.row0 + lane;
+        const uint32_t left = t.row_end - t.row0;
+        float v[8], w;
+        auto fetch = [&](uint32_t l) {
+            w = ws[l];
+#pragma unroll
+            for (uint32_t j = 0; j < 8; ++j) v[j] = lane + 32 * j < left ? xs[l * a.ld_as + 32 * j] : 0.0f;
+        };
+        fetch(0);
+        for (uint32_t l = 0; l < t.steps; ++l, ++n) {
+            const uint32_t slot = n % kScaleSlots;
+            if (!__all_sync(0xFFFFFFFFu, bar_wait(empty + 8 * slot, (n / kScaleSlots & 1) ^ 1, &s.stop, &g_wait_failures))) return;
+#pragma unroll
+            for (uint32_t j = 0; j < 8; ++j) s.scale[slot][lane + 32 * j] = v[j] * w;
+            __syncwarp();
+            if (lane == 0) bar_arrive(full + 8 * slot);
+            if (l + 1 < t.steps) fetch(l + 1);
+        }
+    }
+}
+
+// wgrad: rows of the last stage that belong to the next group are cleared before the products read them (both operands: a zero
+// times the infinity of another group's row is not zero), then the stage is handed to the first CTA.
+__device__ __forceinline__ void clear_rows(const TcArgs& a, Shared& s)
+{
+    const uint32_t lane = threadIdx.x & 31, landed = smem_u32(s.landed), full = in_cta(smem_u32(s.full), 0);
+    uint32_t n = 0;
+    Walk<kWgrad, false> walk;
+    Tile t;
+    for (uint32_t i = blockIdx.x >> 1; walk.get(a, s, i, t); i += gridDim.x >> 1) {
+        const uint32_t panels = (t.nt / 2 + 63) / 64;
+        for (uint32_t l = 0; l < t.steps; ++l, ++n) {
+            const uint32_t st = n % kStages, valid = min(64u, t.row_end - t.row0 - l * 64);
+            if (!__all_sync(0xFFFFFFFFu, bar_wait(landed + 8 * st, n / kStages & 1, &s.stop, &g_wait_failures))) return;
+            if (valid < 64) {
+                for (uint32_t p = 0; p < 2 + panels; ++p) {  // operand A's two panels, then B's: 8 KB each, side by side
+                    uint8_t* panel = s.stage[st] + p * 8192;
+                    for (uint32_t o = valid * 128 + lane * 16; o < 8192; o += 512) *(uint4*)(panel + o) = make_uint4(0, 0, 0, 0);
+                }
+                fence_async();
+            }
+            __syncwarp();
+            if (lane == 0) bar_arrive_cluster(full + 8 * st);
+        }
+    }
+}
+
+template <int OP, bool FP8>
+__device__ __forceinline__ void write_out(const TcArgs& a, Shared& s)
+{
+    const uint32_t lane = threadIdx.x & 31, warp = (threadIdx.x >> 5) - 4, rank = cta_rank();
+    const uint32_t quarter = warp & 3, side = warp >> 2;
+    const uint32_t acc_full = smem_u32(s.acc_full), acc_empty = in_cta(smem_u32(s.acc_empty), 0);
+    const uint32_t scale_full = smem_u32(s.scale_full), scale_empty = smem_u32(s.scale_empty);
+    const uint32_t scratch = smem_u32(s.scratch[warp]);
+    const uint32_t tmem = s.tmem + (quarter * 32 << 16);
+    uint32_t acc = 0;
+    bool ok = true;
+    Walk<OP, FP8> walk;
+    Tile t;
+    for (uint32_t i = blockIdx.x >> 1; walk.get(a, s, i, t); i += gridDim.x >> 1) {
+        if (t.nt == 0) continue;
+        const uint32_t cols = t.nt / 2, col0 = side * cols;  // this warp's columns
+        const uint32_t feature = t.feature + rank * 128 + quarter * 32;
+        // in a row of c: forward counts features from the group's first weight row
+        const int f = OP == kForward ? (int)(feature - t.e * a.n) : (int)feature;
+        const int f_hi = OP == kDgrad ? (int)a.k : (int)a.n;
+        auto put = [&](uint32_t c, const float (&v)[4][2]) {  // columns col0 + c .. + 7
+            if (OP == kWgrad)
+                store_dw(a, (uint64_t)t.e * a.n + feature, feature < a.n ? a.n - feature : 0, t.col0 + col0 + c, v);
+            else
+                store_tokens(a, scratch, t.row0 + col0 + c, t.row_end, f, f_hi, v);
+        };
+        if (FP8) {
+            float sum[4][2][16];
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) sum[c][h][r] = 0.0f;
+            for (uint32_t l = 0; l < t.steps; ++l, ++acc) {
+                const uint32_t slot = acc % kScaleSlots;
+                ok = bar_wait(scale_full + 8 * slot, acc / kScaleSlots & 1, &s.stop, &g_wait_failures) &&
+                     bar_wait(acc_full + 8 * (acc & 1), acc >> 1 & 1, &s.stop, &g_wait_failures);
+                if (!__all_sync(0xFFFFFFFFu, ok)) return;
+                fence_after();
+                const uint32_t from = tmem + (acc & 1) * kTile + col0;
+                const float* sc = s.scale[slot] + col0 + 2 * (lane & 3);
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    if (c * 32 >= cols) break;
+                    float p[2][16];
+                    tmem_load_32x32(from + c * 32, p[0], p[1]);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const uint64_t two = *(const uint64_t*)(sc + c * 32 + j * 8);
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            fma2(sum[c][h][4 * j], sum[c][h][4 * j + 1], p[h][4 * j], p[h][4 * j + 1], two);
+                            fma2(sum[c][h][4 * j + 2], sum[c][h][4 * j + 3], p[h][4 * j + 2], p[h][4 * j + 3], two);
+                        }
+                    }
+                }
+                fence_before();
+                __syncwarp();
+                if (lane == 0) {
+                    bar_arrive_cluster(acc_empty + 8 * (acc & 1));
+                    bar_arrive(scale_empty + 8 * slot);
+                }
+            }
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    if (c * 32 + j * 8 >= cols) break;
+                    const float v[4][2] = {{sum[c][0][4 * j], sum[c][0][4 * j + 1]}, {sum[c][0][4 * j + 2], sum[c][0][4 * j + 3]},
+                                           {sum[c][1][4 * j], sum[c][1][4 * j + 1]}, {sum[c][1][4 * j + 2], sum[c][1][4 * j + 3]}};
+                    put(c * 32 + j * 8, v);
+                }
+        } else {
+            if (t.steps) {
+                ok = bar_wait(acc_full + 8 * (acc & 1), acc >> 1 & 1, &s.stop, &g_wait_failures);
+                if (!__all_sync(0xFFFFFFFFu, ok)) return;
+                fence_after();
+            }
+            for (uint32_t c = 0; c < cols; c += 32) {
+                float p[2][16];
+                if (t.steps) {
+                    tmem_load_32x32(tmem + (acc & 1) * kTile + col0 + c, p[0], p[1]);
+                } else {
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) p[0][r] = p[1][r] = 0.0f;  // dW of a group without rows
+                }
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    if (c + j * 8 >= cols) break;
+                    const float v[4][2] = {{p[0][4 * j], p[0][4 * j + 1]}, {p[0][4 * j + 2], p[0][4 * j + 3]},
+                                           {p[1][4 * j], p[1][4 * j + 1]}, {p[1][4 * j + 2], p[1][4 * j + 3]}};
+                    put(c + j * 8, v);
+                }
+            }
+            if (t.steps) {
+                fence_before();
+                __syncwarp();
+                if (lane == 0) bar_arrive_cluster(acc_empty + 8 * (acc & 1));
+                ++acc;
+            }
+        }
+    }
+}
+
+template <int OP, bool FP8>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
+    tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const TcArgs a)
+{
+    extern __shared__ uint8_t raw[];
+    Shared& s = *(Shared*)(raw + (-smem_u32(raw) & 1023));
+    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) {
+        prefetch_map(&map_a);
+        prefetch_map(&map_b);
+        for (uint32_t i = 0; i < kStages; ++i) {
+            bar_init(smem_u32(&s.full[i]), OP == kWgrad ? 2 : 1);
+            bar_init(smem_u32(&s.empty[i]), 1);
+            bar_init(smem_u32(&s.landed[i]), 1);
+        }
+        for (uint32_t i = 0; i < 2; ++i) {
+            bar_init(smem_u32(&s.acc_full[i]), 1);
+            bar_init(smem_u32(&s.acc_empty[i]), 2 * kEpilogueWarps);
+        }
+        for (uint32_t i = 0; i < kScaleSlots; ++i) {
+            bar_init(smem_u32(&s.scale_full[i]), 1);
+            bar_init(smem_u32(&s.scale_empty[i]), kEpilogueWarps);
+        }
+        s.stop = 0;
+        bar_init_fence();
+    }
+    if (warp == 1) tmem_alloc<2>(smem_u32(&s.tmem), 512);
+    if (warp == 2 && OP != kWgrad) {  // running sum of the groups' token tiles
+        uint32_t before = 0;
+        if (lane == 0) s.tiles_before[0] = 0;
+        for (uint32_t e0 = 0; e0 < a.n_groups; e0 += 32) {
+            uint32_t lo = 0, hi = 0;
+            if (e0 + lane < a.n_groups) group_rows(a.offsets, e0 + lane, a.rows, lo, hi);
+            uint32_t sum = (hi - lo + kTile - 1) / kTile;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const uint32_t up = __shfl_up_sync(0xFFFFFFFFu, sum, o);
+                if (lane >= (uint32_t)o) sum += up;
+            }
+            if (e0 + lane < a.n_groups) s.tiles_before[e0 + lane + 1] = before + sum;
+            before += __shfl_sync(0xFFFFFFFFu, sum, 31);
+        }
+    }
+    fence_before();
+    __syncthreads();
+    cluster_sync();
+    fence_after();
+
+    if (warp < 4) {
+        if (FP8) asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
+        if (warp == 0) {
+            if (lane == 0) produce<OP, FP8>(a, s, &map_a, &map_b);
+        } else if (warp == 1) {
+            if (lane == 0 && cta_rank() == 0) multiply<OP, FP8>(a, s);
+        } else if (warp == 2) {
+            if (FP8) scale_tokens(a, s);
+            if (OP == kWgrad) clear_rows(a, s);
+        }
+    } else {
+        if (FP8) asm volatile("setmaxnreg.inc.sync.aligned.u32 232;");
+        write_out<OP, FP8>(a, s);
+    }
+    __syncwarp();
+    if (*(volatile uint32_t*)&s.stop) {  // a wait ran out: let the copies and products in flight end before the memory is given back
+        const uint64_t since = now_ns();
+        while (now_ns() - since < 10000000ull) __nanosleep(1000);
+    }
+    fence_before();
+    __syncthreads();
+    cluster_sync();
+    fence_after();
+    if (warp == 1) tmem_free<2>(s.tmem, 512);
+}
+
+PFN_cuTensorMapEncodeTiled_v12000 encoder()
+{
+    static PFN_cuTensorMapEncodeTiled_v12000 fn = [] {
+        void* p = nullptr;
+        cudaDriverEntryPointQueryResult r;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &r) != cudaSuccess ||
+            r != cudaDriverEntryPointSuccess) {
+            cudaGetLastError();
+            p = nullptr;
+        }
+        return (PFN_cuTensorMapEncodeTiled_v12000)p;
+    }();
+    return fn;
+}
+
+// A map over rows of `ld` elements, `cols` of them valid, boxes of 128 bytes x box_rows; `groups` > 0 adds a third dimension
+// of `rows` rows each.
+int encode(CUtensorMap* map, const void* base, bool fp8, uint64_t cols, uint64_t rows, uint64_t groups, uint64_t ld, uint32_t box_rows)
+{
+    const uint32_t es = fp8 ? 1 : 2;
+    const cuuint64_t dims[3] = {cols, rows, groups};
+    const cuuint64_t strides[2] = {ld * es, rows * ld * es};
+    const cuuint32_t box[3] = {128 / es, box_rows, 1}, step[3] = {1, 1, 1};
+    PFN_cuTensorMapEncodeTiled_v12000 fn = encoder();
+    const CUresult r = fn ? fn(map, fp8 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, groups ? 3 : 2,
+                               (void*)base, dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                               CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE)
+                          : CUDA_ERROR_NOT_SUPPORTED;
+    if (r != CUDA_SUCCESS) {
+        set_error("tensor map: driver error %d", (int)r);
+        return DR_ERR_CUDA;
+    }
+    return DR_OK;
+}
+
+constexpr size_t kSharedBytes = sizeof(Shared) + 1024;
+
+// Once per device and kernel: shared memory, and the register count that the fp8 kernel's split relies on
+// (384 threads x 168 at launch cover 256 x 232 + 128 x 40).
+template <int OP, bool FP8>
+int prepare_kernel()
+{
+    cudaFuncAttributes at;
+    DR_CUDA(cudaFuncGetAttributes(&at, tc_kernel<OP, FP8>));
+    if (FP8 && at.numRegs * kThreads < 232 * 256 + 40 * 128) {
+        set_error("the fp8 linear kernel was built with %d registers a thread", at.numRegs);
+        return DR_ERR_CUDA;
+    }
+    DR_CUDA(cudaFuncSetAttribute(tc_kernel<OP, FP8>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSharedBytes));
+    return DR_OK;
+}
+
+template <int OP, bool FP8>
+int launch(const LinearCall& c, const CUtensorMap& ma, const CUtensorMap& mb, const TcArgs& a, uint64_t tiles)
+{
+    const uint64_t pairs = (uint64_t)c.lin->sms / 2;
+    const unsigned grid = 2 * (unsigned)(tiles < pairs ? tiles : pairs);
+    tc_kernel<OP, FP8><<<grid, kThreads, kSharedBytes, c.stream>>>(ma, mb, a);
+    cudaError_t err = cudaGetLastError();
+    if (err != cudaSuccess) {
+        set_error("linear kernel launch: %s", cudaGetErrorString(err));
+        return DR_ERR_CUDA;
+    }
+    return DR_OK;
+}
+
+}  // namespace
+
+int prepare_linear_tc()
+{
+    int rc = prepare_kernel<kForward, true>();
+    if (rc == DR_OK) rc = prepare_kernel<kForward, false>();
+    if (rc == DR_OK) rc = prepare_kernel<kDgrad, false>();
+    if (rc == DR_OK) rc = prepare_kernel<kWgrad, false>();
+    return rc;
+}
+
+bool linear_tc_takes(const LinearCall& c)
+{
+    const uint32_t es = c.lin->fp8 ? 1 : 2;
+    const uint64_t bits = (uintptr_t)c.a | (uintptr_t)c.b | c.lda * es | c.ldb * es;
+    return bits % 16 == 0 && c.lda * es < (1ull << 39) && c.ldb * es < (1ull << 39) && c.lin->d.n_groups <= kMaxTcGroups &&
+           c.lin->d.out_features * c.ldb * es < (1ull << 39);
+}
+
+int launch_linear_tc(const LinearCall& c)
+{
+    const dr_linear_desc& d = c.lin->d;
+    const bool fp8 = c.lin->fp8;
+    TcArgs a{};
+    a.offsets = c.offsets;
+    a.a_scale = c.a_scale;
+    a.b_scale = d.scale_dev;
+    a.c = c.c;
+    a.ld_as = c.ld_scale;
+    a.ld_bs = d.scale_ld;
+    a.ldc = c.ldc;
+    a.rows = c.rows;
+    a.n_groups = d.n_groups;
+    a.n = (uint32_t)d.out_features;
+    a.k = (uint32_t)d.in_features;
+    a.c_f32 = c.c_f32;
+    a.accumulate = c.accumulate;
+    CUtensorMap ma, mb;
+    int rc;
+    uint64_t tiles;
+    const uint64_t token_tiles = ((uint64_t)c.rows + kTile - 1) / kTile + (c.offsets ? d.n_groups : 0);
+    if (c.op == kWgrad) {
+        a.feature_tiles = (a.n + kTile - 1) / kTile;
+        a.column_tiles = (a.k + kTile - 1) / kTile;
+        tiles = (uint64_t)a.feature_tiles * a.column_tiles * a.n_groups;
+        a.vector = a.k % 2 == 0 && c.ldc % 2 == 0 && (uintptr_t)c.c % 8 == 0;
+        rc = encode(&ma, c.a, false, a.n, c.rows, 0, c.lda, 64);
+        if (rc == DR_OK) rc = encode(&mb, c.b, false, a.k, c.rows, 0, c.ldb, 64);
+    } else {
+        const uint32_t width = c.op == kForward ? a.n : a.k;
+        a.feature_tiles = (width + (fp8 && a.n % 128 ? 127 : 0) + kTile - 1) / kTile;
+        tiles = token_tiles * a.feature_tiles;
+        a.vector = !c.c_f32 && width % 8 == 0 && c.ldc % 8 == 0 && (uintptr_t)c.c % 16 == 0;
+        if (c.op == kForward)
+            rc = encode(&ma, c.b, fp8, a.k, (uint64_t)a.n * a.n_groups, 0, c.ldb, 128);
+        else
+            rc = encode(&ma, c.b, false, a.k, a.n, a.n_groups, c.ldb, 64);
+        if (rc == DR_OK) rc = encode(&mb, c.a, fp8, c.op == kForward ? a.k : a.n, c.rows, 0, c.lda, 32);
+    }
+    if (rc) return rc;
+    if (tiles > 0x7FFFFFFFull) {
+        set_error("too many output tiles for one launch");
+        return DR_ERR_UNSUPPORTED;
+    }
+    if (c.op == kWgrad) return launch<kWgrad, false>(c, ma, mb, a, tiles);
+    if (c.op == kDgrad) return launch<kDgrad, false>(c, ma, mb, a, tiles);
+    return fp8 ? launch<kForward, true>(c, ma, mb, a, tiles) : launch<kForward, false>(c, ma, mb, a, tiles);
+}
+
+int linear_wait_failures(uint64_t* out)
+{
+    unsigned long long n = 0;
+    DR_CUDA(cudaMemcpyFromSymbol(&n, g_wait_failures, sizeof n));
+    *out = n;
+    return DR_OK;
+}
+
+}  // namespace dr
