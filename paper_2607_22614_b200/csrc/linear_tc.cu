@@ -9,13 +9,13 @@
 //   wgrad    D[n, k] = sum_r dy[r, n] x[r, k]     both MN-major, the contraction runs over a group's rows
 //
 // Roles of a CTA's 12 warps: 0 issues the copies of its half of the operands into a ring of six 32 KB stages; 1 (of the pair's
-// first CTA) issues the products of the pair; 2 multiplies the scales (fp8) or clears the rows of other groups from the last
+// first CTA) issues the products of the pair; 2 copies the tokens' scales (fp8) or clears the rows of other groups from the last
 // stage (wgrad); 4-11 read the accumulators.  Accumulators take half of tensor memory each, two in turn, so that a tile is
 // written out while the next is computed.
 //
 // fp8: one product covers exactly one block of 128 of the contraction, after which its partial sums are scaled by
 // xs[b, r] * ws[n / 128, b] and added to fp32 sums in registers (128 a thread).  A CTA's 128 features are one scale block, so
-// ws is one number per block, and the products of the two scales, one per token, come through shared memory.  The accumulators are
+// ws is one number per block, and the tokens' scales come through shared memory.  The accumulators are
 // read in the fragment layout of 8 x 8 blocks (a thread holds two tokens of four features): a thread then needs the
 // scales of a quarter of the tokens only, which keeps the shared-memory port free for the tensor cores, and two multiply-adds
 // share an instruction.
@@ -36,7 +36,7 @@ __device__ unsigned long long g_wait_failures;
 constexpr uint32_t kStages = 6, kStageBytes = 32768, kOperandBytes = 16384;
 constexpr uint32_t kThreads = 384, kEpilogueWarps = 8;
 constexpr uint32_t kTile = 256;          // features and tokens of a pair's tile
-constexpr uint32_t kScaleSlots = 4;
+constexpr uint32_t kScaleSlots = 8;
 constexpr uint32_t kScratchPitch = 80;   // bytes between tokens of the transpose: 16-byte units of eight rows fall on different banks
 constexpr uint32_t kBand = 16;           // token tiles a band of a large group holds
 
@@ -267,36 +267,25 @@ __device__ __forceinline__ void multiply(const TcArgs& a, Shared& s)
     }
 }
 
-// fp8: the product of the two scales for every token of the tile, one block of the contraction after the other.
-__device__ __forceinline__ void scale_tokens(const TcArgs& a, Shared& s)
+// fp8: the tokens' scales of one block of the contraction after the other, copied ahead of the products that need them.
+__device__ __forceinline__ void copy_scales(const TcArgs& a, Shared& s)
 {
-    const uint32_t lane = threadIdx.x & 31, rank = cta_rank();
+    const uint32_t lane = threadIdx.x & 31, slots = smem_u32(s.scale);
     const uint32_t full = smem_u32(s.scale_full), empty = smem_u32(s.scale_empty);
-    const uint32_t scale_rows = (a.n_groups * a.n + 127) / 128;
     uint32_t n = 0;
     Walk<kForward, true> walk;
     Tile t;
     for (uint32_t i = blockIdx.x >> 1; walk.get(a, s, i, t); i += gridDim.x >> 1) {
         if (t.nt == 0) continue;
-        const uint32_t wr = min((t.feature + rank * 128) / 128, scale_rows - 1);
-        const float* ws = a.b_scale + (uint64_t)wr * a.ld_bs;
-        const float* xs = a.a_scale + t.row0 + lane;
+        const float* xs = a.a_scale + t.row0;
         const uint32_t left = t.row_end - t.row0;
-        float v[8], w;
-        auto fetch = [&](uint32_t l) {
-            w = ws[l];
-#pragma unroll
-            for (uint32_t j = 0; j < 8; ++j) v[j] = lane + 32 * j < left ? xs[l * a.ld_as + 32 * j] : 0.0f;
-        };
-        fetch(0);
-        for (uint32_t l = 0; l < t.steps; ++l, ++n) {
+        for (uint32_t l = 0; l < t.steps; ++l, ++n, xs += a.ld_as) {
             const uint32_t slot = n % kScaleSlots;
             if (!__all_sync(0xFFFFFFFFu, bar_wait(empty + 8 * slot, (n / kScaleSlots & 1) ^ 1, &s.stop, &g_wait_failures))) return;
 #pragma unroll
-            for (uint32_t j = 0; j < 8; ++j) s.scale[slot][lane + 32 * j] = v[j] * w;
-            __syncwarp();
-            if (lane == 0) bar_arrive(full + 8 * slot);
-            if (l + 1 < t.steps) fetch(l + 1);
+            for (uint32_t j = lane; j < kTile; j += 32)  // zeros for columns past the group's rows
+                copy_4(slots + slot * kTile * 4 + j * 4, xs + (j < left ? j : 0), j < left);
+            copies_arrive(full + 8 * slot);
         }
     }
 }
@@ -322,7 +311,7 @@ __device__ __forceinline__ void clear_rows(const TcArgs& a, Shared& s)
                 fence_async();
             }
             __syncwarp();
-            if (lane == 0) bar_arrive_cluster(full + 8 * st);
+            if (lane == 0) bar_arrive_cluster(full + 8 * st, valid < 64);
         }
     }
 }
@@ -361,8 +350,13 @@ __device__ __forceinline__ void write_out(const TcArgs& a, Shared& s)
                 for (int h = 0; h < 2; ++h)
 #pragma unroll
                     for (int r = 0; r < 16; ++r) sum[c][h][r] = 0.0f;
+            // the CTA's 128 features are one block of the weight's scales (a tile past the last feature reads the last one)
+            const float* ws = a.b_scale + (uint64_t)min((t.feature + rank * 128) / 128, (a.n_groups * a.n + 127) / 128 - 1) * a.ld_bs;
+            float w_next = ws[0];
             for (uint32_t l = 0; l < t.steps; ++l, ++acc) {
                 const uint32_t slot = acc % kScaleSlots;
+                const float w = w_next;
+                if (l + 1 < t.steps) w_next = ws[l + 1];
                 ok = bar_wait(scale_full + 8 * slot, acc / kScaleSlots & 1, &s.stop, &g_wait_failures) &&
                      bar_wait(acc_full + 8 * (acc & 1), acc >> 1 & 1, &s.stop, &g_wait_failures);
                 if (!__all_sync(0xFFFFFFFFu, ok)) return;
@@ -376,7 +370,8 @@ __device__ __forceinline__ void write_out(const TcArgs& a, Shared& s)
                     tmem_load_32x32(from + c * 32, p[0], p[1]);
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        const uint64_t two = *(const uint64_t*)(sc + c * 32 + j * 8);
+                        const float2 xs = *(const float2*)(sc + c * 32 + j * 8);
+                        const uint64_t two = pair_of(xs.x * w, xs.y * w);
 #pragma unroll
                         for (int h = 0; h < 2; ++h) {
                             fma2(sum[c][h][4 * j], sum[c][h][4 * j + 1], p[h][4 * j], p[h][4 * j + 1], two);
@@ -452,7 +447,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
             bar_init(smem_u32(&s.acc_empty[i]), 2 * kEpilogueWarps);
         }
         for (uint32_t i = 0; i < kScaleSlots; ++i) {
-            bar_init(smem_u32(&s.scale_full[i]), 1);
+            bar_init(smem_u32(&s.scale_full[i]), 32);
             bar_init(smem_u32(&s.scale_empty[i]), kEpilogueWarps);
         }
         s.stop = 0;
@@ -487,7 +482,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         } else if (warp == 1) {
             if (lane == 0 && cta_rank() == 0) multiply<OP, FP8>(a, s);
         } else if (warp == 2) {
-            if (FP8) scale_tokens(a, s);
+            if (FP8) copy_scales(a, s);
             if (OP == kWgrad) clear_rows(a, s);
         }
     } else {

@@ -46,15 +46,20 @@ __device__ __forceinline__ void bar_arrive(uint32_t bar)
 {
     asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
 }
-// `bar` may lie in another CTA of the cluster (an address of in_cta).
-__device__ __forceinline__ void bar_arrive_cluster(uint32_t bar)
+// `bar` may lie in another CTA of the cluster (an address of in_cta).  What the arrival hands over is tensor memory that has
+// been read (ordered by fence_before) or stages that only the copy unit wrote, so no release at cluster scope, which would
+// stall the warp on a memory barrier, is needed; where the warp itself has written shared memory, `wrote` asks for it.
+__device__ __forceinline__ void bar_arrive_cluster(uint32_t bar, bool wrote = false)
 {
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+    if (wrote)
+        asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+    else
+        asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity)
 {
     uint32_t ok;
-    asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}"
+    asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}"
                  : "=r"(ok)
                  : "r"(bar), "r"(parity)
                  : "memory");
@@ -109,6 +114,16 @@ __device__ __forceinline__ void prefetch_map(const CUtensorMap* map)
 }
 // Generic writes to shared memory become visible to the tensor cores and the copy unit.
 __device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
+// One 4-byte copy to shared memory, a zero when !valid; copies_arrive makes the thread's copies so far arrive on `bar`.
+__device__ __forceinline__ void copy_4(uint32_t dst, const void* src, bool valid)
+{
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(valid ? 4 : 0) : "memory");
+}
+__device__ __forceinline__ void copies_arrive(uint32_t bar)
+{
+    asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
+}
 
 // ---- tensor memory and products --------------------------------------------------------------------------------------
 template <int CTAS>
@@ -188,6 +203,12 @@ __device__ __forceinline__ void tmem_load_32x32(uint32_t addr, float (&a)[16], f
 }
 
 // ---- arithmetic and stores -------------------------------------------------------------------------------------------
+__device__ __forceinline__ uint64_t pair_of(float lo, float hi)
+{
+    uint64_t d;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "f"(lo), "f"(hi));
+    return d;
+}
 // (a0, a1) += (p0, p1) * (s0, s1), two fp32 multiply-adds in one instruction
 __device__ __forceinline__ void fma2(float& a0, float& a1, float p0, float p1, uint64_t s)
 {
