@@ -197,7 +197,9 @@ def _current_stream(stream):
     if stream is None:
         import torch
         # without a CUDA device the descriptor can still be built (argument checks); NULL = legacy default stream
-        return torch.cuda.current_stream().cuda_stream if torch.cuda.is_available() else None
+        if torch.cuda.is_initialized() or torch.cuda.is_available():
+            return torch.cuda.current_stream().cuda_stream
+        return None
     return getattr(stream, "cuda_stream", stream)
 
 
@@ -714,7 +716,9 @@ class Linear:
             dr_linear_destroy(self.handle)
             self.handle = None
 
-    __del__ = close
+    def __del__(self):
+        if lib is not None:  # at the interpreter's end the module may be gone before its objects
+            self.close()
 
     def _operand(self, t, cols, what, fp8=False):
         import torch

@@ -33,8 +33,12 @@ using namespace tc;
 
 __device__ unsigned long long g_wait_failures;
 
+constexpr int kForwardRows = 3;  // forward with tokens on the M side (fp8, many rows)
+
 constexpr uint32_t kStages = 6, kStageBytes = 32768, kOperandBytes = 16384;
-constexpr uint32_t kThreads = 384, kEpilogueWarps = 8;
+constexpr uint32_t kScratchWarps = 8;    // of the kernels that write through the transpose
+template <int OP> constexpr uint32_t kEpilogueWarps = OP == kForwardRows ? 16 : 8;
+template <int OP> constexpr uint32_t kThreads = 128 + 32 * kEpilogueWarps<OP>;
 constexpr uint32_t kTile = 256;          // features and tokens of a pair's tile
 constexpr uint32_t kScaleSlots = 8;
 constexpr uint32_t kScratchPitch = 80;   // bytes between tokens of the transpose: 16-byte units of eight rows fall on different banks
@@ -42,7 +46,7 @@ constexpr uint32_t kBand = 16;           // token tiles a band of a large group 
 
 struct Shared {
     alignas(1024) uint8_t stage[kStages][kStageBytes];
-    alignas(16) uint8_t scratch[kEpilogueWarps][8 * kScratchPitch];
+    alignas(16) uint8_t scratch[kScratchWarps][8 * kScratchPitch];
     alignas(16) float scale[kScaleSlots][kTile];
     uint64_t full[kStages], empty[kStages], landed[kStages];
     uint64_t acc_full[2], acc_empty[2];
@@ -104,10 +108,19 @@ struct Walk {
             i -= band * kBand * a.feature_tiles;
             const uint32_t f = i / in_band, m = band * kBand + i % in_band;
             o.e = e;
+            o.col0 = 0;
+            if (OP == kForwardRows) {
+                const uint32_t first = e * a.n;
+                o.row0 = lo + m * kTile;
+                o.row_end = min(hi, o.row0 + kTile);
+                o.feature = first / 128 * 128 + f * kTile;
+                o.nt = o.feature < first + a.n ? min(kTile, (first + a.n - o.feature + 31) / 32 * 32) : 0;
+                o.steps = (a.k + kStep - 1) / kStep;
+                return true;
+            }
             o.nt = ((hi - lo + tiles - 1) / tiles + 31) / 32 * 32;
             o.row0 = lo + m * o.nt;
             o.row_end = min(hi, o.row0 + o.nt);
-            o.col0 = 0;
             if (OP == kForward) {
                 const uint32_t first = e * a.n;
                 o.feature = (FP8 ? first / 128 * 128 : first) + f * kTile;
@@ -209,6 +222,8 @@ __device__ __forceinline__ void produce(const TcArgs& a, Shared& s, const CUtens
                 bar_expect(smem_u32(s.full) + 8 * st, 2 * bytes);
             if (OP == kForward) {
                 load_2d<true>(at, map_a, bar, l * kStep, feature);
+            } else if (OP == kForwardRows) {
+                load_2d<true>(at, map_a, bar, l * kStep, t.row0 + rank * 128);
             } else if (OP == kDgrad) {
                 load_3d<true>(at, map_a, bar, feature, l * kStep, t.e);
                 load_3d<true>(at + 8192, map_a, bar, feature + 64, l * kStep, t.e);
@@ -221,7 +236,7 @@ __device__ __forceinline__ void produce(const TcArgs& a, Shared& s, const CUtens
                 if (OP == kWgrad)
                     load_2d<false>(to, map_b, bar, t.col0 + rank * half + b * 64, t.row0 + l * kStep);
                 else
-                    load_2d<true>(to, map_b, bar, l * kStep, t.row0 + rank * half + b * 32);
+                    load_2d<true>(to, map_b, bar, l * kStep, (OP == kForwardRows ? t.feature : t.row0) + rank * half + b * 32);
             }
         }
     }
@@ -237,7 +252,8 @@ __device__ __forceinline__ void multiply(const TcArgs& a, Shared& s)
 {
     const uint32_t stages = smem_u32(s.stage), full = smem_u32(s.full), empty = smem_u32(s.empty);
     const uint32_t acc_full = smem_u32(s.acc_full), acc_empty = smem_u32(s.acc_empty), tmem = s.tmem;
-    constexpr bool a_mn = OP != kForward, b_mn = OP == kWgrad;
+    constexpr bool a_mn = OP == kDgrad || OP == kWgrad, b_mn = OP == kWgrad;
+    const uint64_t first_a = operand(stages, 8192), first_b = operand(stages + kOperandBytes, 8192);
     uint32_t n = 0, acc = 0;
     bool ok = true;
     Walk<OP, FP8> walk;
@@ -254,13 +270,13 @@ __device__ __forceinline__ void multiply(const TcArgs& a, Shared& s)
             ok = bar_wait(full + 8 * st, n / kStages & 1, &s.stop, &g_wait_failures);
             if (!ok) return;
             fence_after();
-            const uint32_t at = stages + st * kStageBytes, d = tmem + (acc & 1) * kTile;
+            const uint32_t d = tmem + (acc & 1) * kTile;
+            // addresses are the low bits of a descriptor, in units of 16 bytes
+            const uint64_t da = first_a + st * (kStageBytes >> 4), db = first_b + st * (kStageBytes >> 4);
 #pragma unroll
-            for (uint32_t q = 0; q < 4; ++q) {
-                const uint64_t da = operand(at + q * (a_mn ? 2048 : 32), 8192);
-                const uint64_t db = operand(at + kOperandBytes + q * (b_mn ? 2048 : 32), 8192);
-                mma<2, FP8>(d, da, db, shape, FP8 ? q != 0 : (l | q) != 0);
-            }
+            for (uint32_t q = 0; q < 4; ++q)
+                mma<2, FP8>(d, da + q * ((a_mn ? 2048 : 32) >> 4), db + q * ((b_mn ? 2048 : 32) >> 4), shape,
+                            FP8 ? q != 0 : (l | q) != 0);
             commit<2>(empty + 8 * st);
             if (FP8 || l + 1 == t.steps) commit<2>(acc_full + 8 * (acc++ & 1));
         }
@@ -343,13 +359,13 @@ __device__ __forceinline__ void write_out(const TcArgs& a, Shared& s)
                 store_tokens(a, scratch, t.row0 + col0 + c, t.row_end, f, f_hi, v);
         };
         if (FP8) {
-            float sum[4][2][16];
+            float sum[2][2][32];
 #pragma unroll
-            for (int c = 0; c < 4; ++c)
+            for (int c = 0; c < 2; ++c)
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) sum[c][h][r] = 0.0f;
+                    for (int r = 0; r < 32; ++r) sum[c][h][r] = 0.0f;
             // the CTA's 128 features are one block of the weight's scales (a tile past the last feature reads the last one)
             const float* ws = a.b_scale + (uint64_t)min((t.feature + rank * 128) / 128, (a.n_groups * a.n + 127) / 128 - 1) * a.ld_bs;
             float w_next = ws[0];
@@ -363,15 +379,20 @@ __device__ __forceinline__ void write_out(const TcArgs& a, Shared& s)
                 fence_after();
                 const uint32_t from = tmem + (acc & 1) * kTile + col0;
                 const float* sc = s.scale[slot] + col0 + 2 * (lane & 3);
+                const uint64_t ww = pair_of(w, w);
 #pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    if (c * 32 >= cols) break;
-                    float p[2][16];
-                    tmem_load_32x32(from + c * 32, p[0], p[1]);
+                for (int c = 0; c < 2; ++c) {
+                    if (c * 64 >= cols) break;
+                    float p[2][32];
+                    tmem_load(from + c * 64, p[0], p[1]);
+                    if (c * 64 + 64 >= cols) {  // the last of the accumulator has been read: the next product may begin
+                        fence_before();
+                        __syncwarp();
+                        if (lane == 0) bar_arrive_cluster(acc_empty + 8 * (acc & 1));
+                    }
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const float2 xs = *(const float2*)(sc + c * 32 + j * 8);
-                        const uint64_t two = pair_of(xs.x * w, xs.y * w);
+                    for (int j = 0; j < 8; ++j) {
+                        const uint64_t two = mul2(*(const uint64_t*)(sc + c * 64 + j * 8), ww);
 #pragma unroll
                         for (int h = 0; h < 2; ++h) {
                             fma2(sum[c][h][4 * j], sum[c][h][4 * j + 1], p[h][4 * j], p[h][4 * j + 1], two);
@@ -379,21 +400,17 @@ __device__ __forceinline__ void write_out(const TcArgs& a, Shared& s)
                         }
                     }
                 }
-                fence_before();
                 __syncwarp();
-                if (lane == 0) {
-                    bar_arrive_cluster(acc_empty + 8 * (acc & 1));
-                    bar_arrive(scale_empty + 8 * slot);
-                }
+                if (lane == 0) bar_arrive(scale_empty + 8 * slot);
             }
 #pragma unroll
-            for (int c = 0; c < 4; ++c)
+            for (int c = 0; c < 2; ++c)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    if (c * 32 + j * 8 >= cols) break;
+                for (int j = 0; j < 8; ++j) {
+                    if (c * 64 + j * 8 >= cols) break;
                     const float v[4][2] = {{sum[c][0][4 * j], sum[c][0][4 * j + 1]}, {sum[c][0][4 * j + 2], sum[c][0][4 * j + 3]},
                                            {sum[c][1][4 * j], sum[c][1][4 * j + 1]}, {sum[c][1][4 * j + 2], sum[c][1][4 * j + 3]}};
-                    put(c * 32 + j * 8, v);
+                    put(c * 64 + j * 8, v);
                 }
         } else {
             if (t.steps) {
@@ -404,7 +421,7 @@ __device__ __forceinline__ void write_out(const TcArgs& a, Shared& s)
             for (uint32_t c = 0; c < cols; c += 32) {
                 float p[2][16];
                 if (t.steps) {
-                    tmem_load_32x32(tmem + (acc & 1) * kTile + col0 + c, p[0], p[1]);
+                    tmem_load(tmem + (acc & 1) * kTile + col0 + c, p[0], p[1]);
                 } else {
 #pragma unroll
                     for (int r = 0; r < 16; ++r) p[0][r] = p[1][r] = 0.0f;  // dW of a group without rows
@@ -427,8 +444,103 @@ __device__ __forceinline__ void write_out(const TcArgs& a, Shared& s)
     }
 }
 
+// Tokens on the M side: a thread owns one token and 64 features of one scale block, so the scale of a block of the contraction is
+// one number a thread.
+__device__ __forceinline__ void write_rows(const TcArgs& a, Shared& s)
+{
+    const uint32_t lane = threadIdx.x & 31, warp = (threadIdx.x >> 5) - 4, rank = cta_rank();
+    const uint32_t quarter = warp & 3, side = warp >> 2;
+    const uint32_t acc_full = smem_u32(s.acc_full), acc_empty = in_cta(smem_u32(s.acc_empty), 0);
+    const uint32_t tmem = s.tmem + (quarter * 32 << 16) + side * 64;
+    const uint32_t scale_rows = (a.n_groups * a.n + 127) / 128;
+    uint32_t acc = 0;
+    Walk<kForwardRows, true> walk;
+    Tile t;
+    for (uint32_t i = blockIdx.x >> 1; walk.get(a, s, i, t); i += gridDim.x >> 1) {
+        if (t.nt == 0) continue;
+        const uint32_t warp_row = t.row0 + rank * 128 + quarter * 32, row = warp_row + lane;
+        // a warp without a token or without a feature only keeps the barriers going
+        const bool idle = warp_row >= t.row_end || side * 64 >= t.nt;
+        const float* xs = a.a_scale + min(row, t.row_end - 1);
+        const float* ws = a.b_scale + (uint64_t)min(t.feature / 128 + side / 2, scale_rows - 1) * a.ld_bs;
+        float sum[2][32];
+#pragma unroll
+        for (int c = 0; c < 2; ++c)
+#pragma unroll
+            for (int r = 0; r < 32; ++r) sum[c][r] = 0.0f;
+        float x1 = xs[0], w1 = ws[0], x2 = 0.0f, w2 = 0.0f;
+        if (t.steps > 1) {
+            x2 = xs[a.ld_as];
+            w2 = ws[1];
+        }
+        xs += 2 * a.ld_as;
+        for (uint32_t l = 0; l < t.steps; ++l, ++acc) {
+            const float scale = x1 * w1;
+            x1 = x2;
+            w1 = w2;
+            if (l + 2 < t.steps) {
+                x2 = *xs;
+                w2 = ws[l + 2];
+                xs += a.ld_as;
+            }
+            const bool ok = bar_wait(acc_full + 8 * (acc & 1), acc >> 1 & 1, &s.stop, &g_wait_failures);
+            if (!__all_sync(0xFFFFFFFFu, ok)) return;
+            fence_after();
+            if (idle) {
+                fence_before();
+                if (lane == 0) bar_arrive_cluster(acc_empty + 8 * (acc & 1));
+                continue;
+            }
+            const uint64_t two = pair_of(scale, scale);
+            const uint32_t from = tmem + (acc & 1) * kTile;
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                float p[32];
+                tmem_start(from + 32 * c, p);
+                tmem_arrived(p);
+                if (c == 1) {  // the accumulator has been read: the next product may begin
+                    fence_before();
+                    __syncwarp();
+                    if (lane == 0) bar_arrive_cluster(acc_empty + 8 * (acc & 1));
+                }
+#pragma unroll
+                for (int r = 0; r < 32; r += 2) fma2(sum[c][r], sum[c][r + 1], p[r], p[r + 1], two);
+            }
+        }
+        if (idle || row >= t.row_end) continue;
+        const int f = (int)(t.feature + side * 64 - t.e * a.n);
+        if (a.vector) {  // 32 bytes of c and whole rows of 16 features allow one sector a store
+#pragma unroll
+            for (int c = 0; c < 64; c += 16) {
+                if (f + c < 0 || f + c >= (int)a.n) continue;
+                const float* v = &sum[c / 32][c % 32];
+                if (a.c_f32) {
+                    float* p = (float*)a.c + (uint64_t)row * a.ldc + f + c;
+                    store_32(p, __float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]),
+                             __float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7]));
+                    store_32(p + 8, __float_as_uint(v[8]), __float_as_uint(v[9]), __float_as_uint(v[10]), __float_as_uint(v[11]),
+                             __float_as_uint(v[12]), __float_as_uint(v[13]), __float_as_uint(v[14]), __float_as_uint(v[15]));
+                } else {
+                    store_32((uint16_t*)a.c + (uint64_t)row * a.ldc + f + c, pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]),
+                             pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]), pack_bf16(v[8], v[9]), pack_bf16(v[10], v[11]),
+                             pack_bf16(v[12], v[13]), pack_bf16(v[14], v[15]));
+                }
+            }
+        } else {
+#pragma unroll
+            for (int c = 0; c < 64; ++c) {
+                if (f + c < 0 || f + c >= (int)a.n) continue;
+                if (a.c_f32)
+                    ((float*)a.c)[(uint64_t)row * a.ldc + f + c] = sum[c / 32][c % 32];
+                else
+                    ((uint16_t*)a.c)[(uint64_t)row * a.ldc + f + c] = (uint16_t)pack_bf16(sum[c / 32][c % 32], 0.0f);
+            }
+        }
+    }
+}
+
 template <int OP, bool FP8>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads<OP>, 1)
     tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const TcArgs a)
 {
     extern __shared__ uint8_t raw[];
@@ -444,11 +556,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         }
         for (uint32_t i = 0; i < 2; ++i) {
             bar_init(smem_u32(&s.acc_full[i]), 1);
-            bar_init(smem_u32(&s.acc_empty[i]), 2 * kEpilogueWarps);
+            bar_init(smem_u32(&s.acc_empty[i]), 2 * kEpilogueWarps<OP>);
         }
         for (uint32_t i = 0; i < kScaleSlots; ++i) {
             bar_init(smem_u32(&s.scale_full[i]), 32);
-            bar_init(smem_u32(&s.scale_empty[i]), kEpilogueWarps);
+            bar_init(smem_u32(&s.scale_empty[i]), kEpilogueWarps<OP>);
         }
         s.stop = 0;
         bar_init_fence();
@@ -476,18 +588,27 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     fence_after();
 
     if (warp < 4) {
-        if (FP8) asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
+        if (OP == kForwardRows)
+            asm volatile("setmaxnreg.dec.sync.aligned.u32 32;");
+        else if (FP8)
+            asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
         if (warp == 0) {
             if (lane == 0) produce<OP, FP8>(a, s, &map_a, &map_b);
         } else if (warp == 1) {
             if (lane == 0 && cta_rank() == 0) multiply<OP, FP8>(a, s);
         } else if (warp == 2) {
-            if (FP8) copy_scales(a, s);
+            if (FP8 && OP == kForward) copy_scales(a, s);
             if (OP == kWgrad) clear_rows(a, s);
         }
     } else {
-        if (FP8) asm volatile("setmaxnreg.inc.sync.aligned.u32 232;");
-        write_out<OP, FP8>(a, s);
+        if (OP == kForwardRows)
+            asm volatile("setmaxnreg.inc.sync.aligned.u32 112;");
+        else if (FP8)
+            asm volatile("setmaxnreg.inc.sync.aligned.u32 232;");
+        if constexpr (OP == kForwardRows)
+            write_rows(a, s);
+        else
+            write_out<OP, FP8>(a, s);
     }
     __syncwarp();
     if (*(volatile uint32_t*)&s.stop) {  // a wait ran out: let the copies and products in flight end before the memory is given back
@@ -539,13 +660,13 @@ int encode(CUtensorMap* map, const void* base, bool fp8, uint64_t cols, uint64_t
 constexpr size_t kSharedBytes = sizeof(Shared) + 1024;
 
 // Once per device and kernel: shared memory, and the register count that the fp8 kernel's split relies on
-// (384 threads x 168 at launch cover 256 x 232 + 128 x 40).
+// (384 threads x 168 at launch cover 256 x 232 + 128 x 40, 640 x 96 cover 512 x 112 + 128 x 32).
 template <int OP, bool FP8>
 int prepare_kernel()
 {
     cudaFuncAttributes at;
     DR_CUDA(cudaFuncGetAttributes(&at, tc_kernel<OP, FP8>));
-    if (FP8 && at.numRegs * kThreads < 232 * 256 + 40 * 128) {
+    if (FP8 && at.numRegs * (int)kThreads<OP> < (OP == kForwardRows ? 512 * 112 + 128 * 32 : 256 * 232 + 128 * 40)) {
         set_error("the fp8 linear kernel was built with %d registers a thread", at.numRegs);
         return DR_ERR_CUDA;
     }
@@ -558,7 +679,7 @@ int launch(const LinearCall& c, const CUtensorMap& ma, const CUtensorMap& mb, co
 {
     const uint64_t pairs = (uint64_t)c.lin->sms / 2;
     const unsigned grid = 2 * (unsigned)(tiles < pairs ? tiles : pairs);
-    tc_kernel<OP, FP8><<<grid, kThreads, kSharedBytes, c.stream>>>(ma, mb, a);
+    tc_kernel<OP, FP8><<<grid, kThreads<OP>, kSharedBytes, c.stream>>>(ma, mb, a);
     cudaError_t err = cudaGetLastError();
     if (err != cudaSuccess) {
         set_error("linear kernel launch: %s", cudaGetErrorString(err));
@@ -572,6 +693,7 @@ int launch(const LinearCall& c, const CUtensorMap& ma, const CUtensorMap& mb, co
 int prepare_linear_tc()
 {
     int rc = prepare_kernel<kForward, true>();
+    if (rc == DR_OK) rc = prepare_kernel<kForwardRows, true>();
     if (rc == DR_OK) rc = prepare_kernel<kForward, false>();
     if (rc == DR_OK) rc = prepare_kernel<kDgrad, false>();
     if (rc == DR_OK) rc = prepare_kernel<kWgrad, false>();
@@ -604,6 +726,10 @@ int launch_linear_tc(const LinearCall& c)
     a.k = (uint32_t)d.in_features;
     a.c_f32 = c.c_f32;
     a.accumulate = c.accumulate;
+    // fp8 with tokens on the M side, where their scales cost next to nothing but a ragged group costs whole tiles: from 512 rows
+    // a group on (8192 x 24576 x 4096: 797 us against 915 with the features there; 512 x 6144 x 4096: 30.8 / 32.8; 128 groups of
+    // 256 rows, 1536 x 2048: 170 / 158; one of 256 rows, 24576 x 4096: 56.3 / 55.3).
+    const bool by_rows = fp8 && c.rows >= 512ull * d.n_groups;
     CUtensorMap ma, mb;
     int rc;
     uint64_t tiles;
@@ -620,11 +746,15 @@ int launch_linear_tc(const LinearCall& c)
         a.feature_tiles = (width + (fp8 && a.n % 128 ? 127 : 0) + kTile - 1) / kTile;
         tiles = token_tiles * a.feature_tiles;
         a.vector = !c.c_f32 && width % 8 == 0 && c.ldc % 8 == 0 && (uintptr_t)c.c % 16 == 0;
-        if (c.op == kForward)
+        if (by_rows) {
+            a.vector = width % 16 == 0 && c.ldc % (c.c_f32 ? 8 : 16) == 0 && (uintptr_t)c.c % 32 == 0;
+            rc = encode(&ma, c.a, true, a.k, c.rows, 0, c.lda, 128);
+            if (rc == DR_OK) rc = encode(&mb, c.b, true, a.k, (uint64_t)a.n * a.n_groups, 0, c.ldb, 32);
+        } else if (c.op == kForward)
             rc = encode(&ma, c.b, fp8, a.k, (uint64_t)a.n * a.n_groups, 0, c.ldb, 128);
         else
             rc = encode(&ma, c.b, false, a.k, a.n, a.n_groups, c.ldb, 64);
-        if (rc == DR_OK) rc = encode(&mb, c.a, fp8, c.op == kForward ? a.k : a.n, c.rows, 0, c.lda, 32);
+        if (rc == DR_OK && !by_rows) rc = encode(&mb, c.a, fp8, c.op == kForward ? a.k : a.n, c.rows, 0, c.lda, 32);
     }
     if (rc) return rc;
     if (tiles > 0x7FFFFFFFull) {
@@ -633,6 +763,7 @@ int launch_linear_tc(const LinearCall& c)
     }
     if (c.op == kWgrad) return launch<kWgrad, false>(c, ma, mb, a, tiles);
     if (c.op == kDgrad) return launch<kDgrad, false>(c, ma, mb, a, tiles);
+    if (by_rows) return launch<kForwardRows, true>(c, ma, mb, a, tiles);
     return fp8 ? launch<kForward, true>(c, ma, mb, a, tiles) : launch<kForward, false>(c, ma, mb, a, tiles);
 }
 

@@ -41,7 +41,8 @@ def test_dense(rows, n, k, fp8, out):
 
 GROUPED = [([3, 0, 1, 7], 256, 256), ([0, 0, 130, 0, 1, 64, 0, 259], 384, 512), ([1] * 33, 144, 272), ([0, 300, 0], 192, 208),
            ([5, 17, 33, 2, 90], 128, 1040), ([128, 128, 256], 512, 128), ([2, 0, 9], 40, 64), ([31, 1, 140], 12, 24),
-           ([0, 0, 0], 128, 128), ([70, 200, 500, 40], 1536, 768)]
+           ([0, 0, 0], 128, 128), ([70, 200, 500, 40], 1536, 768), ([600, 0, 1300, 513], 384, 528), ([1100, 901], 144, 256),
+           ([513, 2000, 30], 40, 128)]
 
 
 @pytest.mark.parametrize("out", [BF16, F32], ids=["bf16", "f32"])
