@@ -626,53 +626,85 @@ class Plan:
 
 
 def _matrix(t, what):
-    if t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] > 1):
-        raise ValueError(f"{what} must be a matrix with contiguous rows")
-    if not t.is_cuda:
-        raise ValueError(f"{what} must be a CUDA tensor")
-    return t
+    """(rows, columns, elements between rows) of a CUDA matrix with contiguous rows."""
+    if t.dim() != 2 or not t.is_cuda:
+        raise ValueError(f"{what} must be a CUDA matrix")
+    rows, cols = t.shape
+    ld, step = t.stride()
+    if step != 1 and cols > 1:
+        raise ValueError(f"{what} must have contiguous rows")
+    return rows, cols, ld if rows > 1 else cols  # torch gives any stride to a matrix of one row
 
 
-def _ld(t):
-    """Elements between rows (torch gives any stride to a matrix of one row)."""
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+_codes = None  # torch dtype -> DR_BF16 / DR_F32
 
 
 def _code_of(t, what):
-    import torch
-    code = {torch.bfloat16: DR_BF16, torch.float32: DR_F32}.get(t.dtype)
+    global _codes
+    if _codes is None:
+        import torch
+        _codes = {torch.bfloat16: DR_BF16, torch.float32: DR_F32}
+    code = _codes.get(t.dtype)
     if code is None:
         raise TypeError(f"{what} must be bfloat16 or float32, not {t.dtype}")
     return code
 
 
+_fns = {}
+
+
+def _fn(name):
+    """The C function itself, looked up once."""
+    f = _fns.get(name)
+    if f is None:
+        f = _fns[name] = getattr(lib(), name)
+    return f
+
+
+_raw_stream = None
+
+
+def _stream_of(t, stream):
+    """The handle of `stream`, or of the stream that is current on t's device (torch's own accessor of the raw handle: building
+    a Stream object for it takes 3 us, more than the launch)."""
+    global _raw_stream
+    if stream is not None:
+        return getattr(stream, "cuda_stream", stream)
+    if _raw_stream is None:
+        import torch
+        _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
+            (lambda index: torch.cuda.current_stream(index).cuda_stream)
+    return _raw_stream(t.get_device())
+
+
 def quant_rows(x, codes=None, scales=None, *, row_index=None, swiglu=False, stream=None):
     """dr_quant_rows: x [source rows, cols] (2 * cols with swiglu: gate, then up; bf16 or fp32) -> (codes [rows, cols],
     scales [ceil(cols / 128), rows]).  row_index (int64) gathers rows.  Outputs that are not given are allocated."""
-    import torch
-    _matrix(x, "x")
-    cols = x.shape[1] // 2 if swiglu else x.shape[1]
-    if swiglu and x.shape[1] % 2:
+    src_rows, width, ldx = _matrix(x, "x")
+    cols = width // 2 if swiglu else width
+    if swiglu and width % 2:
         raise ValueError("x holds gate and up side by side: its column count must be even")
-    if row_index is None:
-        rows = x.shape[0]
-    else:
-        if row_index.dtype != torch.int64 or row_index.dim() != 1 or not row_index.is_contiguous() or not row_index.is_cuda:
+    rows, index = src_rows, None
+    if row_index is not None:
+        import torch
+        if row_index.dtype != torch.int64 or row_index.dim() != 1 or not row_index.is_cuda or not row_index.is_contiguous():
             raise ValueError("row_index must be a contiguous int64 CUDA vector")
-        rows = row_index.shape[0]
-    if codes is None:
-        codes = torch.empty(rows, cols, dtype=torch.float8_e4m3fn, device=x.device)
-    if scales is None:
-        scales = torch.empty(-(-cols // 128), rows, dtype=torch.float32, device=x.device)
-    _matrix(codes, "codes")
-    _matrix(scales, "scales")
-    if codes.element_size() != 1 or codes.shape[0] != rows or codes.shape[1] != cols:
+        rows, index = row_index.shape[0], row_index.data_ptr()
+    blocks = -(-cols // 128)
+    if codes is None or scales is None:
+        import torch
+        if codes is None:
+            codes = torch.empty(rows, cols, dtype=torch.float8_e4m3fn, device=x.device)
+        if scales is None:
+            scales = torch.empty(blocks, rows, dtype=torch.float32, device=x.device)
+    got_rows, got_cols, ld_codes = _matrix(codes, "codes")
+    if got_rows != rows or got_cols != cols or codes.element_size() != 1:
         raise ValueError(f"codes must be {rows} x {cols} bytes")
-    if scales.dtype != torch.float32 or scales.shape[0] != -(-cols // 128) or scales.shape[1] != rows:
-        raise ValueError(f"scales must be fp32, {-(-cols // 128)} x {rows}")
-    rc = dr_quant_rows(x.data_ptr(), _code_of(x, "x"), _ld(x), x.shape[0], None if row_index is None else row_index.data_ptr(),
-                       DR_ROWS_SWIGLU if swiglu else DR_ROWS_PLAIN, rows, cols, codes.data_ptr(), _ld(codes),
-                       scales.data_ptr(), _ld(scales), _current_stream(stream))
+    got_blocks, got_rows, ld_scales = _matrix(scales, "scales")
+    if got_rows != rows or got_blocks != blocks or _code_of(scales, "scales") != DR_F32:
+        raise ValueError(f"scales must be fp32, {blocks} x {rows}")
+    rc = _fn("dr_quant_rows")(x.data_ptr(), _code_of(x, "x"), ldx, src_rows, index, DR_ROWS_SWIGLU if swiglu else DR_ROWS_PLAIN,
+                              rows, cols, codes.data_ptr(), ld_codes, scales.data_ptr(), ld_scales, _stream_of(x, stream))
     if rc:
         raise DrError(rc, "dr_quant_rows")
     return codes, scales
@@ -684,28 +716,25 @@ class Linear:
 
     def __init__(self, weight, scale=None, n_groups=1):
         import torch
-        _matrix(weight, "weight")
+        rows, cols, ld = _matrix(weight, "weight")
         fp8 = weight.element_size() == 1
         if not fp8 and weight.dtype != torch.bfloat16:
             raise TypeError(f"weight must be bfloat16 or e4m3 codes, not {weight.dtype}")
-        if n_groups < 1 or weight.shape[0] % n_groups:
+        if n_groups < 1 or rows % n_groups:
             raise ValueError("n_groups must divide the weight's rows")
+        scale_rows = scale_cols = scale_ld = 0
         if scale is not None:
-            _matrix(scale, "scale")
-            if scale.dtype != torch.float32 or scale.shape[0] != -(-weight.shape[0] // 128) or \
-                    scale.shape[1] != -(-weight.shape[1] // 128):
+            scale_rows, scale_cols, scale_ld = _matrix(scale, "scale")
+            if scale.dtype != torch.float32 or scale_rows != -(-rows // 128) or scale_cols != -(-cols // 128):
                 raise ValueError("scale must be fp32 with one value for each 128 x 128 block of the weight")
         self.weight, self.scale, self.n_groups, self.fp8 = weight, scale, n_groups, fp8
-        self.out_features, self.in_features = weight.shape[0] // n_groups, weight.shape[1]
-
-        def span(t):
-            return ((t.shape[0] - 1) * _ld(t) + t.shape[1]) * t.element_size()
-
+        self.out_features, self.in_features = rows // n_groups, cols
         desc = dr_linear_desc(struct_size=C.sizeof(dr_linear_desc), dtype=DR_FP8_E4M3_B128 if fp8 else DR_BF16,
-                              n_groups=n_groups, out_features=self.out_features, in_features=self.in_features,
-                              weight_dev=weight.data_ptr(), weight_bytes=span(weight), weight_ld=_ld(weight),
+                              n_groups=n_groups, out_features=self.out_features, in_features=cols,
+                              weight_dev=weight.data_ptr(), weight_bytes=((rows - 1) * ld + cols) * weight.element_size(), weight_ld=ld,
                               scale_dev=None if scale is None else scale.data_ptr(),
-                              scale_bytes=0 if scale is None else span(scale), scale_ld=0 if scale is None else _ld(scale))
+                              scale_bytes=4 * ((scale_rows - 1) * scale_ld + scale_cols) if scale is not None else 0,
+                              scale_ld=scale_ld)
         rc, self.handle = dr_linear_create(desc)
         if rc:
             self.handle = None
@@ -721,45 +750,44 @@ class Linear:
             self.close()
 
     def _operand(self, t, cols, what, fp8=False):
-        import torch
-        _matrix(t, what)
-        if t.shape[1] != cols:
+        rows, got, ld = _matrix(t, what)
+        if got != cols:
             raise ValueError(f"{what} must have {cols} columns")
-        if t.element_size() != 1 if fp8 else t.dtype != torch.bfloat16:
+        if t.element_size() != 1 if fp8 else _code_of(t, what) != DR_BF16:
             raise TypeError(f"{what} has the wrong type: {t.dtype}")
-        return t
+        return rows, ld
 
     def _offsets(self, offsets):
-        import torch
         if offsets is None:
             return None
-        if offsets.dtype != torch.int32 or not offsets.is_contiguous() or offsets.numel() != self.n_groups + 1 or \
-                not offsets.is_cuda:
+        import torch
+        if offsets.dtype != torch.int32 or offsets.numel() != self.n_groups + 1 or not offsets.is_cuda or not offsets.is_contiguous():
             raise ValueError(f"offsets must be {self.n_groups + 1} int32 on the GPU")
         return offsets.data_ptr()
 
-    def _out(self, out, rows, cols, dtype, device, what):
-        import torch
+    def _out(self, out, rows, cols, dtype, like, what):
         if out is None:
-            return torch.empty(rows, cols, dtype=dtype or torch.bfloat16, device=device)
-        _matrix(out, what)
-        if out.shape[0] != rows or out.shape[1] != cols:
+            import torch
+            out = torch.empty(rows, cols, dtype=dtype or torch.bfloat16, device=like.device)
+            return out, cols
+        got_rows, got_cols, ld = _matrix(out, what)
+        if got_rows != rows or got_cols != cols:
             raise ValueError(f"{what} must be {rows} x {cols}")
-        return out
+        return out, ld
 
     def forward(self, x, x_scale=None, offsets=None, out=None, out_dtype=None, stream=None):
         """dr_linear_forward: y = x W^T, for rows sorted by group where `offsets` (n_groups + 1, int32) is given.  An fp8
         layer takes quant_rows' codes and scales.  Rows of an allocated output that no group owns are not initialised."""
-        self._operand(x, self.in_features, "x", self.fp8)
-        y = self._out(out, x.shape[0], self.out_features, out_dtype, x.device, "out")
-        ps = lds = None
+        rows, ldx = self._operand(x, self.in_features, "x", self.fp8)
+        y, ldy = self._out(out, rows, self.out_features, out_dtype, x, "out")
+        ps, lds = None, 0
         if x_scale is not None:
-            _matrix(x_scale, "x_scale")
-            if x_scale.element_size() != 4 or x_scale.shape[0] != -(-self.in_features // 128) or x_scale.shape[1] < x.shape[0]:
+            blocks, cols, lds = _matrix(x_scale, "x_scale")
+            if blocks != -(-self.in_features // 128) or cols < rows or _code_of(x_scale, "x_scale") != DR_F32:
                 raise ValueError("x_scale must be fp32, one row for each block of 128 columns, one column for each row of x")
-            ps, lds = x_scale.data_ptr(), _ld(x_scale)
-        rc = dr_linear_forward(self.handle, x.data_ptr(), _ld(x), ps, lds or 0, x.shape[0], self._offsets(offsets),
-                               y.data_ptr(), _ld(y), _code_of(y, "out"), _current_stream(stream))
+            ps = x_scale.data_ptr()
+        rc = _fn("dr_linear_forward")(self.handle, x.data_ptr(), ldx, ps, lds, rows, self._offsets(offsets), y.data_ptr(), ldy,
+                                      _code_of(y, "out"), _stream_of(x, stream))
         if rc:
             raise DrError(rc, "dr_linear_forward")
         return y
@@ -768,28 +796,30 @@ class Linear:
 
     def dgrad(self, dy, offsets=None, out=None, out_dtype=None, stream=None):
         """dr_linear_dgrad: the gradient of x, dy W."""
-        self._operand(dy, self.out_features, "dy")
-        dx = self._out(out, dy.shape[0], self.in_features, out_dtype, dy.device, "out")
-        rc = dr_linear_dgrad(self.handle, dy.data_ptr(), _ld(dy), dy.shape[0], self._offsets(offsets), dx.data_ptr(), _ld(dx),
-                             _code_of(dx, "out"), _current_stream(stream))
+        rows, lddy = self._operand(dy, self.out_features, "dy")
+        dx, lddx = self._out(out, rows, self.in_features, out_dtype, dy, "out")
+        rc = _fn("dr_linear_dgrad")(self.handle, dy.data_ptr(), lddy, rows, self._offsets(offsets), dx.data_ptr(), lddx,
+                                    _code_of(dx, "out"), _stream_of(dy, stream))
         if rc:
             raise DrError(rc, "dr_linear_dgrad")
         return dx
 
     def wgrad(self, x, dy, offsets=None, out=None, accumulate=False, stream=None):
         """dr_linear_wgrad: the gradient of the weight in fp32, dy^T x group by group; accumulate adds it to `out`."""
-        import torch
-        self._operand(x, self.in_features, "x")
-        self._operand(dy, self.out_features, "dy")
-        if x.shape[0] != dy.shape[0]:
+        rows, ldx = self._operand(x, self.in_features, "x")
+        dy_rows, lddy = self._operand(dy, self.out_features, "dy")
+        if rows != dy_rows:
             raise ValueError("x and dy must have the same rows")
         if accumulate and out is None:
             raise ValueError("accumulate adds to `out`: give one")
-        dw = self._out(out, self.weight.shape[0], self.in_features, torch.float32, x.device, "out")
-        if dw.dtype != torch.float32:
+        if out is None:
+            import torch
+            out = torch.empty(self.n_groups * self.out_features, self.in_features, dtype=torch.float32, device=x.device)
+        dw, lddw = self._out(out, self.n_groups * self.out_features, self.in_features, None, x, "out")
+        if _code_of(dw, "out") != DR_F32:
             raise TypeError("the gradient of the weight is fp32")
-        rc = dr_linear_wgrad(self.handle, x.data_ptr(), _ld(x), dy.data_ptr(), _ld(dy), x.shape[0], self._offsets(offsets),
-                             dw.data_ptr(), _ld(dw), int(accumulate), _current_stream(stream))
+        rc = _fn("dr_linear_wgrad")(self.handle, x.data_ptr(), ldx, dy.data_ptr(), lddy, rows, self._offsets(offsets),
+                                    dw.data_ptr(), lddw, int(accumulate), _stream_of(x, stream))
         if rc:
             raise DrError(rc, "dr_linear_wgrad")
         return dw

@@ -4,10 +4,15 @@
 
 #include "dr_internal.h"
 
+namespace dr {
+constexpr uint32_t kMaxSplit = 8;  // CTAs of a cluster that share a contraction
+}
+
 struct dr_linear {
     dr_linear_desc d{};  // strides filled in
     int device = -1;
     int sms = 0;
+    uint32_t fit[dr::kMaxSplit + 1] = {};  // clusters of each size that the device runs at the same time
     bool fp8 = false;
 };
 
@@ -41,6 +46,11 @@ bool linear_tc_takes(const LinearCall& c);
 int launch_linear_tc(const LinearCall& c);
 int prepare_linear_tc();                    // once per device
 int linear_wait_failures(uint64_t* out);    // bounded waits that ran out (expected: 0)
+
+// linear_small.cu: forward with few rows a group, the same operands
+int launch_linear_small(const LinearCall& c);
+int prepare_linear_small(uint32_t (&fit)[kMaxSplit + 1]);
+int linear_small_wait_failures(uint64_t* out);
 
 // Rows [lo, hi) of group e, held inside [0, rows] and never descending, whatever the offsets hold.
 __device__ __forceinline__ void group_rows(const int32_t* offsets, uint32_t e, uint32_t rows, uint32_t& lo, uint32_t& hi)

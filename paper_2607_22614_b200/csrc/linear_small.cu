@@ -1,0 +1,519 @@
+// Forward products of few rows (decoding): the weights are read once at the memory's rate, everything else hides behind that.
+//
+// D[n, r] = sum_k W[n, k] x[r, k] with 128 features on the M side of a CTA's product and a group's rows, at most 64 at a time in
+// steps of 16, on its N side.  Bound: HBM, the weights' bytes; a stage is 16 KB of weights and 2 KB for each 16 rows, seven
+// stages keep 112 KB of weights in flight on every SM.  There is no time to lose in filling the machine either: with
+// fewer feature blocks than SMs, a cluster of up to eight CTAs splits the contraction, and its CTAs add their fp32 sums through
+// distributed shared memory, always in the order of their ranks.
+//
+// Roles: warp 0 copies the operands, 1 issues the products, 2 copies the scales (fp8), 4-7 read the accumulators.  fp8 takes a new
+// accumulator (eight of 64 columns in turn) for every block of 128 of the contraction, scales it and adds it to fp32 sums in
+// registers, as the kernel for many rows does.
+#include "linear.h"
+#include "tc_map.h"
+#include "tc_ptx.cuh"
+
+namespace dr {
+namespace {
+
+using namespace tc;
+
+__device__ unsigned long long g_wait_failures;
+
+constexpr uint32_t kRowsTile = 64, kStages = 7, kWeightBytes = 16384, kStageBytes = kWeightBytes + kRowsTile * 128;
+constexpr uint32_t kThreads = 256, kBuffers = 512 / kRowsTile;
+constexpr uint32_t kScratchPitch = 80;
+constexpr uint32_t kTurnPitch = 36;  // floats
+
+struct Shared {
+    alignas(1024) uint8_t stage[kStages][kStageBytes];
+    alignas(16) float turn[4][16][kTurnPitch];              // a warp's features of 16 rows, on their way to the cluster
+    alignas(16) float sums[kRowsTile + kMaxSplit][128];     // [CTA][its rows that end here][features]
+    alignas(16) uint8_t scratch[4][8 * kScratchPitch];
+    alignas(16) float scale[kBuffers][kRowsTile + 4];  // the rows' scales of a block, then the weight's
+    uint64_t full[kStages], empty[kStages];
+    uint64_t acc_full[kBuffers], acc_empty[kBuffers], scale_full[kBuffers], scale_empty[kBuffers];
+    uint64_t sums_full, sums_empty;
+    uint32_t tmem, stop;
+    uint32_t tiles_before[kMaxTcGroups + 1];  // row tiles of the groups before
+};
+
+struct Args {
+    const int32_t* offsets;
+    const float* a_scale;
+    const float* b_scale;
+    void* c;
+    uint64_t ld_as, ld_bs, ldc;
+    uint32_t rows, n_groups, n, k;
+    uint32_t feature_blocks;
+    uint32_t split;  // CTAs of a cluster
+    uint32_t c_f32, vector;
+};
+
+struct Tile {
+    uint32_t e, row0, row_end, feature, nt;  // feature: row of the stacked weight; nt: N of the product
+    uint32_t step0, steps;                   // this CTA's part of the contraction
+};
+
+template <bool FP8>
+struct Walk {
+    static constexpr uint32_t kStep = FP8 ? 128 : 64;
+    uint32_t e = 0;
+    __device__ __forceinline__ bool get(const Args& a, const Shared& s, uint32_t t, Tile& o)
+    {
+        while (e < a.n_groups && t >= s.tiles_before[e + 1] * a.feature_blocks) ++e;
+        if (e >= a.n_groups) return false;
+        uint32_t lo, hi;
+        group_rows(a.offsets, e, a.rows, lo, hi);
+        const uint32_t tiles = s.tiles_before[e + 1] - s.tiles_before[e], i = t - s.tiles_before[e] * a.feature_blocks;
+        const uint32_t f = i / tiles, m = i - f * tiles;  // the tiles of one feature block follow each other: its weights stay in L2
+        const uint32_t first = e * a.n;
+        o.e = e;
+        o.nt = ((hi - lo + tiles - 1) / tiles + 15) / 16 * 16;
+        o.row0 = lo + m * o.nt;
+        o.row_end = min(hi, o.row0 + o.nt);
+        o.feature = (FP8 ? first / 128 * 128 : first) + f * 128;
+        if (o.feature >= first + a.n || o.row0 >= o.row_end) o.nt = 0;
+        const uint32_t all = (a.k + kStep - 1) / kStep, part = a.split > 1 ? cta_rank() : 0;
+        o.step0 = part * all / a.split;
+        o.steps = (part + 1) * all / a.split - o.step0;
+        return true;
+    }
+};
+
+// Eight rows (columns of the accumulator) of the warp's 32 features, as the kernel for many rows stores them.
+__device__ __forceinline__ void store_rows(const Args& a, uint32_t scratch, uint32_t row, uint32_t row_end, int f, const float (&v)[4][2])
+{
+    const uint32_t lane = threadIdx.x & 31;
+    if (a.vector) {
+        __syncwarp();
+        store_transposed(scratch + (lane & 7) * kScratchPitch + (lane >> 3) * 16, pack_bf16(v[0][0], v[0][1]),
+                         pack_bf16(v[1][0], v[1][1]), pack_bf16(v[2][0], v[2][1]), pack_bf16(v[3][0], v[3][1]));
+        __syncwarp();
+        const uint32_t r = row + (lane >> 2);
+        const int ff = f + (int)(lane & 3) * 8;
+        uint32_t w[4];
+        asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];"
+                     : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3])
+                     : "r"(scratch + (lane >> 2) * kScratchPitch + (lane & 3) * 16));
+        if (r < row_end && ff >= 0 && ff < (int)a.n) *(uint4*)((uint16_t*)a.c + (uint64_t)r * a.ldc + ff) = make_uint4(w[0], w[1], w[2], w[3]);
+        return;
+    }
+#pragma unroll
+    for (int g = 0; g < 4; ++g)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const uint32_t r = row + 2 * (lane & 3) + i;
+            const int ff = f + (int)(lane >> 2) + 8 * g;
+            if (r >= row_end || ff < 0 || ff >= (int)a.n) continue;
+            if (a.c_f32)
+                ((float*)a.c)[(uint64_t)r * a.ldc + ff] = v[g][i];
+            else
+                ((uint16_t*)a.c)[(uint64_t)r * a.ldc + ff] = (uint16_t)pack_bf16(v[g][i], 0.0f);
+        }
+}
+
+template <bool FP8>
+__device__ __forceinline__ void produce(const Args& a, Shared& s, const CUtensorMap* map_w, const CUtensorMap* map_x, uint32_t first, uint32_t stride)
+{
+    constexpr uint32_t kStep = Walk<FP8>::kStep;
+    const uint32_t stages = smem_u32(s.stage), full = smem_u32(s.full), empty = smem_u32(s.empty);
+    Turn<kStages> ring;
+    uint32_t used = 0;  // stages in use, up to all of them
+    Walk<FP8> walk;
+    Tile t;
+    bool ok = true;
+    for (uint32_t i = first; ok && walk.get(a, s, i, t); i += stride) {
+        if (t.nt == 0) continue;
+        for (uint32_t l = t.step0; l < t.step0 + t.steps; ++l) {
+            const uint32_t at = stages + ring.slot * kStageBytes, bar = full + 8 * ring.slot;
+            ok = warp_wait(empty + 8 * ring.slot, ring.round ^ 1, &s.stop, &g_wait_failures);
+            if (!ok) break;
+            if (elect()) {
+                bar_expect(bar, kWeightBytes + t.nt * 128);
+                load_2d<false>(at, map_w, bar, l * kStep, t.feature);
+                for (uint32_t r = 0; r < t.nt; r += 16) load_2d<false>(at + kWeightBytes + r * 128, map_x, bar, l * kStep, t.row0 + r);
+            }
+            ring.next();
+            used = min(used + 1, kStages);
+        }
+    }
+    drain(ring, used, empty, &s.stop, &g_wait_failures);
+}
+
+template <bool FP8>
+__device__ __forceinline__ void multiply(const Args& a, Shared& s, uint32_t first, uint32_t stride)
+{
+    const uint32_t full = smem_u32(s.full), empty = smem_u32(s.empty);
+    const uint32_t acc_full = smem_u32(s.acc_full), acc_empty = smem_u32(s.acc_empty), tmem = s.tmem;
+    const uint64_t first_a = operand(smem_u32(s.stage), 0), first_b = operand(smem_u32(s.stage) + kWeightBytes, 0);
+    Turn<kStages> ring;
+    Turn<kBuffers> acc;
+    Walk<FP8> walk;
+    Tile t;
+    for (uint32_t i = first; walk.get(a, s, i, t); i += stride) {
+        if (t.nt == 0) continue;
+        const uint32_t shape = shape_of(FP8, false, false, 128, t.nt);
+        for (uint32_t l = 0; l < t.steps; ++l) {
+            if (FP8 || l == 0)
+                if (!warp_wait(acc_empty + 8 * acc.slot, acc.round ^ 1, &s.stop, &g_wait_failures)) return;
+            if (!warp_wait(full + 8 * ring.slot, ring.round, &s.stop, &g_wait_failures)) return;
+            fence_after();
+            const uint64_t da = first_a + ring.slot * (kStageBytes >> 4), db = first_b + ring.slot * (kStageBytes >> 4);
+            const bool last = FP8 || l + 1 == t.steps;
+            if (elect()) {
+#pragma unroll
+                for (uint32_t q = 0; q < 4; ++q)
+                    mma<1, FP8>(tmem + acc.slot * kRowsTile, da + 2 * q, db + 2 * q, shape, FP8 ? q != 0 : (l | q) != 0);
+                if (last) commit<1>(acc_full + 8 * acc.slot);
+                commit<1>(empty + 8 * ring.slot);
+            }
+            __syncwarp();
+            ring.next();
+            if (last) acc.next();
+        }
+    }
+}
+
+__device__ __forceinline__ void copy_scales(const Args& a, Shared& s, uint32_t first, uint32_t stride)
+{
+    const uint32_t lane = threadIdx.x & 31, full = smem_u32(s.scale_full), empty = smem_u32(s.scale_empty);
+    const uint32_t scale_rows = (a.n_groups * a.n + 127) / 128;
+    uint32_t n = 0;
+    Walk<true> walk;
+    Tile t;
+    for (uint32_t i = first; walk.get(a, s, i, t); i += stride) {
+        if (t.nt == 0) continue;
+        const float* xs = a.a_scale + t.row0;
+        const float* ws = a.b_scale + (uint64_t)min(t.feature / 128, scale_rows - 1) * a.ld_bs;
+        const uint32_t left = t.row_end - t.row0;
+        for (uint32_t l = t.step0; l < t.step0 + t.steps; ++l, ++n) {
+            const uint32_t slot = n % kBuffers, to = smem_u32(s.scale[slot]);
+            if (!__all_sync(0xFFFFFFFFu, bar_wait(empty + 8 * slot, (n / kBuffers & 1) ^ 1, &s.stop, &g_wait_failures))) return;
+#pragma unroll
+            for (uint32_t j = lane; j < kRowsTile; j += 32) copy_4(to + 4 * j, xs + l * a.ld_as + (j < left ? j : 0), j < left);
+            if (lane == 0) copy_4(to + 4 * kRowsTile, ws + l, true);
+            copies_arrive(full + 8 * slot);
+        }
+    }
+}
+
+template <bool FP8>
+__device__ __forceinline__ void write_out(const Args& a, Shared& s, uint32_t first, uint32_t stride)
+{
+    const uint32_t lane = threadIdx.x & 31, warp = (threadIdx.x >> 5) - 4;
+    const uint32_t acc_full = smem_u32(s.acc_full), acc_empty = smem_u32(s.acc_empty);
+    const uint32_t scale_full = smem_u32(s.scale_full), scale_empty = smem_u32(s.scale_empty);
+    const uint32_t scratch = smem_u32(s.scratch[warp]), tmem = s.tmem + (warp * 32 << 16);
+    uint32_t acc = 0, handed = 0;
+    Walk<FP8> walk;
+    Tile t;
+    for (uint32_t i = first; walk.get(a, s, i, t); i += stride) {
+        if (t.nt == 0) continue;
+        float sum[2][2][16];
+        if (FP8 || t.steps == 0) {
+#pragma unroll
+            for (int c = 0; c < 2; ++c)
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) sum[c][h][r] = 0.0f;
+        }
+        const uint32_t products = FP8 ? t.steps : t.steps ? 1 : 0;
+        for (uint32_t l = 0; l < products; ++l, ++acc) {
+            const uint32_t buffer = acc % kBuffers, parity = acc / kBuffers & 1;
+            bool ok = !FP8 || bar_wait(scale_full + 8 * buffer, parity, &s.stop, &g_wait_failures);
+            ok = ok && bar_wait(acc_full + 8 * buffer, parity, &s.stop, &g_wait_failures);
+            if (!__all_sync(0xFFFFFFFFu, ok)) return;
+            fence_after();
+            const uint32_t from = tmem + buffer * kRowsTile;
+            if (FP8) {
+                const float* sc = s.scale[buffer] + 2 * (lane & 3);
+                const float w = s.scale[buffer][kRowsTile];
+                const uint64_t ww = pair_of(w, w);
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    if (c * 32 >= t.nt) break;
+                    float p[2][16];
+                    tmem_load(from + c * 32, p[0], p[1]);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const uint64_t two = mul2(*(const uint64_t*)(sc + c * 32 + j * 8), ww);
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            fma2(sum[c][h][4 * j], sum[c][h][4 * j + 1], p[h][4 * j], p[h][4 * j + 1], two);
+                            fma2(sum[c][h][4 * j + 2], sum[c][h][4 * j + 3], p[h][4 * j + 2], p[h][4 * j + 3], two);
+                        }
+                    }
+                }
+            } else {
+                tmem_load(from, sum[0][0], sum[0][1]);
+                if (t.nt > 32) tmem_load(from + 32, sum[1][0], sum[1][1]);
+            }
+            fence_before();
+            __syncwarp();
+            if (lane == 0) {
+                bar_arrive(acc_empty + 8 * buffer);
+                if (FP8) bar_arrive(scale_empty + 8 * buffer);
+            }
+        }
+        const int f = (int)(t.feature + warp * 32 - t.e * a.n);  // in a row of c
+        if (a.split == 1) {
+#pragma unroll
+            for (int c = 0; c < 2; ++c)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    if (c * 32 + j * 8 >= t.nt) break;
+                    const float v[4][2] = {{sum[c][0][4 * j], sum[c][0][4 * j + 1]}, {sum[c][0][4 * j + 2], sum[c][0][4 * j + 3]},
+                                           {sum[c][1][4 * j], sum[c][1][4 * j + 1]}, {sum[c][1][4 * j + 2], sum[c][1][4 * j + 3]}};
+                    store_rows(a, scratch, t.row0 + c * 32 + j * 8, t.row_end, f, v);
+                }
+            continue;
+        }
+        // Every row of the tile ends in one CTA of the cluster (row r in CTA r mod split): the others send it their sums with
+        // stores that count on its barrier, so that no CTA waits on a fence, and it adds them in the order of the ranks.
+        const uint32_t rank = cta_rank(), rows = t.row_end - t.row0;
+        const uint32_t most = (kRowsTile + a.split - 1) / a.split, owned = rows > rank ? (rows - rank + a.split - 1) / a.split : 0;
+        if (!__all_sync(0xFFFFFFFFu, bar_wait(smem_u32(&s.sums_empty), (handed & 1) ^ 1, &s.stop, &g_wait_failures))) return;
+        if (warp == 0 && lane == 0) bar_expect(smem_u32(&s.sums_full), owned * a.split * 512);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {  // sixteen rows at a time
+            if (c * 16 >= t.nt) break;
+            __syncwarp();
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int g = 0; g < 4; ++g)
+#pragma unroll
+                    for (int q = 0; q < 2; ++q)
+                        s.turn[warp][j * 8 + 2 * (lane & 3) + q][(lane >> 2) + 8 * g] =
+                            sum[c >> 1][g >> 1][4 * ((c & 1) * 2 + j) + 2 * (g & 1) + q];
+            __syncwarp();
+#pragma unroll
+            for (uint32_t i = 0; i < 4; ++i) {
+                const uint32_t r = c * 16 + i * 4 + (lane >> 3);
+                if (r >= rows) continue;
+                const float4 v = *(const float4*)&s.turn[warp][r & 15][(lane & 7) * 4];
+                const uint32_t to = r % a.split;
+                store_counted(in_cta(smem_u32(&s.sums[rank * most + r / a.split][warp * 32 + (lane & 7) * 4]), to), v,
+                              in_cta(smem_u32(&s.sums_full), to));
+            }
+        }
+        if (!__all_sync(0xFFFFFFFFu, bar_wait(smem_u32(&s.sums_full), handed & 1, &s.stop, &g_wait_failures))) return;
+        for (uint32_t o = warp; o < owned; o += 4) {
+            float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+            for (uint32_t q = 0; q < a.split; ++q) {
+                const float4 p = *(const float4*)&s.sums[q * most + o][lane * 4];
+                v[0] += p.x;
+                v[1] += p.y;
+                v[2] += p.z;
+                v[3] += p.w;
+            }
+            const int ff = (int)(t.feature + lane * 4 - t.e * a.n);
+            const uint64_t at = (uint64_t)(t.row0 + rank + o * a.split) * a.ldc;
+            if (a.vector && ff >= 0 && ff < (int)a.n) {  // the rows of c are a multiple of eight features here
+                *(uint2*)((uint16_t*)a.c + at + ff) = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
+            } else if (!a.vector) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    if (ff + j < 0 || ff + j >= (int)a.n) continue;
+                    if (a.c_f32)
+                        ((float*)a.c)[at + ff + j] = v[j];
+                    else
+                        ((uint16_t*)a.c)[at + ff + j] = (uint16_t)pack_bf16(v[j], 0.0f);
+                }
+            }
+        }
+        __syncwarp();
+        if (lane < a.split) bar_arrive_cluster(in_cta(smem_u32(&s.sums_empty), lane));
+        ++handed;
+    }
+}
+
+template <bool FP8>
+__global__ void __launch_bounds__(kThreads, 1)
+    small_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x, const Args a)
+{
+    extern __shared__ uint8_t raw[];
+    Shared& s = *(Shared*)(raw + (-smem_u32(raw) & 1023));
+    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) {
+        prefetch_map(&map_w);
+        prefetch_map(&map_x);
+        for (uint32_t i = 0; i < kStages; ++i) {
+            bar_init(smem_u32(&s.full[i]), 1);
+            bar_init(smem_u32(&s.empty[i]), 1);
+        }
+        for (uint32_t i = 0; i < kBuffers; ++i) {
+            bar_init(smem_u32(&s.acc_full[i]), 1);
+            bar_init(smem_u32(&s.acc_empty[i]), 4);
+            bar_init(smem_u32(&s.scale_full[i]), 32);
+            bar_init(smem_u32(&s.scale_empty[i]), 4);
+        }
+        bar_init(smem_u32(&s.sums_full), 1);
+        bar_init(smem_u32(&s.sums_empty), 4 * a.split);
+        s.stop = 0;
+        bar_init_fence();
+    }
+    if (warp == 1) tmem_alloc<1>(smem_u32(&s.tmem), 512);
+    for (uint32_t e = threadIdx.x; e < a.n_groups; e += kThreads) {
+        uint32_t lo, hi;
+        group_rows(a.offsets, e, a.rows, lo, hi);
+        s.tiles_before[e + 1] = (hi - lo + kRowsTile - 1) / kRowsTile;
+    }
+    fence_before();
+    __syncthreads();
+    if (warp == 2) {  // running sum of the groups' row tiles
+        uint32_t before = 0;
+        if (lane == 0) s.tiles_before[0] = 0;
+        for (uint32_t e0 = 0; e0 < a.n_groups; e0 += 32) {
+            uint32_t sum = e0 + lane < a.n_groups ? s.tiles_before[e0 + lane + 1] : 0;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const uint32_t up = __shfl_up_sync(0xFFFFFFFFu, sum, o);
+                if (lane >= (uint32_t)o) sum += up;
+            }
+            if (e0 + lane < a.n_groups) s.tiles_before[e0 + lane + 1] = before + sum;
+            before += __shfl_sync(0xFFFFFFFFu, sum, 31);
+        }
+    }
+    __syncthreads();
+    if (a.split > 1) cluster_sync();
+    fence_after();
+
+    const uint32_t first = blockIdx.x / a.split, stride = gridDim.x / a.split;
+    if (warp == 0) {
+        produce<FP8>(a, s, &map_w, &map_x, first, stride);
+    } else if (warp == 1) {
+        multiply<FP8>(a, s, first, stride);
+    } else if (warp == 2) {
+        if (FP8) copy_scales(a, s, first, stride);
+    } else if (warp >= 4) {
+        write_out<FP8>(a, s, first, stride);
+    }
+    __syncwarp();
+    if (*(volatile uint32_t*)&s.stop) {  // a wait ran out: let the copies and products in flight end before the memory is given back
+        const uint64_t since = now_ns();
+        while (now_ns() - since < 10000000ull) __nanosleep(1000);
+    }
+    fence_before();
+    __syncthreads();
+    if (a.split > 1) cluster_sync();  // other CTAs may still be reading this one's sums
+    fence_after();
+    if (warp == 1) tmem_free<1>(s.tmem, 512);
+}
+
+constexpr size_t kSharedBytes = sizeof(Shared) + 1024;
+
+// CTAs that share a tile's contraction: `fit[s]` clusters of s CTAs run at the same time, so that `tiles` take
+// ceil(tiles / fit[s]) rounds of 1 / s of the contraction each.  The smallest split within 2 % of the least time wins, each part at
+// least two steps long.
+uint32_t choose_split(uint64_t tiles, const uint32_t (&fit)[kMaxSplit + 1], uint32_t steps)
+{
+    uint32_t best = 1;
+    double least = 0.0;
+    for (uint32_t s = 1; s <= kMaxSplit && (s == 1 || s * 2 <= steps); ++s) {
+        if (fit[s] == 0) continue;
+        const double rounds = (double)((tiles + fit[s] - 1) / fit[s]) / s;
+        if (s == 1 || rounds < 0.98 * least) {
+            best = s;
+            least = rounds;
+        }
+    }
+    return best;
+}
+
+cudaLaunchConfig_t config(cudaLaunchAttribute& attr, uint64_t clusters, uint32_t split, cudaStream_t stream)
+{
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = split;
+    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)(clusters * split));
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = kSharedBytes;
+    cfg.stream = stream;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    return cfg;
+}
+
+template <bool FP8>
+int launch(const LinearCall& c, const CUtensorMap& mw, const CUtensorMap& mx, const Args& a, uint64_t tiles)
+{
+    const uint64_t clusters = c.lin->fit[a.split];
+    cudaLaunchAttribute attr;
+    const cudaLaunchConfig_t cfg = config(attr, tiles < clusters ? tiles : clusters, a.split, c.stream);
+    const cudaError_t err = cudaLaunchKernelEx(&cfg, small_kernel<FP8>, mw, mx, a);
+    if (err != cudaSuccess) {
+        cudaGetLastError();
+        set_error("linear kernel launch: %s", cudaGetErrorString(err));
+        return DR_ERR_CUDA;
+    }
+    return DR_OK;
+}
+
+}  // namespace
+
+int prepare_linear_small(uint32_t (&fit)[kMaxSplit + 1])
+{
+    DR_CUDA(cudaFuncSetAttribute(small_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSharedBytes));
+    DR_CUDA(cudaFuncSetAttribute(small_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSharedBytes));
+    for (uint32_t s = 1; s <= kMaxSplit; ++s) {
+        cudaLaunchAttribute attr;
+        const cudaLaunchConfig_t cfg = config(attr, 64, s, nullptr);
+        int n = 0;
+        DR_CUDA(cudaOccupancyMaxActiveClusters(&n, small_kernel<true>, &cfg));
+        fit[s] = n > 0 ? (uint32_t)n : 0;
+    }
+    if (fit[1] == 0) {
+        set_error("the linear kernel does not fit this device");
+        return DR_ERR_CUDA;
+    }
+    return DR_OK;
+}
+
+int launch_linear_small(const LinearCall& c)
+{
+    const dr_linear_desc& d = c.lin->d;
+    const bool fp8 = c.lin->fp8;
+    Args a{};
+    a.offsets = c.offsets;
+    a.a_scale = c.a_scale;
+    a.b_scale = d.scale_dev;
+    a.c = c.c;
+    a.ld_as = c.ld_scale;
+    a.ld_bs = d.scale_ld;
+    a.ldc = c.ldc;
+    a.rows = c.rows;
+    a.n_groups = d.n_groups;
+    a.n = (uint32_t)d.out_features;
+    a.k = (uint32_t)d.in_features;
+    a.c_f32 = c.c_f32;
+    a.vector = !c.c_f32 && a.n % 8 == 0 && c.ldc % 8 == 0 && (uintptr_t)c.c % 16 == 0;
+    a.feature_blocks = (a.n + (fp8 && a.n % 128 ? 127 : 0) + 127) / 128;
+    // at most one row tile more than full ones for each group that has rows
+    const uint64_t spare = c.offsets ? (c.rows < d.n_groups ? c.rows : d.n_groups) : 0;
+    const uint64_t tiles = (c.offsets ? c.rows / kRowsTile + spare : (c.rows + kRowsTile - 1) / kRowsTile) * a.feature_blocks;
+    if (tiles > 0x7FFFFFFFull) {
+        set_error("too many output tiles for one launch");
+        return DR_ERR_UNSUPPORTED;
+    }
+    const uint32_t step = fp8 ? 128 : 64;
+    a.split = choose_split(tiles, c.lin->fit, (a.k + step - 1) / step);
+    CUtensorMap mw, mx;
+    int rc = encode_map(&mw, c.b, fp8, a.k, (uint64_t)a.n * a.n_groups, 0, c.ldb, 128);
+    if (rc == DR_OK) rc = encode_map(&mx, c.a, fp8, a.k, c.rows, 0, c.lda, 16);
+    if (rc) return rc;
+    return fp8 ? launch<true>(c, mw, mx, a, tiles) : launch<false>(c, mw, mx, a, tiles);
+}
+
+int linear_small_wait_failures(uint64_t* out)
+{
+    unsigned long long n = 0;
+    DR_CUDA(cudaMemcpyFromSymbol(&n, g_wait_failures, sizeof n));
+    *out = n;
+    return DR_OK;
+}
+
+}  // namespace dr

@@ -21,9 +21,8 @@
 // share an instruction.
 //
 // Outputs leave through a 640-byte transpose per warp: eight tokens of 32 features, 64 contiguous bytes a row.
-#include <cudaTypedefs.h>
-
 #include "linear.h"
+#include "tc_map.h"
 #include "tc_ptx.cuh"
 
 namespace dr {
@@ -31,7 +30,7 @@ namespace {
 
 using namespace tc;
 
-__device__ unsigned long long g_wait_failures;
+__device__ unsigned long long g_wait_failures;  // read by dr_diag_linear_wait_failures
 
 constexpr int kForwardRows = 3;  // forward with tokens on the M side (fp8, many rows)
 
@@ -202,7 +201,8 @@ __device__ __forceinline__ void produce(const TcArgs& a, Shared& s, const CUtens
     const uint32_t rank = cta_rank(), stages = smem_u32(s.stage), empty = smem_u32(s.empty);
     // copies signal the first CTA of the pair, which issues the products; in wgrad their own CTA, which may have rows to clear
     const uint32_t full = OP == kWgrad ? smem_u32(s.landed) : in_cta(smem_u32(s.full), 0);
-    uint32_t n = 0;
+    Turn<kStages> ring;
+    uint32_t used = 0;  // stages in use, up to all of them
     bool ok = true;
     Walk<OP, FP8> walk;
     Tile t;
@@ -211,40 +211,39 @@ __device__ __forceinline__ void produce(const TcArgs& a, Shared& s, const CUtens
         const uint32_t half = t.nt / 2, feature = t.feature + rank * 128;
         const uint32_t boxes = OP == kWgrad ? (half + 63) / 64 : (half + 31) / 32, box_bytes = OP == kWgrad ? 8192 : 4096;
         const uint32_t bytes = kOperandBytes + boxes * box_bytes;
-        for (uint32_t l = 0; l < t.steps; ++l, ++n) {
-            const uint32_t st = n % kStages;
-            ok = bar_wait(empty + 8 * st, (n / kStages & 1) ^ 1, &s.stop, &g_wait_failures);
+        for (uint32_t l = 0; l < t.steps; ++l) {
+            const uint32_t at = stages + ring.slot * kStageBytes, bar = full + 8 * ring.slot;
+            ok = warp_wait(empty + 8 * ring.slot, ring.round ^ 1, &s.stop, &g_wait_failures);
             if (!ok) break;
-            const uint32_t at = stages + st * kStageBytes, bar = full + 8 * st;
-            if (OP == kWgrad)
-                bar_expect(bar, bytes);
-            else if (rank == 0)
-                bar_expect(smem_u32(s.full) + 8 * st, 2 * bytes);
-            if (OP == kForward) {
-                load_2d<true>(at, map_a, bar, l * kStep, feature);
-            } else if (OP == kForwardRows) {
-                load_2d<true>(at, map_a, bar, l * kStep, t.row0 + rank * 128);
-            } else if (OP == kDgrad) {
-                load_3d<true>(at, map_a, bar, feature, l * kStep, t.e);
-                load_3d<true>(at + 8192, map_a, bar, feature + 64, l * kStep, t.e);
-            } else {
-                load_2d<false>(at, map_a, bar, feature, t.row0 + l * kStep);
-                load_2d<false>(at + 8192, map_a, bar, feature + 64, t.row0 + l * kStep);
-            }
-            for (uint32_t b = 0; b < boxes; ++b) {
-                const uint32_t to = at + kOperandBytes + b * box_bytes;
+            if (elect()) {
                 if (OP == kWgrad)
-                    load_2d<false>(to, map_b, bar, t.col0 + rank * half + b * 64, t.row0 + l * kStep);
-                else
-                    load_2d<true>(to, map_b, bar, l * kStep, (OP == kForwardRows ? t.feature : t.row0) + rank * half + b * 32);
+                    bar_expect(bar, bytes);
+                else if (rank == 0)
+                    bar_expect(smem_u32(s.full) + 8 * ring.slot, 2 * bytes);
+                if (OP == kForward) {
+                    load_2d<true>(at, map_a, bar, l * kStep, feature);
+                } else if (OP == kForwardRows) {
+                    load_2d<true>(at, map_a, bar, l * kStep, t.row0 + rank * 128);
+                } else if (OP == kDgrad) {
+                    load_3d<true>(at, map_a, bar, feature, l * kStep, t.e);
+                    load_3d<true>(at + 8192, map_a, bar, feature + 64, l * kStep, t.e);
+                } else {
+                    load_2d<false>(at, map_a, bar, feature, t.row0 + l * kStep);
+                    load_2d<false>(at + 8192, map_a, bar, feature + 64, t.row0 + l * kStep);
+                }
+                for (uint32_t b = 0; b < boxes; ++b) {
+                    const uint32_t to = at + kOperandBytes + b * box_bytes;
+                    if (OP == kWgrad)
+                        load_2d<false>(to, map_b, bar, t.col0 + rank * half + b * 64, t.row0 + l * kStep);
+                    else
+                        load_2d<true>(to, map_b, bar, l * kStep, (OP == kForwardRows ? t.feature : t.row0) + rank * half + b * 32);
+                }
             }
+            ring.next();
+            used = min(used + 1, kStages);
         }
     }
-    // every stage given back before this CTA may end: no commit of the pair is still on its way here
-    for (uint32_t q = 0; q < kStages && q < n; ++q) {
-        const uint32_t m = n - 1 - q;
-        if (!bar_wait(empty + 8 * (m % kStages), m / kStages & 1, &s.stop, &g_wait_failures)) break;
-    }
+    if (ok) drain(ring, used, empty, &s.stop, &g_wait_failures);
 }
 
 template <int OP, bool FP8>
@@ -254,31 +253,32 @@ __device__ __forceinline__ void multiply(const TcArgs& a, Shared& s)
     const uint32_t acc_full = smem_u32(s.acc_full), acc_empty = smem_u32(s.acc_empty), tmem = s.tmem;
     constexpr bool a_mn = OP == kDgrad || OP == kWgrad, b_mn = OP == kWgrad;
     const uint64_t first_a = operand(stages, 8192), first_b = operand(stages + kOperandBytes, 8192);
-    uint32_t n = 0, acc = 0;
-    bool ok = true;
+    Turn<kStages> ring;
+    Turn<2> acc;
     Walk<OP, FP8> walk;
     Tile t;
-    for (uint32_t i = blockIdx.x >> 1; ok && walk.get(a, s, i, t); i += gridDim.x >> 1) {
+    for (uint32_t i = blockIdx.x >> 1; walk.get(a, s, i, t); i += gridDim.x >> 1) {
         if (t.nt == 0 || t.steps == 0) continue;
         const uint32_t shape = shape_of(FP8, a_mn, b_mn, 256, t.nt);
-        for (uint32_t l = 0; l < t.steps; ++l, ++n) {
-            if (FP8 || l == 0) {
-                ok = bar_wait(acc_empty + 8 * (acc & 1), (acc >> 1 & 1) ^ 1, &s.stop, &g_wait_failures);
-                if (!ok) return;
-            }
-            const uint32_t st = n % kStages;
-            ok = bar_wait(full + 8 * st, n / kStages & 1, &s.stop, &g_wait_failures);
-            if (!ok) return;
+        for (uint32_t l = 0; l < t.steps; ++l) {
+            if (FP8 || l == 0)
+                if (!warp_wait(acc_empty + 8 * acc.slot, acc.round ^ 1, &s.stop, &g_wait_failures)) return;
+            if (!warp_wait(full + 8 * ring.slot, ring.round, &s.stop, &g_wait_failures)) return;
             fence_after();
-            const uint32_t d = tmem + (acc & 1) * kTile;
             // addresses are the low bits of a descriptor, in units of 16 bytes
-            const uint64_t da = first_a + st * (kStageBytes >> 4), db = first_b + st * (kStageBytes >> 4);
+            const uint64_t da = first_a + ring.slot * (kStageBytes >> 4), db = first_b + ring.slot * (kStageBytes >> 4);
+            const bool last = FP8 || l + 1 == t.steps;
+            if (elect()) {
 #pragma unroll
-            for (uint32_t q = 0; q < 4; ++q)
-                mma<2, FP8>(d, da + q * ((a_mn ? 2048 : 32) >> 4), db + q * ((b_mn ? 2048 : 32) >> 4), shape,
-                            FP8 ? q != 0 : (l | q) != 0);
-            commit<2>(empty + 8 * st);
-            if (FP8 || l + 1 == t.steps) commit<2>(acc_full + 8 * (acc++ & 1));
+                for (uint32_t q = 0; q < 4; ++q)
+                    mma<2, FP8>(tmem + acc.slot * kTile, da + q * ((a_mn ? 2048 : 32) >> 4), db + q * ((b_mn ? 2048 : 32) >> 4), shape,
+                                FP8 ? q != 0 : (l | q) != 0);
+                if (last) commit<2>(acc_full + 8 * acc.slot);
+                commit<2>(empty + 8 * ring.slot);
+            }
+            __syncwarp();
+            ring.next();
+            if (last) acc.next();
         }
     }
 }
@@ -593,9 +593,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads<OP>, 1)
         else if (FP8)
             asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
         if (warp == 0) {
-            if (lane == 0) produce<OP, FP8>(a, s, &map_a, &map_b);
+            produce<OP, FP8>(a, s, &map_a, &map_b);
         } else if (warp == 1) {
-            if (lane == 0 && cta_rank() == 0) multiply<OP, FP8>(a, s);
+            if (cta_rank() == 0) multiply<OP, FP8>(a, s);
         } else if (warp == 2) {
             if (FP8 && OP == kForward) copy_scales(a, s);
             if (OP == kWgrad) clear_rows(a, s);
@@ -620,41 +620,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads<OP>, 1)
     cluster_sync();
     fence_after();
     if (warp == 1) tmem_free<2>(s.tmem, 512);
-}
-
-PFN_cuTensorMapEncodeTiled_v12000 encoder()
-{
-    static PFN_cuTensorMapEncodeTiled_v12000 fn = [] {
-        void* p = nullptr;
-        cudaDriverEntryPointQueryResult r;
-        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &r) != cudaSuccess ||
-            r != cudaDriverEntryPointSuccess) {
-            cudaGetLastError();
-            p = nullptr;
-        }
-        return (PFN_cuTensorMapEncodeTiled_v12000)p;
-    }();
-    return fn;
-}
-
-// A map over rows of `ld` elements, `cols` of them valid, boxes of 128 bytes x box_rows; `groups` > 0 adds a third dimension
-// of `rows` rows each.
-int encode(CUtensorMap* map, const void* base, bool fp8, uint64_t cols, uint64_t rows, uint64_t groups, uint64_t ld, uint32_t box_rows)
-{
-    const uint32_t es = fp8 ? 1 : 2;
-    const cuuint64_t dims[3] = {cols, rows, groups};
-    const cuuint64_t strides[2] = {ld * es, rows * ld * es};
-    const cuuint32_t box[3] = {128 / es, box_rows, 1}, step[3] = {1, 1, 1};
-    PFN_cuTensorMapEncodeTiled_v12000 fn = encoder();
-    const CUresult r = fn ? fn(map, fp8 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, groups ? 3 : 2,
-                               (void*)base, dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-                               CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE)
-                          : CUDA_ERROR_NOT_SUPPORTED;
-    if (r != CUDA_SUCCESS) {
-        set_error("tensor map: driver error %d", (int)r);
-        return DR_ERR_CUDA;
-    }
-    return DR_OK;
 }
 
 constexpr size_t kSharedBytes = sizeof(Shared) + 1024;
@@ -739,8 +704,8 @@ int launch_linear_tc(const LinearCall& c)
         a.column_tiles = (a.k + kTile - 1) / kTile;
         tiles = (uint64_t)a.feature_tiles * a.column_tiles * a.n_groups;
         a.vector = a.k % 2 == 0 && c.ldc % 2 == 0 && (uintptr_t)c.c % 8 == 0;
-        rc = encode(&ma, c.a, false, a.n, c.rows, 0, c.lda, 64);
-        if (rc == DR_OK) rc = encode(&mb, c.b, false, a.k, c.rows, 0, c.ldb, 64);
+        rc = encode_map(&ma, c.a, false, a.n, c.rows, 0, c.lda, 64);
+        if (rc == DR_OK) rc = encode_map(&mb, c.b, false, a.k, c.rows, 0, c.ldb, 64);
     } else {
         const uint32_t width = c.op == kForward ? a.n : a.k;
         a.feature_tiles = (width + (fp8 && a.n % 128 ? 127 : 0) + kTile - 1) / kTile;
@@ -748,13 +713,13 @@ int launch_linear_tc(const LinearCall& c)
         a.vector = !c.c_f32 && width % 8 == 0 && c.ldc % 8 == 0 && (uintptr_t)c.c % 16 == 0;
         if (by_rows) {
             a.vector = width % 16 == 0 && c.ldc % (c.c_f32 ? 8 : 16) == 0 && (uintptr_t)c.c % 32 == 0;
-            rc = encode(&ma, c.a, true, a.k, c.rows, 0, c.lda, 128);
-            if (rc == DR_OK) rc = encode(&mb, c.b, true, a.k, (uint64_t)a.n * a.n_groups, 0, c.ldb, 32);
+            rc = encode_map(&ma, c.a, true, a.k, c.rows, 0, c.lda, 128);
+            if (rc == DR_OK) rc = encode_map(&mb, c.b, true, a.k, (uint64_t)a.n * a.n_groups, 0, c.ldb, 32);
         } else if (c.op == kForward)
-            rc = encode(&ma, c.b, fp8, a.k, (uint64_t)a.n * a.n_groups, 0, c.ldb, 128);
+            rc = encode_map(&ma, c.b, fp8, a.k, (uint64_t)a.n * a.n_groups, 0, c.ldb, 128);
         else
-            rc = encode(&ma, c.b, false, a.k, a.n, a.n_groups, c.ldb, 64);
-        if (rc == DR_OK && !by_rows) rc = encode(&mb, c.a, fp8, c.op == kForward ? a.k : a.n, c.rows, 0, c.lda, 32);
+            rc = encode_map(&ma, c.b, false, a.k, a.n, a.n_groups, c.ldb, 64);
+        if (rc == DR_OK && !by_rows) rc = encode_map(&mb, c.a, fp8, c.op == kForward ? a.k : a.n, c.rows, 0, c.lda, 32);
     }
     if (rc) return rc;
     if (tiles > 0x7FFFFFFFull) {

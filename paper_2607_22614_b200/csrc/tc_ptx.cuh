@@ -86,6 +86,59 @@ __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile
     return true;
 }
 
+// The same by a whole warp, with one answer for all lanes.  The roles that issue copies and products run their loops with all lanes
+// and let one elected lane issue: the compiler then keeps addresses and descriptors in uniform registers, where these
+// instructions want them (with a single lane in the loop every operand is moved there first: 70 cycles a product, measured).
+static __device__ __noinline__ bool warp_wait_long(uint32_t bar, uint32_t parity, volatile uint32_t* stop, unsigned long long* failures)
+{
+    return __all_sync(0xFFFFFFFFu, bar_wait(bar, parity, stop, failures));
+}
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile uint32_t* stop, unsigned long long* failures)
+{
+    if (__all_sync(0xFFFFFFFFu, bar_try(bar, parity))) return true;
+    return warp_wait_long(bar, parity, stop, failures);
+}
+__device__ __forceinline__ bool elect()
+{
+    uint32_t p;
+    asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xFFFFFFFF;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(p));
+    return p;
+}
+// A place in a ring of N slots and the parity of its round.
+template <uint32_t N>
+struct Turn {
+    uint32_t slot = 0, round = 0;
+    __device__ __forceinline__ void next()
+    {
+        if (++slot == N) {
+            slot = 0;
+            round ^= 1;
+        }
+    }
+};
+
+// Waits until the last `used` slots before the ring's place have been given back: their copies have landed and the commits that
+// freed them have arrived, so that the CTA may end.
+template <uint32_t N>
+__device__ __forceinline__ void drain(Turn<N> ring, uint32_t used, uint32_t empty, volatile uint32_t* stop, unsigned long long* failures)
+{
+    for (; used; --used) {
+        if (ring.slot-- == 0) {
+            ring.slot = N - 1;
+            ring.round ^= 1;
+        }
+        if (!warp_wait(empty + 8 * ring.slot, ring.round, stop, failures)) return;
+    }
+}
+
+// 16 bytes to the shared memory of a CTA of the cluster, counted on a barrier of that CTA: whoever waits for the barrier sees them.
+__device__ __forceinline__ void store_counted(uint32_t dst, const float4& v, uint32_t bar)
+{
+    asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v4.b32 [%0], {%1, %2, %3, %4}, [%5];" ::"r"(dst),
+                 "r"(__float_as_uint(v.x)), "r"(__float_as_uint(v.y)), "r"(__float_as_uint(v.z)), "r"(__float_as_uint(v.w)), "r"(bar)
+                 : "memory");
+}
+
 // ---- tensor-map copies ---------------------------------------------------------------------------------------------
 // Completion is counted in bytes on `bar`, which for the PAIR form may lie in either CTA of the pair.
 template <bool PAIR>
