@@ -41,7 +41,7 @@ struct LinearCall {
 int launch_linear_simt(const LinearCall& c);  // linear_simt.cu: every stride and alignment
 
 // linear_tc.cu: tensor cores, for operands that tensor maps can read
-constexpr uint32_t kMaxTcGroups = 1024;     // groups whose tile counts fit a CTA's table
+constexpr uint32_t kMaxTcGroups = 512;      // groups whose tile counts fit a CTA's table
 bool linear_tc_takes(const LinearCall& c);
 int launch_linear_tc(const LinearCall& c);
 int prepare_linear_tc();                    // once per device

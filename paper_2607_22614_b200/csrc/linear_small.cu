@@ -334,8 +334,12 @@ template <bool FP8>
 __global__ void __launch_bounds__(kThreads, 1)
     small_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x, const Args a)
 {
-    extern __shared__ uint8_t raw[];
-    Shared& s = *(Shared*)(raw + (-smem_u32(raw) & 1023));
+    extern __shared__ __align__(1024) uint8_t raw[];
+    Shared& s = *(Shared*)raw;
+    if (smem_u32(raw) & 1023) {  // the swizzled stages need the alignment asked for; nothing has been started yet
+        if (threadIdx.x == 0) atomicAdd(&g_wait_failures, 1ull);
+        return;
+    }
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         prefetch_map(&map_w);
@@ -403,7 +407,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     if (warp == 1) tmem_free<1>(s.tmem, 512);
 }
 
-constexpr size_t kSharedBytes = sizeof(Shared) + 1024;
+constexpr size_t kSharedBytes = sizeof(Shared);
 
 // CTAs that share a tile's contraction: `fit[s]` clusters of s CTAs run at the same time, so that `tiles` take
 // ceil(tiles / fit[s]) rounds of 1 / s of the contraction each.  The smallest split within 2 % of the least time wins, each part at

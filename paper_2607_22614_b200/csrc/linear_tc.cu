@@ -34,25 +34,36 @@ __device__ unsigned long long g_wait_failures;  // read by dr_diag_linear_wait_f
 
 constexpr int kForwardRows = 3;  // forward with tokens on the M side (fp8, many rows)
 
-constexpr uint32_t kStages = 6, kStageBytes = 32768, kOperandBytes = 16384;
-constexpr uint32_t kScratchWarps = 8;    // of the kernels that write through the transpose
-template <int OP> constexpr uint32_t kEpilogueWarps = OP == kForwardRows ? 16 : 8;
-template <int OP> constexpr uint32_t kThreads = 128 + 32 * kEpilogueWarps<OP>;
+template <int OP> constexpr uint32_t kStages = OP == kForwardRows ? 5 : 6;
+constexpr uint32_t kStageBytes = 32768, kOperandBytes = 16384;
+constexpr uint32_t kEpilogueWarps = 8;
+constexpr uint32_t kThreads = 128 + 32 * kEpilogueWarps;
 constexpr uint32_t kTile = 256;          // features and tokens of a pair's tile
 constexpr uint32_t kScaleSlots = 8;
 constexpr uint32_t kScratchPitch = 80;   // bytes between tokens of the transpose: 16-byte units of eight rows fall on different banks
 constexpr uint32_t kBand = 16;           // token tiles a band of a large group holds
 
-struct Shared {
-    alignas(1024) uint8_t stage[kStages][kStageBytes];
-    alignas(16) uint8_t scratch[kScratchWarps][8 * kScratchPitch];
-    alignas(16) float scale[kScaleSlots][kTile];
-    uint64_t full[kStages], empty[kStages], landed[kStages];
+struct Barriers {
+    uint64_t full[6], empty[6], landed[6];
     uint64_t acc_full[2], acc_empty[2];
     uint64_t scale_full[kScaleSlots], scale_empty[kScaleSlots];
     uint32_t tmem, stop;
     uint32_t tiles_before[kMaxTcGroups + 1];  // token tiles of the groups before
 };
+template <int OP>
+struct Buffers {
+    alignas(1024) uint8_t stage[kStages<OP>][kStageBytes];
+    alignas(16) uint8_t scratch[kEpilogueWarps][8 * kScratchPitch];
+    alignas(16) float scale[kScaleSlots][kTile];
+};
+template <>
+struct Buffers<kForwardRows> {
+    alignas(1024) uint8_t stage[kStages<kForwardRows>][kStageBytes];
+    alignas(1024) uint8_t out[8][2][4096];  // twice 32 rows of 64 bf16 for each warp, on their way out
+};
+template <int OP>
+struct Shared : Buffers<OP>, Barriers {};
+static_assert(sizeof(Shared<kForward>) <= 227 * 1024 && sizeof(Shared<kForwardRows>) <= 227 * 1024, "shared memory of a CTA");
 
 struct TcArgs {
     const int32_t* offsets;
@@ -62,7 +73,7 @@ struct TcArgs {
     uint64_t ld_as, ld_bs, ldc;
     uint32_t rows, n_groups, n, k;
     uint32_t feature_tiles, column_tiles;  // column_tiles: wgrad's tiles of in_features
-    uint32_t c_f32, accumulate, vector;
+    uint32_t c_f32, accumulate, vector, bulk_out;
 };
 
 // One tile of a pair.
@@ -81,7 +92,7 @@ struct Walk {
 
     // Tile t of all, ascending t; false past the last.  A tile without features (fp8 groups that are not whole scale blocks
     // have one tile fewer here and there) comes back with nt = 0.
-    __device__ __forceinline__ bool get(const TcArgs& a, const Shared& s, uint32_t t, Tile& o)
+    __device__ __forceinline__ bool get(const TcArgs& a, const Barriers& s, uint32_t t, Tile& o)
     {
         if constexpr (OP == kWgrad) {
             const uint32_t per = a.feature_tiles * a.column_tiles;
@@ -195,13 +206,13 @@ __device__ __forceinline__ void store_dw(const TcArgs& a, uint64_t row, uint32_t
 }
 
 template <int OP, bool FP8>
-__device__ __forceinline__ void produce(const TcArgs& a, Shared& s, const CUtensorMap* map_a, const CUtensorMap* map_b)
+__device__ __forceinline__ void produce(const TcArgs& a, Shared<OP>& s, const CUtensorMap* map_a, const CUtensorMap* map_b)
 {
     constexpr uint32_t kStep = Walk<OP, FP8>::kStep;
     const uint32_t rank = cta_rank(), stages = smem_u32(s.stage), empty = smem_u32(s.empty);
     // copies signal the first CTA of the pair, which issues the products; in wgrad their own CTA, which may have rows to clear
     const uint32_t full = OP == kWgrad ? smem_u32(s.landed) : in_cta(smem_u32(s.full), 0);
-    Turn<kStages> ring;
+    Turn<kStages<OP>> ring;
     uint32_t used = 0;  // stages in use, up to all of them
     bool ok = true;
     Walk<OP, FP8> walk;
@@ -240,20 +251,20 @@ __device__ __forceinline__ void produce(const TcArgs& a, Shared& s, const CUtens
                 }
             }
             ring.next();
-            used = min(used + 1, kStages);
+            used = min(used + 1, kStages<OP>);
         }
     }
     if (ok) drain(ring, used, empty, &s.stop, &g_wait_failures);
 }
 
 template <int OP, bool FP8>
-__device__ __forceinline__ void multiply(const TcArgs& a, Shared& s)
+__device__ __forceinline__ void multiply(const TcArgs& a, Shared<OP>& s)
 {
     const uint32_t stages = smem_u32(s.stage), full = smem_u32(s.full), empty = smem_u32(s.empty);
     const uint32_t acc_full = smem_u32(s.acc_full), acc_empty = smem_u32(s.acc_empty), tmem = s.tmem;
     constexpr bool a_mn = OP == kDgrad || OP == kWgrad, b_mn = OP == kWgrad;
     const uint64_t first_a = operand(stages, 8192), first_b = operand(stages + kOperandBytes, 8192);
-    Turn<kStages> ring;
+    Turn<kStages<OP>> ring;
     Turn<2> acc;
     Walk<OP, FP8> walk;
     Tile t;
@@ -284,7 +295,7 @@ __device__ __forceinline__ void multiply(const TcArgs& a, Shared& s)
 }
 
 // fp8: the tokens' scales of one block of the contraction after the other, copied ahead of the products that need them.
-__device__ __forceinline__ void copy_scales(const TcArgs& a, Shared& s)
+__device__ __forceinline__ void copy_scales(const TcArgs& a, Shared<kForward>& s)
 {
     const uint32_t lane = threadIdx.x & 31, slots = smem_u32(s.scale);
     const uint32_t full = smem_u32(s.scale_full), empty = smem_u32(s.scale_empty);
@@ -308,7 +319,7 @@ __device__ __forceinline__ void copy_scales(const TcArgs& a, Shared& s)
 
 // wgrad: rows of the last stage that belong to the next group are cleared before the products read them (both operands: a zero
 // times the infinity of another group's row is not zero), then the stage is handed to the first CTA.
-__device__ __forceinline__ void clear_rows(const TcArgs& a, Shared& s)
+__device__ __forceinline__ void clear_rows(const TcArgs& a, Shared<kWgrad>& s)
 {
     const uint32_t lane = threadIdx.x & 31, landed = smem_u32(s.landed), full = in_cta(smem_u32(s.full), 0);
     uint32_t n = 0;
@@ -317,8 +328,8 @@ __device__ __forceinline__ void clear_rows(const TcArgs& a, Shared& s)
     for (uint32_t i = blockIdx.x >> 1; walk.get(a, s, i, t); i += gridDim.x >> 1) {
         const uint32_t panels = (t.nt / 2 + 63) / 64;
         for (uint32_t l = 0; l < t.steps; ++l, ++n) {
-            const uint32_t st = n % kStages, valid = min(64u, t.row_end - t.row0 - l * 64);
-            if (!__all_sync(0xFFFFFFFFu, bar_wait(landed + 8 * st, n / kStages & 1, &s.stop, &g_wait_failures))) return;
+            const uint32_t st = n % kStages<kWgrad>, valid = min(64u, t.row_end - t.row0 - l * 64);
+            if (!__all_sync(0xFFFFFFFFu, bar_wait(landed + 8 * st, n / kStages<kWgrad> & 1, &s.stop, &g_wait_failures))) return;
             if (valid < 64) {
                 for (uint32_t p = 0; p < 2 + panels; ++p) {  // operand A's two panels, then B's: 8 KB each, side by side
                     uint8_t* panel = s.stage[st] + p * 8192;
@@ -333,7 +344,7 @@ __device__ __forceinline__ void clear_rows(const TcArgs& a, Shared& s)
 }
 
 template <int OP, bool FP8>
-__device__ __forceinline__ void write_out(const TcArgs& a, Shared& s)
+__device__ __forceinline__ void write_out(const TcArgs& a, Shared<OP>& s)
 {
     const uint32_t lane = threadIdx.x & 31, warp = (threadIdx.x >> 5) - 4, rank = cta_rank();
     const uint32_t quarter = warp & 3, side = warp >> 2;
@@ -444,41 +455,52 @@ __device__ __forceinline__ void write_out(const TcArgs& a, Shared& s)
     }
 }
 
-// Tokens on the M side: a thread owns one token and 64 features of one scale block, so the scale of a block of the contraction is
+// Tokens on the M side: a thread owns one token and 128 features of one scale block, so the scale of a block of the contraction is
 // one number a thread.
-__device__ __forceinline__ void write_rows(const TcArgs& a, Shared& s)
+__device__ __forceinline__ void write_rows(const TcArgs& a, Shared<kForwardRows>& s, const CUtensorMap* map_c)
 {
     const uint32_t lane = threadIdx.x & 31, warp = (threadIdx.x >> 5) - 4, rank = cta_rank();
     const uint32_t quarter = warp & 3, side = warp >> 2;
     const uint32_t acc_full = smem_u32(s.acc_full), acc_empty = in_cta(smem_u32(s.acc_empty), 0);
-    const uint32_t tmem = s.tmem + (quarter * 32 << 16) + side * 64;
+    const uint32_t tmem = s.tmem + (quarter * 32 << 16) + side * 128;
     const uint32_t scale_rows = (a.n_groups * a.n + 127) / 128;
-    uint32_t acc = 0;
+    const uint32_t out = smem_u32(s.out[warp][0]);
+    uint32_t acc = 0, i = blockIdx.x >> 1;
     Walk<kForwardRows, true> walk;
     Tile t;
-    for (uint32_t i = blockIdx.x >> 1; walk.get(a, s, i, t); i += gridDim.x >> 1) {
-        if (t.nt == 0) continue;
-        const uint32_t warp_row = t.row0 + rank * 128 + quarter * 32, row = warp_row + lane;
+    const float *xs, *ws;
+    float x1, w1, x2, w2;
+    // the next tile with features, and the first two scales of this thread's row in it
+    auto next_tile = [&]() {
+        do {
+            if (!walk.get(a, s, i, t)) return false;
+            i += gridDim.x >> 1;
+        } while (t.nt == 0);
+        xs = a.a_scale + min(t.row0 + rank * 128 + quarter * 32 + lane, t.row_end - 1);
+        ws = a.b_scale + (uint64_t)min(t.feature / 128 + side, scale_rows - 1) * a.ld_bs;
+        x1 = xs[0];
+        w1 = ws[0];
+        x2 = t.steps > 1 ? xs[a.ld_as] : 0.0f;
+        w2 = t.steps > 1 ? ws[1] : 0.0f;
+        xs += 2 * a.ld_as;
+        return true;
+    };
+    bool more = next_tile();
+    while (more) {
+        const uint32_t warp_row = t.row0 + rank * 128 + quarter * 32, row_end = t.row_end, steps = t.steps;
         // a warp without a token or without a feature only keeps the barriers going
-        const bool idle = warp_row >= t.row_end || side * 64 >= t.nt;
-        const float* xs = a.a_scale + min(row, t.row_end - 1);
-        const float* ws = a.b_scale + (uint64_t)min(t.feature / 128 + side / 2, scale_rows - 1) * a.ld_bs;
-        float sum[2][32];
+        const bool idle = warp_row >= row_end || side * 128 >= t.nt;
+        const int f = (int)(t.feature + side * 128 - t.e * a.n);
+        float sum[4][32];
 #pragma unroll
-        for (int c = 0; c < 2; ++c)
+        for (int c = 0; c < 4; ++c)
 #pragma unroll
             for (int r = 0; r < 32; ++r) sum[c][r] = 0.0f;
-        float x1 = xs[0], w1 = ws[0], x2 = 0.0f, w2 = 0.0f;
-        if (t.steps > 1) {
-            x2 = xs[a.ld_as];
-            w2 = ws[1];
-        }
-        xs += 2 * a.ld_as;
-        for (uint32_t l = 0; l < t.steps; ++l, ++acc) {
+        for (uint32_t l = 0; l < steps; ++l, ++acc) {
             const float scale = x1 * w1;
             x1 = x2;
             w1 = w2;
-            if (l + 2 < t.steps) {
+            if (l + 2 < steps) {
                 x2 = *xs;
                 w2 = ws[l + 2];
                 xs += a.ld_as;
@@ -493,74 +515,104 @@ __device__ __forceinline__ void write_rows(const TcArgs& a, Shared& s)
             }
             const uint64_t two = pair_of(scale, scale);
             const uint32_t from = tmem + (acc & 1) * kTile;
+            float p[2][32];
+            tmem_start(from, p[0]);
 #pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                float p[32];
-                tmem_start(from + 32 * c, p);
-                tmem_arrived(p);
-                if (c == 1) {  // the accumulator has been read: the next product may begin
+            for (int c = 0; c < 4; ++c) {
+                tmem_arrived(p[c & 1]);
+                if (c < 3) {
+                    tmem_start(from + 32 * (c + 1), p[(c + 1) & 1]);
+                } else {  // the accumulator has been read: the next product may begin
                     fence_before();
                     __syncwarp();
                     if (lane == 0) bar_arrive_cluster(acc_empty + 8 * (acc & 1));
                 }
 #pragma unroll
-                for (int r = 0; r < 32; r += 2) fma2(sum[c][r], sum[c][r + 1], p[r], p[r + 1], two);
+                for (int r = 0; r < 32; r += 2) fma2(sum[c][r], sum[c][r + 1], p[c & 1][r], p[c & 1][r + 1], two);
             }
         }
-        if (idle || row >= t.row_end) continue;
-        const int f = (int)(t.feature + side * 64 - t.e * a.n);
-        if (a.vector) {  // 32 bytes of c and whole rows of 16 features allow one sector a store
+        more = next_tile();  // its scales are on their way while this tile leaves
+        if (idle) continue;
+        const uint32_t row = warp_row + lane;
+        if (a.bulk_out && warp_row + 32 <= row_end && f >= 0 && f + 128 <= (int)a.n) {
+            // Whole blocks of 32 rows x 128 features leave through the copy unit while the next tile is computed: stored at once by
+            // every SM, they would hold up the products for 7 000 cycles a tile.  Rows of 128 bytes, their 16-byte units
+            // swizzled as the map says.
+            asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");  // (the lane that started the previous one)
+            __syncwarp();
 #pragma unroll
-            for (int c = 0; c < 64; c += 16) {
-                if (f + c < 0 || f + c >= (int)a.n) continue;
-                const float* v = &sum[c / 32][c % 32];
-                if (a.c_f32) {
-                    float* p = (float*)a.c + (uint64_t)row * a.ldc + f + c;
-                    store_32(p, __float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]),
-                             __float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7]));
-                    store_32(p + 8, __float_as_uint(v[8]), __float_as_uint(v[9]), __float_as_uint(v[10]), __float_as_uint(v[11]),
-                             __float_as_uint(v[12]), __float_as_uint(v[13]), __float_as_uint(v[14]), __float_as_uint(v[15]));
-                } else {
-                    store_32((uint16_t*)a.c + (uint64_t)row * a.ldc + f + c, pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]),
-                             pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]), pack_bf16(v[8], v[9]), pack_bf16(v[10], v[11]),
-                             pack_bf16(v[12], v[13]), pack_bf16(v[14], v[15]));
-                }
+            for (uint32_t c = 0; c < 16; ++c) {
+                const float* v = &sum[c / 4][c % 4 * 8];
+                store_shared(out + c / 8 * 4096 + lane * 128 + (c % 8 ^ (lane & 7)) * 16, pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]),
+                             pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
             }
-        } else {
+            fence_async();
+            __syncwarp();
+            if (lane == 0) {
+                store_2d(map_c, out, f, (int)warp_row);
+                store_2d(map_c, out + 4096, f + 64, (int)warp_row);
+                asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+            }
+        } else if (row < row_end) {
+            if (a.vector) {  // 32 bytes of c and whole rows of 16 features allow one sector a store
 #pragma unroll
-            for (int c = 0; c < 64; ++c) {
-                if (f + c < 0 || f + c >= (int)a.n) continue;
-                if (a.c_f32)
-                    ((float*)a.c)[(uint64_t)row * a.ldc + f + c] = sum[c / 32][c % 32];
-                else
-                    ((uint16_t*)a.c)[(uint64_t)row * a.ldc + f + c] = (uint16_t)pack_bf16(sum[c / 32][c % 32], 0.0f);
+                for (int c = 0; c < 128; c += 16) {
+                    if (f + c < 0 || f + c >= (int)a.n) continue;
+                    const float* v = &sum[c / 32][c % 32];
+                    if (a.c_f32) {
+                        float* p = (float*)a.c + (uint64_t)row * a.ldc + f + c;
+                        store_32(p, __float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]),
+                                 __float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7]));
+                        store_32(p + 8, __float_as_uint(v[8]), __float_as_uint(v[9]), __float_as_uint(v[10]), __float_as_uint(v[11]),
+                                 __float_as_uint(v[12]), __float_as_uint(v[13]), __float_as_uint(v[14]), __float_as_uint(v[15]));
+                    } else {
+                        store_32((uint16_t*)a.c + (uint64_t)row * a.ldc + f + c, pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]),
+                                 pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]), pack_bf16(v[8], v[9]), pack_bf16(v[10], v[11]),
+                                 pack_bf16(v[12], v[13]), pack_bf16(v[14], v[15]));
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int c = 0; c < 128; ++c) {
+                    if (f + c < 0 || f + c >= (int)a.n) continue;
+                    if (a.c_f32)
+                        ((float*)a.c)[(uint64_t)row * a.ldc + f + c] = sum[c / 32][c % 32];
+                    else
+                        ((uint16_t*)a.c)[(uint64_t)row * a.ldc + f + c] = (uint16_t)pack_bf16(sum[c / 32][c % 32], 0.0f);
+                }
             }
         }
     }
+    asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");  // the last block has left before the CTA may end
 }
 
 template <int OP, bool FP8>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads<OP>, 1)
-    tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const TcArgs a)
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
+    tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
+              const __grid_constant__ CUtensorMap map_c, const TcArgs a)
 {
-    extern __shared__ uint8_t raw[];
-    Shared& s = *(Shared*)(raw + (-smem_u32(raw) & 1023));
+    extern __shared__ __align__(1024) uint8_t raw[];
+    Shared<OP>& s = *(Shared<OP>*)raw;
+    if (smem_u32(raw) & 1023) {  // the swizzled stages need the alignment asked for; nothing has been started yet
+        if (threadIdx.x == 0) atomicAdd(&g_wait_failures, 1ull);
+        return;
+    }
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         prefetch_map(&map_a);
         prefetch_map(&map_b);
-        for (uint32_t i = 0; i < kStages; ++i) {
+        for (uint32_t i = 0; i < kStages<OP>; ++i) {
             bar_init(smem_u32(&s.full[i]), OP == kWgrad ? 2 : 1);
             bar_init(smem_u32(&s.empty[i]), 1);
             bar_init(smem_u32(&s.landed[i]), 1);
         }
         for (uint32_t i = 0; i < 2; ++i) {
             bar_init(smem_u32(&s.acc_full[i]), 1);
-            bar_init(smem_u32(&s.acc_empty[i]), 2 * kEpilogueWarps<OP>);
+            bar_init(smem_u32(&s.acc_empty[i]), 2 * kEpilogueWarps);
         }
         for (uint32_t i = 0; i < kScaleSlots; ++i) {
             bar_init(smem_u32(&s.scale_full[i]), 32);
-            bar_init(smem_u32(&s.scale_empty[i]), kEpilogueWarps<OP>);
+            bar_init(smem_u32(&s.scale_empty[i]), kEpilogueWarps);
         }
         s.stop = 0;
         bar_init_fence();
@@ -588,25 +640,19 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads<OP>, 1)
     fence_after();
 
     if (warp < 4) {
-        if (OP == kForwardRows)
-            asm volatile("setmaxnreg.dec.sync.aligned.u32 32;");
-        else if (FP8)
-            asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
+        if (FP8) asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
         if (warp == 0) {
             produce<OP, FP8>(a, s, &map_a, &map_b);
         } else if (warp == 1) {
             if (cta_rank() == 0) multiply<OP, FP8>(a, s);
         } else if (warp == 2) {
-            if (FP8 && OP == kForward) copy_scales(a, s);
-            if (OP == kWgrad) clear_rows(a, s);
+            if constexpr (FP8 && OP == kForward) copy_scales(a, s);
+            if constexpr (OP == kWgrad) clear_rows(a, s);
         }
     } else {
-        if (OP == kForwardRows)
-            asm volatile("setmaxnreg.inc.sync.aligned.u32 112;");
-        else if (FP8)
-            asm volatile("setmaxnreg.inc.sync.aligned.u32 232;");
+        if (FP8) asm volatile("setmaxnreg.inc.sync.aligned.u32 232;");
         if constexpr (OP == kForwardRows)
-            write_rows(a, s);
+            write_rows(a, s, &map_c);
         else
             write_out<OP, FP8>(a, s);
     }
@@ -622,29 +668,27 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads<OP>, 1)
     if (warp == 1) tmem_free<2>(s.tmem, 512);
 }
 
-constexpr size_t kSharedBytes = sizeof(Shared) + 1024;
-
 // Once per device and kernel: shared memory, and the register count that the fp8 kernel's split relies on
-// (384 threads x 168 at launch cover 256 x 232 + 128 x 40, 640 x 96 cover 512 x 112 + 128 x 32).
+// (384 threads x 168 at launch cover 256 x 232 + 128 x 40).
 template <int OP, bool FP8>
 int prepare_kernel()
 {
     cudaFuncAttributes at;
     DR_CUDA(cudaFuncGetAttributes(&at, tc_kernel<OP, FP8>));
-    if (FP8 && at.numRegs * (int)kThreads<OP> < (OP == kForwardRows ? 512 * 112 + 128 * 32 : 256 * 232 + 128 * 40)) {
+    if (FP8 && at.numRegs * (int)kThreads < 256 * 232 + 128 * 40) {
         set_error("the fp8 linear kernel was built with %d registers a thread", at.numRegs);
         return DR_ERR_CUDA;
     }
-    DR_CUDA(cudaFuncSetAttribute(tc_kernel<OP, FP8>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSharedBytes));
+    DR_CUDA(cudaFuncSetAttribute(tc_kernel<OP, FP8>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Shared<OP>)));
     return DR_OK;
 }
 
 template <int OP, bool FP8>
-int launch(const LinearCall& c, const CUtensorMap& ma, const CUtensorMap& mb, const TcArgs& a, uint64_t tiles)
+int launch(const LinearCall& c, const CUtensorMap& ma, const CUtensorMap& mb, const CUtensorMap& mc, const TcArgs& a, uint64_t tiles)
 {
     const uint64_t pairs = (uint64_t)c.lin->sms / 2;
     const unsigned grid = 2 * (unsigned)(tiles < pairs ? tiles : pairs);
-    tc_kernel<OP, FP8><<<grid, kThreads<OP>, kSharedBytes, c.stream>>>(ma, mb, a);
+    tc_kernel<OP, FP8><<<grid, kThreads, sizeof(Shared<OP>), c.stream>>>(ma, mb, mc, a);
     cudaError_t err = cudaGetLastError();
     if (err != cudaSuccess) {
         set_error("linear kernel launch: %s", cudaGetErrorString(err));
@@ -695,7 +739,7 @@ int launch_linear_tc(const LinearCall& c)
     // a group on (8192 x 24576 x 4096: 797 us against 915 with the features there; 512 x 6144 x 4096: 30.8 / 32.8; 128 groups of
     // 256 rows, 1536 x 2048: 170 / 158; one of 256 rows, 24576 x 4096: 56.3 / 55.3).
     const bool by_rows = fp8 && c.rows >= 512ull * d.n_groups;
-    CUtensorMap ma, mb;
+    CUtensorMap ma, mb, mc{};
     int rc;
     uint64_t tiles;
     const uint64_t token_tiles = ((uint64_t)c.rows + kTile - 1) / kTile + (c.offsets ? d.n_groups : 0);
@@ -715,6 +759,8 @@ int launch_linear_tc(const LinearCall& c)
             a.vector = width % 16 == 0 && c.ldc % (c.c_f32 ? 8 : 16) == 0 && (uintptr_t)c.c % 32 == 0;
             rc = encode_map(&ma, c.a, true, a.k, c.rows, 0, c.lda, 128);
             if (rc == DR_OK) rc = encode_map(&mb, c.b, true, a.k, (uint64_t)a.n * a.n_groups, 0, c.ldb, 32);
+            a.bulk_out = !c.c_f32 && a.n % 8 == 0 && c.ldc % 8 == 0 && (uintptr_t)c.c % 16 == 0 && c.ldc < (1ull << 38);
+            if (rc == DR_OK && a.bulk_out) rc = encode_map(&mc, c.c, false, a.n, c.rows, 0, c.ldc, 32);
         } else if (c.op == kForward)
             rc = encode_map(&ma, c.b, fp8, a.k, (uint64_t)a.n * a.n_groups, 0, c.ldb, 128);
         else
@@ -726,10 +772,10 @@ int launch_linear_tc(const LinearCall& c)
         set_error("too many output tiles for one launch");
         return DR_ERR_UNSUPPORTED;
     }
-    if (c.op == kWgrad) return launch<kWgrad, false>(c, ma, mb, a, tiles);
-    if (c.op == kDgrad) return launch<kDgrad, false>(c, ma, mb, a, tiles);
-    if (by_rows) return launch<kForwardRows, true>(c, ma, mb, a, tiles);
-    return fp8 ? launch<kForward, true>(c, ma, mb, a, tiles) : launch<kForward, false>(c, ma, mb, a, tiles);
+    if (c.op == kWgrad) return launch<kWgrad, false>(c, ma, mb, mc, a, tiles);
+    if (c.op == kDgrad) return launch<kDgrad, false>(c, ma, mb, mc, a, tiles);
+    if (by_rows) return launch<kForwardRows, true>(c, ma, mb, mc, a, tiles);
+    return fp8 ? launch<kForward, true>(c, ma, mb, mc, a, tiles) : launch<kForward, false>(c, ma, mb, mc, a, tiles);
 }
 
 int linear_wait_failures(uint64_t* out)
