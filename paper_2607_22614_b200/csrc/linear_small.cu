@@ -6,7 +6,8 @@
 // fewer feature blocks than SMs, a cluster of up to eight CTAs splits the contraction, and its CTAs add their fp32 sums through
 // distributed shared memory, always in the order of their ranks.
 //
-// Roles: warp 0 copies the operands, 1 issues the products, 2 copies the scales (fp8), 4-7 read the accumulators.  fp8 takes a new
+// Roles: warp 0 copies the operands, 1 issues the products, 2 copies the scales (fp8), 3 finds the tiles,
+// 4-7 read the accumulators.  fp8 takes a new
 // accumulator (eight of 64 columns in turn) for every block of 128 of the contraction, scales it and adds it to fp32 sums in
 // registers, as the kernel for many rows does.
 #include "linear.h"
@@ -25,6 +26,11 @@ constexpr uint32_t kThreads = 256, kBuffers = 512 / kRowsTile;
 constexpr uint32_t kScratchPitch = 80;
 constexpr uint32_t kTurnPitch = 36;  // floats
 
+struct Tile {
+    uint32_t e, row0, row_end, feature, nt;  // feature: row of the stacked weight; nt: N of the product
+    uint32_t step0, steps;                   // this CTA's part of the contraction
+};
+
 struct Shared {
     alignas(1024) uint8_t stage[kStages][kStageBytes];
     alignas(16) float turn[4][16][kTurnPitch];              // a warp's features of 16 rows, on their way to the cluster
@@ -34,6 +40,7 @@ struct Shared {
     uint64_t full[kStages], empty[kStages];
     uint64_t acc_full[kBuffers], acc_empty[kBuffers], scale_full[kBuffers], scale_empty[kBuffers];
     uint64_t sums_full, sums_empty;
+    TileRing<Tile> tiles;
     uint32_t tmem, stop;
     uint32_t tiles_before[kMaxTcGroups + 1];  // row tiles of the groups before
 };
@@ -48,11 +55,6 @@ struct Args {
     uint32_t feature_blocks;
     uint32_t split;  // CTAs of a cluster
     uint32_t c_f32, vector;
-};
-
-struct Tile {
-    uint32_t e, row0, row_end, feature, nt;  // feature: row of the stacked weight; nt: N of the product
-    uint32_t step0, steps;                   // this CTA's part of the contraction
 };
 
 template <bool FP8>
@@ -113,18 +115,31 @@ __device__ __forceinline__ void store_rows(const Args& a, uint32_t scratch, uint
         }
 }
 
+// Finds the cluster's tiles for the other warps.
 template <bool FP8>
-__device__ __forceinline__ void produce(const Args& a, Shared& s, const CUtensorMap* map_w, const CUtensorMap* map_x, uint32_t first, uint32_t stride)
+__device__ __forceinline__ void schedule(const Args& a, Shared& s)
+{
+    Walk<FP8> walk;
+    Turn<kTilesAhead> turn;
+    Tile t;
+    const uint32_t stride = gridDim.x / a.split;
+    for (uint32_t i = blockIdx.x / a.split; walk.get(a, s, i, t); i += stride)
+        if (t.nt && !s.tiles.put(t, turn, &s.stop, &g_wait_failures)) return;
+    t.nt = kNoTile;
+    s.tiles.put(t, turn, &s.stop, &g_wait_failures);
+}
+
+template <bool FP8>
+__device__ __forceinline__ void produce(const Args& a, Shared& s, const CUtensorMap* map_w, const CUtensorMap* map_x)
 {
     constexpr uint32_t kStep = Walk<FP8>::kStep;
     const uint32_t stages = smem_u32(s.stage), full = smem_u32(s.full), empty = smem_u32(s.empty);
     Turn<kStages> ring;
     uint32_t used = 0;  // stages in use, up to all of them
-    Walk<FP8> walk;
+    Turn<kTilesAhead> turn;
     Tile t;
     bool ok = true;
-    for (uint32_t i = first; ok && walk.get(a, s, i, t); i += stride) {
-        if (t.nt == 0) continue;
+    while (ok && s.tiles.get(t, turn, &s.stop, &g_wait_failures)) {
         for (uint32_t l = t.step0; l < t.step0 + t.steps; ++l) {
             const uint32_t at = stages + ring.slot * kStageBytes, bar = full + 8 * ring.slot;
             ok = warp_wait(empty + 8 * ring.slot, ring.round ^ 1, &s.stop, &g_wait_failures);
@@ -142,17 +157,16 @@ __device__ __forceinline__ void produce(const Args& a, Shared& s, const CUtensor
 }
 
 template <bool FP8>
-__device__ __forceinline__ void multiply(const Args& a, Shared& s, uint32_t first, uint32_t stride)
+__device__ __forceinline__ void multiply(const Args& a, Shared& s)
 {
     const uint32_t full = smem_u32(s.full), empty = smem_u32(s.empty);
     const uint32_t acc_full = smem_u32(s.acc_full), acc_empty = smem_u32(s.acc_empty), tmem = s.tmem;
     const uint64_t first_a = operand(smem_u32(s.stage), 0), first_b = operand(smem_u32(s.stage) + kWeightBytes, 0);
     Turn<kStages> ring;
     Turn<kBuffers> acc;
-    Walk<FP8> walk;
+    Turn<kTilesAhead> turn;
     Tile t;
-    for (uint32_t i = first; walk.get(a, s, i, t); i += stride) {
-        if (t.nt == 0) continue;
+    while (s.tiles.get(t, turn, &s.stop, &g_wait_failures)) {
         const uint32_t shape = shape_of(FP8, false, false, 128, t.nt);
         for (uint32_t l = 0; l < t.steps; ++l) {
             if (FP8 || l == 0)
@@ -175,15 +189,14 @@ __device__ __forceinline__ void multiply(const Args& a, Shared& s, uint32_t firs
     }
 }
 
-__device__ __forceinline__ void copy_scales(const Args& a, Shared& s, uint32_t first, uint32_t stride)
+__device__ __forceinline__ void copy_scales(const Args& a, Shared& s)
 {
     const uint32_t lane = threadIdx.x & 31, full = smem_u32(s.scale_full), empty = smem_u32(s.scale_empty);
     const uint32_t scale_rows = (a.n_groups * a.n + 127) / 128;
     uint32_t n = 0;
-    Walk<true> walk;
+    Turn<kTilesAhead> turn;
     Tile t;
-    for (uint32_t i = first; walk.get(a, s, i, t); i += stride) {
-        if (t.nt == 0) continue;
+    while (s.tiles.get(t, turn, &s.stop, &g_wait_failures)) {
         const float* xs = a.a_scale + t.row0;
         const float* ws = a.b_scale + (uint64_t)min(t.feature / 128, scale_rows - 1) * a.ld_bs;
         const uint32_t left = t.row_end - t.row0;
@@ -199,17 +212,16 @@ __device__ __forceinline__ void copy_scales(const Args& a, Shared& s, uint32_t f
 }
 
 template <bool FP8>
-__device__ __forceinline__ void write_out(const Args& a, Shared& s, uint32_t first, uint32_t stride)
+__device__ __forceinline__ void write_out(const Args& a, Shared& s)
 {
     const uint32_t lane = threadIdx.x & 31, warp = (threadIdx.x >> 5) - 4;
     const uint32_t acc_full = smem_u32(s.acc_full), acc_empty = smem_u32(s.acc_empty);
     const uint32_t scale_full = smem_u32(s.scale_full), scale_empty = smem_u32(s.scale_empty);
     const uint32_t scratch = smem_u32(s.scratch[warp]), tmem = s.tmem + (warp * 32 << 16);
     uint32_t acc = 0, handed = 0;
-    Walk<FP8> walk;
+    Turn<kTilesAhead> turn;
     Tile t;
-    for (uint32_t i = first; walk.get(a, s, i, t); i += stride) {
-        if (t.nt == 0) continue;
+    while (s.tiles.get(t, turn, &s.stop, &g_wait_failures)) {
         float sum[2][2][16];
         if (FP8 || t.steps == 0) {
 #pragma unroll
@@ -356,6 +368,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         bar_init(smem_u32(&s.sums_full), 1);
         bar_init(smem_u32(&s.sums_empty), 4 * a.split);
+        s.tiles.init(2 + FP8 + 4);  // readers: the copies, the products, the scales, the accumulators
         s.stop = 0;
         bar_init_fence();
     }
@@ -385,15 +398,16 @@ __global__ void __launch_bounds__(kThreads, 1)
     if (a.split > 1) cluster_sync();
     fence_after();
 
-    const uint32_t first = blockIdx.x / a.split, stride = gridDim.x / a.split;
     if (warp == 0) {
-        produce<FP8>(a, s, &map_w, &map_x, first, stride);
+        produce<FP8>(a, s, &map_w, &map_x);
     } else if (warp == 1) {
-        multiply<FP8>(a, s, first, stride);
+        multiply<FP8>(a, s);
     } else if (warp == 2) {
-        if (FP8) copy_scales(a, s, first, stride);
-    } else if (warp >= 4) {
-        write_out<FP8>(a, s, first, stride);
+        if (FP8) copy_scales(a, s);
+    } else if (warp == 3) {
+        schedule<FP8>(a, s);
+    } else {
+        write_out<FP8>(a, s);
     }
     __syncwarp();
     if (*(volatile uint32_t*)&s.stop) {  // a wait ran out: let the copies and products in flight end before the memory is given back

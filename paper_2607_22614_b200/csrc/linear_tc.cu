@@ -10,7 +10,7 @@
 //
 // Roles of a CTA's 12 warps: 0 issues the copies of its half of the operands into a ring of six 32 KB stages; 1 (of the pair's
 // first CTA) issues the products of the pair; 2 copies the tokens' scales (fp8) or clears the rows of other groups from the last
-// stage (wgrad); 4-11 read the accumulators.  Accumulators take half of tensor memory each, two in turn, so that a tile is
+// stage (wgrad); 3 finds the tiles; 4-11 read the accumulators.  Accumulators take half of tensor memory each, two in turn, so that a tile is
 // written out while the next is computed.
 //
 // fp8: one product covers exactly one block of 128 of the contraction, after which its partial sums are scaled by
@@ -43,7 +43,17 @@ constexpr uint32_t kScaleSlots = 8;
 constexpr uint32_t kScratchPitch = 80;   // bytes between tokens of the transpose: 16-byte units of eight rows fall on different banks
 constexpr uint32_t kBand = 16;           // token tiles a band of a large group holds
 
+// One tile of a pair.
+struct Tile {
+    uint32_t e, row0, row_end;  // tokens [row0, row_end); wgrad: the group's rows
+    uint32_t feature;           // first of the pair's 256 outputs on the M side (forward: row of the stacked weight)
+    uint32_t col0;              // wgrad: first of its columns
+    uint32_t nt;                // N of the product, a multiple of 32
+    uint32_t steps;             // stages of the contraction
+};
+
 struct Barriers {
+    TileRing<Tile> tiles;
     uint64_t full[6], empty[6], landed[6];
     uint64_t acc_full[2], acc_empty[2];
     uint64_t scale_full[kScaleSlots], scale_empty[kScaleSlots];
@@ -74,15 +84,6 @@ struct TcArgs {
     uint32_t rows, n_groups, n, k;
     uint32_t feature_tiles, column_tiles;  // column_tiles: wgrad's tiles of in_features
     uint32_t c_f32, accumulate, vector, bulk_out;
-};
-
-// One tile of a pair.
-struct Tile {
-    uint32_t e, row0, row_end;  // tokens [row0, row_end); wgrad: the group's rows
-    uint32_t feature;           // first of the pair's 256 outputs on the M side (forward: row of the stacked weight)
-    uint32_t col0;              // wgrad: first of its columns
-    uint32_t nt;                // N of the product, a multiple of 32
-    uint32_t steps;             // stages of the contraction
 };
 
 template <int OP, bool FP8>
@@ -205,6 +206,19 @@ __device__ __forceinline__ void store_dw(const TcArgs& a, uint64_t row, uint32_t
     }
 }
 
+// Finds the pair's tiles for the other warps.
+template <int OP, bool FP8>
+__device__ __forceinline__ void schedule(const TcArgs& a, Shared<OP>& s)
+{
+    Walk<OP, FP8> walk;
+    Turn<kTilesAhead> at;
+    Tile t;
+    for (uint32_t i = blockIdx.x >> 1; walk.get(a, s, i, t); i += gridDim.x >> 1)
+        if (t.nt && !s.tiles.put(t, at, &s.stop, &g_wait_failures)) return;
+    t.nt = kNoTile;
+    s.tiles.put(t, at, &s.stop, &g_wait_failures);
+}
+
 template <int OP, bool FP8>
 __device__ __forceinline__ void produce(const TcArgs& a, Shared<OP>& s, const CUtensorMap* map_a, const CUtensorMap* map_b)
 {
@@ -215,15 +229,14 @@ __device__ __forceinline__ void produce(const TcArgs& a, Shared<OP>& s, const CU
     Turn<kStages<OP>> ring;
     uint32_t used = 0;  // stages in use, up to all of them
     bool ok = true;
-    Walk<OP, FP8> walk;
+    Turn<kTilesAhead> at;
     Tile t;
-    for (uint32_t i = blockIdx.x >> 1; ok && walk.get(a, s, i, t); i += gridDim.x >> 1) {
-        if (t.nt == 0) continue;
+    while (ok && s.tiles.get(t, at, &s.stop, &g_wait_failures)) {
         const uint32_t half = t.nt / 2, feature = t.feature + rank * 128;
         const uint32_t boxes = OP == kWgrad ? (half + 63) / 64 : (half + 31) / 32, box_bytes = OP == kWgrad ? 8192 : 4096;
         const uint32_t bytes = kOperandBytes + boxes * box_bytes;
         for (uint32_t l = 0; l < t.steps; ++l) {
-            const uint32_t at = stages + ring.slot * kStageBytes, bar = full + 8 * ring.slot;
+            const uint32_t to = stages + ring.slot * kStageBytes, bar = full + 8 * ring.slot;
             ok = warp_wait(empty + 8 * ring.slot, ring.round ^ 1, &s.stop, &g_wait_failures);
             if (!ok) break;
             if (elect()) {
@@ -232,22 +245,22 @@ __device__ __forceinline__ void produce(const TcArgs& a, Shared<OP>& s, const CU
                 else if (rank == 0)
                     bar_expect(smem_u32(s.full) + 8 * ring.slot, 2 * bytes);
                 if (OP == kForward) {
-                    load_2d<true>(at, map_a, bar, l * kStep, feature);
+                    load_2d<true>(to, map_a, bar, l * kStep, feature);
                 } else if (OP == kForwardRows) {
-                    load_2d<true>(at, map_a, bar, l * kStep, t.row0 + rank * 128);
+                    load_2d<true>(to, map_a, bar, l * kStep, t.row0 + rank * 128);
                 } else if (OP == kDgrad) {
-                    load_3d<true>(at, map_a, bar, feature, l * kStep, t.e);
-                    load_3d<true>(at + 8192, map_a, bar, feature + 64, l * kStep, t.e);
+                    load_3d<true>(to, map_a, bar, feature, l * kStep, t.e);
+                    load_3d<true>(to + 8192, map_a, bar, feature + 64, l * kStep, t.e);
                 } else {
-                    load_2d<false>(at, map_a, bar, feature, t.row0 + l * kStep);
-                    load_2d<false>(at + 8192, map_a, bar, feature + 64, t.row0 + l * kStep);
+                    load_2d<false>(to, map_a, bar, feature, t.row0 + l * kStep);
+                    load_2d<false>(to + 8192, map_a, bar, feature + 64, t.row0 + l * kStep);
                 }
                 for (uint32_t b = 0; b < boxes; ++b) {
-                    const uint32_t to = at + kOperandBytes + b * box_bytes;
+                    const uint32_t box = to + kOperandBytes + b * box_bytes;
                     if (OP == kWgrad)
-                        load_2d<false>(to, map_b, bar, t.col0 + rank * half + b * 64, t.row0 + l * kStep);
+                        load_2d<false>(box, map_b, bar, t.col0 + rank * half + b * 64, t.row0 + l * kStep);
                     else
-                        load_2d<true>(to, map_b, bar, l * kStep, (OP == kForwardRows ? t.feature : t.row0) + rank * half + b * 32);
+                        load_2d<true>(box, map_b, bar, l * kStep, (OP == kForwardRows ? t.feature : t.row0) + rank * half + b * 32);
                 }
             }
             ring.next();
@@ -266,10 +279,10 @@ __device__ __forceinline__ void multiply(const TcArgs& a, Shared<OP>& s)
     const uint64_t first_a = operand(stages, 8192), first_b = operand(stages + kOperandBytes, 8192);
     Turn<kStages<OP>> ring;
     Turn<2> acc;
-    Walk<OP, FP8> walk;
+    Turn<kTilesAhead> at;
     Tile t;
-    for (uint32_t i = blockIdx.x >> 1; walk.get(a, s, i, t); i += gridDim.x >> 1) {
-        if (t.nt == 0 || t.steps == 0) continue;
+    while (s.tiles.get(t, at, &s.stop, &g_wait_failures)) {
+        if (t.steps == 0) continue;
         const uint32_t shape = shape_of(FP8, a_mn, b_mn, 256, t.nt);
         for (uint32_t l = 0; l < t.steps; ++l) {
             if (FP8 || l == 0)
@@ -300,10 +313,9 @@ __device__ __forceinline__ void copy_scales(const TcArgs& a, Shared<kForward>& s
     const uint32_t lane = threadIdx.x & 31, slots = smem_u32(s.scale);
     const uint32_t full = smem_u32(s.scale_full), empty = smem_u32(s.scale_empty);
     uint32_t n = 0;
-    Walk<kForward, true> walk;
+    Turn<kTilesAhead> at;
     Tile t;
-    for (uint32_t i = blockIdx.x >> 1; walk.get(a, s, i, t); i += gridDim.x >> 1) {
-        if (t.nt == 0) continue;
+    while (s.tiles.get(t, at, &s.stop, &g_wait_failures)) {
         const float* xs = a.a_scale + t.row0;
         const uint32_t left = t.row_end - t.row0;
         for (uint32_t l = 0; l < t.steps; ++l, ++n, xs += a.ld_as) {
@@ -323,9 +335,9 @@ __device__ __forceinline__ void clear_rows(const TcArgs& a, Shared<kWgrad>& s)
 {
     const uint32_t lane = threadIdx.x & 31, landed = smem_u32(s.landed), full = in_cta(smem_u32(s.full), 0);
     uint32_t n = 0;
-    Walk<kWgrad, false> walk;
+    Turn<kTilesAhead> at;
     Tile t;
-    for (uint32_t i = blockIdx.x >> 1; walk.get(a, s, i, t); i += gridDim.x >> 1) {
+    while (s.tiles.get(t, at, &s.stop, &g_wait_failures)) {
         const uint32_t panels = (t.nt / 2 + 63) / 64;
         for (uint32_t l = 0; l < t.steps; ++l, ++n) {
             const uint32_t st = n % kStages<kWgrad>, valid = min(64u, t.row_end - t.row0 - l * 64);
@@ -354,10 +366,9 @@ __device__ __forceinline__ void write_out(const TcArgs& a, Shared<OP>& s)
     const uint32_t tmem = s.tmem + (quarter * 32 << 16);
     uint32_t acc = 0;
     bool ok = true;
-    Walk<OP, FP8> walk;
+    Turn<kTilesAhead> at;
     Tile t;
-    for (uint32_t i = blockIdx.x >> 1; walk.get(a, s, i, t); i += gridDim.x >> 1) {
-        if (t.nt == 0) continue;
+    while (s.tiles.get(t, at, &s.stop, &g_wait_failures)) {
         const uint32_t cols = t.nt / 2, col0 = side * cols;  // this warp's columns
         const uint32_t feature = t.feature + rank * 128 + quarter * 32;
         // in a row of c: forward counts features from the group's first weight row
@@ -465,17 +476,14 @@ __device__ __forceinline__ void write_rows(const TcArgs& a, Shared<kForwardRows>
     const uint32_t tmem = s.tmem + (quarter * 32 << 16) + side * 128;
     const uint32_t scale_rows = (a.n_groups * a.n + 127) / 128;
     const uint32_t out = smem_u32(s.out[warp][0]);
-    uint32_t acc = 0, i = blockIdx.x >> 1;
-    Walk<kForwardRows, true> walk;
+    uint32_t acc = 0;
+    Turn<kTilesAhead> at;
     Tile t;
     const float *xs, *ws;
     float x1, w1, x2, w2;
-    // the next tile with features, and the first two scales of this thread's row in it
+    // the next tile, and the first two scales of this thread's row in it
     auto next_tile = [&]() {
-        do {
-            if (!walk.get(a, s, i, t)) return false;
-            i += gridDim.x >> 1;
-        } while (t.nt == 0);
+        if (!s.tiles.get(t, at, &s.stop, &g_wait_failures)) return false;
         xs = a.a_scale + min(t.row0 + rank * 128 + quarter * 32 + lane, t.row_end - 1);
         ws = a.b_scale + (uint64_t)min(t.feature / 128 + side, scale_rows - 1) * a.ld_bs;
         x1 = xs[0];
@@ -614,6 +622,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
             bar_init(smem_u32(&s.scale_full[i]), 32);
             bar_init(smem_u32(&s.scale_empty[i]), kEpilogueWarps);
         }
+        // readers: the copies, the products (first CTA), the scales or cleared rows, the accumulators
+        s.tiles.init(1 + (cta_rank() == 0) + (OP == kWgrad || (OP == kForward && FP8)) + kEpilogueWarps);
         s.stop = 0;
         bar_init_fence();
     }
@@ -648,6 +658,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         } else if (warp == 2) {
             if constexpr (FP8 && OP == kForward) copy_scales(a, s);
             if constexpr (OP == kWgrad) clear_rows(a, s);
+        } else {
+            schedule<OP, FP8>(a, s);
         }
     } else {
         if (FP8) asm volatile("setmaxnreg.inc.sync.aligned.u32 232;");

@@ -131,6 +131,43 @@ __device__ __forceinline__ void drain(Turn<N> ring, uint32_t used, uint32_t empt
     }
 }
 
+// Tiles that one warp of a CTA finds (the divisions and the walk over ragged groups take some 900 cycles) and the others read, up
+// to four ahead.  A tile with nt = kNoTile ends the loop.
+constexpr uint32_t kTilesAhead = 4, kNoTile = 0xFFFFFFFFu;
+template <class T>
+struct TileRing {
+    T tile[kTilesAhead];
+    uint64_t full[kTilesAhead], empty[kTilesAhead];
+    __device__ __forceinline__ void init(uint32_t readers)  // warps that read every tile
+    {
+        for (uint32_t i = 0; i < kTilesAhead; ++i) {
+            bar_init(smem_u32(&full[i]), 1);
+            bar_init(smem_u32(&empty[i]), readers);
+        }
+    }
+    // by a whole warp
+    __device__ __forceinline__ bool put(const T& t, Turn<kTilesAhead>& at, volatile uint32_t* stop, unsigned long long* failures)
+    {
+        if (!__all_sync(0xFFFFFFFFu, bar_wait(smem_u32(&empty[at.slot]), at.round ^ 1, stop, failures))) return false;
+        if ((threadIdx.x & 31) == 0) {
+            tile[at.slot] = t;
+            bar_arrive(smem_u32(&full[at.slot]));
+        }
+        __syncwarp();
+        at.next();
+        return true;
+    }
+    __device__ __forceinline__ bool get(T& t, Turn<kTilesAhead>& at, volatile uint32_t* stop, unsigned long long* failures)
+    {
+        if (!__all_sync(0xFFFFFFFFu, bar_wait(smem_u32(&full[at.slot]), at.round, stop, failures))) return false;
+        t = tile[at.slot];
+        __syncwarp();
+        if ((threadIdx.x & 31) == 0) bar_arrive(smem_u32(&empty[at.slot]));
+        at.next();
+        return t.nt != kNoTile;
+    }
+};
+
 // 16 bytes to the shared memory of a CTA of the cluster, counted on a barrier of that CTA: whoever waits for the barrier sees them.
 __device__ __forceinline__ void store_counted(uint32_t dst, const float4& v, uint32_t bar)
 {
