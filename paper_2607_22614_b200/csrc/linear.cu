@@ -69,8 +69,8 @@ int check_gradient(const dr_linear* lin)
 }
 
 // Up to this many rows a group (on average) the kernel that reads weights 128 features at a time wins over pairs of CTAs: in us,
-// 1 x 6144 x 4096 fp8 9.5 / 17.0, 64 x 24576 x 4096 33.6 / 33.2, 128 x 6144 x 4096 22.4 / 18.5; 128 groups, 32 rows each,
-// 1536 x 2048 fp8 71.8 / 94.2, bf16 2048 x 768 68.5 / 67.7.
+// fp8 1 x 6144 x 4096 10.0 / 17.0, 80 x 4096 x 4096 13.5 / 18.2, 128 x 24576 x 4096 41.5 / 35.4; 128 groups of 1536 x 2048, 32 rows each
+// 71.6 / 100, 64 rows each 110 / 113; bf16 64 x 6144 x 4096 15.0 / 16.9, 128 groups of 48 rows 133 / 134.
 constexpr uint64_t kSmallRows = 64;
 
 int launch(const LinearCall& c)

@@ -39,7 +39,6 @@ constexpr uint32_t kStageBytes = 32768, kOperandBytes = 16384;
 constexpr uint32_t kEpilogueWarps = 8;
 constexpr uint32_t kThreads = 128 + 32 * kEpilogueWarps;
 constexpr uint32_t kTile = 256;          // features and tokens of a pair's tile
-constexpr uint32_t kScaleSlots = 8;
 constexpr uint32_t kScratchPitch = 80;   // bytes between tokens of the transpose: 16-byte units of eight rows fall on different banks
 constexpr uint32_t kBand = 16;           // token tiles a band of a large group holds
 
@@ -56,7 +55,6 @@ struct Barriers {
     TileRing<Tile> tiles;
     uint64_t full[6], empty[6], landed[6];
     uint64_t acc_full[2], acc_empty[2];
-    uint64_t scale_full[kScaleSlots], scale_empty[kScaleSlots];
     uint32_t tmem, stop;
     uint32_t tiles_before[kMaxTcGroups + 1];  // token tiles of the groups before
 };
@@ -64,7 +62,6 @@ template <int OP>
 struct Buffers {
     alignas(1024) uint8_t stage[kStages<OP>][kStageBytes];
     alignas(16) uint8_t scratch[kEpilogueWarps][8 * kScratchPitch];
-    alignas(16) float scale[kScaleSlots][kTile];
 };
 template <>
 struct Buffers<kForwardRows> {
@@ -307,28 +304,6 @@ __device__ __forceinline__ void multiply(const TcArgs& a, Shared<OP>& s)
     }
 }
 
-// fp8: the tokens' scales of one block of the contraction after the other, copied ahead of the products that need them.
-__device__ __forceinline__ void copy_scales(const TcArgs& a, Shared<kForward>& s)
-{
-    const uint32_t lane = threadIdx.x & 31, slots = smem_u32(s.scale);
-    const uint32_t full = smem_u32(s.scale_full), empty = smem_u32(s.scale_empty);
-    uint32_t n = 0;
-    Turn<kTilesAhead> at;
-    Tile t;
-    while (s.tiles.get(t, at, &s.stop, &g_wait_failures)) {
-        const float* xs = a.a_scale + t.row0;
-        const uint32_t left = t.row_end - t.row0;
-        for (uint32_t l = 0; l < t.steps; ++l, ++n, xs += a.ld_as) {
-            const uint32_t slot = n % kScaleSlots;
-            if (!__all_sync(0xFFFFFFFFu, bar_wait(empty + 8 * slot, (n / kScaleSlots & 1) ^ 1, &s.stop, &g_wait_failures))) return;
-#pragma unroll
-            for (uint32_t j = lane; j < kTile; j += 32)  // zeros for columns past the group's rows
-                copy_4(slots + slot * kTile * 4 + j * 4, xs + (j < left ? j : 0), j < left);
-            copies_arrive(full + 8 * slot);
-        }
-    }
-}
-
 // wgrad: rows of the last stage that belong to the next group are cleared before the products read them (both operands: a zero
 // times the infinity of another group's row is not zero), then the stage is handed to the first CTA.
 __device__ __forceinline__ void clear_rows(const TcArgs& a, Shared<kWgrad>& s)
@@ -361,7 +336,6 @@ __device__ __forceinline__ void write_out(const TcArgs& a, Shared<OP>& s)
     const uint32_t lane = threadIdx.x & 31, warp = (threadIdx.x >> 5) - 4, rank = cta_rank();
     const uint32_t quarter = warp & 3, side = warp >> 2;
     const uint32_t acc_full = smem_u32(s.acc_full), acc_empty = in_cta(smem_u32(s.acc_empty), 0);
-    const uint32_t scale_full = smem_u32(s.scale_full), scale_empty = smem_u32(s.scale_empty);
     const uint32_t scratch = smem_u32(s.scratch[warp]);
     const uint32_t tmem = s.tmem + (quarter * 32 << 16);
     uint32_t acc = 0;
@@ -380,88 +354,32 @@ __device__ __forceinline__ void write_out(const TcArgs& a, Shared<OP>& s)
             else
                 store_tokens(a, scratch, t.row0 + col0 + c, t.row_end, f, f_hi, v);
         };
-        if (FP8) {
-            float sum[2][2][32];
-#pragma unroll
-            for (int c = 0; c < 2; ++c)
-#pragma unroll
-                for (int h = 0; h < 2; ++h)
-#pragma unroll
-                    for (int r = 0; r < 32; ++r) sum[c][h][r] = 0.0f;
-            // the CTA's 128 features are one block of the weight's scales (a tile past the last feature reads the last one)
-            const float* ws = a.b_scale + (uint64_t)min((t.feature + rank * 128) / 128, (a.n_groups * a.n + 127) / 128 - 1) * a.ld_bs;
-            float w_next = ws[0];
-            for (uint32_t l = 0; l < t.steps; ++l, ++acc) {
-                const uint32_t slot = acc % kScaleSlots;
-                const float w = w_next;
-                if (l + 1 < t.steps) w_next = ws[l + 1];
-                ok = bar_wait(scale_full + 8 * slot, acc / kScaleSlots & 1, &s.stop, &g_wait_failures) &&
-                     bar_wait(acc_full + 8 * (acc & 1), acc >> 1 & 1, &s.stop, &g_wait_failures);
-                if (!__all_sync(0xFFFFFFFFu, ok)) return;
-                fence_after();
-                const uint32_t from = tmem + (acc & 1) * kTile + col0;
-                const float* sc = s.scale[slot] + col0 + 2 * (lane & 3);
-                const uint64_t ww = pair_of(w, w);
-#pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    if (c * 64 >= cols) break;
-                    float p[2][32];
-                    tmem_load(from + c * 64, p[0], p[1]);
-                    if (c * 64 + 64 >= cols) {  // the last of the accumulator has been read: the next product may begin
-                        fence_before();
-                        __syncwarp();
-                        if (lane == 0) bar_arrive_cluster(acc_empty + 8 * (acc & 1));
-                    }
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const uint64_t two = mul2(*(const uint64_t*)(sc + c * 64 + j * 8), ww);
-#pragma unroll
-                        for (int h = 0; h < 2; ++h) {
-                            fma2(sum[c][h][4 * j], sum[c][h][4 * j + 1], p[h][4 * j], p[h][4 * j + 1], two);
-                            fma2(sum[c][h][4 * j + 2], sum[c][h][4 * j + 3], p[h][4 * j + 2], p[h][4 * j + 3], two);
-                        }
-                    }
-                }
-                __syncwarp();
-                if (lane == 0) bar_arrive(scale_empty + 8 * slot);
-            }
-#pragma unroll
-            for (int c = 0; c < 2; ++c)
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    if (c * 64 + j * 8 >= cols) break;
-                    const float v[4][2] = {{sum[c][0][4 * j], sum[c][0][4 * j + 1]}, {sum[c][0][4 * j + 2], sum[c][0][4 * j + 3]},
-                                           {sum[c][1][4 * j], sum[c][1][4 * j + 1]}, {sum[c][1][4 * j + 2], sum[c][1][4 * j + 3]}};
-                    put(c * 64 + j * 8, v);
-                }
-        } else {
+        if (t.steps) {
+            ok = bar_wait(acc_full + 8 * (acc & 1), acc >> 1 & 1, &s.stop, &g_wait_failures);
+            if (!__all_sync(0xFFFFFFFFu, ok)) return;
+            fence_after();
+        }
+        for (uint32_t c = 0; c < cols; c += 32) {
+            float p[2][16];
             if (t.steps) {
-                ok = bar_wait(acc_full + 8 * (acc & 1), acc >> 1 & 1, &s.stop, &g_wait_failures);
-                if (!__all_sync(0xFFFFFFFFu, ok)) return;
-                fence_after();
-            }
-            for (uint32_t c = 0; c < cols; c += 32) {
-                float p[2][16];
-                if (t.steps) {
-                    tmem_load(tmem + (acc & 1) * kTile + col0 + c, p[0], p[1]);
-                } else {
+                tmem_load(tmem + (acc & 1) * kTile + col0 + c, p[0], p[1]);
+            } else {
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) p[0][r] = p[1][r] = 0.0f;  // dW of a group without rows
-                }
+                for (int r = 0; r < 16; ++r) p[0][r] = p[1][r] = 0.0f;  // dW of a group without rows
+            }
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    if (c + j * 8 >= cols) break;
-                    const float v[4][2] = {{p[0][4 * j], p[0][4 * j + 1]}, {p[0][4 * j + 2], p[0][4 * j + 3]},
-                                           {p[1][4 * j], p[1][4 * j + 1]}, {p[1][4 * j + 2], p[1][4 * j + 3]}};
-                    put(c + j * 8, v);
-                }
+            for (int j = 0; j < 4; ++j) {
+                if (c + j * 8 >= cols) break;
+                const float v[4][2] = {{p[0][4 * j], p[0][4 * j + 1]}, {p[0][4 * j + 2], p[0][4 * j + 3]},
+                                       {p[1][4 * j], p[1][4 * j + 1]}, {p[1][4 * j + 2], p[1][4 * j + 3]}};
+                put(c + j * 8, v);
             }
-            if (t.steps) {
-                fence_before();
-                __syncwarp();
-                if (lane == 0) bar_arrive_cluster(acc_empty + 8 * (acc & 1));
-                ++acc;
-            }
+        }
+        if (t.steps) {
+            fence_before();
+            __syncwarp();
+            if (lane == 0) bar_arrive_cluster(acc_empty + 8 * (acc & 1));
+            ++acc;
         }
     }
 }
@@ -618,12 +536,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
             bar_init(smem_u32(&s.acc_full[i]), 1);
             bar_init(smem_u32(&s.acc_empty[i]), 2 * kEpilogueWarps);
         }
-        for (uint32_t i = 0; i < kScaleSlots; ++i) {
-            bar_init(smem_u32(&s.scale_full[i]), 32);
-            bar_init(smem_u32(&s.scale_empty[i]), kEpilogueWarps);
-        }
-        // readers: the copies, the products (first CTA), the scales or cleared rows, the accumulators
-        s.tiles.init(1 + (cta_rank() == 0) + (OP == kWgrad || (OP == kForward && FP8)) + kEpilogueWarps);
+        // readers: the copies, the products (first CTA), the cleared rows, the accumulators
+        s.tiles.init(1 + (cta_rank() == 0) + (OP == kWgrad) + kEpilogueWarps);
         s.stop = 0;
         bar_init_fence();
     }
@@ -656,7 +570,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         } else if (warp == 1) {
             if (cta_rank() == 0) multiply<OP, FP8>(a, s);
         } else if (warp == 2) {
-            if constexpr (FP8 && OP == kForward) copy_scales(a, s);
             if constexpr (OP == kWgrad) clear_rows(a, s);
         } else {
             schedule<OP, FP8>(a, s);
@@ -713,8 +626,7 @@ int launch(const LinearCall& c, const CUtensorMap& ma, const CUtensorMap& mb, co
 
 int prepare_linear_tc()
 {
-    int rc = prepare_kernel<kForward, true>();
-    if (rc == DR_OK) rc = prepare_kernel<kForwardRows, true>();
+    int rc = prepare_kernel<kForwardRows, true>();
     if (rc == DR_OK) rc = prepare_kernel<kForward, false>();
     if (rc == DR_OK) rc = prepare_kernel<kDgrad, false>();
     if (rc == DR_OK) rc = prepare_kernel<kWgrad, false>();
@@ -747,10 +659,6 @@ int launch_linear_tc(const LinearCall& c)
     a.k = (uint32_t)d.in_features;
     a.c_f32 = c.c_f32;
     a.accumulate = c.accumulate;
-    // fp8 with tokens on the M side, where their scales cost next to nothing but a ragged group costs whole tiles: from 512 rows
-    // a group on (8192 x 24576 x 4096: 797 us against 915 with the features there; 512 x 6144 x 4096: 30.8 / 32.8; 128 groups of
-    // 256 rows, 1536 x 2048: 170 / 158; one of 256 rows, 24576 x 4096: 56.3 / 55.3).
-    const bool by_rows = fp8 && c.rows >= 512ull * d.n_groups;
     CUtensorMap ma, mb, mc{};
     int rc;
     uint64_t tiles;
@@ -767,17 +675,17 @@ int launch_linear_tc(const LinearCall& c)
         a.feature_tiles = (width + (fp8 && a.n % 128 ? 127 : 0) + kTile - 1) / kTile;
         tiles = token_tiles * a.feature_tiles;
         a.vector = !c.c_f32 && width % 8 == 0 && c.ldc % 8 == 0 && (uintptr_t)c.c % 16 == 0;
-        if (by_rows) {
+        if (fp8) {
             a.vector = width % 16 == 0 && c.ldc % (c.c_f32 ? 8 : 16) == 0 && (uintptr_t)c.c % 32 == 0;
             rc = encode_map(&ma, c.a, true, a.k, c.rows, 0, c.lda, 128);
             if (rc == DR_OK) rc = encode_map(&mb, c.b, true, a.k, (uint64_t)a.n * a.n_groups, 0, c.ldb, 32);
             a.bulk_out = !c.c_f32 && a.n % 8 == 0 && c.ldc % 8 == 0 && (uintptr_t)c.c % 16 == 0 && c.ldc < (1ull << 38);
             if (rc == DR_OK && a.bulk_out) rc = encode_map(&mc, c.c, false, a.n, c.rows, 0, c.ldc, 32);
         } else if (c.op == kForward)
-            rc = encode_map(&ma, c.b, fp8, a.k, (uint64_t)a.n * a.n_groups, 0, c.ldb, 128);
+            rc = encode_map(&ma, c.b, false, a.k, (uint64_t)a.n * a.n_groups, 0, c.ldb, 128);
         else
             rc = encode_map(&ma, c.b, false, a.k, a.n, a.n_groups, c.ldb, 64);
-        if (rc == DR_OK && !by_rows) rc = encode_map(&mb, c.a, fp8, c.op == kForward ? a.k : a.n, c.rows, 0, c.lda, 32);
+        if (rc == DR_OK && !fp8) rc = encode_map(&mb, c.a, false, c.op == kForward ? a.k : a.n, c.rows, 0, c.lda, 32);
     }
     if (rc) return rc;
     if (tiles > 0x7FFFFFFFull) {
@@ -786,8 +694,7 @@ int launch_linear_tc(const LinearCall& c)
     }
     if (c.op == kWgrad) return launch<kWgrad, false>(c, ma, mb, mc, a, tiles);
     if (c.op == kDgrad) return launch<kDgrad, false>(c, ma, mb, mc, a, tiles);
-    if (by_rows) return launch<kForwardRows, true>(c, ma, mb, mc, a, tiles);
-    return fp8 ? launch<kForward, true>(c, ma, mb, mc, a, tiles) : launch<kForward, false>(c, ma, mb, mc, a, tiles);
+    return fp8 ? launch<kForwardRows, true>(c, ma, mb, mc, a, tiles) : launch<kForward, false>(c, ma, mb, mc, a, tiles);
 }
 
 int linear_wait_failures(uint64_t* out)
