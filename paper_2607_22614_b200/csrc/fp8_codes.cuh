@@ -70,6 +70,32 @@ __device__ __forceinline__ uint2 quantise8(const float* x, float scale, float re
     return q;
 }
 
+// The same codes without a test and a branch: every quotient is corrected.  For kernels that the conversions' and comparisons'
+// pipe bounds (the rows of activations: 8192 x 12288 bf16 75 us with the test, 56 without): the tests' integer minima cost more
+// there than multiply-adds, and more values are in doubt than in a weight (3.5e-5 of a block's maximum and less is below 2^-6).
+//
+// x / scale rounded to nearest, from t = x * fl32(1 / scale) by two of Markstein's corrections: the remainder x - t scale is exact in a
+// fused multiply-add, and adding it back rounds once; the first makes t faithful, the second correctly rounded.  For
+// scales in [2^-100, 2^126], where neither the remainders that can matter (|t| >= 2^-11) nor the reciprocal leave the normal range.
+__device__ __forceinline__ float quotient(float x, float scale, float recip)
+{
+    float t = __fmul_rn(x, recip);
+    t = fmaf(-fmaf(t, scale, -x), recip, t);  // (these signs keep a zero's)
+    return fmaf(-fmaf(t, scale, -x), recip, t);
+}
+__device__ __forceinline__ uint2 quantise8_corrected(const float* x, float scale, float recip)
+{
+    float t[8];
+    if (scale >= 7.8886091e-31f && scale <= 8.5070592e+37f) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) t[k] = quotient(x[k], scale, recip);
+    } else {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) t[k] = __fdiv_rn(x[k], scale);
+    }
+    return pack8(t);
+}
+
 // Stored scale of a block whose largest magnitude is m: m / 448 held inside the normal fp32 range, so that a block whose
 // m / 448 underflows (the all-zero block among them) and a block holding an infinity keep finite, normal scales.
 __device__ __forceinline__ float scale_of(float m)

@@ -34,7 +34,7 @@ __device__ unsigned long long g_wait_failures;  // read by dr_diag_linear_wait_f
 
 constexpr int kForwardRows = 3;  // forward with tokens on the M side (fp8, many rows)
 
-template <int OP> constexpr uint32_t kStages = OP == kForwardRows ? 5 : 6;
+template <int OP> constexpr uint32_t kStages = OP == kForwardRows || OP == kWgrad ? 5 : 6;
 constexpr uint32_t kStageBytes = 32768, kOperandBytes = 16384;
 constexpr uint32_t kEpilogueWarps = 8;
 constexpr uint32_t kThreads = 128 + 32 * kEpilogueWarps;
@@ -68,9 +68,14 @@ struct Buffers<kForwardRows> {
     alignas(1024) uint8_t stage[kStages<kForwardRows>][kStageBytes];
     alignas(1024) uint8_t out[8][2][4096];  // twice 32 rows of 64 bf16 for each warp, on their way out
 };
+template <>
+struct Buffers<kWgrad> {
+    alignas(1024) uint8_t stage[kStages<kWgrad>][kStageBytes];
+    alignas(1024) uint8_t out[8][2][4096];  // twice 32 rows of 32 fp32 for each warp
+};
 template <int OP>
 struct Shared : Buffers<OP>, Barriers {};
-static_assert(sizeof(Shared<kForward>) <= 227 * 1024 && sizeof(Shared<kForwardRows>) <= 227 * 1024, "shared memory of a CTA");
+static_assert(sizeof(Shared<kForward>) <= 227 * 1024 && sizeof(Shared<kForwardRows>) <= 227 * 1024 && sizeof(Shared<kWgrad>) <= 227 * 1024, "shared memory of a CTA");
 
 struct TcArgs {
     const int32_t* offsets;
@@ -177,30 +182,6 @@ __device__ __forceinline__ void store_tokens(const TcArgs& a, uint32_t scratch, 
             else
                 ((uint16_t*)a.c)[(uint64_t)r * a.ldc + ff] = (uint16_t)pack_bf16(v[g][i], 0.0f);
         }
-}
-
-// The same eight columns of dW: rows are the warp's 32 features.
-__device__ __forceinline__ void store_dw(const TcArgs& a, uint64_t row, uint32_t rows_left, uint32_t col, const float (&v)[4][2])
-{
-    const uint32_t lane = threadIdx.x & 31, c = col + 2 * (lane & 3);
-#pragma unroll
-    for (int g = 0; g < 4; ++g) {
-        const uint32_t r = (lane >> 2) + 8 * g;
-        if (r >= rows_left || c >= a.k) continue;
-        float* p = (float*)a.c + (row + r) * a.ldc + c;
-        if (a.vector) {
-            float2 w = make_float2(v[g][0], v[g][1]);
-            if (a.accumulate) {
-                const float2 was = *(float2*)p;
-                w.x += was.x;
-                w.y += was.y;
-            }
-            *(float2*)p = w;
-        } else {
-            p[0] = a.accumulate ? p[0] + v[g][0] : v[g][0];
-            if (c + 1 < a.k) p[1] = a.accumulate ? p[1] + v[g][1] : v[g][1];
-        }
-    }
 }
 
 // Finds the pair's tiles for the other warps.
@@ -330,7 +311,75 @@ __device__ __forceinline__ void clear_rows(const TcArgs& a, Shared<kWgrad>& s)
     }
 }
 
-template <int OP, bool FP8>
+// dW leaves through the copy unit, 32 rows x 32 columns at a time, two blocks of a warp in flight: the map's third dimension is the group,
+// so that it clips at the group's last row, and the addition to an accumulated gradient is the copy unit's too (each
+// element once a call, so the result does not depend on an order).
+__device__ __forceinline__ void write_dw(const TcArgs& a, Shared<kWgrad>& s, const CUtensorMap* map_c)
+{
+    const uint32_t lane = threadIdx.x & 31, warp = (threadIdx.x >> 5) - 4, rank = cta_rank();
+    const uint32_t quarter = warp & 3, side = warp >> 2;
+    const uint32_t acc_full = smem_u32(s.acc_full), acc_empty = in_cta(smem_u32(s.acc_empty), 0);
+    const uint32_t tmem = s.tmem + (quarter * 32 << 16), out = smem_u32(s.out[warp][0]);
+    Turn<2> acc;
+    Turn<kTilesAhead> at;
+    Tile t;
+    uint32_t blocks = 0;
+    while (s.tiles.get(t, at, &s.stop, &g_wait_failures)) {
+        const uint32_t cols = t.nt / 2, col0 = side * cols;  // this warp's columns, a multiple of 16
+        const uint32_t row = t.feature + rank * 128 + quarter * 32;
+        if (t.steps) {
+            if (!__all_sync(0xFFFFFFFFu, bar_wait(acc_full + 8 * acc.slot, acc.round, &s.stop, &g_wait_failures))) return;
+            fence_after();
+        }
+        // blocks of 32 columns; a last one of 16 ends where the next warp's columns (or the matrix) begin, and is stored directly
+        for (uint32_t c = 0; c < cols; c += 32) {
+            float v[32];
+            if (t.steps) {
+                tmem_start(tmem + acc.slot * kTile + col0 + c, v);
+                tmem_arrived(v);
+            } else {
+#pragma unroll
+                for (int r = 0; r < 32; ++r) v[r] = 0.0f;  // dW of a group without rows
+            }
+            const uint32_t col = t.col0 + col0 + c;
+            if (!a.bulk_out || c + 32 > cols) {
+                const uint32_t end = min(a.k, t.col0 + col0 + cols);
+                if (row + lane < a.n) {
+                    float* p = (float*)a.c + ((uint64_t)t.e * a.n + row + lane) * a.ldc;
+#pragma unroll
+                    for (int r = 0; r < 32; ++r)
+                        if (col + r < end) p[col + r] = a.accumulate ? p[col + r] + v[r] : v[r];
+                }
+                continue;
+            }
+            const uint32_t to = out + (blocks++ & 1) * 4096;
+            if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");  // the block before the last has left
+            __syncwarp();
+#pragma unroll
+            for (uint32_t q = 0; q < 8; ++q)
+                store_shared(to + lane * 128 + (q ^ (lane & 7)) * 16, __float_as_uint(v[4 * q]), __float_as_uint(v[4 * q + 1]),
+                             __float_as_uint(v[4 * q + 2]), __float_as_uint(v[4 * q + 3]));
+            fence_async();
+            __syncwarp();
+            if (lane == 0 && row < a.n && col < a.k) {
+                if (a.accumulate)
+                    add_3d(map_c, to, (int)col, (int)row, (int)t.e);
+                else
+                    store_3d(map_c, to, (int)col, (int)row, (int)t.e);
+                asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+            }
+        }
+        if (t.steps) {
+            fence_before();
+            __syncwarp();
+            if (lane == 0) bar_arrive_cluster(acc_empty + 8 * acc.slot);
+            acc.next();
+        }
+    }
+    asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");  // the last block has left before the CTA may end
+}
+
+template <int OP>
 __device__ __forceinline__ void write_out(const TcArgs& a, Shared<OP>& s)
 {
     const uint32_t lane = threadIdx.x & 31, warp = (threadIdx.x >> 5) - 4, rank = cta_rank();
@@ -338,49 +387,32 @@ __device__ __forceinline__ void write_out(const TcArgs& a, Shared<OP>& s)
     const uint32_t acc_full = smem_u32(s.acc_full), acc_empty = in_cta(smem_u32(s.acc_empty), 0);
     const uint32_t scratch = smem_u32(s.scratch[warp]);
     const uint32_t tmem = s.tmem + (quarter * 32 << 16);
-    uint32_t acc = 0;
-    bool ok = true;
+    Turn<2> acc;
     Turn<kTilesAhead> at;
     Tile t;
     while (s.tiles.get(t, at, &s.stop, &g_wait_failures)) {
-        const uint32_t cols = t.nt / 2, col0 = side * cols;  // this warp's columns
+        const uint32_t cols = t.nt / 2, col0 = side * cols;  // this warp's tokens
         const uint32_t feature = t.feature + rank * 128 + quarter * 32;
         // in a row of c: forward counts features from the group's first weight row
         const int f = OP == kForward ? (int)(feature - t.e * a.n) : (int)feature;
         const int f_hi = OP == kDgrad ? (int)a.k : (int)a.n;
-        auto put = [&](uint32_t c, const float (&v)[4][2]) {  // columns col0 + c .. + 7
-            if (OP == kWgrad)
-                store_dw(a, (uint64_t)t.e * a.n + feature, feature < a.n ? a.n - feature : 0, t.col0 + col0 + c, v);
-            else
-                store_tokens(a, scratch, t.row0 + col0 + c, t.row_end, f, f_hi, v);
-        };
-        if (t.steps) {
-            ok = bar_wait(acc_full + 8 * (acc & 1), acc >> 1 & 1, &s.stop, &g_wait_failures);
-            if (!__all_sync(0xFFFFFFFFu, ok)) return;
-            fence_after();
-        }
+        if (!__all_sync(0xFFFFFFFFu, bar_wait(acc_full + 8 * acc.slot, acc.round, &s.stop, &g_wait_failures))) return;
+        fence_after();
         for (uint32_t c = 0; c < cols; c += 32) {
             float p[2][16];
-            if (t.steps) {
-                tmem_load(tmem + (acc & 1) * kTile + col0 + c, p[0], p[1]);
-            } else {
-#pragma unroll
-                for (int r = 0; r < 16; ++r) p[0][r] = p[1][r] = 0.0f;  // dW of a group without rows
-            }
+            tmem_load(tmem + acc.slot * kTile + col0 + c, p[0], p[1]);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 if (c + j * 8 >= cols) break;
                 const float v[4][2] = {{p[0][4 * j], p[0][4 * j + 1]}, {p[0][4 * j + 2], p[0][4 * j + 3]},
                                        {p[1][4 * j], p[1][4 * j + 1]}, {p[1][4 * j + 2], p[1][4 * j + 3]}};
-                put(c + j * 8, v);
+                store_tokens(a, scratch, t.row0 + col0 + c + j * 8, t.row_end, f, f_hi, v);
             }
         }
-        if (t.steps) {
-            fence_before();
-            __syncwarp();
-            if (lane == 0) bar_arrive_cluster(acc_empty + 8 * (acc & 1));
-            ++acc;
-        }
+        fence_before();
+        __syncwarp();
+        if (lane == 0) bar_arrive_cluster(acc_empty + 8 * acc.slot);
+        acc.next();
     }
 }
 
@@ -578,8 +610,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         if (FP8) asm volatile("setmaxnreg.inc.sync.aligned.u32 232;");
         if constexpr (OP == kForwardRows)
             write_rows(a, s, &map_c);
+        else if constexpr (OP == kWgrad)
+            write_dw(a, s, &map_c);
         else
-            write_out<OP, FP8>(a, s);
+            write_out(a, s);
     }
     __syncwarp();
     if (*(volatile uint32_t*)&s.stop) {  // a wait ran out: let the copies and products in flight end before the memory is given back
@@ -667,9 +701,10 @@ int launch_linear_tc(const LinearCall& c)
         a.feature_tiles = (a.n + kTile - 1) / kTile;
         a.column_tiles = (a.k + kTile - 1) / kTile;
         tiles = (uint64_t)a.feature_tiles * a.column_tiles * a.n_groups;
-        a.vector = a.k % 2 == 0 && c.ldc % 2 == 0 && (uintptr_t)c.c % 8 == 0;
+        a.bulk_out = c.ldc % 4 == 0 && (uintptr_t)c.c % 16 == 0 && (uint64_t)a.n * c.ldc < (1ull << 37);
         rc = encode_map(&ma, c.a, false, a.n, c.rows, 0, c.lda, 64);
         if (rc == DR_OK) rc = encode_map(&mb, c.b, false, a.k, c.rows, 0, c.ldb, 64);
+        if (rc == DR_OK && a.bulk_out) rc = encode_map_f32(&mc, c.c, a.k, a.n, a.n_groups, c.ldc, 32);
     } else {
         const uint32_t width = c.op == kForward ? a.n : a.k;
         a.feature_tiles = (width + (fp8 && a.n % 128 ? 127 : 0) + kTile - 1) / kTile;

@@ -29,6 +29,7 @@ def _same(codes, scales, v):
     nan = torch.isnan(v)
     assert torch.equal(torch.isnan(got), nan)
     assert torch.equal(got[~nan], want[~nan])
+    assert torch.equal(torch.signbit(got[~nan]), torch.signbit(v[~nan]))  # -0 and what rounds to it keep their sign
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
