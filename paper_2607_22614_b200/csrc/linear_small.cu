@@ -23,6 +23,7 @@ __device__ unsigned long long g_wait_failures;
 
 constexpr uint32_t kRowsTile = 64, kStages = 7, kWeightBytes = 16384, kStageBytes = kWeightBytes + kRowsTile * 128;
 constexpr uint32_t kThreads = 256, kBuffers = 512 / kRowsTile;
+constexpr uint32_t kTurn = 2, kTurns = kBuffers / kTurn;  // blocks of the contraction handed over at a time (fp8)
 constexpr uint32_t kScratchPitch = 80;
 constexpr uint32_t kTurnPitch = 36;  // floats
 
@@ -38,7 +39,7 @@ struct Shared {
     alignas(16) uint8_t scratch[4][8 * kScratchPitch];
     alignas(16) float scale[kBuffers][kRowsTile + 4];  // the rows' scales of a block, then the weight's
     uint64_t full[kStages], empty[kStages];
-    uint64_t acc_full[kBuffers], acc_empty[kBuffers], scale_full[kBuffers], scale_empty[kBuffers];
+    uint64_t acc_full[kTurns], acc_empty[kTurns], scale_full[kTurns], scale_empty[kTurns];
     uint64_t sums_full, sums_empty;
     TileRing<Tile> tiles;
     uint32_t tmem, stop;
@@ -163,22 +164,23 @@ __device__ __forceinline__ void multiply(const Args& a, Shared& s)
     const uint32_t acc_full = smem_u32(s.acc_full), acc_empty = smem_u32(s.acc_empty), tmem = s.tmem;
     const uint64_t first_a = operand(smem_u32(s.stage), 0), first_b = operand(smem_u32(s.stage) + kWeightBytes, 0);
     Turn<kStages> ring;
-    Turn<kBuffers> acc;
+    Turn<kTurns> acc;
     Turn<kTilesAhead> turn;
     Tile t;
     while (s.tiles.get(t, turn, &s.stop, &g_wait_failures)) {
         const uint32_t shape = shape_of(FP8, false, false, 128, t.nt);
         for (uint32_t l = 0; l < t.steps; ++l) {
-            if (FP8 || l == 0)
+            const uint32_t in_turn = FP8 ? l % kTurn : 0;
+            if (FP8 ? in_turn == 0 : l == 0)
                 if (!warp_wait(acc_empty + 8 * acc.slot, acc.round ^ 1, &s.stop, &g_wait_failures)) return;
             if (!warp_wait(full + 8 * ring.slot, ring.round, &s.stop, &g_wait_failures)) return;
             fence_after();
             const uint64_t da = first_a + ring.slot * (kStageBytes >> 4), db = first_b + ring.slot * (kStageBytes >> 4);
-            const bool last = FP8 || l + 1 == t.steps;
+            const uint32_t d = tmem + (acc.slot * kTurn + in_turn) * kRowsTile;
+            const bool last = l + 1 == t.steps || (FP8 && in_turn + 1 == kTurn);
             if (elect()) {
 #pragma unroll
-                for (uint32_t q = 0; q < 4; ++q)
-                    mma<1, FP8>(tmem + acc.slot * kRowsTile, da + 2 * q, db + 2 * q, shape, FP8 ? q != 0 : (l | q) != 0);
+                for (uint32_t q = 0; q < 4; ++q) mma<1, FP8>(d, da + 2 * q, db + 2 * q, shape, FP8 ? q != 0 : (l | q) != 0);
                 if (last) commit<1>(acc_full + 8 * acc.slot);
                 commit<1>(empty + 8 * ring.slot);
             }
@@ -193,20 +195,26 @@ __device__ __forceinline__ void copy_scales(const Args& a, Shared& s)
 {
     const uint32_t lane = threadIdx.x & 31, full = smem_u32(s.scale_full), empty = smem_u32(s.scale_empty);
     const uint32_t scale_rows = (a.n_groups * a.n + 127) / 128;
-    uint32_t n = 0;
+    Turn<kTurns> acc;
     Turn<kTilesAhead> turn;
     Tile t;
     while (s.tiles.get(t, turn, &s.stop, &g_wait_failures)) {
         const float* xs = a.a_scale + t.row0;
         const float* ws = a.b_scale + (uint64_t)min(t.feature / 128, scale_rows - 1) * a.ld_bs;
         const uint32_t left = t.row_end - t.row0;
-        for (uint32_t l = t.step0; l < t.step0 + t.steps; ++l, ++n) {
-            const uint32_t slot = n % kBuffers, to = smem_u32(s.scale[slot]);
-            if (!__all_sync(0xFFFFFFFFu, bar_wait(empty + 8 * slot, (n / kBuffers & 1) ^ 1, &s.stop, &g_wait_failures))) return;
+        for (uint32_t l = 0; l < t.steps; l += kTurn) {
+            if (!__all_sync(0xFFFFFFFFu, bar_wait(empty + 8 * acc.slot, acc.round ^ 1, &s.stop, &g_wait_failures))) return;
 #pragma unroll
-            for (uint32_t j = lane; j < kRowsTile; j += 32) copy_4(to + 4 * j, xs + l * a.ld_as + (j < left ? j : 0), j < left);
-            if (lane == 0) copy_4(to + 4 * kRowsTile, ws + l, true);
-            copies_arrive(full + 8 * slot);
+            for (uint32_t q = 0; q < kTurn; ++q) {
+                if (l + q >= t.steps) break;
+                const uint32_t to = smem_u32(s.scale[acc.slot * kTurn + q]);
+                const float* from = xs + (t.step0 + l + q) * a.ld_as;
+#pragma unroll
+                for (uint32_t j = lane; j < kRowsTile; j += 32) copy_4(to + 4 * j, from + (j < left ? j : 0), j < left);
+                if (lane == 0) copy_4(to + 4 * kRowsTile, ws + t.step0 + l + q, true);
+            }
+            copies_arrive(full + 8 * acc.slot);
+            acc.next();
         }
     }
 }
@@ -218,12 +226,15 @@ __device__ __forceinline__ void write_out(const Args& a, Shared& s)
     const uint32_t acc_full = smem_u32(s.acc_full), acc_empty = smem_u32(s.acc_empty);
     const uint32_t scale_full = smem_u32(s.scale_full), scale_empty = smem_u32(s.scale_empty);
     const uint32_t scratch = smem_u32(s.scratch[warp]), tmem = s.tmem + (warp * 32 << 16);
-    uint32_t acc = 0, handed = 0;
+    Turn<kTurns> acc;
+    uint32_t handed = 0;
+    // r / split for the rows of a tile: exact for r < 64 and split <= 8
+    const uint32_t magic = (65536 + a.split - 1) / a.split;
     Turn<kTilesAhead> turn;
     Tile t;
     while (s.tiles.get(t, turn, &s.stop, &g_wait_failures)) {
         float sum[2][2][16];
-        if (FP8 || t.steps == 0) {
+        if (FP8) {
 #pragma unroll
             for (int c = 0; c < 2; ++c)
 #pragma unroll
@@ -231,30 +242,33 @@ __device__ __forceinline__ void write_out(const Args& a, Shared& s)
 #pragma unroll
                     for (int r = 0; r < 16; ++r) sum[c][h][r] = 0.0f;
         }
-        const uint32_t products = FP8 ? t.steps : t.steps ? 1 : 0;
-        for (uint32_t l = 0; l < products; ++l, ++acc) {
-            const uint32_t buffer = acc % kBuffers, parity = acc / kBuffers & 1;
-            bool ok = !FP8 || bar_wait(scale_full + 8 * buffer, parity, &s.stop, &g_wait_failures);
-            ok = ok && bar_wait(acc_full + 8 * buffer, parity, &s.stop, &g_wait_failures);
+        for (uint32_t l = 0; l < t.steps; l += FP8 ? kTurn : t.steps) {
+            bool ok = !FP8 || bar_wait(scale_full + 8 * acc.slot, acc.round, &s.stop, &g_wait_failures);
+            ok = ok && bar_wait(acc_full + 8 * acc.slot, acc.round, &s.stop, &g_wait_failures);
             if (!__all_sync(0xFFFFFFFFu, ok)) return;
             fence_after();
-            const uint32_t from = tmem + buffer * kRowsTile;
+            const uint32_t from = tmem + acc.slot * kTurn * kRowsTile;
             if (FP8) {
-                const float* sc = s.scale[buffer] + 2 * (lane & 3);
-                const float w = s.scale[buffer][kRowsTile];
-                const uint64_t ww = pair_of(w, w);
 #pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    if (c * 32 >= t.nt) break;
-                    float p[2][16];
-                    tmem_load(from + c * 32, p[0], p[1]);
+                for (uint32_t q = 0; q < kTurn; ++q) {
+                    if (l + q >= t.steps) break;
+                    const float* sc = s.scale[acc.slot * kTurn + q];
+                    const float w = sc[kRowsTile];
+                    const uint64_t ww = pair_of(w, w);
+                    sc += 2 * (lane & 3);
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const uint64_t two = mul2(*(const uint64_t*)(sc + c * 32 + j * 8), ww);
+                    for (int c = 0; c < 2; ++c) {
+                        if (c * 32 >= t.nt) break;
+                        float p[2][16];
+                        tmem_load(from + q * kRowsTile + c * 32, p[0], p[1]);
 #pragma unroll
-                        for (int h = 0; h < 2; ++h) {
-                            fma2(sum[c][h][4 * j], sum[c][h][4 * j + 1], p[h][4 * j], p[h][4 * j + 1], two);
-                            fma2(sum[c][h][4 * j + 2], sum[c][h][4 * j + 3], p[h][4 * j + 2], p[h][4 * j + 3], two);
+                        for (int j = 0; j < 4; ++j) {
+                            const uint64_t two = mul2(*(const uint64_t*)(sc + c * 32 + j * 8), ww);
+#pragma unroll
+                            for (int h = 0; h < 2; ++h) {
+                                fma2(sum[c][h][4 * j], sum[c][h][4 * j + 1], p[h][4 * j], p[h][4 * j + 1], two);
+                                fma2(sum[c][h][4 * j + 2], sum[c][h][4 * j + 3], p[h][4 * j + 2], p[h][4 * j + 3], two);
+                            }
                         }
                     }
                 }
@@ -265,9 +279,10 @@ __device__ __forceinline__ void write_out(const Args& a, Shared& s)
             fence_before();
             __syncwarp();
             if (lane == 0) {
-                bar_arrive(acc_empty + 8 * buffer);
-                if (FP8) bar_arrive(scale_empty + 8 * buffer);
+                bar_arrive(acc_empty + 8 * acc.slot);
+                if (FP8) bar_arrive(scale_empty + 8 * acc.slot);
             }
+            acc.next();
         }
         const int f = (int)(t.feature + warp * 32 - t.e * a.n);  // in a row of c
         if (a.split == 1) {
@@ -285,7 +300,7 @@ __device__ __forceinline__ void write_out(const Args& a, Shared& s)
         // Every row of the tile ends in one CTA of the cluster (row r in CTA r mod split): the others send it their sums with
         // stores that count on its barrier, so that no CTA waits on a fence, and it adds them in the order of the ranks.
         const uint32_t rank = cta_rank(), rows = t.row_end - t.row0;
-        const uint32_t most = (kRowsTile + a.split - 1) / a.split, owned = rows > rank ? (rows - rank + a.split - 1) / a.split : 0;
+        const uint32_t most = (kRowsTile - 1) * magic / 65536 + 1, owned = rows > rank ? (rows - 1 - rank) * magic / 65536 + 1 : 0;
         if (!__all_sync(0xFFFFFFFFu, bar_wait(smem_u32(&s.sums_empty), (handed & 1) ^ 1, &s.stop, &g_wait_failures))) return;
         if (warp == 0 && lane == 0) bar_expect(smem_u32(&s.sums_full), owned * a.split * 512);
 #pragma unroll
@@ -306,8 +321,8 @@ __device__ __forceinline__ void write_out(const Args& a, Shared& s)
                 const uint32_t r = c * 16 + i * 4 + (lane >> 3);
                 if (r >= rows) continue;
                 const float4 v = *(const float4*)&s.turn[warp][r & 15][(lane & 7) * 4];
-                const uint32_t to = r % a.split;
-                store_counted(in_cta(smem_u32(&s.sums[rank * most + r / a.split][warp * 32 + (lane & 7) * 4]), to), v,
+                const uint32_t nth = r * magic / 65536, to = r - nth * a.split;
+                store_counted(in_cta(smem_u32(&s.sums[rank * most + nth][warp * 32 + (lane & 7) * 4]), to), v,
                               in_cta(smem_u32(&s.sums_full), to));
             }
         }
@@ -360,7 +375,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             bar_init(smem_u32(&s.full[i]), 1);
             bar_init(smem_u32(&s.empty[i]), 1);
         }
-        for (uint32_t i = 0; i < kBuffers; ++i) {
+        for (uint32_t i = 0; i < kTurns; ++i) {
             bar_init(smem_u32(&s.acc_full[i]), 1);
             bar_init(smem_u32(&s.acc_empty[i]), 4);
             bar_init(smem_u32(&s.scale_full[i]), 32);
@@ -424,18 +439,18 @@ __global__ void __launch_bounds__(kThreads, 1)
 constexpr size_t kSharedBytes = sizeof(Shared);
 
 // CTAs that share a tile's contraction: `fit[s]` clusters of s CTAs run at the same time, so that `tiles` take
-// ceil(tiles / fit[s]) rounds of 1 / s of the contraction each.  The smallest split within 2 % of the least time wins, each part at
-// least two steps long.
+// ceil(tiles / fit[s]) rounds.  A round is 1 / s of the contraction and the end of a tile, which costs about two steps' time, or
+// eight with an exchange (measured, 64 rows: a step of 128 takes 0.3 us, the exchange 2.5 us).
 uint32_t choose_split(uint64_t tiles, const uint32_t (&fit)[kMaxSplit + 1], uint32_t steps)
 {
     uint32_t best = 1;
-    double least = 0.0;
+    uint64_t least = ~0ull;
     for (uint32_t s = 1; s <= kMaxSplit && (s == 1 || s * 2 <= steps); ++s) {
         if (fit[s] == 0) continue;
-        const double rounds = (double)((tiles + fit[s] - 1) / fit[s]) / s;
-        if (s == 1 || rounds < 0.98 * least) {
+        const uint64_t time = ((tiles + fit[s] - 1) / fit[s]) * ((steps + s - 1) / s + (s == 1 ? 2 : 8));
+        if (time < least) {
             best = s;
-            least = rounds;
+            least = time;
         }
     }
     return best;
