@@ -3,6 +3,7 @@
 #include <cuda_runtime.h>
 
 #include "dr_internal.h"
+#include "overlap.cuh"
 
 namespace dr {
 constexpr uint32_t kMaxSplit = 8;  // CTAs of a cluster that share a contraction

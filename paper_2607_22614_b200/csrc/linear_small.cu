@@ -388,6 +388,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         bar_init_fence();
     }
     if (warp == 1) tmem_alloc<1>(smem_u32(&s.tmem), 512);
+    after_previous();
     for (uint32_t e = threadIdx.x; e < a.n_groups; e += kThreads) {
         uint32_t lo, hi;
         group_rows(a.offsets, e, a.rows, lo, hi);
@@ -440,14 +441,14 @@ constexpr size_t kSharedBytes = sizeof(Shared);
 
 // CTAs that share a tile's contraction: `fit[s]` clusters of s CTAs run at the same time, so that `tiles` take
 // ceil(tiles / fit[s]) rounds.  A round is 1 / s of the contraction and the end of a tile, which costs about two steps' time, or
-// eight with an exchange (measured, 64 rows: a step of 128 takes 0.3 us, the exchange 2.5 us).
-uint32_t choose_split(uint64_t tiles, const uint32_t (&fit)[kMaxSplit + 1], uint32_t steps)
+// five to eight with an exchange of 16 to 64 rows (measured, 64 rows: a step of 128 takes 0.3 us, the exchange 2.5 us).
+uint32_t choose_split(uint64_t tiles, const uint32_t (&fit)[kMaxSplit + 1], uint32_t steps, uint32_t rows)
 {
     uint32_t best = 1;
     uint64_t least = ~0ull;
     for (uint32_t s = 1; s <= kMaxSplit && (s == 1 || s * 2 <= steps); ++s) {
         if (fit[s] == 0) continue;
-        const uint64_t time = ((tiles + fit[s] - 1) / fit[s]) * ((steps + s - 1) / s + (s == 1 ? 2 : 8));
+        const uint64_t time = ((tiles + fit[s] - 1) / fit[s]) * ((steps + s - 1) / s + (s == 1 ? 2 : 4 + (rows + 15) / 16));
         if (time < least) {
             best = s;
             least = time;
@@ -456,18 +457,19 @@ uint32_t choose_split(uint64_t tiles, const uint32_t (&fit)[kMaxSplit + 1], uint
     return best;
 }
 
-cudaLaunchConfig_t config(cudaLaunchAttribute& attr, uint64_t clusters, uint32_t split, cudaStream_t stream)
+cudaLaunchConfig_t config(cudaLaunchAttribute (&attr)[2], uint64_t clusters, uint32_t split, cudaStream_t stream)
 {
-    attr.id = cudaLaunchAttributeClusterDimension;
-    attr.val.clusterDim.x = split;
-    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = split;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    attr[1] = overlap_attribute();
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)(clusters * split));
     cfg.blockDim = dim3(kThreads);
     cfg.dynamicSmemBytes = kSharedBytes;
     cfg.stream = stream;
-    cfg.attrs = &attr;
-    cfg.numAttrs = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
     return cfg;
 }
 
@@ -475,7 +477,7 @@ template <bool FP8>
 int launch(const LinearCall& c, const CUtensorMap& mw, const CUtensorMap& mx, const Args& a, uint64_t tiles)
 {
     const uint64_t clusters = c.lin->fit[a.split];
-    cudaLaunchAttribute attr;
+    cudaLaunchAttribute attr[2];
     const cudaLaunchConfig_t cfg = config(attr, tiles < clusters ? tiles : clusters, a.split, c.stream);
     const cudaError_t err = cudaLaunchKernelEx(&cfg, small_kernel<FP8>, mw, mx, a);
     if (err != cudaSuccess) {
@@ -493,7 +495,7 @@ int prepare_linear_small(uint32_t (&fit)[kMaxSplit + 1])
     DR_CUDA(cudaFuncSetAttribute(small_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSharedBytes));
     DR_CUDA(cudaFuncSetAttribute(small_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSharedBytes));
     for (uint32_t s = 1; s <= kMaxSplit; ++s) {
-        cudaLaunchAttribute attr;
+        cudaLaunchAttribute attr[2];
         const cudaLaunchConfig_t cfg = config(attr, 64, s, nullptr);
         int n = 0;
         DR_CUDA(cudaOccupancyMaxActiveClusters(&n, small_kernel<true>, &cfg));
@@ -533,7 +535,7 @@ int launch_linear_small(const LinearCall& c)
         return DR_ERR_UNSUPPORTED;
     }
     const uint32_t step = fp8 ? 128 : 64;
-    a.split = choose_split(tiles, c.lin->fit, (a.k + step - 1) / step);
+    a.split = choose_split(tiles, c.lin->fit, (a.k + step - 1) / step, c.rows < kRowsTile ? c.rows : kRowsTile);
     CUtensorMap mw, mx;
     int rc = encode_map(&mw, c.b, fp8, a.k, (uint64_t)a.n * a.n_groups, 0, c.ldb, 128);
     if (rc == DR_OK) rc = encode_map(&mx, c.a, fp8, a.k, c.rows, 0, c.lda, 16);

@@ -574,6 +574,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         bar_init_fence();
     }
     if (warp == 1) tmem_alloc<2>(smem_u32(&s.tmem), 512);
+    after_previous();
     if (warp == 2 && OP != kWgrad) {  // running sum of the groups' token tiles
         uint32_t before = 0;
         if (lane == 0) s.tiles_before[0] = 0;
@@ -647,9 +648,17 @@ int launch(const LinearCall& c, const CUtensorMap& ma, const CUtensorMap& mb, co
 {
     const uint64_t pairs = (uint64_t)c.lin->sms / 2;
     const unsigned grid = 2 * (unsigned)(tiles < pairs ? tiles : pairs);
-    tc_kernel<OP, FP8><<<grid, kThreads, sizeof(Shared<OP>), c.stream>>>(ma, mb, mc, a);
-    cudaError_t err = cudaGetLastError();
+    cudaLaunchAttribute attr = overlap_attribute();
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(grid);
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = sizeof(Shared<OP>);
+    cfg.stream = c.stream;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    const cudaError_t err = cudaLaunchKernelEx(&cfg, tc_kernel<OP, FP8>, ma, mb, mc, a);
     if (err != cudaSuccess) {
+        cudaGetLastError();
         set_error("linear kernel launch: %s", cudaGetErrorString(err));
         return DR_ERR_CUDA;
     }

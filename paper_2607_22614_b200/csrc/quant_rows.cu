@@ -16,6 +16,7 @@
 
 #include "dr_internal.h"
 #include "fp8_codes.cuh"
+#include "overlap.cuh"
 
 namespace dr {
 namespace {
@@ -107,6 +108,7 @@ __global__ void __launch_bounds__(32 * kWarps, SWIGLU ? 4 : 3) rows_kernel(const
     const uint64_t row0 = (uint64_t)tile * kRows;
     const uint32_t c = part * 512 + lane * 16;
     uint32_t x[RPW][kRaw], up[SWIGLU ? RPW : 1][kRaw];
+    after_previous();
 #pragma unroll
     for (int i = 0; i < RPW; ++i) {
         const uint64_t r = row0 + warp * RPW + i;
@@ -160,12 +162,17 @@ __global__ void __launch_bounds__(32 * kWarps, SWIGLU ? 4 : 3) rows_kernel(const
 template <bool F32, bool SWIGLU, int VEC>
 int launch(const RowsArgs& a, int rpw, uint64_t blocks, cudaStream_t stream)
 {
-    if (rpw == kManyRows<F32, SWIGLU>)
-        rows_kernel<F32, SWIGLU, VEC, kManyRows<F32, SWIGLU>><<<(unsigned)blocks, 32 * kWarps, 0, stream>>>(a);
-    else
-        rows_kernel<F32, SWIGLU, VEC, 1><<<(unsigned)blocks, 32 * kWarps, 0, stream>>>(a);
-    cudaError_t e = cudaGetLastError();
+    cudaLaunchAttribute attr = overlap_attribute();
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)blocks);
+    cfg.blockDim = dim3(32 * kWarps);
+    cfg.stream = stream;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    constexpr int many = kManyRows<F32, SWIGLU>;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, rpw == many ? rows_kernel<F32, SWIGLU, VEC, many> : rows_kernel<F32, SWIGLU, VEC, 1>, a);
     if (e != cudaSuccess) {
+        cudaGetLastError();
         set_error("row quantisation launch: %s", cudaGetErrorString(e));
         return DR_ERR_CUDA;
     }
