@@ -540,24 +540,30 @@ class Plan:
 
     _stream = staticmethod(_current_stream)
 
-    def linear(self, arena, name, n_groups=None):
-        """The Linear layer over rollout tensor `name` ("layers.0.qkv", "layers.3.w13", ...) of `arena` (a uint8 CUDA
-        tensor that dr_reshard writes).  n_groups: experts stacked in w13 / w2; taken from the plan when it is None."""
+    def view(self, arena, name):
+        """Rollout tensor `name` ("layers.0.qkv", "layers.3.w13", ...) of `arena` (a uint8 CUDA tensor that dr_reshard writes), as
+        (payload [rows, cols] in its own type, block scales or None)."""
         import torch
         t = next((t for t in self.tensors() if t.name.decode() == name), None)
         if t is None:
             raise KeyError(f"the plan has no rollout tensor {name!r}")
-        if t.elem_size == 4:
-            raise TypeError("a linear layer needs bf16 or fp8 weights")
-        if n_groups is None:
-            n_groups = max(1, self.experts) if name.rsplit(".", 1)[-1] in ("w13", "w2") else 1
 
         def part(off, rows, cols, dtype, size):
             return arena[off:off + rows * cols * size].view(dtype).view(rows, cols)
 
-        w = part(t.arena_off, t.rows, t.cols, torch.float8_e4m3fn if t.quantised else torch.bfloat16, t.elem_size)
-        s = part(t.scale_off, t.scale_rows, t.scale_cols, torch.float32, 4) if t.quantised else None
-        return Linear(w, s, n_groups=n_groups)
+        types = {1: torch.float8_e4m3fn, 2: torch.bfloat16, 4: torch.float32}
+        return (part(t.arena_off, t.rows, t.cols, types[t.elem_size], t.elem_size),
+                part(t.scale_off, t.scale_rows, t.scale_cols, torch.float32, 4) if t.quantised else None)
+
+    def linear(self, arena, name, n_groups=None):
+        """The Linear layer over rollout tensor `name` of `arena`.  n_groups: experts stacked in w13 / w2; taken from the plan
+        when it is None."""
+        weight, scale = self.view(arena, name)
+        if weight.element_size() == 4:
+            raise TypeError("a linear layer needs bf16 or fp8 weights")
+        if n_groups is None:
+            n_groups = max(1, self.experts) if name.rsplit(".", 1)[-1] in ("w13", "w2") else 1
+        return Linear(weight, scale, n_groups=n_groups)
 
     def reshard(self, src, dst, stream=None):
         """src: CUDA tensor holding the flat fp32 buffer; dst: CUDA tensor holding the rollout arena."""

@@ -1,6 +1,8 @@
 // Entry points of the linear layers: argument checks, the handle, choice of kernel.
 #include "linear.h"
 
+#include <cstring>
+#include <mutex>
 #include <new>
 
 using namespace dr;
@@ -47,6 +49,28 @@ int check_rows(const dr_linear* lin, uint64_t rows, const int32_t* offsets, cons
         set_error("a pointer is not aligned to its element size");
         return DR_ERR_ALIGN;
     }
+    return DR_OK;
+}
+
+// Once per device: shared memory for the kernels, and how many clusters of each size run at the same time.
+constexpr int kDevices = 64;
+std::mutex g_prepare;
+bool g_prepared[kDevices];
+uint32_t g_fit[kDevices][kMaxSplit + 1];
+
+int prepare_device(int dev, uint32_t (&fit)[kMaxSplit + 1])
+{
+    std::lock_guard<std::mutex> hold(g_prepare);
+    const bool known = dev >= 0 && dev < kDevices;
+    if (!known || !g_prepared[dev]) {
+        int rc = prepare_linear_tc();
+        if (rc == DR_OK) rc = prepare_linear_small(fit);
+        if (rc) return rc;
+        if (!known) return DR_OK;
+        memcpy(g_fit[dev], fit, sizeof fit);
+        g_prepared[dev] = true;
+    }
+    memcpy(fit, g_fit[dev], sizeof fit);
     return DR_OK;
 }
 
@@ -139,8 +163,7 @@ int dr_linear_create(const dr_linear_desc* desc, dr_linear** out)
     DR_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
     dr_linear* lin = new (std::nothrow) dr_linear();
     if (!lin) return DR_ERR_NOMEM;
-    int rc = prepare_linear_tc();
-    if (rc == DR_OK) rc = prepare_linear_small(lin->fit);
+    const int rc = prepare_device(dev, lin->fit);
     if (rc) {
         delete lin;
         return rc;

@@ -333,6 +333,8 @@ __device__ __forceinline__ void write_dw(const TcArgs& a, Shared<kWgrad>& s, con
         }
         // blocks of 32 columns; a last one of 16 ends where the next warp's columns (or the matrix) begin, and is stored directly
         for (uint32_t c = 0; c < cols; c += 32) {
+            const uint32_t col = t.col0 + col0 + c;
+            if (row >= a.n || col >= a.k) break;  // nothing of dW there (and every block that takes a buffer starts one store)
             float v[32];
             if (t.steps) {
                 tmem_start(tmem + acc.slot * kTile + col0 + c, v);
@@ -341,7 +343,6 @@ __device__ __forceinline__ void write_dw(const TcArgs& a, Shared<kWgrad>& s, con
 #pragma unroll
                 for (int r = 0; r < 32; ++r) v[r] = 0.0f;  // dW of a group without rows
             }
-            const uint32_t col = t.col0 + col0 + c;
             if (!a.bulk_out || c + 32 > cols) {
                 const uint32_t end = min(a.k, t.col0 + col0 + cols);
                 if (row + lane < a.n) {
@@ -361,7 +362,7 @@ __device__ __forceinline__ void write_dw(const TcArgs& a, Shared<kWgrad>& s, con
                              __float_as_uint(v[4 * q + 2]), __float_as_uint(v[4 * q + 3]));
             fence_async();
             __syncwarp();
-            if (lane == 0 && row < a.n && col < a.k) {
+            if (lane == 0) {
                 if (a.accumulate)
                     add_3d(map_c, to, (int)col, (int)row, (int)t.e);
                 else

@@ -130,7 +130,8 @@ def test_offsets_out_of_range_stay_inside():
 
 GRADS = [([40], 256, 256), ([3, 0, 1, 7], 256, 384), ([0, 0, 130, 0, 1, 64, 0, 259], 384, 512), ([1] * 33, 144, 272),
          ([0, 300, 0], 192, 208), ([63, 64, 65, 66], 128, 136), ([2, 0, 9], 40, 64), ([31, 1, 140], 12, 24), ([0, 0, 0], 128, 128),
-         ([7, 20], 130, 201), ([600, 70], 1536, 768)]
+         ([7, 20], 130, 201), ([600, 70], 1536, 768), ([1, 2, 1, 90, 0, 7, 90, 2, 1, 0, 64] * 3, 544, 192), ([3, 0, 65] * 9, 400, 656),
+         ([1, 0, 2] * 11, 896, 304)]
 
 
 @pytest.mark.parametrize("out", [BF16, F32], ids=["bf16", "f32"])
