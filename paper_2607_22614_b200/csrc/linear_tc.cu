@@ -54,7 +54,7 @@ struct Tile {
 struct Barriers {
     TileRing<Tile> tiles;
     uint64_t full[6], empty[6], landed[6];
-    uint64_t acc_full[2], acc_empty[2];
+    alignas(16) uint64_t acc_full[2], acc_empty[2];  // (the readers flip bit 3 of their addresses)
     uint32_t tmem, stop;
     uint32_t tiles_before[kMaxTcGroups + 1];  // token tiles of the groups before
 };
@@ -423,11 +423,10 @@ __device__ __forceinline__ void write_rows(const TcArgs& a, Shared<kForwardRows>
 {
     const uint32_t lane = threadIdx.x & 31, warp = (threadIdx.x >> 5) - 4, rank = cta_rank();
     const uint32_t quarter = warp & 3, side = warp >> 2;
-    const uint32_t acc_full = smem_u32(s.acc_full), acc_empty = in_cta(smem_u32(s.acc_empty), 0);
-    const uint32_t tmem = s.tmem + (quarter * 32 << 16) + side * 128;
+    uint32_t filled = smem_u32(s.acc_full), emptied = in_cta(smem_u32(s.acc_empty), 0), parity = 0;
+    uint32_t from = s.tmem + (quarter * 32 << 16) + side * 128;  // all 512 columns are this CTA's: the accumulators start at 0 and 256
     const uint32_t scale_rows = (a.n_groups * a.n + 127) / 128;
     const uint32_t out = smem_u32(s.out[warp][0]);
-    uint32_t acc = 0;
     Turn<kTilesAhead> at;
     Tile t;
     const float *xs, *ws;
@@ -441,7 +440,10 @@ __device__ __forceinline__ void write_rows(const TcArgs& a, Shared<kForwardRows>
         w1 = ws[0];
         x2 = t.steps > 1 ? xs[a.ld_as] : 0.0f;
         w2 = t.steps > 1 ? ws[1] : 0.0f;
-        xs += 2 * a.ld_as;
+        if (t.steps > 2) {
+            xs += 2 * a.ld_as;
+            ws += 2;
+        }
         return true;
     };
     bool more = next_tile();
@@ -455,40 +457,44 @@ __device__ __forceinline__ void write_rows(const TcArgs& a, Shared<kForwardRows>
         for (int c = 0; c < 4; ++c)
 #pragma unroll
             for (int r = 0; r < 32; ++r) sum[c][r] = 0.0f;
-        for (uint32_t l = 0; l < steps; ++l, ++acc) {
+        for (uint32_t left = steps; left; --left) {
             const float scale = x1 * w1;
+            const uint64_t two = pair_of(scale, scale);
+            if (!__all_sync(0xFFFFFFFFu, bar_wait(filled, parity, &s.stop, &g_wait_failures))) return;
+            fence_after();
+            float p[2][32];
+            if (!idle) tmem_start(from, p[0]);
+            // in the shadow of the loads: the scales of the step after the next (the last two steps read the last again)
             x1 = x2;
             w1 = w2;
-            if (l + 2 < steps) {
-                x2 = *xs;
-                w2 = ws[l + 2];
+            x2 = *xs;
+            w2 = *ws;
+            if (left > 3) {
                 xs += a.ld_as;
+                ++ws;
             }
-            const bool ok = bar_wait(acc_full + 8 * (acc & 1), acc >> 1 & 1, &s.stop, &g_wait_failures);
-            if (!__all_sync(0xFFFFFFFFu, ok)) return;
-            fence_after();
             if (idle) {
                 fence_before();
-                if (lane == 0) bar_arrive_cluster(acc_empty + 8 * (acc & 1));
-                continue;
-            }
-            const uint64_t two = pair_of(scale, scale);
-            const uint32_t from = tmem + (acc & 1) * kTile;
-            float p[2][32];
-            tmem_start(from, p[0]);
+                if (lane == 0) bar_arrive_cluster(emptied);
+            } else {
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                tmem_arrived(p[c & 1]);
-                if (c < 3) {
-                    tmem_start(from + 32 * (c + 1), p[(c + 1) & 1]);
-                } else {  // the accumulator has been read: the next product may begin
-                    fence_before();
-                    __syncwarp();
-                    if (lane == 0) bar_arrive_cluster(acc_empty + 8 * (acc & 1));
+                for (int c = 0; c < 4; ++c) {
+                    tmem_arrived(p[c & 1]);
+                    if (c < 3) {
+                        tmem_start(from + 32 * (c + 1), p[(c + 1) & 1]);
+                    } else {  // the accumulator has been read: the next product may begin
+                        fence_before();
+                        __syncwarp();
+                        if (lane == 0) bar_arrive_cluster(emptied);
+                    }
+#pragma unroll
+                    for (int r = 0; r < 32; r += 2) fma2(sum[c][r], sum[c][r + 1], p[c & 1][r], p[c & 1][r + 1], two);
                 }
-#pragma unroll
-                for (int r = 0; r < 32; r += 2) fma2(sum[c][r], sum[c][r + 1], p[c & 1][r], p[c & 1][r + 1], two);
             }
+            from ^= kTile;  // the other accumulator and its barriers
+            filled ^= 8;
+            emptied ^= 8;
+            parity ^= from & kTile ? 0 : 1;
         }
         more = next_tile();  // its scales are on their way while this tile leaves
         if (idle) continue;
