@@ -77,21 +77,47 @@ __device__ __forceinline__ uint2 quantise8(const float* x, float scale, float re
 // x / scale rounded to nearest, from t = x * fl32(1 / scale) by two of Markstein's corrections: the remainder x - t scale is exact in a
 // fused multiply-add, and adding it back rounds once; the first makes t faithful, the second correctly rounded.  For
 // scales in [2^-100, 2^126], where neither the remainders that can matter (|t| >= 2^-11) nor the reciprocal leave the normal range.
-__device__ __forceinline__ float quotient(float x, float scale, float recip)
+// The caller gives -x, so that the remainder x - t scale comes out negated without another instruction and a zero keeps its
+// sign.  PACKED takes two values an instruction: 3 % less time from bf16, where instructions bound (8192 x 12288: 54.8 against
+// 56.1 us, through SwiGLU 107 against 110), 12 % more from fp32, where the memory does (81.6 against 72.8).
+__device__ __forceinline__ uint64_t two_of(float lo, float hi)
 {
-    float t = __fmul_rn(x, recip);
-    t = fmaf(-fmaf(t, scale, -x), recip, t);  // (these signs keep a zero's)
-    return fmaf(-fmaf(t, scale, -x), recip, t);
+    uint64_t d;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "f"(lo), "f"(hi));
+    return d;
 }
-__device__ __forceinline__ uint2 quantise8_corrected(const float* x, float scale, float recip)
+__device__ __forceinline__ uint64_t fma_two(uint64_t a, uint64_t b, uint64_t c)
+{
+    uint64_t d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+template <bool PACKED>
+__device__ __forceinline__ uint2 quantise8_corrected(const float* minus_x, float scale, float recip)
 {
     float t[8];
-    if (scale >= 7.8886091e-31f && scale <= 8.5070592e+37f) {
+    const bool in_range = scale >= 7.8886091e-31f && scale <= 8.5070592e+37f;
+    if (!PACKED && in_range) {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) t[k] = quotient(x[k], scale, recip);
+        for (int k = 0; k < 8; ++k) {
+            t[k] = __fmul_rn(minus_x[k], -recip);
+            t[k] = fmaf(fmaf(t[k], scale, minus_x[k]), -recip, t[k]);
+            t[k] = fmaf(fmaf(t[k], scale, minus_x[k]), -recip, t[k]);
+        }
+    } else if (in_range) {
+        const uint64_t minus_r = two_of(-recip, -recip), s = two_of(scale, scale);
+#pragma unroll
+        for (int k = 0; k < 8; k += 2) {
+            const uint64_t nx = two_of(minus_x[k], minus_x[k + 1]);
+            uint64_t q;
+            asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(q) : "l"(nx), "l"(minus_r));
+            q = fma_two(fma_two(q, s, nx), minus_r, q);
+            q = fma_two(fma_two(q, s, nx), minus_r, q);
+            asm("mov.b64 {%0, %1}, %2;" : "=f"(t[k]), "=f"(t[k + 1]) : "l"(q));
+        }
     } else {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) t[k] = __fdiv_rn(x[k], scale);
+        for (int k = 0; k < 8; ++k) t[k] = __fdiv_rn(-minus_x[k], scale);
     }
     return pack8(t);
 }

@@ -9,7 +9,7 @@
 // over sixteen values.  A CTA covers 8 * RPW rows of 512 columns: a warp starts the loads of its RPW rows before it reduces any
 // of them, and the scales of a column block, side by side in memory, leave as one contiguous store per CTA instead
 // of one 4-byte store per row.  The exact division is quantise8_corrected's.
-// Measured, 8192 x 12288: from bf16 56 us = 5.4 TB/s, from fp32 73 us = 6.8 TB/s, through SwiGLU from bf16 111 us = 4.5 TB/s: there
+// Measured, 8192 x 12288: from bf16 55 us = 5.5 TB/s, from fp32 73 us = 6.9 TB/s, through SwiGLU from bf16 107 us = 4.7 TB/s: there
 // the arithmetic (an exponential, a reciprocal and some twenty more instructions a value; 81 % of the issue slots) bounds.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
@@ -123,11 +123,17 @@ __global__ void __launch_bounds__(32 * kWarps, SWIGLU ? 4 : 3) rows_kernel(const
     for (int i = 0; i < RPW; ++i) {
         const uint32_t lr = warp * RPW + i;
         const uint64_t r = row0 + lr;
+        // v holds the negated values, as quantise8_corrected wants them: turned over two at a time where they come from bf16
         float v[16], m = 0.0f;
+        if (!F32) {
+#pragma unroll
+            for (int k = 0; k < kRaw; ++k) (SWIGLU ? up[i] : x[i])[k] ^= 0x80008000u;
+        }
 #pragma unroll
         for (int k = 0; k < 16; ++k) {
             v[k] = value<F32>(x[i], k);
             if (SWIGLU) v[k] = swiglu(v[k], value<F32>(up[i], k));
+            if (F32) v[k] = -v[k];
             m = fmaxf(m, fabsf(v[k]));  // fmaxf drops NaN operands
         }
 #pragma unroll
@@ -137,7 +143,7 @@ __global__ void __launch_bounds__(32 * kWarps, SWIGLU ? 4 : 3) rows_kernel(const
         if (r < a.rows && c < a.cols) {
             uint2 q[2];
 #pragma unroll
-            for (int h = 0; h < 2; ++h) q[h] = quantise8_corrected(v + 8 * h, scale, recip);
+            for (int h = 0; h < 2; ++h) q[h] = quantise8_corrected<!F32>(v + 8 * h, scale, recip);
             uint8_t* dst = a.codes + r * a.ld_codes + c;
             if (VEC == 2) {
                 *(uint4*)dst = make_uint4(q[0].x, q[0].y, q[1].x, q[1].y);
