@@ -1,26 +1,35 @@
 // Linear layers on the tensor cores: pairs of CTAs, 256 x 256 tiles, tcgen05 products fed by tensor-map copies.
 //
-// Every product is taken transposed: the weight's features (wgrad: the rows of dW) are the M side of the product, 128 to
-// each CTA of a pair, and the tokens its N side.  N is an operand of the instruction, so a ragged group costs 32-row
-// steps and not whole tiles: a group's rows are cut into equal tiles of at most 256.
+//   forward bf16  D[n, r] = sum_k W[n, k] x[r, k]      both operands contiguous along the contraction
+//   forward fp8   D[r, n], the same sum with the tokens on the M side
+//   dgrad         D[k, r] = sum_n W[n, k] dy[r, n]     W contiguous along its outputs (MN-major)
+//   wgrad         D[n, k] = sum_r dy[r, n] x[r, k]     both MN-major, the contraction runs over a group's rows
 //
-//   forward  D[n, r] = sum_k W[n, k] x[r, k]      both operands contiguous along the contraction
-//   dgrad    D[k, r] = sum_n W[n, k] dy[r, n]     W contiguous along its outputs (MN-major)
-//   wgrad    D[n, k] = sum_r dy[r, n] x[r, k]     both MN-major, the contraction runs over a group's rows
+// A pair computes 256 outputs of the M side (128 in each CTA's tensor memory) by up to 256 of the N side, of which each CTA holds
+// half in shared memory: 32 KB a stage and CTA for 512 cycles of products, which is what the L2 can deliver and the
+// shared memory can both take in and give out; a CTA on its own would need half as much again.  N is an operand of the
+// instruction, so with the tokens there (bf16) a ragged group costs 32-row steps and not whole tiles: a group's rows are cut into
+// equal tiles of at most 256.
 //
-// Roles of a CTA's 12 warps: 0 issues the copies of its half of the operands into a ring of six 32 KB stages; 1 (of the pair's
-// first CTA) issues the products of the pair; 2 copies the tokens' scales (fp8) or clears the rows of other groups from the last
-// stage (wgrad); 3 finds the tiles; 4-11 read the accumulators.  Accumulators take half of tensor memory each, two in turn, so that a tile is
-// written out while the next is computed.
+// Roles of a CTA's 12 warps: 0 issues the copies of its half of the operands into a ring of five or six stages; 1 (of the pair's
+// first CTA) issues the products of the pair; 2 clears the rows of other groups from the last stage (wgrad); 3 finds the tiles; 4-11
+// read the accumulators.  Accumulators take half of tensor memory each, two in turn, so that a tile is written out while
+// the next is computed.  Pairs walk the tiles in a fixed order (token tiles innermost, in bands of sixteen, so that a band's tokens
+// and a few weight tiles stay in L2) and every sum is taken in a fixed order.
 //
 // fp8: one product covers exactly one block of 128 of the contraction, after which its partial sums are scaled by
-// xs[b, r] * ws[n / 128, b] and added to fp32 sums in registers (128 a thread).  A CTA's 128 features are one scale block, so
-// ws is one number per block, and the tokens' scales come through shared memory.  The accumulators are
-// read in the fragment layout of 8 x 8 blocks (a thread holds two tokens of four features): a thread then needs the
-// scales of a quarter of the tokens only, which keeps the shared-memory port free for the tensor cores, and two multiply-adds
-// share an instruction.
+// xs[b, r] * ws[n / 128, b] and added to fp32 sums in registers (128 a thread).  A thread owns one token and 128 features of one scale
+// block, so that factor is one number a thread and two multiply-adds share an instruction.  What bounds it is the way of an
+// accumulator back to the products: each step ends in a barrier between the two, and two accumulators fit tensor memory.
+// (Features on the M side need one factor a column: 915 us where this takes 666.  Halves of 128 columns with four accumulators
+// in turn double the reads of the M operand: no gain.  Sixteen warps of 64 columns: slower, 862 against 836 then.)
 //
-// Outputs leave through a 640-byte transpose per warp: eight tokens of 32 features, 64 contiguous bytes a row.
+// Stores: bf16 outputs with features on the M side go through a 640-byte transpose per warp (eight tokens of 32 features, 64
+// contiguous bytes a row); fp8 outputs and dW leave as whole blocks through the copy unit, in the background.
+//
+// Measured, alone / back to back at the power limit: bf16 8192 x 24576 x 4096 1.01 / 1.17 ms (1.63 / 1.42 PFLOP/s; a library product
+// of 8192^3 reaches 1.67 / 1.39), fp8 the same 0.67 / 0.77 ms (2.48 / 2.15); 128 groups of 256 rows, 1536 x 2048: bf16 183 / 219 us,
+// fp8 128 / 142, dgrad 173 / 216, wgrad 386 / 361 (1.6 GB of dW).
 #include "linear.h"
 #include "tc_map.h"
 #include "tc_ptx.cuh"

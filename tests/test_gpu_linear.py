@@ -336,3 +336,39 @@ def test_refusals_with_a_device():
                 lambda: layer.forward(x.t(), None, off), lambda: layer.forward(x.cpu(), None, off)):
         with pytest.raises((ValueError, TypeError)):
             bad()
+
+
+@pytest.mark.parametrize("fp8", [True, False], ids=["fp8", "bf16"])
+def test_offsets_past_32_bits(fp8):
+    """Rows that lie more than 2^32 elements behind the first, in x, y and dx."""
+    rows, n, k, ld = 70001, 64, 128, 65536
+    g = gen(1)
+    wide = torch.empty(rows, ld, dtype=torch.uint8 if fp8 else BF16, device=DEV)
+    out = torch.empty(rows, ld, dtype=BF16, device=DEV)
+    x = torch.randn(rows, k, device=DEV, generator=g)
+    w = torch.randn(n, k, device=DEV, generator=g) * 0.05
+    if fp8:
+        xq, xs = dr.quant_rows(x, wide[:, :k])
+        wq, ws = quant_weight(w)
+        xd, wd = wide_rows(xq.contiguous().view(torch.float8_e4m3fn), xs), wide_weight(wq, ws)
+    else:
+        xq, xs, wq, ws = wide[:, :k], None, w.bfloat16(), None
+        xq.copy_(x)
+        xd, wd = xq.double(), wq.double()
+    layer = dr.Linear(wq, ws)
+    layer.forward(xq, xs, out=out[:, :n])
+    want, tol = product(xd, wd.t(), BF16)
+    check(out[:, :n], want, tol)
+    if not fp8:
+        layer.dgrad(out[:, :n], out=wide[:, 256:256 + k])
+        want, tol = product(out[:, :n].double(), wd, BF16)
+        check(wide[:, 256:256 + k], want, tol)
+        dw = layer.wgrad(xq, out[:, :n])
+        want, tol = product(out[:, :n].double().t(), xd, F32)
+        check(dw, want, tol)
+
+
+def test_zz_no_wait_ran_out():
+    """After everything above: no kernel gave up waiting for its copies or products."""
+    rc, failures = dr.dr_diag_linear_wait_failures()
+    assert rc == 0 and failures == 0
