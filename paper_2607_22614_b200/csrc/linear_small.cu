@@ -1,8 +1,9 @@
 // Forward products of few rows (decoding): the weights are read once at the memory's rate, everything else hides behind that.
 //
 // D[n, r] = sum_k W[n, k] x[r, k] with 128 features on the M side of a CTA's product and a group's rows, at most 64 at a time in
-// steps of 16, on its N side.  Bound: HBM, the weights' bytes; a stage is 16 KB of weights and 2 KB for each 16 rows, seven
-// stages keep 112 KB of weights in flight on every SM.  There is no time to lose in filling the machine either: with
+// steps of 16, on its N side.  Bound: HBM, the weights' bytes; a stage holds two steps of the contraction, 32 KB of weights and 4 KB for
+// each 16 rows, and three stages keep 96 KB of weights in flight on every SM.  What else costs time is the issuing of a step (waits,
+// products, commits), hence the two steps a stage.  There is no time to lose in filling the machine either: with
 // fewer feature blocks than SMs, a cluster of up to eight CTAs splits the contraction, and its CTAs add their fp32 sums through
 // distributed shared memory, always in the order of their ranks.
 //
@@ -21,9 +22,11 @@ using namespace tc;
 
 __device__ unsigned long long g_wait_failures;
 
-constexpr uint32_t kRowsTile = 64, kStages = 7, kWeightBytes = 16384, kStageBytes = kWeightBytes + kRowsTile * 128;
+constexpr uint32_t kTurn = 2;  // steps of the contraction that a stage holds and that are handed over at a time
+constexpr uint32_t kRowsTile = 64, kStages = 3, kWeightBytes = 16384, kRowBytes = kRowsTile * 128;
+constexpr uint32_t kStageBytes = kTurn * (kWeightBytes + kRowBytes);  // weights of each step, then rows of each step
 constexpr uint32_t kThreads = 256, kBuffers = 512 / kRowsTile;
-constexpr uint32_t kTurn = 2, kTurns = kBuffers / kTurn;  // blocks of the contraction handed over at a time (fp8)
+constexpr uint32_t kTurns = kBuffers / kTurn;
 constexpr uint32_t kScratchPitch = 80;
 constexpr uint32_t kTurnPitch = 36;  // floats
 
@@ -141,14 +144,16 @@ __device__ __forceinline__ void produce(const Args& a, Shared& s, const CUtensor
     Tile t;
     bool ok = true;
     while (ok && s.tiles.get(t, turn, &s.stop, &g_wait_failures)) {
-        for (uint32_t l = t.step0; l < t.step0 + t.steps; ++l) {
-            const uint32_t at = stages + ring.slot * kStageBytes, bar = full + 8 * ring.slot;
+        for (uint32_t l = 0; l < t.steps; l += kTurn) {
+            const uint32_t at = stages + ring.slot * kStageBytes, bar = full + 8 * ring.slot, steps = min(kTurn, t.steps - l);
             ok = warp_wait(empty + 8 * ring.slot, ring.round ^ 1, &s.stop, &g_wait_failures);
             if (!ok) break;
             if (elect()) {
-                bar_expect(bar, kWeightBytes + t.nt * 128);
-                load_2d<false>(at, map_w, bar, l * kStep, t.feature);
-                for (uint32_t r = 0; r < t.nt; r += 16) load_2d<false>(at + kWeightBytes + r * 128, map_x, bar, l * kStep, t.row0 + r);
+                bar_expect(bar, steps * (kWeightBytes + t.nt * 128));
+                for (uint32_t q = 0; q < steps; ++q) load_2d<false>(at + q * kWeightBytes, map_w, bar, (t.step0 + l + q) * kStep, t.feature);
+                for (uint32_t q = 0; q < steps; ++q)
+                    for (uint32_t r = 0; r < t.nt; r += 16)
+                        load_2d<false>(at + kTurn * kWeightBytes + q * kRowBytes + r * 128, map_x, bar, (t.step0 + l + q) * kStep, t.row0 + r);
             }
             ring.next();
             used = min(used + 1, kStages);
@@ -162,25 +167,30 @@ __device__ __forceinline__ void multiply(const Args& a, Shared& s)
 {
     const uint32_t full = smem_u32(s.full), empty = smem_u32(s.empty);
     const uint32_t acc_full = smem_u32(s.acc_full), acc_empty = smem_u32(s.acc_empty), tmem = s.tmem;
-    const uint64_t first_a = operand(smem_u32(s.stage), 0), first_b = operand(smem_u32(s.stage) + kWeightBytes, 0);
+    const uint64_t first_a = operand(smem_u32(s.stage), 0), first_b = operand(smem_u32(s.stage) + kTurn * kWeightBytes, 0);
     Turn<kStages> ring;
     Turn<kTurns> acc;
     Turn<kTilesAhead> turn;
     Tile t;
     while (s.tiles.get(t, turn, &s.stop, &g_wait_failures)) {
         const uint32_t shape = shape_of(FP8, false, false, 128, t.nt);
-        for (uint32_t l = 0; l < t.steps; ++l) {
-            const uint32_t in_turn = FP8 ? l % kTurn : 0;
-            if (FP8 ? in_turn == 0 : l == 0)
+        for (uint32_t l = 0; l < t.steps; l += kTurn) {
+            if (FP8 || l == 0)
                 if (!warp_wait(acc_empty + 8 * acc.slot, acc.round ^ 1, &s.stop, &g_wait_failures)) return;
             if (!warp_wait(full + 8 * ring.slot, ring.round, &s.stop, &g_wait_failures)) return;
             fence_after();
             const uint64_t da = first_a + ring.slot * (kStageBytes >> 4), db = first_b + ring.slot * (kStageBytes >> 4);
-            const uint32_t d = tmem + (acc.slot * kTurn + in_turn) * kRowsTile;
-            const bool last = l + 1 == t.steps || (FP8 && in_turn + 1 == kTurn);
+            const uint32_t d = tmem + acc.slot * kTurn * kRowsTile;
+            const bool last = FP8 || l + kTurn >= t.steps, both = l + 1 < t.steps;
             if (elect()) {
 #pragma unroll
                 for (uint32_t q = 0; q < 4; ++q) mma<1, FP8>(d, da + 2 * q, db + 2 * q, shape, FP8 ? q != 0 : (l | q) != 0);
+                if (both) {
+#pragma unroll
+                    for (uint32_t q = 0; q < 4; ++q)
+                        mma<1, FP8>(d + (FP8 ? kRowsTile : 0), da + (kWeightBytes >> 4) + 2 * q, db + (kRowBytes >> 4) + 2 * q, shape,
+                                    FP8 ? q != 0 : 1);
+                }
                 if (last) commit<1>(acc_full + 8 * acc.slot);
                 commit<1>(empty + 8 * ring.slot);
             }
