@@ -8,7 +8,7 @@
 // distributed shared memory, always in the order of their ranks.
 //
 // Roles: warp 0 copies the operands, 1 issues the products, 2 copies the scales (fp8), 3 finds the tiles,
-// 4-7 read the accumulators.  fp8 takes a new
+// 4-11 read the accumulators.  fp8 takes a new
 // accumulator (eight of 64 columns in turn) for every block of 128 of the contraction, scales it and adds it to fp32 sums in
 // registers, as the kernel for many rows does.
 #include "linear.h"
@@ -25,7 +25,7 @@ __device__ unsigned long long g_wait_failures;
 constexpr uint32_t kTurn = 2;  // steps of the contraction that a stage holds and that are handed over at a time
 constexpr uint32_t kRowsTile = 64, kStages = 3, kWeightBytes = 16384, kRowBytes = kRowsTile * 128;
 constexpr uint32_t kStageBytes = kTurn * (kWeightBytes + kRowBytes);  // weights of each step, then rows of each step
-constexpr uint32_t kThreads = 256, kBuffers = 512 / kRowsTile;
+constexpr uint32_t kReaders = 8, kThreads = 128 + 32 * kReaders, kBuffers = 512 / kRowsTile;
 constexpr uint32_t kTurns = kBuffers / kTurn;
 constexpr uint32_t kScratchPitch = 80;
 constexpr uint32_t kTurnPitch = 36;  // floats
@@ -37,9 +37,9 @@ struct Tile {
 
 struct Shared {
     alignas(1024) uint8_t stage[kStages][kStageBytes];
-    alignas(16) float turn[4][16][kTurnPitch];              // a warp's features of 16 rows, on their way to the cluster
+    alignas(16) float turn[kReaders][16][kTurnPitch];              // a warp's features of 16 rows, on their way to the cluster
     alignas(16) float sums[kRowsTile + kMaxSplit][128];     // [CTA][its rows that end here][features]
-    alignas(16) uint8_t scratch[4][8 * kScratchPitch];
+    alignas(16) uint8_t scratch[kReaders][8 * kScratchPitch];
     alignas(16) float scale[kBuffers][kRowsTile + 4];  // the rows' scales of a block, then the weight's
     uint64_t full[kStages], empty[kStages];
     uint64_t acc_full[kTurns], acc_empty[kTurns], scale_full[kTurns], scale_empty[kTurns];
@@ -235,7 +235,8 @@ __device__ __forceinline__ void write_out(const Args& a, Shared& s)
     const uint32_t lane = threadIdx.x & 31, warp = (threadIdx.x >> 5) - 4;
     const uint32_t acc_full = smem_u32(s.acc_full), acc_empty = smem_u32(s.acc_empty);
     const uint32_t scale_full = smem_u32(s.scale_full), scale_empty = smem_u32(s.scale_empty);
-    const uint32_t scratch = smem_u32(s.scratch[warp]), tmem = s.tmem + (warp * 32 << 16);
+    const uint32_t quarter = warp & 3, side = warp >> 2;  // 32 features, and 32 of the rows
+    const uint32_t scratch = smem_u32(s.scratch[warp]), tmem = s.tmem + (quarter * 32 << 16) + side * 32;
     Turn<kTurns> acc;
     uint32_t handed = 0;
     // r / split for the rows of a tile: exact for r < 64 and split <= 8
@@ -243,14 +244,13 @@ __device__ __forceinline__ void write_out(const Args& a, Shared& s)
     Turn<kTilesAhead> turn;
     Tile t;
     while (s.tiles.get(t, turn, &s.stop, &g_wait_failures)) {
-        float sum[2][2][16];
+        const bool idle = side * 32 >= t.nt;  // (such a warp only keeps the barriers going)
+        float sum[2][16];
         if (FP8) {
 #pragma unroll
-            for (int c = 0; c < 2; ++c)
+            for (int h = 0; h < 2; ++h)
 #pragma unroll
-                for (int h = 0; h < 2; ++h)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) sum[c][h][r] = 0.0f;
+                for (int r = 0; r < 16; ++r) sum[h][r] = 0.0f;
         }
         for (uint32_t l = 0; l < t.steps; l += FP8 ? kTurn : t.steps) {
             bool ok = !FP8 || bar_wait(scale_full + 8 * acc.slot, acc.round, &s.stop, &g_wait_failures);
@@ -258,33 +258,29 @@ __device__ __forceinline__ void write_out(const Args& a, Shared& s)
             if (!__all_sync(0xFFFFFFFFu, ok)) return;
             fence_after();
             const uint32_t from = tmem + acc.slot * kTurn * kRowsTile;
-            if (FP8) {
+            if (idle) {
+            } else if (FP8) {
 #pragma unroll
                 for (uint32_t q = 0; q < kTurn; ++q) {
                     if (l + q >= t.steps) break;
                     const float* sc = s.scale[acc.slot * kTurn + q];
                     const float w = sc[kRowsTile];
                     const uint64_t ww = pair_of(w, w);
-                    sc += 2 * (lane & 3);
+                    sc += side * 32 + 2 * (lane & 3);
+                    float p[2][16];
+                    tmem_load(from + q * kRowsTile, p[0], p[1]);
 #pragma unroll
-                    for (int c = 0; c < 2; ++c) {
-                        if (c * 32 >= t.nt) break;
-                        float p[2][16];
-                        tmem_load(from + q * kRowsTile + c * 32, p[0], p[1]);
+                    for (int j = 0; j < 4; ++j) {
+                        const uint64_t two = mul2(*(const uint64_t*)(sc + j * 8), ww);
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            const uint64_t two = mul2(*(const uint64_t*)(sc + c * 32 + j * 8), ww);
-#pragma unroll
-                            for (int h = 0; h < 2; ++h) {
-                                fma2(sum[c][h][4 * j], sum[c][h][4 * j + 1], p[h][4 * j], p[h][4 * j + 1], two);
-                                fma2(sum[c][h][4 * j + 2], sum[c][h][4 * j + 3], p[h][4 * j + 2], p[h][4 * j + 3], two);
-                            }
+                        for (int h = 0; h < 2; ++h) {
+                            fma2(sum[h][4 * j], sum[h][4 * j + 1], p[h][4 * j], p[h][4 * j + 1], two);
+                            fma2(sum[h][4 * j + 2], sum[h][4 * j + 3], p[h][4 * j + 2], p[h][4 * j + 3], two);
                         }
                     }
                 }
             } else {
-                tmem_load(from, sum[0][0], sum[0][1]);
-                if (t.nt > 32) tmem_load(from + 32, sum[1][0], sum[1][1]);
+                tmem_load(from, sum[0], sum[1]);
             }
             fence_before();
             __syncwarp();
@@ -294,17 +290,16 @@ __device__ __forceinline__ void write_out(const Args& a, Shared& s)
             }
             acc.next();
         }
-        const int f = (int)(t.feature + warp * 32 - t.e * a.n);  // in a row of c
+        const int f = (int)(t.feature + quarter * 32 - t.e * a.n);  // in a row of c
         if (a.split == 1) {
 #pragma unroll
-            for (int c = 0; c < 2; ++c)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    if (c * 32 + j * 8 >= t.nt) break;
-                    const float v[4][2] = {{sum[c][0][4 * j], sum[c][0][4 * j + 1]}, {sum[c][0][4 * j + 2], sum[c][0][4 * j + 3]},
-                                           {sum[c][1][4 * j], sum[c][1][4 * j + 1]}, {sum[c][1][4 * j + 2], sum[c][1][4 * j + 3]}};
-                    store_rows(a, scratch, t.row0 + c * 32 + j * 8, t.row_end, f, v);
-                }
+            for (int j = 0; j < 4; ++j) {
+                const uint32_t c = side * 32 + j * 8;
+                if (c >= t.nt) break;
+                const float v[4][2] = {{sum[0][4 * j], sum[0][4 * j + 1]}, {sum[0][4 * j + 2], sum[0][4 * j + 3]},
+                                       {sum[1][4 * j], sum[1][4 * j + 1]}, {sum[1][4 * j + 2], sum[1][4 * j + 3]}};
+                store_rows(a, scratch, t.row0 + c, t.row_end, f, v);
+            }
             continue;
         }
         // Every row of the tile ends in one CTA of the cluster (row r in CTA r mod split): the others send it their sums with
@@ -314,8 +309,8 @@ __device__ __forceinline__ void write_out(const Args& a, Shared& s)
         if (!__all_sync(0xFFFFFFFFu, bar_wait(smem_u32(&s.sums_empty), (handed & 1) ^ 1, &s.stop, &g_wait_failures))) return;
         if (warp == 0 && lane == 0) bar_expect(smem_u32(&s.sums_full), owned * a.split * 512);
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {  // sixteen rows at a time
-            if (c * 16 >= t.nt) break;
+        for (int c = 0; c < 2; ++c) {  // sixteen rows at a time
+            if (side * 32 + c * 16 >= t.nt) break;
             __syncwarp();
 #pragma unroll
             for (int j = 0; j < 2; ++j)
@@ -324,20 +319,20 @@ __device__ __forceinline__ void write_out(const Args& a, Shared& s)
 #pragma unroll
                     for (int q = 0; q < 2; ++q)
                         s.turn[warp][j * 8 + 2 * (lane & 3) + q][(lane >> 2) + 8 * g] =
-                            sum[c >> 1][g >> 1][4 * ((c & 1) * 2 + j) + 2 * (g & 1) + q];
+                            sum[g >> 1][4 * (c * 2 + j) + 2 * (g & 1) + q];
             __syncwarp();
 #pragma unroll
             for (uint32_t i = 0; i < 4; ++i) {
-                const uint32_t r = c * 16 + i * 4 + (lane >> 3);
+                const uint32_t r = side * 32 + c * 16 + i * 4 + (lane >> 3);
                 if (r >= rows) continue;
                 const float4 v = *(const float4*)&s.turn[warp][r & 15][(lane & 7) * 4];
                 const uint32_t nth = r * magic / 65536, to = r - nth * a.split;
-                store_counted(in_cta(smem_u32(&s.sums[rank * most + nth][warp * 32 + (lane & 7) * 4]), to), v,
+                store_counted(in_cta(smem_u32(&s.sums[rank * most + nth][quarter * 32 + (lane & 7) * 4]), to), v,
                               in_cta(smem_u32(&s.sums_full), to));
             }
         }
         if (!__all_sync(0xFFFFFFFFu, bar_wait(smem_u32(&s.sums_full), handed & 1, &s.stop, &g_wait_failures))) return;
-        for (uint32_t o = warp; o < owned; o += 4) {
+        for (uint32_t o = warp; o < owned; o += kReaders) {
             float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
             for (uint32_t q = 0; q < a.split; ++q) {
                 const float4 p = *(const float4*)&s.sums[q * most + o][lane * 4];
@@ -387,13 +382,13 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         for (uint32_t i = 0; i < kTurns; ++i) {
             bar_init(smem_u32(&s.acc_full[i]), 1);
-            bar_init(smem_u32(&s.acc_empty[i]), 4);
+            bar_init(smem_u32(&s.acc_empty[i]), kReaders);
             bar_init(smem_u32(&s.scale_full[i]), 32);
-            bar_init(smem_u32(&s.scale_empty[i]), 4);
+            bar_init(smem_u32(&s.scale_empty[i]), kReaders);
         }
         bar_init(smem_u32(&s.sums_full), 1);
-        bar_init(smem_u32(&s.sums_empty), 4 * a.split);
-        s.tiles.init(2 + FP8 + 4);  // readers: the copies, the products, the scales, the accumulators
+        bar_init(smem_u32(&s.sums_empty), kReaders * a.split);
+        s.tiles.init(2 + FP8 + kReaders);  // readers: the copies, the products, the scales, the accumulators
         s.stop = 0;
         bar_init_fence();
     }
