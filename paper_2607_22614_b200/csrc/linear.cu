@@ -93,8 +93,8 @@ int check_gradient(const dr_linear* lin)
 }
 
 // Up to this many rows a group (on average) the kernel that reads weights 128 features at a time wins over pairs of CTAs: in us,
-// fp8 1 x 6144 x 4096 10.0 / 17.0, 80 x 4096 x 4096 13.5 / 18.2, 128 x 24576 x 4096 41.5 / 35.4; 128 groups of 1536 x 2048, 32 rows each
-// 71.6 / 100, 64 rows each 110 / 113; bf16 64 x 6144 x 4096 15.0 / 16.9, 128 groups of 48 rows 133 / 134.
+// pairs second, fp8 1 x 6144 x 4096 8.1 / 17.0, 64 x 6144 x 4096 10.1 / 17.5; 128 groups of 1536 x 2048, 32 rows each 71 / 100, bf16 48 rows
+// each 133 / 134.  Beyond 64 rows it reads the weights more than once: 128 x 24576 x 4096 fp8 41 / 35.
 constexpr uint64_t kSmallRows = 64;
 
 int launch(const LinearCall& c)

@@ -294,7 +294,7 @@ __device__ __forceinline__ void commit(uint32_t bar)
     else
         asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
-// 32 lanes x 32 or 64 columns of the warp's quarter of tensor memory, complete on return (the wait is part of the statement, so
+// 32 lanes x 32 columns of the warp's quarter of tensor memory, complete on return (the wait is part of the statement, so
 // that no use of the registers can move above it).  With t the lane of the warp: a[4 j + 0, 1] = columns 8 j + 2 (t % 4) + {0, 1}
 // of lane t / 4, a[4 j + 2, 3] the same of lane t / 4 + 8; b: of lanes t / 4 + 16 and t / 4 + 24.
 __device__ __forceinline__ void tmem_load(uint32_t addr, float (&a)[16], float (&b)[16])
@@ -307,17 +307,6 @@ __device__ __forceinline__ void tmem_load(uint32_t addr, float (&a)[16], float (
                  : "r"(addr), "r"(addr + (16u << 16))
                  : "memory");
 }
-__device__ __forceinline__ void tmem_load(uint32_t addr, float (&a)[32], float (&b)[32])
-{
-    asm volatile("tcgen05.ld.sync.aligned.16x256b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%64];\n"
-                 "tcgen05.ld.sync.aligned.16x256b.x8.b32 {%32,%33,%34,%35,%36,%37,%38,%39,%40,%41,%42,%43,%44,%45,%46,%47,%48,%49,%50,%51,%52,%53,%54,%55,%56,%57,%58,%59,%60,%61,%62,%63}, [%65];\n"
-                 "tcgen05.wait::ld.sync.aligned;"
-                 : "=f"(a[0]), "=f"(a[1]), "=f"(a[2]), "=f"(a[3]), "=f"(a[4]), "=f"(a[5]), "=f"(a[6]), "=f"(a[7]), "=f"(a[8]), "=f"(a[9]), "=f"(a[10]), "=f"(a[11]), "=f"(a[12]), "=f"(a[13]), "=f"(a[14]), "=f"(a[15]), "=f"(a[16]), "=f"(a[17]), "=f"(a[18]), "=f"(a[19]), "=f"(a[20]), "=f"(a[21]), "=f"(a[22]), "=f"(a[23]), "=f"(a[24]), "=f"(a[25]), "=f"(a[26]), "=f"(a[27]), "=f"(a[28]), "=f"(a[29]), "=f"(a[30]), "=f"(a[31]),
-                   "=f"(b[0]), "=f"(b[1]), "=f"(b[2]), "=f"(b[3]), "=f"(b[4]), "=f"(b[5]), "=f"(b[6]), "=f"(b[7]), "=f"(b[8]), "=f"(b[9]), "=f"(b[10]), "=f"(b[11]), "=f"(b[12]), "=f"(b[13]), "=f"(b[14]), "=f"(b[15]), "=f"(b[16]), "=f"(b[17]), "=f"(b[18]), "=f"(b[19]), "=f"(b[20]), "=f"(b[21]), "=f"(b[22]), "=f"(b[23]), "=f"(b[24]), "=f"(b[25]), "=f"(b[26]), "=f"(b[27]), "=f"(b[28]), "=f"(b[29]), "=f"(b[30]), "=f"(b[31])
-                 : "r"(addr), "r"(addr + (16u << 16))
-                 : "memory");
-}
-
 // 32 columns of the thread's own lane.  The load is only started: tmem_arrived(v) makes the registers usable.
 __device__ __forceinline__ void tmem_start(uint32_t addr, float (&v)[32])
 {
