@@ -4,24 +4,6 @@
 
 namespace dr {
 
-__device__ __forceinline__ void ld256f(const void* p, float (&v)[8])
-{
-    asm volatile("ld.global.nc.L1::no_allocate.v8.f32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
-                 : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7])
-                 : "l"(p));
-}
-__device__ __forceinline__ void ld128f(const void* p, float* v)
-{
-    asm volatile("ld.global.nc.L1::no_allocate.v4.f32 {%0,%1,%2,%3}, [%4];"
-                 : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3])
-                 : "l"(p));
-}
-__device__ __forceinline__ float ld32f(const void* p)
-{
-    float v;
-    asm volatile("ld.global.nc.L1::no_allocate.f32 %0, [%1];" : "=f"(v) : "l"(p));
-    return v;
-}
 // two fp32 -> two e4m3 bytes: round to nearest even, saturate to +-448; a NaN of either sign comes out
 // as 0x7F (checked against the oracle on sources made of every bit pattern)
 __device__ __forceinline__ uint32_t cvt_e4m3x2(float lo, float hi)

@@ -35,6 +35,25 @@ constexpr int kRowsPerPass = kQThreads / 16;   // 16 threads cover one 128-colum
 constexpr int kPasses = 128 / kRowsPerPass;    // block rows per thread
 static_assert(kQThreads >= 128 && 128 % kRowsPerPass == 0, "thread count must tile the block");
 
+__device__ __forceinline__ void ld256f(const void* p, float (&v)[8])
+{
+    asm volatile("ld.global.nc.L1::no_allocate.v8.f32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                 : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7])
+                 : "l"(p));
+}
+__device__ __forceinline__ void ld128f(const void* p, float* v)
+{
+    asm volatile("ld.global.nc.L1::no_allocate.v4.f32 {%0,%1,%2,%3}, [%4];"
+                 : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3])
+                 : "l"(p));
+}
+__device__ __forceinline__ float ld32f(const void* p)
+{
+    float v;
+    asm volatile("ld.global.nc.L1::no_allocate.f32 %0, [%1];" : "=f"(v) : "l"(p));
+    return v;
+}
+
 // One 128 x 128 block.  FAST: the block is whole (128 rows, 128 columns inside the tensor), its rows allow
 // 256-bit loads and the buffers' bases are 32-byte aligned, so no access needs a predicate.
 template <bool FAST>

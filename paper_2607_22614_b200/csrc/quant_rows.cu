@@ -53,6 +53,8 @@ __device__ __forceinline__ float scale_of_row(float m)
 }
 
 // Sixteen raw values of a row from column c on (zeros past `cols`): 8 registers of bf16 pairs or 16 of fp32.
+// Coherent loads that stay behind after_previous(): the kernel is already running while the previous one writes its x, so x
+// is not read-only for the kernel's lifetime, as non-coherent loads (.nc, __ldg) would need.
 // VEC 2: 32-byte aligned and whole groups of sixteen columns; 1: 16-byte aligned and whole groups of eight; 0: any.
 template <bool F32, int VEC>
 __device__ __forceinline__ void load16(const void* row, uint32_t c, uint32_t cols, uint32_t (&w)[F32 ? 16 : 8])
@@ -64,19 +66,20 @@ __device__ __forceinline__ void load16(const void* row, uint32_t c, uint32_t col
         if (c >= cols) return;
 #pragma unroll
         for (int k = 0; k < n; k += 8)
-            asm volatile("ld.global.nc.L1::no_allocate.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+            asm volatile("ld.global.L1::no_allocate.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
                          : "=r"(w[k]), "=r"(w[k + 1]), "=r"(w[k + 2]), "=r"(w[k + 3]), "=r"(w[k + 4]), "=r"(w[k + 5]),
                            "=r"(w[k + 6]), "=r"(w[k + 7])
-                         : "l"((const char*)row + (uint64_t)c * (F32 ? 4 : 2) + 4 * k));
+                         : "l"((const char*)row + (uint64_t)c * (F32 ? 4 : 2) + 4 * k)
+                         : "memory");
     } else if (VEC == 1) {
 #pragma unroll
         for (int k = 0; k < n; k += 4) {
-            uint4 q = make_uint4(0, 0, 0, 0);
-            if (c + k * (F32 ? 1 : 2) < cols) q = __ldg((const uint4*)((const char*)row + (uint64_t)c * (F32 ? 4 : 2) + 4 * k));
-            w[k] = q.x;
-            w[k + 1] = q.y;
-            w[k + 2] = q.z;
-            w[k + 3] = q.w;
+            w[k] = w[k + 1] = w[k + 2] = w[k + 3] = 0;
+            if (c + k * (F32 ? 1 : 2) < cols)
+                asm volatile("ld.global.L1::no_allocate.v4.b32 {%0,%1,%2,%3}, [%4];"
+                             : "=r"(w[k]), "=r"(w[k + 1]), "=r"(w[k + 2]), "=r"(w[k + 3])
+                             : "l"((const char*)row + (uint64_t)c * (F32 ? 4 : 2) + 4 * k)
+                             : "memory");
         }
     } else {
 #pragma unroll
@@ -109,11 +112,15 @@ __global__ void __launch_bounds__(32 * kWarps, SWIGLU ? 4 : 3) rows_kernel(const
     const uint32_t c = part * 512 + lane * 16;
     uint32_t x[RPW][kRaw], up[SWIGLU ? RPW : 1][kRaw];
     after_previous();
+    int64_t from[RPW];  // all indices first: the rows' loads keep their order, and each would wait for its own index
 #pragma unroll
     for (int i = 0; i < RPW; ++i) {
         const uint64_t r = row0 + warp * RPW + i;
-        int64_t src = -1;
-        if (r < a.rows) src = a.index ? a.index[r] : (int64_t)r;
+        from[i] = r < a.rows ? a.index ? a.index[r] : (int64_t)r : -1;
+    }
+#pragma unroll
+    for (int i = 0; i < RPW; ++i) {
+        const int64_t src = from[i];
         const bool ok = src >= 0 && (uint64_t)src < a.src_rows;
         const char* row = (const char*)a.x + (ok ? (uint64_t)src : 0) * a.ldx * (F32 ? 4 : 2);
         load16<F32, VEC>(row, c, ok ? a.cols : 0, x[i]);
