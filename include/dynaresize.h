@@ -543,7 +543,8 @@ int dr_shard_range(uint64_t flat_elems, uint32_t world, uint32_t rank, uint64_t*
  *   scales_dev: fp32, scale of row r and column block b at scales[b * ld_scales + r] (ld_scales >= rows:
  *               the scales of one column block lie side by side, as dr_linear_forward reads them)
  * Asynchronous on cuda_stream, allocates nothing, may be captured.  rows = 0 does nothing.
- * Errors (before launch): DR_ERR_INVALID, DR_ERR_UNSUPPORTED (x_dtype, form, dimension above 2^31 - 1),
+ * Errors (before launch): DR_ERR_INVALID (NULL, no columns, a leading dimension below its row, above 2^40 or
+ * beyond 2^60 elements over all rows, too few source rows), DR_ERR_UNSUPPORTED (x_dtype, form, dimension above 2^31 - 1),
  * DR_ERR_ALIGN (a pointer off its element size), DR_ERR_CUDA.  16-byte aligned bases and rows take the vector path,
  * others an element-wise one, same result.
  */
@@ -571,9 +572,10 @@ typedef struct dr_linear_desc {
 } dr_linear_desc;
 typedef struct dr_linear dr_linear;
 
-/* Checks the descriptor and records it for the current device.  Errors: DR_ERR_INVALID, DR_ERR_UNSUPPORTED
- * (dtype; a dimension above 2^31 - 1), DR_ERR_SIZE (weight_bytes / scale_bytes too small), DR_ERR_ALIGN (a pointer off its
- * element size), DR_ERR_NOMEM, DR_ERR_CUDA. */
+/* Checks the descriptor and records it for the current device.  Errors: DR_ERR_INVALID (a leading
+ * dimension below its row, above 2^40 or beyond 2^60 elements over all rows among them), DR_ERR_UNSUPPORTED
+ * (dtype; a dimension above 2^31 - 1), DR_ERR_SIZE (weight_bytes / scale_bytes too small), DR_ERR_ALIGN (a
+ * pointer off its element size), DR_ERR_NOMEM, DR_ERR_CUDA. */
 int dr_linear_create(const dr_linear_desc* desc, dr_linear** out);
 int dr_linear_destroy(dr_linear* lin); /* NULL is accepted; launches already enqueued may still run */
 
@@ -599,7 +601,7 @@ int dr_linear_destroy(dr_linear* lin); /* NULL is accepted; launches already enq
  * device value on the host, and leave the handle unmodified: concurrent calls on different streams are allowed, and
  * (after one ordinary call has loaded the module) they may be captured into a CUDA graph.  rows = 0 does
  * nothing (dr_linear_wgrad without accumulate: writes zeros).
- * Errors (before launch): DR_ERR_INVALID (NULL, a leading dimension below the row's length, missing offsets or
+ * Errors (before launch): DR_ERR_INVALID (NULL, a leading dimension out of the range that dr_linear_create takes, missing offsets or
  * scales, scales for a bf16 layer), DR_ERR_UNSUPPORTED (dtype, fp8 gradients, dimensions above 2^31 - 1), DR_ERR_ALIGN (a
  * pointer off its element size), DR_ERR_STATE (another current device), DR_ERR_CUDA.
  */

@@ -173,4 +173,17 @@ std::vector<HostSeg> window_segments(const std::vector<HostSeg>& segs, uint64_t 
 int launch_forward_tables(uint32_t elem_size, const DevSeg* d_segs, uint32_t n_segs, const uint32_t* d_hints,
                           uint32_t hint_shift, uint64_t n_tiles, const void* flat, void* arena, void* stream, bool bulk);
 
+// Whether `rows` rows of `cols` elements, `ld` apart, are something that 64-bit offsets (in bytes, and in the kernels' and tensor
+// maps' products of a row count and a pitch) describe without wrapping around.
+inline bool pitch_ok(uint64_t rows, uint64_t cols, uint64_t ld)
+{
+    return ld >= cols && ld <= 1ull << 40 && (rows < 2 || ld <= (1ull << 60) / (rows - 1));
+}
+// Whether they fit `bytes` bytes.
+inline bool rows_fit(uint64_t rows, uint64_t cols, uint64_t ld, uint32_t es, uint64_t bytes)
+{
+    const uint64_t have = bytes / es;
+    return have >= cols && (rows < 2 || (have - cols) / (rows - 1) >= ld);
+}
+
 }  // namespace dr

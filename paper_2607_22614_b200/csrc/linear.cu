@@ -41,8 +41,8 @@ int check_rows(const dr_linear* lin, uint64_t rows, const int32_t* offsets, cons
         set_error("NULL buffer");
         return DR_ERR_INVALID;
     }
-    if (ldp < p_cols || ldq < q_cols) {
-        set_error("leading dimension below the row's length");
+    if (!pitch_ok(rows, p_cols, ldp) || !pitch_ok(rows, q_cols, ldq)) {
+        set_error("leading dimension below the row's length or out of range");
         return DR_ERR_INVALID;
     }
     if ((uintptr_t)p % p_es || (uintptr_t)q % q_es || (uintptr_t)offsets % 4) {
@@ -143,7 +143,7 @@ int dr_linear_create(const dr_linear_desc* desc, dr_linear** out)
         set_error("NULL weight, fp8 without scales or bf16 with them");
         return DR_ERR_INVALID;
     }
-    if (d.weight_ld < d.in_features || (fp8 && d.scale_ld < sc) || d.weight_ld > (1ull << 40) || d.scale_ld > (1ull << 40)) {
+    if (!pitch_ok(rows, d.in_features, d.weight_ld) || (fp8 && !pitch_ok(sr, sc, d.scale_ld))) {
         set_error("leading dimension out of range");
         return DR_ERR_INVALID;
     }
@@ -152,8 +152,7 @@ int dr_linear_create(const dr_linear_desc* desc, dr_linear** out)
         set_error("a pointer is not aligned to its element size");
         return DR_ERR_ALIGN;
     }
-    if (d.weight_bytes < ((rows - 1) * d.weight_ld + d.in_features) * es ||
-        (fp8 && d.scale_bytes < ((sr - 1) * d.scale_ld + sc) * 4)) {
+    if (!rows_fit(rows, d.in_features, d.weight_ld, es, d.weight_bytes) || (fp8 && !rows_fit(sr, sc, d.scale_ld, 4, d.scale_bytes))) {
         set_error("weight or scales smaller than the layer");
         return DR_ERR_SIZE;
     }
@@ -206,7 +205,7 @@ int dr_linear_forward(const dr_linear* lin, const void* x_dev, uint64_t ldx, con
     rc = check_rows(lin, rows, offsets_dev, x_dev, ldx, d.in_features, lin->fp8 ? 1 : 2, y_dev, ldy, d.out_features,
                     y_dtype == DR_F32 ? 4 : 2);
     if (rc) return rc;
-    if (lin->fp8 ? rows && (!x_scale_dev || ld_scale < rows) : x_scale_dev != nullptr) {
+    if (lin->fp8 ? rows && (!x_scale_dev || !pitch_ok((d.in_features + 127) / 128, rows, ld_scale)) : x_scale_dev != nullptr) {
         set_error("an fp8 layer needs x's scales (ld_scale >= rows), a bf16 layer takes none");
         return DR_ERR_INVALID;
     }
@@ -245,8 +244,8 @@ int dr_linear_wgrad(const dr_linear* lin, const void* x_dev, uint64_t ldx, const
     const dr_linear_desc& d = lin->d;
     rc = check_rows(lin, rows, offsets_dev, x_dev, ldx, d.in_features, 2, dy_dev, lddy, d.out_features, 2);
     if (rc) return rc;
-    if (!dw_dev || lddw < d.in_features || accumulate > 1) {
-        set_error("NULL dw, leading dimension below the row's length, or accumulate not 0 / 1");
+    if (!dw_dev || !pitch_ok(d.out_features * d.n_groups, d.in_features, lddw) || accumulate > 1) {
+        set_error("NULL dw, leading dimension below the row's length or out of range, or accumulate not 0 / 1");
         return DR_ERR_INVALID;
     }
     if ((uintptr_t)dw_dev % 4) {

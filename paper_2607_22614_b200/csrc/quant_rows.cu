@@ -228,8 +228,9 @@ extern "C" int dr_quant_rows(const void* x_dev, uint32_t x_dtype, uint64_t ldx, 
         return DR_ERR_UNSUPPORTED;
     }
     const uint64_t width = form == DR_ROWS_SWIGLU ? 2 * cols : cols;
-    if (cols == 0 || ldx < width || ld_codes < cols || ld_scales < rows || (!row_index_dev && src_rows < rows)) {
-        set_error("no columns, a leading dimension below its row, or fewer source rows than rows");
+    if (cols == 0 || !pitch_ok(src_rows, width, ldx) || !pitch_ok(rows, cols, ld_codes) || !pitch_ok((cols + 127) / 128, rows, ld_scales) ||
+        (!row_index_dev && src_rows < rows)) {
+        set_error("no columns, a leading dimension below its row or out of range, or fewer source rows than rows");
         return DR_ERR_INVALID;
     }
     if (rows == 0) return DR_OK;
