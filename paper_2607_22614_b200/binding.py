@@ -667,6 +667,25 @@ def _fn(name):
     return f
 
 
+_current_device = None
+
+
+def _same_device(device, *operands):
+    """Raises unless every operand that is given lives on GPU `device`: a kernel of one GPU must not get another's addresses."""
+    for t in operands:
+        if t is not None and t.get_device() != device:
+            raise ValueError(f"an operand is on GPU {t.get_device()}, the others are on GPU {device}")
+
+
+def _on_current_device(device, what):
+    global _current_device
+    if _current_device is None:
+        import torch
+        _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+    if device != _current_device():
+        raise ValueError(f"{what} is on GPU {device}, which is not the current one: call under torch.cuda.device({device})")
+
+
 _raw_stream = None
 
 
@@ -685,8 +704,12 @@ def _stream_of(t, stream):
 
 def quant_rows(x, codes=None, scales=None, *, row_index=None, swiglu=False, stream=None):
     """dr_quant_rows: x [source rows, cols] (2 * cols with swiglu: gate, then up; bf16 or fp32) -> (codes [rows, cols],
-    scales [ceil(cols / 128), rows]).  row_index (int64) gathers rows.  Outputs that are not given are allocated."""
+    scales [ceil(cols / 128), rows]).  row_index (int64) gathers rows.  Outputs that are not given are allocated.  All
+    operands live on the current GPU."""
     src_rows, width, ldx = _matrix(x, "x")
+    device = x.get_device()
+    _on_current_device(device, "x")
+    _same_device(device, row_index, codes, scales)
     cols = width // 2 if swiglu else width
     if swiglu and width % 2:
         raise ValueError("x holds gate and up side by side: its column count must be even")
@@ -718,7 +741,8 @@ def quant_rows(x, codes=None, scales=None, *, row_index=None, swiglu=False, stre
 
 class Linear:
     """Owns one ``dr_linear``: a weight [n_groups * out, in] (bf16, or e4m3 codes with `scale`, one fp32 per 128 x 128
-    block of the stacked matrix), its products and, for bf16, its gradients.  Keeps references to both tensors."""
+    block of the stacked matrix), its products and, for bf16, its gradients.  Keeps references to both tensors.  The weight
+    and every operand of a product live on one GPU, which is the current one."""
 
     def __init__(self, weight, scale=None, n_groups=1):
         import torch
@@ -733,6 +757,9 @@ class Linear:
             scale_rows, scale_cols, scale_ld = _matrix(scale, "scale")
             if scale.dtype != torch.float32 or scale_rows != -(-rows // 128) or scale_cols != -(-cols // 128):
                 raise ValueError("scale must be fp32 with one value for each 128 x 128 block of the weight")
+        self.device = weight.get_device()
+        _on_current_device(self.device, "weight")
+        _same_device(self.device, scale)
         self.weight, self.scale, self.n_groups, self.fp8 = weight, scale, n_groups, fp8
         self.out_features, self.in_features = rows // n_groups, cols
         desc = dr_linear_desc(struct_size=C.sizeof(dr_linear_desc), dtype=DR_FP8_E4M3_B128 if fp8 else DR_BF16,
@@ -785,6 +812,7 @@ class Linear:
         """dr_linear_forward: y = x W^T, for rows sorted by group where `offsets` (n_groups + 1, int32) is given.  An fp8
         layer takes quant_rows' codes and scales.  Rows of an allocated output that no group owns are not initialised."""
         rows, ldx = self._operand(x, self.in_features, "x", self.fp8)
+        _same_device(self.device, x, x_scale, offsets, out)
         y, ldy = self._out(out, rows, self.out_features, out_dtype, x, "out")
         ps, lds = None, 0
         if x_scale is not None:
@@ -803,6 +831,7 @@ class Linear:
     def dgrad(self, dy, offsets=None, out=None, out_dtype=None, stream=None):
         """dr_linear_dgrad: the gradient of x, dy W."""
         rows, lddy = self._operand(dy, self.out_features, "dy")
+        _same_device(self.device, dy, offsets, out)
         dx, lddx = self._out(out, rows, self.in_features, out_dtype, dy, "out")
         rc = _fn("dr_linear_dgrad")(self.handle, dy.data_ptr(), lddy, rows, self._offsets(offsets), dx.data_ptr(), lddx,
                                     _code_of(dx, "out"), _stream_of(dy, stream))
@@ -816,6 +845,7 @@ class Linear:
         dy_rows, lddy = self._operand(dy, self.out_features, "dy")
         if rows != dy_rows:
             raise ValueError("x and dy must have the same rows")
+        _same_device(self.device, x, dy, offsets, out)
         if accumulate and out is None:
             raise ValueError("accumulate adds to `out`: give one")
         if out is None:
