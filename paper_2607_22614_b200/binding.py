@@ -702,10 +702,23 @@ def _stream_of(t, stream):
     return _raw_stream(t.get_device())
 
 
+def _empty(rows, cols, dtype, device, stream):
+    """An output of the call, from the memory of the stream that the call runs on: a block of the current stream's memory may
+    still be used by work queued there, which `stream` does not wait for."""
+    import torch
+    if stream is None:
+        return torch.empty(rows, cols, dtype=dtype, device=device)
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(getattr(stream, "cuda_stream", stream), device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(rows, cols, dtype=dtype, device=device)
+
+
 def quant_rows(x, codes=None, scales=None, *, row_index=None, swiglu=False, stream=None):
     """dr_quant_rows: x [source rows, cols] (2 * cols with swiglu: gate, then up; bf16 or fp32) -> (codes [rows, cols],
     scales [ceil(cols / 128), rows]).  row_index (int64) gathers rows.  Outputs that are not given are allocated.  All
-    operands live on the current GPU."""
+    operands live on the current GPU.  `stream` (default: the current one) is where the call runs and where its allocated
+    outputs belong; the caller orders the operands that other streams write, as with any torch call under that stream."""
     src_rows, width, ldx = _matrix(x, "x")
     device = x.get_device()
     _on_current_device(device, "x")
@@ -723,9 +736,9 @@ def quant_rows(x, codes=None, scales=None, *, row_index=None, swiglu=False, stre
     if codes is None or scales is None:
         import torch
         if codes is None:
-            codes = torch.empty(rows, cols, dtype=torch.float8_e4m3fn, device=x.device)
+            codes = _empty(rows, cols, torch.float8_e4m3fn, x.device, stream)
         if scales is None:
-            scales = torch.empty(blocks, rows, dtype=torch.float32, device=x.device)
+            scales = _empty(blocks, rows, torch.float32, x.device, stream)
     got_rows, got_cols, ld_codes = _matrix(codes, "codes")
     if got_rows != rows or got_cols != cols or codes.element_size() != 1:
         raise ValueError(f"codes must be {rows} x {cols} bytes")
@@ -742,7 +755,7 @@ def quant_rows(x, codes=None, scales=None, *, row_index=None, swiglu=False, stre
 class Linear:
     """Owns one ``dr_linear``: a weight [n_groups * out, in] (bf16, or e4m3 codes with `scale`, one fp32 per 128 x 128
     block of the stacked matrix), its products and, for bf16, its gradients.  Keeps references to both tensors.  The weight
-    and every operand of a product live on one GPU, which is the current one."""
+    and every operand of a product live on one GPU, which is the current one.  `stream` is as in quant_rows."""
 
     def __init__(self, weight, scale=None, n_groups=1):
         import torch
@@ -798,14 +811,13 @@ class Linear:
             raise ValueError(f"offsets must be {self.n_groups + 1} int32 on the GPU")
         return offsets.data_ptr()
 
-    def _out(self, out, rows, cols, dtype, like, what):
+    def _out(self, out, rows, cols, dtype, like, stream):
         if out is None:
             import torch
-            out = torch.empty(rows, cols, dtype=dtype or torch.bfloat16, device=like.device)
-            return out, cols
-        got_rows, got_cols, ld = _matrix(out, what)
+            return _empty(rows, cols, dtype or torch.bfloat16, like.device, stream), cols
+        got_rows, got_cols, ld = _matrix(out, "out")
         if got_rows != rows or got_cols != cols:
-            raise ValueError(f"{what} must be {rows} x {cols}")
+            raise ValueError(f"out must be {rows} x {cols}")
         return out, ld
 
     def forward(self, x, x_scale=None, offsets=None, out=None, out_dtype=None, stream=None):
@@ -813,7 +825,7 @@ class Linear:
         layer takes quant_rows' codes and scales.  Rows of an allocated output that no group owns are not initialised."""
         rows, ldx = self._operand(x, self.in_features, "x", self.fp8)
         _same_device(self.device, x, x_scale, offsets, out)
-        y, ldy = self._out(out, rows, self.out_features, out_dtype, x, "out")
+        y, ldy = self._out(out, rows, self.out_features, out_dtype, x, stream)
         ps, lds = None, 0
         if x_scale is not None:
             blocks, cols, lds = _matrix(x_scale, "x_scale")
@@ -832,7 +844,7 @@ class Linear:
         """dr_linear_dgrad: the gradient of x, dy W."""
         rows, lddy = self._operand(dy, self.out_features, "dy")
         _same_device(self.device, dy, offsets, out)
-        dx, lddx = self._out(out, rows, self.in_features, out_dtype, dy, "out")
+        dx, lddx = self._out(out, rows, self.in_features, out_dtype, dy, stream)
         rc = _fn("dr_linear_dgrad")(self.handle, dy.data_ptr(), lddy, rows, self._offsets(offsets), dx.data_ptr(), lddx,
                                     _code_of(dx, "out"), _stream_of(dy, stream))
         if rc:
@@ -848,10 +860,8 @@ class Linear:
         _same_device(self.device, x, dy, offsets, out)
         if accumulate and out is None:
             raise ValueError("accumulate adds to `out`: give one")
-        if out is None:
-            import torch
-            out = torch.empty(self.n_groups * self.out_features, self.in_features, dtype=torch.float32, device=x.device)
-        dw, lddw = self._out(out, self.n_groups * self.out_features, self.in_features, None, x, "out")
+        import torch
+        dw, lddw = self._out(out, self.n_groups * self.out_features, self.in_features, torch.float32, x, stream)
         if _code_of(dw, "out") != DR_F32:
             raise TypeError("the gradient of the weight is fp32")
         rc = _fn("dr_linear_wgrad")(self.handle, x.data_ptr(), ldx, dy.data_ptr(), lddy, rows, self._offsets(offsets),

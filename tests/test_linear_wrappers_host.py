@@ -117,3 +117,48 @@ def test_a_layer_of_another_gpu_is_refused(calls):
         with pytest.raises(ValueError, match="GPU 1"):
             dr.Linear(**kw)
     assert not calls
+
+
+@pytest.mark.parametrize("given", [False, True], ids=["allocated", "given"])
+@pytest.mark.parametrize("raw", [False, True], ids=["stream", "handle"])
+def test_allocated_outputs_belong_to_the_stream_of_the_call(calls, monkeypatch, raw, given):
+    """Memory that the current stream has freed may still be in use there: another stream must not be handed it."""
+    entered, made_in = [], []
+
+    class Stream:
+        def __init__(self, handle, device=None):
+            self.cuda_stream = handle
+
+    class Under:
+        def __init__(self, stream):
+            self.stream = stream
+
+        def __enter__(self):
+            entered.append(self.stream.cuda_stream)
+
+        def __exit__(self, *_):
+            entered.pop()
+
+    def empty(*shape, dtype, device):
+        made_in.append(entered[-1] if entered else "current")
+        return Stand(*shape, dtype=dtype)
+
+    monkeypatch.setattr(torch, "empty", empty)
+    monkeypatch.setattr(torch.cuda, "Stream", Stream)
+    monkeypatch.setattr(torch.cuda, "ExternalStream", Stream)
+    monkeypatch.setattr(torch.cuda, "stream", Under)
+    layer, off = _layer(), Stand(3, dtype=I32)
+    del calls[:]
+    for at in (None, 77 if raw else Stream(77)):
+        kw = [dict(stream=at) for _ in range(4)]
+        if given:
+            kw[0].update(codes=Stand(5, 256, dtype=E4M3), scales=Stand(2, 5, dtype=F32))
+            kw[1].update(out=Stand(5, 128))
+            kw[2].update(out=Stand(5, 256))
+            kw[3].update(out=Stand(256, 256, dtype=F32))
+        dr.quant_rows(Stand(5, 256), **kw[0])
+        layer.forward(Stand(5, 256), None, off, **kw[1])
+        layer.dgrad(Stand(5, 128), off, **kw[2])
+        layer.wgrad(Stand(5, 256), Stand(5, 128), off, **kw[3])
+    assert made_in == ([] if given else ["current"] * 5 + [77] * 5)
+    assert [c[1][-1] for c in calls] == [100] * 4 + [77] * 4
