@@ -656,6 +656,18 @@ def _code_of(t, what):
     return code
 
 
+_code_types = None
+
+
+def _holds_codes(t):
+    """Whether t holds e4m3 codes: as torch's e4m3fn, or as bytes.  Other types of one byte (e5m2, e4m3fnuz, int8, bool) have other values."""
+    global _code_types
+    if _code_types is None:
+        import torch
+        _code_types = (torch.float8_e4m3fn, torch.uint8)
+    return t.dtype in _code_types
+
+
 _fns = {}
 
 
@@ -740,8 +752,8 @@ def quant_rows(x, codes=None, scales=None, *, row_index=None, swiglu=False, stre
         if scales is None:
             scales = _empty(blocks, rows, torch.float32, x.device, stream)
     got_rows, got_cols, ld_codes = _matrix(codes, "codes")
-    if got_rows != rows or got_cols != cols or codes.element_size() != 1:
-        raise ValueError(f"codes must be {rows} x {cols} bytes")
+    if got_rows != rows or got_cols != cols or not _holds_codes(codes):
+        raise ValueError(f"codes must be {rows} x {cols} of float8_e4m3fn or uint8")
     got_blocks, got_rows, ld_scales = _matrix(scales, "scales")
     if got_rows != rows or got_blocks != blocks or _code_of(scales, "scales") != DR_F32:
         raise ValueError(f"scales must be fp32, {blocks} x {rows}")
@@ -760,9 +772,9 @@ class Linear:
     def __init__(self, weight, scale=None, n_groups=1):
         import torch
         rows, cols, ld = _matrix(weight, "weight")
-        fp8 = weight.element_size() == 1
+        fp8 = _holds_codes(weight)
         if not fp8 and weight.dtype != torch.bfloat16:
-            raise TypeError(f"weight must be bfloat16 or e4m3 codes, not {weight.dtype}")
+            raise TypeError(f"weight must be bfloat16 or e4m3 codes (float8_e4m3fn or uint8), not {weight.dtype}")
         if n_groups < 1 or rows % n_groups:
             raise ValueError("n_groups must divide the weight's rows")
         scale_rows = scale_cols = scale_ld = 0
@@ -799,7 +811,7 @@ class Linear:
         rows, got, ld = _matrix(t, what)
         if got != cols:
             raise ValueError(f"{what} must have {cols} columns")
-        if t.element_size() != 1 if fp8 else _code_of(t, what) != DR_BF16:
+        if not _holds_codes(t) if fp8 else _code_of(t, what) != DR_BF16:
             raise TypeError(f"{what} has the wrong type: {t.dtype}")
         return rows, ld
 

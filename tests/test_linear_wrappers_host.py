@@ -162,3 +162,26 @@ def test_allocated_outputs_belong_to_the_stream_of_the_call(calls, monkeypatch, 
         layer.wgrad(Stand(5, 256), Stand(5, 128), off, **kw[3])
     assert made_in == ([] if given else ["current"] * 5 + [77] * 5)
     assert [c[1][-1] for c in calls] == [100] * 4 + [77] * 4
+
+
+BYTES = [torch.float8_e5m2, torch.float8_e4m3fnuz, torch.float8_e5m2fnuz, torch.int8, torch.bool]
+
+
+@pytest.mark.parametrize("dtype", BYTES, ids=str)
+def test_other_types_of_one_byte_are_not_codes(calls, dtype):
+    layer = _layer(fp8=True)
+    del calls[:]
+    with pytest.raises(TypeError):
+        dr.Linear(Stand(128, 256, dtype=dtype), Stand(1, 2, dtype=F32))
+    with pytest.raises(TypeError):
+        layer.forward(Stand(5, 256, dtype=dtype), Stand(2, 5, dtype=F32), Stand(3, dtype=I32), out=Stand(5, 128))
+    with pytest.raises(ValueError):
+        dr.quant_rows(Stand(5, 256), Stand(5, 256, dtype=dtype), Stand(2, 5, dtype=F32))
+    assert not calls
+
+
+def test_codes_may_be_bytes(calls):
+    layer = dr.Linear(Stand(128, 256, dtype=torch.uint8), Stand(1, 2, dtype=F32))
+    codes, scales = dr.quant_rows(Stand(5, 256), Stand(5, 256, dtype=torch.uint8), Stand(2, 5, dtype=F32))
+    layer.forward(codes, scales, out=Stand(5, 128))
+    assert layer.fp8 and [c[0] for c in calls] == ["dr_linear_create", "dr_quant_rows", "dr_linear_forward"]
