@@ -1,7 +1,9 @@
 // Linear layers by plain fp32 arithmetic: the form that takes every stride and alignment.
 //
 // One CTA of 256 threads per 64 x 64 tile of the output, four by four outputs a thread, the contraction in steps of 16 through
-// shared memory with scalar loads.  fp8 operands are widened to code * scale as they are stored there.  The tensor-core
+// shared memory with scalar loads.  fp8 operands are widened to their codes' values; the sums of a block of 128 of the contraction are
+// scaled by the product of the two scales, as in the tensor-core kernels (code * scale may overflow where that product does
+// not: a row that holds an infinity has the scale FLT_MAX).  The tensor-core
 // kernels read their operands with tensor maps, which need bases and row pitches that are multiples of 16 bytes; what
 // cannot be read that way comes here.  Bound: fp32 FMA issue (two shared loads of four per sixteen FMAs).
 #include <cuda_bf16.h>
@@ -74,7 +76,7 @@ __global__ void __launch_bounds__(256) simt_kernel(const SimtArgs s)
     const uint32_t i_end = OP == kWgrad ? s.n : hi, j_end = OP == kForward ? s.n : s.k;
     const uint64_t w0 = (uint64_t)e * s.n;  // the group's first row in the stacked weight
 
-    float acc[4][4] = {};
+    float acc[4][4] = {}, sum[4][4] = {};  // fp8: acc of one block of the contraction, sum of the scaled blocks
     const uint32_t ti = tid >> 4, tj = tid & 15;
     for (uint32_t l0 = 0; l0 < len; l0 += kL) {
 #pragma unroll
@@ -89,7 +91,7 @@ __global__ void __launch_bounds__(256) simt_kernel(const SimtArgs s)
                     if (OP == kWgrad)
                         v = bf(s.a, (uint64_t)(lo + l0 + l) * s.lda + i0 + i);
                     else if (FP8)
-                        v = e4m3(s.a, (uint64_t)(i0 + i) * s.lda + l0 + l) * s.a_scale[(uint64_t)((l0 + l) >> 7) * s.ld_as + i0 + i];
+                        v = e4m3(s.a, (uint64_t)(i0 + i) * s.lda + l0 + l);
                     else
                         v = bf(s.a, (uint64_t)(i0 + i) * s.lda + l0 + l);
                 }
@@ -105,7 +107,7 @@ __global__ void __launch_bounds__(256) simt_kernel(const SimtArgs s)
                     else if (OP == kDgrad)
                         v = bf(s.b, (w0 + l0 + l) * s.ldb + j0 + j);
                     else if (FP8)
-                        v = e4m3(s.b, (w0 + j0 + j) * s.ldb + l0 + l) * s.b_scale[((w0 + j0 + j) >> 7) * s.ld_bs + ((l0 + l) >> 7)];
+                        v = e4m3(s.b, (w0 + j0 + j) * s.ldb + l0 + l);
                     else
                         v = bf(s.b, (w0 + j0 + j) * s.ldb + l0 + l);
                 }
@@ -123,6 +125,29 @@ __global__ void __launch_bounds__(256) simt_kernel(const SimtArgs s)
                 for (int r = 0; r < 4; ++r) acc[p][r] = fmaf(av[p], bv[r], acc[p][r]);
         }
         __syncthreads();
+        if (FP8 && ((l0 + kL) % 128 == 0 || l0 + kL >= len)) {
+            const uint32_t b = l0 >> 7;
+            float xs[4], ws[4];
+#pragma unroll
+            for (int p = 0; p < 4; ++p) {
+                const uint32_t i = i0 + ti * 4 + p, j = j0 + tj * 4 + p;
+                xs[p] = i < i_end ? s.a_scale[b * s.ld_as + i] : 0.0f;
+                ws[p] = j < j_end ? s.b_scale[((w0 + j) >> 7) * s.ld_bs + b] : 0.0f;
+            }
+#pragma unroll
+            for (int p = 0; p < 4; ++p)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    sum[p][r] = fmaf(__fmul_rn(xs[p], ws[r]), acc[p][r], sum[p][r]);
+                    acc[p][r] = 0.0f;
+                }
+        }
+    }
+    if (FP8) {
+#pragma unroll
+        for (int p = 0; p < 4; ++p)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) acc[p][r] = sum[p][r];
     }
 #pragma unroll
     for (int p = 0; p < 4; ++p) {
