@@ -621,6 +621,14 @@ int dr_linear_wgrad(const dr_linear* lin, const void* x_dev, uint64_t ldx, const
 int dr_diag_linear_wait_failures(uint64_t* count);
 
 /*
+ * dr_diag_linear_waits -- test hook (the paper has no counterpart).  Calls of this process that follow let their tensor-core
+ * kernels wait at most limit_us (0: the ordinary 2 s; not more), and with starve = 1 leave their copies out, so that
+ * every wait for an operand runs out: the kernel gives up, its output stays unwritten, the counter above rises, and nothing
+ * faults or hangs.  (0, 0) restores the ordinary calls.  Host only.  DR_ERR_INVALID.
+ */
+int dr_diag_linear_waits(uint32_t limit_us, uint32_t starve);
+
+/*
  * Hysteresis-guided reconfiguration (Sec. 3.4; host only, no CUDA).  The controller only decides WHEN to
  * move between pre-specified topologies, listed from most-Training to most-Rollout (e.g. 6:2, 5:3, 4:4).
  * Per step: imbalance = (t_rollout - t_train) / max(t_rollout, t_train).  A step signals "towards

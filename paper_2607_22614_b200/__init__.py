@@ -12,5 +12,5 @@ from .binding import (  # noqa: F401
     dr_model_spec, dr_src_layout, dr_dst_layout, dr_plan_info, dr_tensor_desc, dr_segment_desc, dr_stage_desc,
     dr_stage_stats, dr_chunk_fn, DR_MAX_STAGE_BUFS, EXPORTS,
     Linear, quant_rows, dr_linear_desc, dr_linear_create, dr_linear_destroy, dr_linear_forward, dr_linear_dgrad, dr_linear_wgrad,
-    dr_diag_linear_wait_failures, dr_quant_rows, DR_ROWS_PLAIN, DR_ROWS_SWIGLU,
+    dr_diag_linear_wait_failures, dr_diag_linear_waits, dr_quant_rows, DR_ROWS_PLAIN, DR_ROWS_SWIGLU,
 )

@@ -23,7 +23,7 @@ DR_STAGE_DIR_OUT, DR_STAGE_DIR_IN = 0, 1
 EXPORTS = ["dr_plan_create", "dr_plan_create_host", "dr_plan_window_host", "dr_plan_query", "dr_plan_tensor", "dr_plan_segment",
            "dr_reshard", "dr_reshard_inverse", "dr_plan_group", "dr_reshard_groups", "dr_reshard_static", "dr_plan_ranges", "dr_reshard_push", "dr_reshard_stream", "dr_shard_range", "dr_stage_out", "dr_stage_in", "dr_stage_begin", "dr_stage_wait_buffer", "dr_stage_poll", "dr_stage_end", "dr_plan_destroy", "dr_strerror",
            "dr_last_error", "dr_probe_stream", "dr_host_copy", "dr_diag_bulk_wait_failures", "dr_diag_bulk_starve", "dr_ctl_create", "dr_ctl_observe", "dr_ctl_break_even", "dr_ctl_destroy",
-           "dr_quant_rows", "dr_linear_create", "dr_linear_destroy", "dr_linear_forward", "dr_linear_dgrad", "dr_linear_wgrad", "dr_diag_linear_wait_failures"]
+           "dr_quant_rows", "dr_linear_create", "dr_linear_destroy", "dr_linear_forward", "dr_linear_dgrad", "dr_linear_wgrad", "dr_diag_linear_wait_failures", "dr_diag_linear_waits"]
 
 u8, u32, u64, i64, vp = C.c_uint8, C.c_uint32, C.c_uint64, C.c_int64, C.c_void_p
 
@@ -161,6 +161,7 @@ def lib() -> C.CDLL:
         L.dr_linear_dgrad.argtypes = [vp, vp, u64, u64, vp, vp, u64, u32, vp]
         L.dr_linear_wgrad.argtypes = [vp, vp, u64, vp, u64, u64, vp, vp, u64, u32, vp]
         L.dr_diag_linear_wait_failures.argtypes = [P(u64)]
+        L.dr_diag_linear_waits.argtypes = [u32, u32]
         for n in EXPORTS:
             getattr(L, n).restype = C.c_int
         L.dr_strerror.argtypes = [C.c_int]
@@ -372,6 +373,10 @@ def dr_diag_bulk_wait_failures():
 def dr_diag_linear_wait_failures():
     n = u64()
     return lib().dr_diag_linear_wait_failures(C.byref(n)), n.value
+
+
+def dr_diag_linear_waits(limit_us, starve):
+    return lib().dr_diag_linear_waits(limit_us, starve)
 
 
 def dr_diag_bulk_starve(on):

@@ -1,6 +1,7 @@
 // Entry points of the linear layers: argument checks, the handle, choice of kernel.
 #include "linear.h"
 
+#include <atomic>
 #include <cstring>
 #include <mutex>
 #include <new>
@@ -10,6 +11,10 @@ using namespace dr;
 namespace {
 
 constexpr uint64_t kMaxDim = 0x7FFFFFFFull;
+
+constexpr uint32_t kWaitUs = 2000000;
+std::atomic<uint32_t> g_wait_us{kWaitUs};
+std::atomic<bool> g_starve{false};
 
 int check_layer(const dr_linear* lin)
 {
@@ -109,6 +114,11 @@ int launch(const LinearCall& c)
 
 }  // namespace
 
+namespace dr {
+uint32_t wait_limit_us() { return g_wait_us.load(std::memory_order_relaxed); }
+bool waits_starve() { return g_starve.load(std::memory_order_relaxed); }
+}  // namespace dr
+
 extern "C" {
 
 int dr_linear_create(const dr_linear_desc* desc, dr_linear** out)
@@ -186,6 +196,17 @@ int dr_diag_linear_wait_failures(uint64_t* count)
     if (rc == DR_OK) rc = linear_small_wait_failures(&small);
     *count += small;
     return rc;
+}
+
+int dr_diag_linear_waits(uint32_t limit_us, uint32_t starve)
+{
+    if (limit_us > kWaitUs || starve > 1) {
+        set_error("a limit above the ordinary one, or starve not 0 / 1");
+        return DR_ERR_INVALID;
+    }
+    g_wait_us = limit_us ? limit_us : kWaitUs;
+    g_starve = starve != 0;
+    return DR_OK;
 }
 
 int dr_linear_destroy(dr_linear* lin)

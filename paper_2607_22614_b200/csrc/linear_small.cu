@@ -45,7 +45,8 @@ struct Shared {
     uint64_t acc_full[kTurns], acc_empty[kTurns], scale_full[kTurns], scale_empty[kTurns];
     uint64_t sums_full, sums_empty;
     TileRing<Tile> tiles;
-    uint32_t tmem, stop;
+    uint32_t tmem;
+    Limit limit;
     uint32_t tiles_before[kMaxTcGroups + 1];  // row tiles of the groups before
 };
 
@@ -59,6 +60,7 @@ struct Args {
     uint32_t feature_blocks;
     uint32_t split;  // CTAs of a cluster
     uint32_t c_f32, vector;
+    uint32_t limit_us, starve;
 };
 
 template <bool FP8>
@@ -128,9 +130,9 @@ __device__ __forceinline__ void schedule(const Args& a, Shared& s)
     Tile t;
     const uint32_t stride = gridDim.x / a.split;
     for (uint32_t i = blockIdx.x / a.split; walk.get(a, s, i, t); i += stride)
-        if (t.nt && !s.tiles.put(t, turn, &s.stop, &g_wait_failures)) return;
+        if (t.nt && !s.tiles.put(t, turn, &s.limit, &g_wait_failures)) return;
     t.nt = kNoTile;
-    s.tiles.put(t, turn, &s.stop, &g_wait_failures);
+    s.tiles.put(t, turn, &s.limit, &g_wait_failures);
 }
 
 template <bool FP8>
@@ -143,12 +145,12 @@ __device__ __forceinline__ void produce(const Args& a, Shared& s, const CUtensor
     Turn<kTilesAhead> turn;
     Tile t;
     bool ok = true;
-    while (ok && s.tiles.get(t, turn, &s.stop, &g_wait_failures)) {
+    while (ok && s.tiles.get(t, turn, &s.limit, &g_wait_failures)) {
         for (uint32_t l = 0; l < t.steps; l += kTurn) {
             const uint32_t at = stages + ring.slot * kStageBytes, bar = full + 8 * ring.slot, steps = min(kTurn, t.steps - l);
-            ok = warp_wait(empty + 8 * ring.slot, ring.round ^ 1, &s.stop, &g_wait_failures);
+            ok = warp_wait(empty + 8 * ring.slot, ring.round ^ 1, &s.limit, &g_wait_failures);
             if (!ok) break;
-            if (elect()) {
+            if (!a.starve && elect()) {
                 bar_expect(bar, steps * (kWeightBytes + t.nt * 128));
                 for (uint32_t q = 0; q < steps; ++q) load_2d<false>(at + q * kWeightBytes, map_w, bar, (t.step0 + l + q) * kStep, t.feature);
                 for (uint32_t q = 0; q < steps; ++q)
@@ -159,7 +161,7 @@ __device__ __forceinline__ void produce(const Args& a, Shared& s, const CUtensor
             used = min(used + 1, kStages);
         }
     }
-    drain(ring, used, empty, &s.stop, &g_wait_failures);
+    drain(ring, used, empty, &s.limit, &g_wait_failures);
 }
 
 template <bool FP8>
@@ -172,12 +174,12 @@ __device__ __forceinline__ void multiply(const Args& a, Shared& s)
     Turn<kTurns> acc;
     Turn<kTilesAhead> turn;
     Tile t;
-    while (s.tiles.get(t, turn, &s.stop, &g_wait_failures)) {
+    while (s.tiles.get(t, turn, &s.limit, &g_wait_failures)) {
         const uint32_t shape = shape_of(FP8, false, false, 128, t.nt);
         for (uint32_t l = 0; l < t.steps; l += kTurn) {
             if (FP8 || l == 0)
-                if (!warp_wait(acc_empty + 8 * acc.slot, acc.round ^ 1, &s.stop, &g_wait_failures)) return;
-            if (!warp_wait(full + 8 * ring.slot, ring.round, &s.stop, &g_wait_failures)) return;
+                if (!warp_wait(acc_empty + 8 * acc.slot, acc.round ^ 1, &s.limit, &g_wait_failures)) return;
+            if (!warp_wait(full + 8 * ring.slot, ring.round, &s.limit, &g_wait_failures)) return;
             fence_after();
             const uint64_t da = first_a + ring.slot * (kStageBytes >> 4), db = first_b + ring.slot * (kStageBytes >> 4);
             const uint32_t d = tmem + acc.slot * kTurn * kRowsTile;
@@ -208,12 +210,12 @@ __device__ __forceinline__ void copy_scales(const Args& a, Shared& s)
     Turn<kTurns> acc;
     Turn<kTilesAhead> turn;
     Tile t;
-    while (s.tiles.get(t, turn, &s.stop, &g_wait_failures)) {
+    while (s.tiles.get(t, turn, &s.limit, &g_wait_failures)) {
         const float* xs = a.a_scale + t.row0;
         const float* ws = a.b_scale + (uint64_t)min(t.feature / 128, scale_rows - 1) * a.ld_bs;
         const uint32_t left = t.row_end - t.row0;
         for (uint32_t l = 0; l < t.steps; l += kTurn) {
-            if (!__all_sync(0xFFFFFFFFu, bar_wait(empty + 8 * acc.slot, acc.round ^ 1, &s.stop, &g_wait_failures))) return;
+            if (!__all_sync(0xFFFFFFFFu, bar_wait(empty + 8 * acc.slot, acc.round ^ 1, &s.limit, &g_wait_failures))) return;
 #pragma unroll
             for (uint32_t q = 0; q < kTurn; ++q) {
                 if (l + q >= t.steps) break;
@@ -243,7 +245,7 @@ __device__ __forceinline__ void write_out(const Args& a, Shared& s)
     const uint32_t magic = (65536 + a.split - 1) / a.split;
     Turn<kTilesAhead> turn;
     Tile t;
-    while (s.tiles.get(t, turn, &s.stop, &g_wait_failures)) {
+    while (s.tiles.get(t, turn, &s.limit, &g_wait_failures)) {
         const bool idle = side * 32 >= t.nt;  // (such a warp only keeps the barriers going)
         float sum[2][16];
         if (FP8) {
@@ -253,8 +255,8 @@ __device__ __forceinline__ void write_out(const Args& a, Shared& s)
                 for (int r = 0; r < 16; ++r) sum[h][r] = 0.0f;
         }
         for (uint32_t l = 0; l < t.steps; l += FP8 ? kTurn : t.steps) {
-            bool ok = !FP8 || bar_wait(scale_full + 8 * acc.slot, acc.round, &s.stop, &g_wait_failures);
-            ok = ok && bar_wait(acc_full + 8 * acc.slot, acc.round, &s.stop, &g_wait_failures);
+            bool ok = !FP8 || bar_wait(scale_full + 8 * acc.slot, acc.round, &s.limit, &g_wait_failures);
+            ok = ok && bar_wait(acc_full + 8 * acc.slot, acc.round, &s.limit, &g_wait_failures);
             if (!__all_sync(0xFFFFFFFFu, ok)) return;
             fence_after();
             const uint32_t from = tmem + acc.slot * kTurn * kRowsTile;
@@ -306,7 +308,7 @@ __device__ __forceinline__ void write_out(const Args& a, Shared& s)
         // stores that count on its barrier, so that no CTA waits on a fence, and it adds them in the order of the ranks.
         const uint32_t rank = cta_rank(), rows = t.row_end - t.row0;
         const uint32_t most = (kRowsTile - 1) * magic / 65536 + 1, owned = rows > rank ? (rows - 1 - rank) * magic / 65536 + 1 : 0;
-        if (!__all_sync(0xFFFFFFFFu, bar_wait(smem_u32(&s.sums_empty), (handed & 1) ^ 1, &s.stop, &g_wait_failures))) return;
+        if (!__all_sync(0xFFFFFFFFu, bar_wait(smem_u32(&s.sums_empty), (handed & 1) ^ 1, &s.limit, &g_wait_failures))) return;
         if (warp == 0 && lane == 0) bar_expect(smem_u32(&s.sums_full), owned * a.split * 512);
 #pragma unroll
         for (int c = 0; c < 2; ++c) {  // sixteen rows at a time
@@ -331,7 +333,7 @@ __device__ __forceinline__ void write_out(const Args& a, Shared& s)
                               in_cta(smem_u32(&s.sums_full), to));
             }
         }
-        if (!__all_sync(0xFFFFFFFFu, bar_wait(smem_u32(&s.sums_full), handed & 1, &s.stop, &g_wait_failures))) return;
+        if (!__all_sync(0xFFFFFFFFu, bar_wait(smem_u32(&s.sums_full), handed & 1, &s.limit, &g_wait_failures))) return;
         for (uint32_t o = warp; o < owned; o += kReaders) {
             float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
             for (uint32_t q = 0; q < a.split; ++q) {
@@ -389,7 +391,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         bar_init(smem_u32(&s.sums_full), 1);
         bar_init(smem_u32(&s.sums_empty), kReaders * a.split);
         s.tiles.init(2 + FP8 + kReaders);  // readers: the copies, the products, the scales, the accumulators
-        s.stop = 0;
+        s.limit.stop = 0;
+        s.limit.us = a.limit_us;
         bar_init_fence();
     }
     if (warp == 1) tmem_alloc<1>(smem_u32(&s.tmem), 512);
@@ -431,13 +434,11 @@ __global__ void __launch_bounds__(kThreads, 1)
         write_out<FP8>(a, s);
     }
     __syncwarp();
-    if (*(volatile uint32_t*)&s.stop) {  // a wait ran out: let the copies and products in flight end before the memory is given back
-        const uint64_t since = now_ns();
-        while (now_ns() - since < 10000000ull) __nanosleep(1000);
-    }
+    let_copies_end(&s.limit);
     fence_before();
     __syncthreads();
     if (a.split > 1) cluster_sync();  // other CTAs may still be reading this one's sums
+    let_copies_end(&s.limit);
     fence_after();
     if (warp == 1) tmem_free<1>(s.tmem, 512);
 }
@@ -530,6 +531,8 @@ int launch_linear_small(const LinearCall& c)
     a.n = (uint32_t)d.out_features;
     a.k = (uint32_t)d.in_features;
     a.c_f32 = c.c_f32;
+    a.limit_us = wait_limit_us();
+    a.starve = waits_starve();
     a.vector = !c.c_f32 && a.n % 8 == 0 && c.ldc % 8 == 0 && (uintptr_t)c.c % 16 == 0;
     a.feature_blocks = (a.n + (fp8 && a.n % 128 ? 127 : 0) + 127) / 128;
     // at most one row tile more than full ones for each group that has rows

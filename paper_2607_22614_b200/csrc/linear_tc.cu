@@ -64,7 +64,8 @@ struct Barriers {
     TileRing<Tile> tiles;
     uint64_t full[6], empty[6], landed[6];
     alignas(16) uint64_t acc_full[2], acc_empty[2];  // (the readers flip bit 3 of their addresses)
-    uint32_t tmem, stop;
+    uint32_t tmem;
+    Limit limit;
     uint32_t tiles_before[kMaxTcGroups + 1];  // token tiles of the groups before
 };
 template <int OP>
@@ -95,6 +96,7 @@ struct TcArgs {
     uint32_t rows, n_groups, n, k;
     uint32_t feature_tiles, column_tiles;  // column_tiles: wgrad's tiles of in_features
     uint32_t c_f32, accumulate, vector, bulk_out;
+    uint32_t limit_us, starve;
 };
 
 template <int OP, bool FP8>
@@ -201,9 +203,9 @@ __device__ __forceinline__ void schedule(const TcArgs& a, Shared<OP>& s)
     Turn<kTilesAhead> at;
     Tile t;
     for (uint32_t i = blockIdx.x >> 1; walk.get(a, s, i, t); i += gridDim.x >> 1)
-        if (t.nt && !s.tiles.put(t, at, &s.stop, &g_wait_failures)) return;
+        if (t.nt && !s.tiles.put(t, at, &s.limit, &g_wait_failures)) return;
     t.nt = kNoTile;
-    s.tiles.put(t, at, &s.stop, &g_wait_failures);
+    s.tiles.put(t, at, &s.limit, &g_wait_failures);
 }
 
 template <int OP, bool FP8>
@@ -218,15 +220,15 @@ __device__ __forceinline__ void produce(const TcArgs& a, Shared<OP>& s, const CU
     bool ok = true;
     Turn<kTilesAhead> at;
     Tile t;
-    while (ok && s.tiles.get(t, at, &s.stop, &g_wait_failures)) {
+    while (ok && s.tiles.get(t, at, &s.limit, &g_wait_failures)) {
         const uint32_t half = t.nt / 2, feature = t.feature + rank * 128;
         const uint32_t boxes = OP == kWgrad ? (half + 63) / 64 : (half + 31) / 32, box_bytes = OP == kWgrad ? 8192 : 4096;
         const uint32_t bytes = kOperandBytes + boxes * box_bytes;
         for (uint32_t l = 0; l < t.steps; ++l) {
             const uint32_t to = stages + ring.slot * kStageBytes, bar = full + 8 * ring.slot;
-            ok = warp_wait(empty + 8 * ring.slot, ring.round ^ 1, &s.stop, &g_wait_failures);
+            ok = warp_wait(empty + 8 * ring.slot, ring.round ^ 1, &s.limit, &g_wait_failures);
             if (!ok) break;
-            if (elect()) {
+            if (!a.starve && elect()) {
                 if (OP == kWgrad)
                     bar_expect(bar, bytes);
                 else if (rank == 0)
@@ -254,7 +256,7 @@ __device__ __forceinline__ void produce(const TcArgs& a, Shared<OP>& s, const CU
             used = min(used + 1, kStages<OP>);
         }
     }
-    if (ok) drain(ring, used, empty, &s.stop, &g_wait_failures);
+    if (ok) drain(ring, used, empty, &s.limit, &g_wait_failures);
 }
 
 template <int OP, bool FP8>
@@ -268,13 +270,13 @@ __device__ __forceinline__ void multiply(const TcArgs& a, Shared<OP>& s)
     Turn<2> acc;
     Turn<kTilesAhead> at;
     Tile t;
-    while (s.tiles.get(t, at, &s.stop, &g_wait_failures)) {
+    while (s.tiles.get(t, at, &s.limit, &g_wait_failures)) {
         if (t.steps == 0) continue;
         const uint32_t shape = shape_of(FP8, a_mn, b_mn, 256, t.nt);
         for (uint32_t l = 0; l < t.steps; ++l) {
             if (FP8 || l == 0)
-                if (!warp_wait(acc_empty + 8 * acc.slot, acc.round ^ 1, &s.stop, &g_wait_failures)) return;
-            if (!warp_wait(full + 8 * ring.slot, ring.round, &s.stop, &g_wait_failures)) return;
+                if (!warp_wait(acc_empty + 8 * acc.slot, acc.round ^ 1, &s.limit, &g_wait_failures)) return;
+            if (!warp_wait(full + 8 * ring.slot, ring.round, &s.limit, &g_wait_failures)) return;
             fence_after();
             // addresses are the low bits of a descriptor, in units of 16 bytes
             const uint64_t da = first_a + ring.slot * (kStageBytes >> 4), db = first_b + ring.slot * (kStageBytes >> 4);
@@ -302,11 +304,11 @@ __device__ __forceinline__ void clear_rows(const TcArgs& a, Shared<kWgrad>& s)
     uint32_t n = 0;
     Turn<kTilesAhead> at;
     Tile t;
-    while (s.tiles.get(t, at, &s.stop, &g_wait_failures)) {
+    while (s.tiles.get(t, at, &s.limit, &g_wait_failures)) {
         const uint32_t panels = (t.nt / 2 + 63) / 64;
         for (uint32_t l = 0; l < t.steps; ++l, ++n) {
             const uint32_t st = n % kStages<kWgrad>, valid = min(64u, t.row_end - t.row0 - l * 64);
-            if (!__all_sync(0xFFFFFFFFu, bar_wait(landed + 8 * st, n / kStages<kWgrad> & 1, &s.stop, &g_wait_failures))) return;
+            if (!__all_sync(0xFFFFFFFFu, bar_wait(landed + 8 * st, n / kStages<kWgrad> & 1, &s.limit, &g_wait_failures))) return;
             if (valid < 64) {
                 for (uint32_t p = 0; p < 2 + panels; ++p) {  // operand A's two panels, then B's: 8 KB each, side by side
                     uint8_t* panel = s.stage[st] + p * 8192;
@@ -333,11 +335,11 @@ __device__ __forceinline__ void write_dw(const TcArgs& a, Shared<kWgrad>& s, con
     Turn<kTilesAhead> at;
     Tile t;
     uint32_t blocks = 0;
-    while (s.tiles.get(t, at, &s.stop, &g_wait_failures)) {
+    while (s.tiles.get(t, at, &s.limit, &g_wait_failures)) {
         const uint32_t cols = t.nt / 2, col0 = side * cols;  // this warp's columns, a multiple of 16
         const uint32_t row = t.feature + rank * 128 + quarter * 32;
         if (t.steps) {
-            if (!__all_sync(0xFFFFFFFFu, bar_wait(acc_full + 8 * acc.slot, acc.round, &s.stop, &g_wait_failures))) return;
+            if (!__all_sync(0xFFFFFFFFu, bar_wait(acc_full + 8 * acc.slot, acc.round, &s.limit, &g_wait_failures))) return;
             fence_after();
         }
         // blocks of 32 columns; a last one of 16 ends where the next warp's columns (or the matrix) begin, and is stored directly
@@ -400,13 +402,13 @@ __device__ __forceinline__ void write_out(const TcArgs& a, Shared<OP>& s)
     Turn<2> acc;
     Turn<kTilesAhead> at;
     Tile t;
-    while (s.tiles.get(t, at, &s.stop, &g_wait_failures)) {
+    while (s.tiles.get(t, at, &s.limit, &g_wait_failures)) {
         const uint32_t cols = t.nt / 2, col0 = side * cols;  // this warp's tokens
         const uint32_t feature = t.feature + rank * 128 + quarter * 32;
         // in a row of c: forward counts features from the group's first weight row
         const int f = OP == kForward ? (int)(feature - t.e * a.n) : (int)feature;
         const int f_hi = OP == kDgrad ? (int)a.k : (int)a.n;
-        if (!__all_sync(0xFFFFFFFFu, bar_wait(acc_full + 8 * acc.slot, acc.round, &s.stop, &g_wait_failures))) return;
+        if (!__all_sync(0xFFFFFFFFu, bar_wait(acc_full + 8 * acc.slot, acc.round, &s.limit, &g_wait_failures))) return;
         fence_after();
         for (uint32_t c = 0; c < cols; c += 32) {
             float p[2][16];
@@ -442,7 +444,7 @@ __device__ __forceinline__ void write_rows(const TcArgs& a, Shared<kForwardRows>
     float x1, w1, x2, w2;
     // the next tile, and the first two scales of this thread's row in it
     auto next_tile = [&]() {
-        if (!s.tiles.get(t, at, &s.stop, &g_wait_failures)) return false;
+        if (!s.tiles.get(t, at, &s.limit, &g_wait_failures)) return false;
         xs = a.a_scale + min(t.row0 + rank * 128 + quarter * 32 + lane, t.row_end - 1);
         ws = a.b_scale + (uint64_t)min(t.feature / 128 + side, scale_rows - 1) * a.ld_bs;
         x1 = xs[0];
@@ -469,7 +471,7 @@ __device__ __forceinline__ void write_rows(const TcArgs& a, Shared<kForwardRows>
         for (uint32_t left = steps; left; --left) {
             const float scale = x1 * w1;
             const uint64_t two = pair_of(scale, scale);
-            if (!__all_sync(0xFFFFFFFFu, bar_wait(filled, parity, &s.stop, &g_wait_failures))) return;
+            if (!__all_sync(0xFFFFFFFFu, bar_wait(filled, parity, &s.limit, &g_wait_failures))) return;
             fence_after();
             float p[2][32];
             if (!idle) tmem_start(from, p[0]);
@@ -586,7 +588,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         }
         // readers: the copies, the products (first CTA), the cleared rows, the accumulators
         s.tiles.init(1 + (cta_rank() == 0) + (OP == kWgrad) + kEpilogueWarps);
-        s.stop = 0;
+        s.limit.stop = 0;
+        s.limit.us = a.limit_us;
         bar_init_fence();
     }
     if (warp == 1) tmem_alloc<2>(smem_u32(&s.tmem), 512);
@@ -633,13 +636,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
             write_out(a, s);
     }
     __syncwarp();
-    if (*(volatile uint32_t*)&s.stop) {  // a wait ran out: let the copies and products in flight end before the memory is given back
-        const uint64_t since = now_ns();
-        while (now_ns() - since < 10000000ull) __nanosleep(1000);
-    }
+    let_copies_end(&s.limit);
     fence_before();
     __syncthreads();
     cluster_sync();
+    let_copies_end(&s.limit);
     fence_after();
     if (warp == 1) tmem_free<2>(s.tmem, 512);
 }
@@ -717,6 +718,8 @@ int launch_linear_tc(const LinearCall& c)
     a.n = (uint32_t)d.out_features;
     a.k = (uint32_t)d.in_features;
     a.c_f32 = c.c_f32;
+    a.limit_us = wait_limit_us();
+    a.starve = waits_starve();
     a.accumulate = c.accumulate;
     CUtensorMap ma, mb, mc{};
     int rc;

@@ -66,19 +66,22 @@ __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity)
     return ok;
 }
 
-// Waits for the phase of this parity to complete, at most kWaitNs.  A wait that runs out (which nothing in these kernels should
+// How long the CTA's waits may take, and whether one of them has run out.
+struct Limit {
+    uint32_t stop, us;
+};
+// Waits for the phase of this parity to complete, at most limit->us.  A wait that runs out (which nothing in these kernels should
 // make happen) raises the CTA's `stop` flag and counts in *failures; every role then leaves its loop at its next wait.
-constexpr uint64_t kWaitNs = 2000000000ull;
-__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile uint32_t* stop, unsigned long long* failures)
+__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile Limit* limit, unsigned long long* failures)
 {
     uint64_t since = 0;
     for (uint32_t n = 1; !bar_try(bar, parity); ++n) {
         if (n & 63) continue;
-        if (*stop) return false;
+        if (limit->stop) return false;
         const uint64_t t = now_ns();
         if (since == 0) since = t;
-        if (t - since > kWaitNs) {
-            *stop = 1;
+        if (t - since > limit->us * 1000ull) {
+            limit->stop = 1;
             atomicAdd(failures, 1ull);
             return false;
         }
@@ -89,20 +92,28 @@ __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile
 // The same by a whole warp, with one answer for all lanes.  The roles that issue copies and products run their loops with all lanes
 // and let one elected lane issue: the compiler then keeps addresses and descriptors in uniform registers, where these
 // instructions want them (with a single lane in the loop every operand is moved there first: 70 cycles a product, measured).
-static __device__ __noinline__ bool warp_wait_long(uint32_t bar, uint32_t parity, volatile uint32_t* stop, unsigned long long* failures)
+static __device__ __noinline__ bool warp_wait_long(uint32_t bar, uint32_t parity, volatile Limit* limit, unsigned long long* failures)
 {
-    return __all_sync(0xFFFFFFFFu, bar_wait(bar, parity, stop, failures));
+    return __all_sync(0xFFFFFFFFu, bar_wait(bar, parity, limit, failures));
 }
-__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile uint32_t* stop, unsigned long long* failures)
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile Limit* limit, unsigned long long* failures)
 {
     if (__all_sync(0xFFFFFFFFu, bar_try(bar, parity))) return true;
-    return warp_wait_long(bar, parity, stop, failures);
+    return warp_wait_long(bar, parity, limit, failures);
 }
 __device__ __forceinline__ bool elect()
 {
     uint32_t p;
     asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xFFFFFFFF;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(p));
     return p;
+}
+// For a CTA that has given up: its copies and products in flight end meanwhile.  Before the cluster's last barrier, so that the others
+// outlive what this CTA has sent them, and behind it, so that this CTA outlives what they have sent.
+__device__ __forceinline__ void let_copies_end(const volatile Limit* limit)
+{
+    if (!limit->stop) return;
+    const uint64_t since = now_ns();
+    while (now_ns() - since < 10000000ull) __nanosleep(1000);
 }
 // A place in a ring of N slots and the parity of its round.
 template <uint32_t N>
@@ -120,14 +131,14 @@ struct Turn {
 // Waits until the last `used` slots before the ring's place have been given back: their copies have landed and the commits that
 // freed them have arrived, so that the CTA may end.
 template <uint32_t N>
-__device__ __forceinline__ void drain(Turn<N> ring, uint32_t used, uint32_t empty, volatile uint32_t* stop, unsigned long long* failures)
+__device__ __forceinline__ void drain(Turn<N> ring, uint32_t used, uint32_t empty, volatile Limit* limit, unsigned long long* failures)
 {
     for (; used; --used) {
         if (ring.slot-- == 0) {
             ring.slot = N - 1;
             ring.round ^= 1;
         }
-        if (!warp_wait(empty + 8 * ring.slot, ring.round, stop, failures)) return;
+        if (!warp_wait(empty + 8 * ring.slot, ring.round, limit, failures)) return;
     }
 }
 
@@ -146,9 +157,9 @@ struct TileRing {
         }
     }
     // by a whole warp
-    __device__ __forceinline__ bool put(const T& t, Turn<kTilesAhead>& at, volatile uint32_t* stop, unsigned long long* failures)
+    __device__ __forceinline__ bool put(const T& t, Turn<kTilesAhead>& at, volatile Limit* limit, unsigned long long* failures)
     {
-        if (!__all_sync(0xFFFFFFFFu, bar_wait(smem_u32(&empty[at.slot]), at.round ^ 1, stop, failures))) return false;
+        if (!__all_sync(0xFFFFFFFFu, bar_wait(smem_u32(&empty[at.slot]), at.round ^ 1, limit, failures))) return false;
         if ((threadIdx.x & 31) == 0) {
             tile[at.slot] = t;
             bar_arrive(smem_u32(&full[at.slot]));
@@ -157,9 +168,9 @@ struct TileRing {
         at.next();
         return true;
     }
-    __device__ __forceinline__ bool get(T& t, Turn<kTilesAhead>& at, volatile uint32_t* stop, unsigned long long* failures)
+    __device__ __forceinline__ bool get(T& t, Turn<kTilesAhead>& at, volatile Limit* limit, unsigned long long* failures)
     {
-        if (!__all_sync(0xFFFFFFFFu, bar_wait(smem_u32(&full[at.slot]), at.round, stop, failures))) return false;
+        if (!__all_sync(0xFFFFFFFFu, bar_wait(smem_u32(&full[at.slot]), at.round, limit, failures))) return false;
         t = tile[at.slot];
         __syncwarp();
         if ((threadIdx.x & 31) == 0) bar_arrive(smem_u32(&empty[at.slot]));

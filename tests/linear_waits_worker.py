@@ -1,0 +1,66 @@
+"""Child process of the tests of the linear layers' bounded waits: the counter that it raises is the process's own.
+
+    python linear_waits_worker.py give_up
+"""
+import os
+import sys
+
+sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
+sys.path.insert(0, os.path.dirname(os.path.abspath(__file__)))
+
+import torch
+
+import paper_2607_22614_b200 as dr
+from linear_util import DEV, gen, offsets_of, quant_weight
+
+BF16, F32 = torch.bfloat16, torch.float32
+
+
+def count():
+    rc, n = dr.dr_diag_linear_wait_failures()
+    assert rc == 0
+    return n
+
+
+def calls():
+    """Every tensor-core kernel in its forms: few rows with and without a split contraction, pairs of CTAs, dense and ragged, gradients."""
+    for sizes, n, k in (([5], 256, 1024), ([40], 8192, 512), ([300], 512, 512), ([3, 0, 60, 17], 384, 512), ([600, 0, 301], 384, 512)):
+        groups, rows = len(sizes), sum(sizes)
+        off = None if groups == 1 else offsets_of(sizes)[0]
+        x = torch.randn(rows, k, device=DEV, generator=gen(rows)).bfloat16()
+        dy = torch.randn(rows, n, device=DEV, generator=gen(n)).bfloat16()
+        w = torch.randn(groups * n, k, device=DEV, generator=gen(k)) * 0.05
+        bf, q8 = dr.Linear(w.bfloat16(), n_groups=groups), dr.Linear(*quant_weight(w), n_groups=groups)
+        xq, xs = dr.quant_rows(x)
+        name = f"{sizes} x {n} x {k}"
+        yield f"bf16 {name}", lambda out: bf.forward(x, None, off, out=out), (rows, n, BF16)
+        yield f"fp8 {name}", lambda out: q8.forward(xq, xs, off, out=out), (rows, n, BF16)
+        yield f"dgrad {name}", lambda out: bf.dgrad(dy, off, out=out), (rows, k, BF16)
+        yield f"wgrad {name}", lambda out: bf.wgrad(x, dy, off, out=out), (groups * n, k, F32)
+
+
+def give_up():
+    """Without its copies a kernel gives up, says so, and leaves a device on which the next call is right."""
+    assert dr.dr_diag_linear_waits(2000001, 0) < 0 and dr.dr_diag_linear_waits(0, 2) < 0
+    for name, call, (rows, cols, dtype) in calls():
+        want = call(torch.empty(rows, cols, dtype=dtype, device=DEV)).clone()
+        torch.cuda.synchronize()
+        before = count()
+        got = torch.full((rows, cols), 9.0, dtype=dtype, device=DEV)
+        assert dr.dr_diag_linear_waits(20000, 1) == 0
+        call(got)
+        assert dr.dr_diag_linear_waits(0, 0) == 0
+        torch.cuda.synchronize()
+        after = count()
+        assert after > before, f"{name}: no wait ran out"
+        assert (got[:3] == 9.0).all(), f"{name}: an output without operands"
+        call(got)
+        torch.cuda.synchronize()
+        assert torch.equal(got, want) and count() == after, f"{name}: the next call"
+        print(name, after - before, flush=True)
+    assert before > 0
+
+
+if __name__ == "__main__":
+    {"give_up": give_up}[sys.argv[1]]()
+    print("done")
