@@ -615,8 +615,9 @@ int dr_linear_wgrad(const dr_linear* lin, const void* x_dev, uint64_t ldx, const
 
 /*
  * dr_diag_linear_wait_failures -- diagnostic: the tensor-core kernels of the linear layers wait for their copies and products
- * with a limit (2 s); a wait that runs out ends the kernel with its output incomplete and counts here.  *count = such
- * events on the current device since the library was loaded; expected 0.  Synchronous.  DR_ERR_INVALID, DR_ERR_CUDA.
+ * with a limit (2 s); a wait that runs out ends the kernel with its output incomplete and counts here.  *count = such waiting
+ * threads on the current device since the library was loaded; expected 0.  Waits for all work that the device
+ * has been given, on every stream (so it cannot be captured).  DR_ERR_INVALID, DR_ERR_CUDA.
  */
 int dr_diag_linear_wait_failures(uint64_t* count);
 

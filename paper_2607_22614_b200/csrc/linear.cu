@@ -191,6 +191,8 @@ int dr_diag_linear_wait_failures(uint64_t* count)
         set_error("NULL argument");
         return DR_ERR_INVALID;
     }
+    // calls may run on streams that the default stream, which the counters are read on, does not wait for
+    DR_CUDA(cudaDeviceSynchronize());
     uint64_t small = 0;
     int rc = linear_wait_failures(count);
     if (rc == DR_OK) rc = linear_small_wait_failures(&small);

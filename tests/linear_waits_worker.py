@@ -1,6 +1,6 @@
 """Child process of the tests of the linear layers' bounded waits: the counter that it raises is the process's own.
 
-    python linear_waits_worker.py give_up
+    python linear_waits_worker.py give_up | counted_at_once
 """
 import os
 import sys
@@ -61,6 +61,20 @@ def give_up():
     assert before > 0
 
 
+def counted_at_once():
+    """The counter read right behind a call on a stream of its own, which the default stream does not wait for."""
+    side = torch.cuda.Stream()
+    for name, call, (rows, cols, dtype) in calls():
+        out = torch.zeros(rows, cols, dtype=dtype, device=DEV)
+        torch.cuda.synchronize()
+        before = count()
+        assert dr.dr_diag_linear_waits(50000, 1) == 0
+        with torch.cuda.stream(side):
+            call(out)
+        assert dr.dr_diag_linear_waits(0, 0) == 0
+        assert count() > before, f"{name}: read too early"
+
+
 if __name__ == "__main__":
-    {"give_up": give_up}[sys.argv[1]]()
+    {"give_up": give_up, "counted_at_once": counted_at_once}[sys.argv[1]]()
     print("done")

@@ -17,3 +17,7 @@ def _run(part):
 
 def test_kernels_that_give_up_say_so_and_leave_the_device_usable():
     _run("give_up")
+
+
+def test_the_counter_waits_for_every_stream():
+    _run("counted_at_once")
