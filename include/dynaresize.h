@@ -615,7 +615,7 @@ int dr_linear_wgrad(const dr_linear* lin, const void* x_dev, uint64_t ldx, const
 
 /*
  * dr_diag_linear_wait_failures -- diagnostic: the tensor-core kernels of the linear layers wait for their copies and products
- * with a limit (2 s); a wait that runs out ends the kernel with its output incomplete and counts here.  *count = such waiting
+ * with a limit (2 s, and 10 us for every 64 of the contraction); a wait that runs out ends the kernel with its output incomplete and counts here.  *count = such waiting
  * threads on the current device since the library was loaded; expected 0.  Waits for all work that the device
  * has been given, on every stream (so it cannot be captured).  DR_ERR_INVALID, DR_ERR_CUDA.
  */
@@ -623,7 +623,7 @@ int dr_diag_linear_wait_failures(uint64_t* count);
 
 /*
  * dr_diag_linear_waits -- test hook (the paper has no counterpart).  Calls of this process that follow let their tensor-core
- * kernels wait at most limit_us (0: the ordinary 2 s; not more), and with starve = 1 leave their copies out, so that
+ * kernels wait at most limit_us (0: the ordinary 2 s; not more) and 10 us for every 64 of the contraction, and with starve = 1 leave their copies out, so that
  * every wait for an operand runs out: the kernel gives up, its output stays unwritten, the counter above rises, and nothing
  * faults or hangs.  (0, 0) restores the ordinary calls.  Host only.  DR_ERR_INVALID.
  */

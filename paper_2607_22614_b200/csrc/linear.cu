@@ -12,7 +12,9 @@ namespace {
 
 constexpr uint64_t kMaxDim = 0x7FFFFFFFull;
 
-constexpr uint32_t kWaitUs = 2000000;
+// A role may wait for a whole tile (bf16 accumulators are handed over at its end), and a contraction may have up to 2^25 steps: at 0.2 to
+// 0.4 us each that is 10 s, so the limit grows with them.
+constexpr uint32_t kWaitUs = 2000000, kStepWaitUs = 10;
 std::atomic<uint32_t> g_wait_us{kWaitUs};
 std::atomic<bool> g_starve{false};
 
@@ -115,7 +117,11 @@ int launch(const LinearCall& c)
 }  // namespace
 
 namespace dr {
-uint32_t wait_limit_us() { return g_wait_us.load(std::memory_order_relaxed); }
+uint32_t wait_limit_us(uint64_t steps)
+{
+    const uint64_t us = g_wait_us.load(std::memory_order_relaxed) + steps * kStepWaitUs;
+    return us < 0xFFFFFFFFull ? (uint32_t)us : 0xFFFFFFFFu;
+}
 bool waits_starve() { return g_starve.load(std::memory_order_relaxed); }
 }  // namespace dr
 

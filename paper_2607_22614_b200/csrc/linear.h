@@ -47,7 +47,7 @@ bool linear_tc_takes(const LinearCall& c);
 int launch_linear_tc(const LinearCall& c);
 int prepare_linear_tc();                    // once per device
 int linear_wait_failures(uint64_t* out);    // bounded waits that ran out (expected: 0)
-uint32_t wait_limit_us();                   // how long a wait may take
+uint32_t wait_limit_us(uint64_t steps);     // how long a wait may take when a tile's contraction has so many steps
 bool waits_starve();                        // test hook: the copies are left out
 
 // linear_small.cu: forward with few rows a group, the same operands

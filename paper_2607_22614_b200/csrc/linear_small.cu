@@ -531,7 +531,7 @@ int launch_linear_small(const LinearCall& c)
     a.n = (uint32_t)d.out_features;
     a.k = (uint32_t)d.in_features;
     a.c_f32 = c.c_f32;
-    a.limit_us = wait_limit_us();
+    a.limit_us = wait_limit_us((a.k + 63ull) / 64);
     a.starve = waits_starve();
     a.vector = !c.c_f32 && a.n % 8 == 0 && c.ldc % 8 == 0 && (uintptr_t)c.c % 16 == 0;
     a.feature_blocks = (a.n + (fp8 && a.n % 128 ? 127 : 0) + 127) / 128;

@@ -718,7 +718,8 @@ int launch_linear_tc(const LinearCall& c)
     a.n = (uint32_t)d.out_features;
     a.k = (uint32_t)d.in_features;
     a.c_f32 = c.c_f32;
-    a.limit_us = wait_limit_us();
+    const uint64_t contraction = c.op == kWgrad ? c.rows : c.op == kDgrad ? a.n : a.k;
+    a.limit_us = wait_limit_us((contraction + 63) / 64);
     a.starve = waits_starve();
     a.accumulate = c.accumulate;
     CUtensorMap ma, mb, mc{};

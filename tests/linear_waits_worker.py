@@ -1,6 +1,6 @@
 """Child process of the tests of the linear layers' bounded waits: the counter that it raises is the process's own.
 
-    python linear_waits_worker.py give_up | counted_at_once
+    python linear_waits_worker.py give_up | counted_at_once | long_contractions
 """
 import os
 import sys
@@ -75,6 +75,37 @@ def counted_at_once():
         assert count() > before, f"{name}: read too early"
 
 
+def long_contractions():
+    """A tile that takes many times the limit's fixed part (1 ms here, 2 s in earnest, where the contraction may be 2^25 steps long):
+    the limit has to grow with the contraction.  All other values are zero, so the result shows whether the last step was taken."""
+    def of(rows, cols, step):
+        """Zeros, and ones in the first and last positions of the contraction (along the rows or along the columns)."""
+        t = torch.zeros(rows, cols, dtype=BF16, device=DEV)
+        for at in (0, -1):
+            (t[at] if step == "rows" else t[:, at]).fill_(1)
+        return t
+
+    long = 1 << 23
+    layer = dr.Linear(torch.zeros(64, 64, dtype=BF16, device=DEV))
+    x, dy = of(long, 64, "rows"), of(long, 64, "rows")
+    wide = dr.Linear(of(128, long, "cols"))
+    few, many = of(4, long, "cols"), of(100, long, "cols")
+    back = dr.Linear(of(long, 64, "rows"))
+    gy = of(100, long, "cols")
+    for name, call in (("wgrad", lambda: layer.wgrad(x, dy)), ("few rows", lambda: wide.forward(few, out_dtype=F32)),
+                       ("many rows", lambda: wide.forward(many, out_dtype=F32)), ("dgrad", lambda: back.dgrad(gy, out_dtype=F32))):
+        assert dr.dr_diag_linear_waits(1000, 0) == 0
+        a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        a.record()
+        got = call()
+        b.record()
+        assert dr.dr_diag_linear_waits(0, 0) == 0
+        assert count() == 0, f"{name}: a wait ran out"
+        assert (got == 2).all(), name
+        print(f"{name}: {a.elapsed_time(b):.1f} ms", flush=True)
+        assert a.elapsed_time(b) > 2.0, "too short a contraction to show anything"
+
+
 if __name__ == "__main__":
-    {"give_up": give_up, "counted_at_once": counted_at_once}[sys.argv[1]]()
+    {"give_up": give_up, "counted_at_once": counted_at_once, "long_contractions": long_contractions}[sys.argv[1]]()
     print("done")

@@ -21,3 +21,7 @@ def test_kernels_that_give_up_say_so_and_leave_the_device_usable():
 
 def test_the_counter_waits_for_every_stream():
     _run("counted_at_once")
+
+
+def test_the_limit_grows_with_the_contraction():
+    _run("long_contractions")
