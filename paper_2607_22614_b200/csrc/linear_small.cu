@@ -308,7 +308,7 @@ __device__ __forceinline__ void write_out(const Args& a, Shared& s)
         // stores that count on its barrier, so that no CTA waits on a fence, and it adds them in the order of the ranks.
         const uint32_t rank = cta_rank(), rows = t.row_end - t.row0;
         const uint32_t most = (kRowsTile - 1) * magic / 65536 + 1, owned = rows > rank ? (rows - 1 - rank) * magic / 65536 + 1 : 0;
-        if (!__all_sync(0xFFFFFFFFu, bar_wait(smem_u32(&s.sums_empty), (handed & 1) ^ 1, &s.limit, &g_wait_failures))) return;
+        if (!__all_sync(0xFFFFFFFFu, bar_wait<true>(smem_u32(&s.sums_empty), (handed & 1) ^ 1, &s.limit, &g_wait_failures))) return;
         if (warp == 0 && lane == 0) bar_expect(smem_u32(&s.sums_full), owned * a.split * 512);
 #pragma unroll
         for (int c = 0; c < 2; ++c) {  // sixteen rows at a time
@@ -333,7 +333,7 @@ __device__ __forceinline__ void write_out(const Args& a, Shared& s)
                               in_cta(smem_u32(&s.sums_full), to));
             }
         }
-        if (!__all_sync(0xFFFFFFFFu, bar_wait(smem_u32(&s.sums_full), handed & 1, &s.limit, &g_wait_failures))) return;
+        if (!__all_sync(0xFFFFFFFFu, bar_wait<true>(smem_u32(&s.sums_full), handed & 1, &s.limit, &g_wait_failures))) return;
         for (uint32_t o = warp; o < owned; o += kReaders) {
             float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
             for (uint32_t q = 0; q < a.split; ++q) {
@@ -359,7 +359,7 @@ __device__ __forceinline__ void write_out(const Args& a, Shared& s)
             }
         }
         __syncwarp();
-        if (lane < a.split) bar_arrive_cluster(in_cta(smem_u32(&s.sums_empty), lane));
+        if (lane < a.split) bar_arrive_cluster(in_cta(smem_u32(&s.sums_empty), lane), true);
         ++handed;
     }
 }

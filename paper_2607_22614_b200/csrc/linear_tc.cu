@@ -276,7 +276,8 @@ __device__ __forceinline__ void multiply(const TcArgs& a, Shared<OP>& s)
         for (uint32_t l = 0; l < t.steps; ++l) {
             if (FP8 || l == 0)
                 if (!warp_wait(acc_empty + 8 * acc.slot, acc.round ^ 1, &s.limit, &g_wait_failures)) return;
-            if (!warp_wait(full + 8 * ring.slot, ring.round, &s.limit, &g_wait_failures)) return;
+            // (wgrad: the other CTA may have cleared rows of its stage)
+            if (!warp_wait<OP == kWgrad>(full + 8 * ring.slot, ring.round, &s.limit, &g_wait_failures)) return;
             fence_after();
             // addresses are the low bits of a descriptor, in units of 16 bytes
             const uint64_t da = first_a + ring.slot * (kStageBytes >> 4), db = first_b + ring.slot * (kStageBytes >> 4);

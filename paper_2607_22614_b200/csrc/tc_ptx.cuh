@@ -48,21 +48,30 @@ __device__ __forceinline__ void bar_arrive(uint32_t bar)
 }
 // `bar` may lie in another CTA of the cluster (an address of in_cta).  What the arrival hands over is tensor memory that has
 // been read (ordered by fence_before) or stages that only the copy unit wrote, so no release at cluster scope, which would
-// stall the warp on a memory barrier, is needed; where the warp itself has written shared memory, `wrote` asks for it.
-__device__ __forceinline__ void bar_arrive_cluster(uint32_t bar, bool wrote = false)
+// stall the warp on a memory barrier, is needed; where the warp itself has written or read ordinary shared memory that the other
+// CTA will read or write, `release` asks for it, and the wait for that barrier acquires at cluster scope.
+__device__ __forceinline__ void bar_arrive_cluster(uint32_t bar, bool release = false)
 {
-    if (wrote)
+    if (release)
         asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
     else
         asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
+// CLUSTER: what other CTAs of the cluster released with their arrivals (or sent with store_counted) is acquired.
+template <bool CLUSTER = false>
 __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity)
 {
     uint32_t ok;
-    asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}"
-                 : "=r"(ok)
-                 : "r"(bar), "r"(parity)
-                 : "memory");
+    if (CLUSTER)
+        asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}"
+                     : "=r"(ok)
+                     : "r"(bar), "r"(parity)
+                     : "memory");
+    else
+        asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}"
+                     : "=r"(ok)
+                     : "r"(bar), "r"(parity)
+                     : "memory");
     return ok;
 }
 
@@ -72,10 +81,11 @@ struct Limit {
 };
 // Waits for the phase of this parity to complete, at most limit->us.  A wait that runs out (which nothing in these kernels should
 // make happen) raises the CTA's `stop` flag and counts in *failures; every role then leaves its loop at its next wait.
+template <bool CLUSTER = false>
 __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile Limit* limit, unsigned long long* failures)
 {
     uint64_t since = 0;
-    for (uint32_t n = 1; !bar_try(bar, parity); ++n) {
+    for (uint32_t n = 1; !bar_try<CLUSTER>(bar, parity); ++n) {
         if (n & 63) continue;
         if (limit->stop) return false;
         const uint64_t t = now_ns();
@@ -92,14 +102,16 @@ __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile
 // The same by a whole warp, with one answer for all lanes.  The roles that issue copies and products run their loops with all lanes
 // and let one elected lane issue: the compiler then keeps addresses and descriptors in uniform registers, where these
 // instructions want them (with a single lane in the loop every operand is moved there first: 70 cycles a product, measured).
+template <bool CLUSTER>
 static __device__ __noinline__ bool warp_wait_long(uint32_t bar, uint32_t parity, volatile Limit* limit, unsigned long long* failures)
 {
-    return __all_sync(0xFFFFFFFFu, bar_wait(bar, parity, limit, failures));
+    return __all_sync(0xFFFFFFFFu, bar_wait<CLUSTER>(bar, parity, limit, failures));
 }
+template <bool CLUSTER = false>
 __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile Limit* limit, unsigned long long* failures)
 {
-    if (__all_sync(0xFFFFFFFFu, bar_try(bar, parity))) return true;
-    return warp_wait_long(bar, parity, limit, failures);
+    if (__all_sync(0xFFFFFFFFu, bar_try<CLUSTER>(bar, parity))) return true;
+    return warp_wait_long<CLUSTER>(bar, parity, limit, failures);
 }
 __device__ __forceinline__ bool elect()
 {

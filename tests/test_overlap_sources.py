@@ -36,3 +36,16 @@ def test_no_non_coherent_load(source):
     for name in sorted(_reached(source, set())):
         found = NON_COHERENT.search(_text(name))
         assert not found, f"{source} reaches {name}: {found.group(0)}"
+
+
+# Ordinary shared memory that passes between CTAs of a cluster: the sums that few rows' CTAs exchange (written by the others, read
+# here, written again), and the rows that wgrad clears before the other CTA issues the products.
+CLUSTER_SCOPE = [("linear_small.cu", r"bar_wait<true>\([^;]*sums_empty", 1), ("linear_small.cu", r"bar_wait<true>\([^;]*sums_full", 1),
+                 ("linear_small.cu", r"bar_arrive_cluster\([^;]*sums_empty[^;]*, true\)", 1),
+                 ("linear_tc.cu", r"bar_arrive_cluster\(full[^;]*, valid < 64\)", 1), ("linear_tc.cu", r"warp_wait<OP == kWgrad>\(full", 1),
+                 ("tc_ptx.cuh", r"mbarrier\.arrive\.release\.cluster", 1), ("tc_ptx.cuh", r"mbarrier\.try_wait\.parity\.acquire\.cluster", 1)]
+
+
+@pytest.mark.parametrize("name,form,times", CLUSTER_SCOPE)
+def test_memory_handed_to_another_cta_is_released_and_acquired_at_cluster_scope(name, form, times):
+    assert len(re.findall(form, _text(name))) == times
