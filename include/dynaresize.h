@@ -595,7 +595,8 @@ int dr_linear_destroy(dr_linear* lin); /* NULL is accepted; launches already enq
  * dr_linear_wgrad -- dW_e[n, k] = sum over rows r of group e of dy[r, n] x[r, k], fp32, laid out as the weight
  *               ([n_groups * out_features] rows of lddw floats: the positions of the same tensor in the arena of a DR_F32
  *               plan, from where dr_reshard_inverse takes it to the flat gradient buffer).  accumulate = 0: dW is written,
- *               zeros for a group without rows; 1: the sum is added to it.  bf16 layers only.
+ *               zeros for a group without rows; 1: the sum is added to it (one fp32 addition, rounded to nearest, subnormals kept).
+ *               bf16 layers only.
  * Rows of other groups never enter a sum, whatever they hold (infinities and NaNs included).  Sums are taken in a fixed order:
  * the same call gives the same bits.  The calls only enqueue kernels on cuda_stream, allocate nothing, read no
  * device value on the host, and leave the handle unmodified: concurrent calls on different streams are allowed, and
