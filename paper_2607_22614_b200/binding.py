@@ -719,6 +719,17 @@ def _stream_of(t, stream):
     return _raw_stream(t.get_device())
 
 
+def _outside_autograd(*tensors):
+    """Raises where autograd would be expected to follow: the kernels write through raw pointers, and the result would come back
+    without a graph, as if nothing depended on it."""
+    for t in tensors:
+        if t.requires_grad:
+            import torch
+            if torch.is_grad_enabled():
+                raise RuntimeError("an operand requires a gradient, which this call does not record: make it under torch.no_grad() or on "
+                                   "detached tensors, and take the gradients with Linear.dgrad and Linear.wgrad")
+
+
 def _empty(rows, cols, dtype, device, stream):
     """An output of the call, from the memory of the stream that the call runs on: a block of the current stream's memory may
     still be used by work queued there, which `stream` does not wait for."""
@@ -735,11 +746,12 @@ def quant_rows(x, codes=None, scales=None, *, row_index=None, swiglu=False, stre
     """dr_quant_rows: x [source rows, cols] (2 * cols with swiglu: gate, then up; bf16 or fp32) -> (codes [rows, cols],
     scales [ceil(cols / 128), rows]).  row_index (int64) gathers rows.  Outputs that are not given are allocated.  All
     operands live on the current GPU.  `stream` (default: the current one) is where the call runs and where its allocated
-    outputs belong; the caller orders the operands that other streams write, as with any torch call under that stream."""
+    outputs belong; the caller orders the operands that other streams write, as with any torch call under that stream.  Not recorded by autograd (an x that requires a gradient is refused)."""
     src_rows, width, ldx = _matrix(x, "x")
     device = x.get_device()
     _on_current_device(device, "x")
     _same_device(device, row_index, codes, scales)
+    _outside_autograd(x)
     cols = width // 2 if swiglu else width
     if swiglu and width % 2:
         raise ValueError("x holds gate and up side by side: its column count must be even")
@@ -839,9 +851,11 @@ class Linear:
 
     def forward(self, x, x_scale=None, offsets=None, out=None, out_dtype=None, stream=None):
         """dr_linear_forward: y = x W^T, for rows sorted by group where `offsets` (n_groups + 1, int32) is given.  An fp8
-        layer takes quant_rows' codes and scales.  Rows of an allocated output that no group owns are not initialised."""
+        layer takes quant_rows' codes and scales.  Rows of an allocated output that no group owns are not initialised.  Not
+        recorded by autograd: operands that require a gradient are refused while gradients are enabled."""
         rows, ldx = self._operand(x, self.in_features, "x", self.fp8)
         _same_device(self.device, x, x_scale, offsets, out)
+        _outside_autograd(x, self.weight)
         y, ldy = self._out(out, rows, self.out_features, out_dtype, x, stream)
         ps, lds = None, 0
         if x_scale is not None:

@@ -185,3 +185,23 @@ def test_codes_may_be_bytes(calls):
     codes, scales = dr.quant_rows(Stand(5, 256), Stand(5, 256, dtype=torch.uint8), Stand(2, 5, dtype=F32))
     layer.forward(codes, scales, out=Stand(5, 128))
     assert layer.fp8 and [c[0] for c in calls] == ["dr_linear_create", "dr_quant_rows", "dr_linear_forward"]
+
+
+def test_a_product_that_autograd_would_follow_is_refused(calls):
+    layer, off = _layer(), Stand(3, dtype=I32)
+    x, trained = Stand(5, 256, requires_grad=True), dr.Linear(Stand(256, 256, requires_grad=True), n_groups=2)
+    del calls[:]
+    with pytest.raises(RuntimeError, match="no_grad"):
+        layer.forward(x, None, off, out=Stand(5, 128))
+    with pytest.raises(RuntimeError, match="no_grad"):
+        trained(Stand(5, 256), None, off, out=Stand(5, 128))
+    with pytest.raises(RuntimeError, match="no_grad"):
+        dr.quant_rows(x, Stand(5, 256, dtype=E4M3), Stand(2, 5, dtype=F32))
+    assert not calls
+    with torch.no_grad():
+        layer.forward(x, None, off, out=Stand(5, 128))
+        trained(x, None, off, out=Stand(5, 128))
+        dr.quant_rows(x, Stand(5, 256, dtype=E4M3), Stand(2, 5, dtype=F32))
+    layer.wgrad(x, Stand(5, 128, requires_grad=True), off, out=Stand(256, 256, dtype=F32))  # (gradients are what is asked for)
+    layer.dgrad(Stand(5, 128, requires_grad=True), off, out=Stand(5, 256))
+    assert len(calls) == 5
