@@ -101,11 +101,12 @@ struct TcArgs {
 
 template <int OP, bool FP8>
 struct Walk {
+    static_assert(FP8 == (OP == kForwardRows), "fp8 has its tokens on the M side");
     static constexpr uint32_t kStep = FP8 ? 128 : 64;
     uint32_t e = 0;
 
     // Tile t of all, ascending t; false past the last.  A tile without features (fp8 groups that are not whole scale blocks
-    // have one tile fewer here and there) comes back with nt = 0.
+    // have one tile fewer here and there) or without rows comes back with nt = 0.
     __device__ __forceinline__ bool get(const TcArgs& a, const Barriers& s, uint32_t t, Tile& o)
     {
         if constexpr (OP == kWgrad) {
@@ -145,15 +146,8 @@ struct Walk {
             o.nt = ((hi - lo + tiles - 1) / tiles + 31) / 32 * 32;
             o.row0 = lo + m * o.nt;
             o.row_end = min(hi, o.row0 + o.nt);
-            if (OP == kForward) {
-                const uint32_t first = e * a.n;
-                o.feature = (FP8 ? first / 128 * 128 : first) + f * kTile;
-                o.steps = (a.k + kStep - 1) / kStep;
-                if (o.feature >= first + a.n) o.nt = 0;
-            } else {
-                o.feature = f * kTile;
-                o.steps = (a.n + kStep - 1) / kStep;
-            }
+            o.feature = (OP == kForward ? e * a.n : 0) + f * kTile;
+            o.steps = ((OP == kForward ? a.k : a.n) + kStep - 1) / kStep;
             if (o.row0 >= o.row_end) o.nt = 0;  // 32-row steps can leave a last tile without rows
             return true;
         }
@@ -161,7 +155,8 @@ struct Walk {
 };
 
 // Eight tokens (columns c .. c + 7 of the tile) of the warp's 32 features: v[g][i] = token 2 (t % 4) + i of feature t / 4 + 8 g.
-// `f` is the warp's first feature among the outputs of a row of c, valid from f_lo to f_hi.
+// `f` is the warp's first feature among the outputs of a row of c, of which there are f_hi (a tile's last features may lie past
+// 2^31, as negative numbers).
 __device__ __forceinline__ void store_tokens(const TcArgs& a, uint32_t scratch, uint32_t row, uint32_t row_end, int f, int f_hi,
                                              const float (&v)[4][2])
 {
