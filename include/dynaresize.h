@@ -544,7 +544,7 @@ int dr_shard_range(uint64_t flat_elems, uint32_t world, uint32_t rank, uint64_t*
  *               the scales of one column block lie side by side, as dr_linear_forward reads them)
  * Asynchronous on cuda_stream, allocates nothing, may be captured.  rows = 0 does nothing.
  * Errors (before launch): DR_ERR_INVALID (NULL, no columns, a leading dimension below its row, above 2^40 or
- * beyond 2^60 elements over all rows, too few source rows), DR_ERR_UNSUPPORTED (x_dtype, form, dimension above 2^31 - 1),
+ * beyond 2^60 elements over all rows, too few source rows), DR_ERR_UNSUPPORTED (x_dtype, form, 2^31 rows, 2^30 columns),
  * DR_ERR_ALIGN (a pointer off its element size), DR_ERR_CUDA.  16-byte aligned bases and rows take the vector path,
  * others an element-wise one, same result.
  */
@@ -574,7 +574,7 @@ typedef struct dr_linear dr_linear;
 
 /* Checks the descriptor and records it for the current device.  Errors: DR_ERR_INVALID (a leading
  * dimension below its row, above 2^40 or beyond 2^60 elements over all rows among them), DR_ERR_UNSUPPORTED
- * (dtype; a dimension above 2^31 - 1), DR_ERR_SIZE (weight_bytes / scale_bytes too small), DR_ERR_ALIGN (a
+ * (dtype; features in all groups together above 2^31 - 512), DR_ERR_SIZE (weight_bytes / scale_bytes too small), DR_ERR_ALIGN (a
  * pointer off its element size), DR_ERR_NOMEM, DR_ERR_CUDA. */
 int dr_linear_create(const dr_linear_desc* desc, dr_linear** out);
 int dr_linear_destroy(dr_linear* lin); /* NULL is accepted; launches already enqueued may still run */
@@ -603,7 +603,7 @@ int dr_linear_destroy(dr_linear* lin); /* NULL is accepted; launches already enq
  * (after one ordinary call has loaded the module) they may be captured into a CUDA graph.  rows = 0 does
  * nothing (dr_linear_wgrad without accumulate: writes zeros).
  * Errors (before launch): DR_ERR_INVALID (NULL, a leading dimension out of the range that dr_linear_create takes, missing offsets or
- * scales, scales for a bf16 layer), DR_ERR_UNSUPPORTED (dtype, fp8 gradients, dimensions above 2^31 - 1), DR_ERR_ALIGN (a
+ * scales, scales for a bf16 layer), DR_ERR_UNSUPPORTED (dtype, fp8 gradients, more than 2^31 - 1 rows), DR_ERR_ALIGN (a
  * pointer off its element size), DR_ERR_STATE (another current device), DR_ERR_CUDA.
  */
 int dr_linear_forward(const dr_linear* lin, const void* x_dev, uint64_t ldx, const float* x_scale_dev, uint64_t ld_scale,

@@ -10,7 +10,8 @@ using namespace dr;
 
 namespace {
 
-constexpr uint64_t kMaxDim = 0x7FFFFFFFull;
+constexpr uint64_t kMaxRows = 0x7FFFFFFFull;
+constexpr uint64_t kMaxFeatures = 0x7FFFFFFFull - 511;  // the kernels count features in int, up to two tiles past the last
 
 // A role may wait for a whole tile (bf16 accumulators are handed over at its end), and a contraction may have up to 2^25 steps: at 0.2 to
 // 0.4 us each that is 10 s, so the limit grows with them.
@@ -36,7 +37,7 @@ int check_layer(const dr_linear* lin)
 int check_rows(const dr_linear* lin, uint64_t rows, const int32_t* offsets, const void* p, uint64_t ldp, uint64_t p_cols,
                uint32_t p_es, const void* q, uint64_t ldq, uint64_t q_cols, uint32_t q_es)
 {
-    if (rows > kMaxDim) {
+    if (rows > kMaxRows) {
         set_error("more than 2^31 - 1 rows");
         return DR_ERR_UNSUPPORTED;
     }
@@ -148,8 +149,8 @@ int dr_linear_create(const dr_linear_desc* desc, dr_linear** out)
         set_error("zero layer dimension");
         return DR_ERR_INVALID;
     }
-    if (d.out_features > kMaxDim || d.in_features > kMaxDim || d.n_groups > kMaxDim || d.out_features * d.n_groups > kMaxDim) {
-        set_error("layer dimension above 2^31 - 1");
+    if (d.out_features > kMaxFeatures || d.in_features > kMaxFeatures || d.n_groups > kMaxFeatures || d.out_features * d.n_groups > kMaxFeatures) {
+        set_error("layer dimension above 2^31 - 512");
         return DR_ERR_UNSUPPORTED;
     }
     const uint64_t rows = d.out_features * d.n_groups, sr = (rows + 127) / 128, sc = (d.in_features + 127) / 128;

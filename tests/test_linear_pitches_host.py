@@ -41,3 +41,13 @@ def test_quant_rows_refuses_what_wraps(kw, status):
     a.update(kw)
     assert dr.dr_quant_rows(*a.values(), None) == status
 
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(out_features=(1 << 31) - 511), B.DR_ERR_UNSUPPORTED), (dict(in_features=(1 << 31) - 511), B.DR_ERR_UNSUPPORTED),
+    (dict(n_groups=(1 << 31) - 511, out_features=1), B.DR_ERR_UNSUPPORTED), (dict(n_groups=2, out_features=(1 << 30) - 255), B.DR_ERR_UNSUPPORTED),
+    (dict(out_features=(1 << 31) - 512), B.DR_ERR_SIZE), (dict(in_features=(1 << 31) - 512), B.DR_ERR_SIZE),
+    (dict(n_groups=2, out_features=(1 << 30) - 256), B.DR_ERR_SIZE)])
+def test_features_leave_room_for_the_last_tiles(kw, status):
+    """The kernels' tiles end up to two tiles past the last feature, which they count in int."""
+    assert _create(**kw, weight_bytes=64) == status
