@@ -74,6 +74,18 @@ __device__ __forceinline__ uint64_t fma_two(uint64_t a, uint64_t b, uint64_t c)
     asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
     return d;
 }
+__device__ __forceinline__ uint64_t mul_two(uint64_t a, uint64_t b)
+{
+    uint64_t d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+__device__ __forceinline__ uint64_t add_two(uint64_t a, uint64_t b)
+{
+    uint64_t d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
 template <bool PACKED>
 __device__ __forceinline__ uint2 quantise8_corrected(const float* minus_x, float scale, float recip)
 {
@@ -91,8 +103,7 @@ __device__ __forceinline__ uint2 quantise8_corrected(const float* minus_x, float
 #pragma unroll
         for (int k = 0; k < 8; k += 2) {
             const uint64_t nx = two_of(minus_x[k], minus_x[k + 1]);
-            uint64_t q;
-            asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(q) : "l"(nx), "l"(minus_r));
+            uint64_t q = mul_two(nx, minus_r);
             q = fma_two(fma_two(q, s, nx), minus_r, q);
             q = fma_two(fma_two(q, s, nx), minus_r, q);
             asm("mov.b64 {%0, %1}, %2;" : "=f"(t[k]), "=f"(t[k + 1]) : "l"(q));

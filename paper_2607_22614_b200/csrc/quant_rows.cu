@@ -9,7 +9,7 @@
 // over sixteen values.  A CTA covers 8 * RPW rows of 512 columns: a warp starts the loads of its RPW rows before it reduces any
 // of them, and the scales of a column block, side by side in memory, leave as one contiguous store per CTA instead
 // of one 4-byte store per row.  The exact division is quantise8_corrected's.
-// Measured, 8192 x 12288: from bf16 55 us = 5.5 TB/s, from fp32 73 us = 6.9 TB/s, through SwiGLU from bf16 107 us = 4.7 TB/s: there
+// Measured, 8192 x 12288, twenty calls in a graph: from bf16 54 us = 5.6 TB/s, from fp32 73 us = 6.9 TB/s, through SwiGLU from bf16 107 us = 4.7 TB/s: there
 // the arithmetic (an exponential, a reciprocal and some twenty more instructions a value; 81 % of the issue slots) bounds.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
@@ -34,12 +34,23 @@ struct RowsArgs {
     uint32_t rows, cols, col_tiles;  // col_tiles = ceil(cols / 512)
 };
 
-// silu(g) * u in fp32.  With e = e^-|g| the sigmoid is 1 / (1 + e) or e / (1 + e): the divisor stays in [1, 2], where the
-// approximate division is good to 2 ulp and nothing overflows, however large |g| is.
-__device__ __forceinline__ float swiglu(float g, float u)
+// -silu(g) * u of two values, in fp32.  With e = e^-|g| the sigmoid is h / (1 + e), h = 1 or e: the divisor stays in [1, 2], and nothing
+// overflows, however large |g| is.  From s = h * fl(1 / (1 + e)), the remainder h - s (1 + e) comes out with one rounding
+// as (h - s) - s e, where h - s is exact (s lies between h / 2 and h), and adding it back corrects s: what is left is the error
+// of e, of one rounding of the sigmoid and of two products (0.83 units of 2^-24 rms over normal values; 1.02 with the uncorrected quotient, 0.87
+// for g / (1 + exp(-g)) * u with a division rounded to nearest).  Signs are turned over by the reciprocal, so that quantise8_corrected's
+// negated values cost nothing.
+__device__ __forceinline__ void swiglu(float g0, float g1, float u0, float u1, float& v0, float& v1)
 {
-    const float e = expf(-fabsf(g));
-    return __fdividef(g >= 0.0f ? g : g * e, 1.0f + e) * u;
+    const float e0 = expf(-fabsf(g0)), e1 = expf(-fabsf(g1));
+    float r0, r1;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r0) : "f"(-1.0f - e0));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r1) : "f"(-1.0f - e1));
+    const uint64_t h = two_of(g0 >= 0.0f ? 1.0f : e0, g1 >= 0.0f ? 1.0f : e1), r = two_of(r0, r1);
+    uint64_t s = mul_two(h, r);
+    s = fma_two(fma_two(s, two_of(e0, e1), add_two(h, s)), r, s);
+    s = mul_two(mul_two(two_of(g0, g1), s), two_of(u0, u1));
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(v0), "=f"(v1) : "l"(s));
 }
 
 // m / 448 rounded to nearest, by one step of Markstein's correction: q = m * fl(1 / 448) is within an ulp, the remainder m - 448 q
@@ -132,16 +143,19 @@ __global__ void __launch_bounds__(32 * kWarps, SWIGLU ? 4 : 3) rows_kernel(const
         const uint64_t r = row0 + lr;
         // v holds the negated values, as quantise8_corrected wants them: turned over two at a time where they come from bf16
         float v[16], m = 0.0f;
-        if (!F32) {
+        if (!F32 && !SWIGLU) {
 #pragma unroll
-            for (int k = 0; k < kRaw; ++k) (SWIGLU ? up[i] : x[i])[k] ^= 0x80008000u;
+            for (int k = 0; k < kRaw; ++k) x[i][k] ^= 0x80008000u;
         }
 #pragma unroll
-        for (int k = 0; k < 16; ++k) {
-            v[k] = value<F32>(x[i], k);
-            if (SWIGLU) v[k] = swiglu(v[k], value<F32>(up[i], k));
-            if (F32) v[k] = -v[k];
-            m = fmaxf(m, fabsf(v[k]));  // fmaxf drops NaN operands
+        for (int k = 0; k < 16; k += 2) {
+            if (SWIGLU) {
+                swiglu(value<F32>(x[i], k), value<F32>(x[i], k + 1), value<F32>(up[i], k), value<F32>(up[i], k + 1), v[k], v[k + 1]);
+            } else {
+                v[k] = F32 ? -value<F32>(x[i], k) : value<F32>(x[i], k);
+                v[k + 1] = F32 ? -value<F32>(x[i], k + 1) : value<F32>(x[i], k + 1);
+            }
+            m = fmaxf(m, fmaxf(fabsf(v[k]), fabsf(v[k + 1])));  // fmaxf drops NaN operands
         }
 #pragma unroll
         for (int o = 4; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
