@@ -636,10 +636,17 @@ class Plan:
         return StageJob(job, desc)
 
 
-def _matrix(t, what):
-    """(rows, columns, elements between rows) of a CUDA matrix with contiguous rows."""
-    if t.dim() != 2 or not t.is_cuda:
+def _elsewhere(t, what, device):
+    """The error for an operand that does not live on GPU `device`: a kernel of one GPU must not get another's addresses."""
+    return ValueError(f"{what} must be on GPU {device}, not on " + (f"GPU {t.get_device()}" if t.is_cuda else "the CPU"))
+
+
+def _matrix(t, what, device):
+    """(rows, columns, elements between rows) of a matrix with contiguous rows on GPU `device`."""
+    if t.dim() != 2:
         raise ValueError(f"{what} must be a CUDA matrix")
+    if t.get_device() != device:
+        raise _elsewhere(t, what, device)
     rows, cols = t.shape
     ld, step = t.stride()
     if step != 1 and cols > 1:
@@ -684,30 +691,25 @@ def _fn(name):
     return f
 
 
-_current_device = None
-
-
-def _same_device(device, *operands):
-    """Raises unless every operand that is given lives on GPU `device`: a kernel of one GPU must not get another's addresses."""
-    for t in operands:
-        if t is not None and t.get_device() != device:
-            raise ValueError(f"an operand is on GPU {t.get_device()}, the others are on GPU {device}")
-
-
-def _on_current_device(device, what):
+def _current_device():
+    """Index of the current GPU (from its second call on, torch's own accessor)."""
     global _current_device
-    if _current_device is None:
-        import torch
-        _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
-    if device != _current_device():
-        raise ValueError(f"{what} is on GPU {device}, which is not the current one: call under torch.cuda.device({device})")
+    import torch
+    _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+    return torch.cuda.current_device()
+
+
+def _not_current(t, what):
+    if not t.is_cuda:
+        return ValueError(f"{what} must be a CUDA matrix")
+    return ValueError(f"{what} is on GPU {t.get_device()}, which is not the current one: call under torch.cuda.device")
 
 
 _raw_stream = None
 
 
-def _stream_of(t, stream):
-    """The handle of `stream`, or of the stream that is current on t's device (torch's own accessor of the raw handle: building
+def _stream_of(device, stream):
+    """The handle of `stream`, or of the stream that is current on GPU `device` (torch's own accessor of the raw handle: building
     a Stream object for it takes 3 us, more than the launch)."""
     global _raw_stream
     if stream is not None:
@@ -716,18 +718,16 @@ def _stream_of(t, stream):
         import torch
         _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
             (lambda index: torch.cuda.current_stream(index).cuda_stream)
-    return _raw_stream(t.get_device())
+    return _raw_stream(device)
 
 
-def _outside_autograd(*tensors):
-    """Raises where autograd would be expected to follow: the kernels write through raw pointers, and the result would come back
-    without a graph, as if nothing depended on it."""
-    for t in tensors:
-        if t.requires_grad:
-            import torch
-            if torch.is_grad_enabled():
-                raise RuntimeError("an operand requires a gradient, which this call does not record: make it under torch.no_grad() or on "
-                                   "detached tensors, and take the gradients with Linear.dgrad and Linear.wgrad")
+def _refuse_autograd(what):
+    """Raises while gradients are enabled: the kernels write through raw pointers, and the result would come back without a
+    graph, as if nothing depended on `what`, which requires a gradient."""
+    import torch
+    if torch.is_grad_enabled():
+        raise RuntimeError(f"{what} requires a gradient, which this call does not record: make it under torch.no_grad() or on detached "
+                           "tensors, and take the gradients with Linear.dgrad and Linear.wgrad")
 
 
 def _empty(rows, cols, dtype, device, stream):
@@ -747,11 +747,12 @@ def quant_rows(x, codes=None, scales=None, *, row_index=None, swiglu=False, stre
     scales [ceil(cols / 128), rows]).  row_index (int64) gathers rows.  Outputs that are not given are allocated.  All
     operands live on the current GPU.  `stream` (default: the current one) is where the call runs and where its allocated
     outputs belong; the caller orders the operands that other streams write, as with any torch call under that stream.  Not recorded by autograd (an x that requires a gradient is refused)."""
-    src_rows, width, ldx = _matrix(x, "x")
     device = x.get_device()
-    _on_current_device(device, "x")
-    _same_device(device, row_index, codes, scales)
-    _outside_autograd(x)
+    if device < 0 or device != _current_device():
+        raise _not_current(x, "x")
+    src_rows, width, ldx = _matrix(x, "x", device)
+    if x.requires_grad:
+        _refuse_autograd("x")
     cols = width // 2 if swiglu else width
     if swiglu and width % 2:
         raise ValueError("x holds gate and up side by side: its column count must be even")
@@ -760,6 +761,8 @@ def quant_rows(x, codes=None, scales=None, *, row_index=None, swiglu=False, stre
         import torch
         if row_index.dtype != torch.int64 or row_index.dim() != 1 or not row_index.is_cuda or not row_index.is_contiguous():
             raise ValueError("row_index must be a contiguous int64 CUDA vector")
+        if row_index.get_device() != device:
+            raise _elsewhere(row_index, "row_index", device)
         rows, index = row_index.shape[0], row_index.data_ptr()
     blocks = -(-cols // 128)
     if codes is None or scales is None:
@@ -768,14 +771,14 @@ def quant_rows(x, codes=None, scales=None, *, row_index=None, swiglu=False, stre
             codes = _empty(rows, cols, torch.float8_e4m3fn, x.device, stream)
         if scales is None:
             scales = _empty(blocks, rows, torch.float32, x.device, stream)
-    got_rows, got_cols, ld_codes = _matrix(codes, "codes")
+    got_rows, got_cols, ld_codes = _matrix(codes, "codes", device)
     if got_rows != rows or got_cols != cols or not _holds_codes(codes):
         raise ValueError(f"codes must be {rows} x {cols} of float8_e4m3fn or uint8")
-    got_blocks, got_rows, ld_scales = _matrix(scales, "scales")
+    got_blocks, got_rows, ld_scales = _matrix(scales, "scales", device)
     if got_rows != rows or got_blocks != blocks or _code_of(scales, "scales") != DR_F32:
         raise ValueError(f"scales must be fp32, {blocks} x {rows}")
     rc = _fn("dr_quant_rows")(x.data_ptr(), _code_of(x, "x"), ldx, src_rows, index, DR_ROWS_SWIGLU if swiglu else DR_ROWS_PLAIN,
-                              rows, cols, codes.data_ptr(), ld_codes, scales.data_ptr(), ld_scales, _stream_of(x, stream))
+                              rows, cols, codes.data_ptr(), ld_codes, scales.data_ptr(), ld_scales, _stream_of(device, stream))
     if rc:
         raise DrError(rc, "dr_quant_rows")
     return codes, scales
@@ -788,7 +791,10 @@ class Linear:
 
     def __init__(self, weight, scale=None, n_groups=1):
         import torch
-        rows, cols, ld = _matrix(weight, "weight")
+        self.device = weight.get_device()
+        if self.device < 0 or self.device != _current_device():
+            raise _not_current(weight, "weight")
+        rows, cols, ld = _matrix(weight, "weight", self.device)
         fp8 = _holds_codes(weight)
         if not fp8 and weight.dtype != torch.bfloat16:
             raise TypeError(f"weight must be bfloat16 or e4m3 codes (float8_e4m3fn or uint8), not {weight.dtype}")
@@ -796,12 +802,9 @@ class Linear:
             raise ValueError("n_groups must divide the weight's rows")
         scale_rows = scale_cols = scale_ld = 0
         if scale is not None:
-            scale_rows, scale_cols, scale_ld = _matrix(scale, "scale")
+            scale_rows, scale_cols, scale_ld = _matrix(scale, "scale", self.device)
             if scale.dtype != torch.float32 or scale_rows != -(-rows // 128) or scale_cols != -(-cols // 128):
                 raise ValueError("scale must be fp32 with one value for each 128 x 128 block of the weight")
-        self.device = weight.get_device()
-        _on_current_device(self.device, "weight")
-        _same_device(self.device, scale)
         self.weight, self.scale, self.n_groups, self.fp8 = weight, scale, n_groups, fp8
         self.out_features, self.in_features = rows // n_groups, cols
         desc = dr_linear_desc(struct_size=C.sizeof(dr_linear_desc), dtype=DR_FP8_E4M3_B128 if fp8 else DR_BF16,
@@ -825,7 +828,7 @@ class Linear:
             self.close()
 
     def _operand(self, t, cols, what, fp8=False):
-        rows, got, ld = _matrix(t, what)
+        rows, got, ld = _matrix(t, what, self.device)
         if got != cols:
             raise ValueError(f"{what} must have {cols} columns")
         if not _holds_codes(t) if fp8 else _code_of(t, what) != DR_BF16:
@@ -838,13 +841,15 @@ class Linear:
         import torch
         if offsets.dtype != torch.int32 or offsets.numel() != self.n_groups + 1 or not offsets.is_cuda or not offsets.is_contiguous():
             raise ValueError(f"offsets must be {self.n_groups + 1} int32 on the GPU")
+        if offsets.get_device() != self.device:
+            raise _elsewhere(offsets, "offsets", self.device)
         return offsets.data_ptr()
 
     def _out(self, out, rows, cols, dtype, like, stream):
         if out is None:
             import torch
             return _empty(rows, cols, dtype or torch.bfloat16, like.device, stream), cols
-        got_rows, got_cols, ld = _matrix(out, "out")
+        got_rows, got_cols, ld = _matrix(out, "out", self.device)
         if got_rows != rows or got_cols != cols:
             raise ValueError(f"out must be {rows} x {cols}")
         return out, ld
@@ -854,17 +859,17 @@ class Linear:
         layer takes quant_rows' codes and scales.  Rows of an allocated output that no group owns are not initialised.  Not
         recorded by autograd: operands that require a gradient are refused while gradients are enabled."""
         rows, ldx = self._operand(x, self.in_features, "x", self.fp8)
-        _same_device(self.device, x, x_scale, offsets, out)
-        _outside_autograd(x, self.weight)
+        if x.requires_grad or self.weight.requires_grad:
+            _refuse_autograd("x or the weight")
         y, ldy = self._out(out, rows, self.out_features, out_dtype, x, stream)
         ps, lds = None, 0
         if x_scale is not None:
-            blocks, cols, lds = _matrix(x_scale, "x_scale")
+            blocks, cols, lds = _matrix(x_scale, "x_scale", self.device)
             if blocks != -(-self.in_features // 128) or cols < rows or _code_of(x_scale, "x_scale") != DR_F32:
                 raise ValueError("x_scale must be fp32, one row for each block of 128 columns, one column for each row of x")
             ps = x_scale.data_ptr()
         rc = _fn("dr_linear_forward")(self.handle, x.data_ptr(), ldx, ps, lds, rows, self._offsets(offsets), y.data_ptr(), ldy,
-                                      _code_of(y, "out"), _stream_of(x, stream))
+                                      _code_of(y, "out"), _stream_of(self.device, stream))
         if rc:
             raise DrError(rc, "dr_linear_forward")
         return y
@@ -874,10 +879,9 @@ class Linear:
     def dgrad(self, dy, offsets=None, out=None, out_dtype=None, stream=None):
         """dr_linear_dgrad: the gradient of x, dy W."""
         rows, lddy = self._operand(dy, self.out_features, "dy")
-        _same_device(self.device, dy, offsets, out)
         dx, lddx = self._out(out, rows, self.in_features, out_dtype, dy, stream)
         rc = _fn("dr_linear_dgrad")(self.handle, dy.data_ptr(), lddy, rows, self._offsets(offsets), dx.data_ptr(), lddx,
-                                    _code_of(dx, "out"), _stream_of(dy, stream))
+                                    _code_of(dx, "out"), _stream_of(self.device, stream))
         if rc:
             raise DrError(rc, "dr_linear_dgrad")
         return dx
@@ -888,7 +892,6 @@ class Linear:
         dy_rows, lddy = self._operand(dy, self.out_features, "dy")
         if rows != dy_rows:
             raise ValueError("x and dy must have the same rows")
-        _same_device(self.device, x, dy, offsets, out)
         if accumulate and out is None:
             raise ValueError("accumulate adds to `out`: give one")
         import torch
@@ -896,7 +899,7 @@ class Linear:
         if _code_of(dw, "out") != DR_F32:
             raise TypeError("the gradient of the weight is fp32")
         rc = _fn("dr_linear_wgrad")(self.handle, x.data_ptr(), ldx, dy.data_ptr(), lddy, rows, self._offsets(offsets),
-                                    dw.data_ptr(), lddw, int(accumulate), _stream_of(x, stream))
+                                    dw.data_ptr(), lddw, int(accumulate), _stream_of(self.device, stream))
         if rc:
             raise DrError(rc, "dr_linear_wgrad")
         return dw
