@@ -61,7 +61,7 @@ __device__ __forceinline__ uint2 quantise8(const float* x, float scale, float re
 // scales in [2^-100, 2^126], where neither the remainders that can matter (|t| >= 2^-11) nor the reciprocal leave the normal range.
 // The caller gives -x, so that the remainder x - t scale comes out negated without another instruction and a zero keeps its
 // sign.  PACKED takes two values an instruction: 3 % less time from bf16, where instructions bound (8192 x 12288: 54.8 against
-// 56.1 us, through SwiGLU 107 against 110), 12 % more from fp32, where the memory does (81.6 against 72.8).
+// 56.1 us), 12 % more from fp32, where the memory does (81.6 against 72.8).
 __device__ __forceinline__ uint64_t two_of(float lo, float hi)
 {
     uint64_t d;

@@ -101,8 +101,9 @@ int check_gradient(const dr_linear* lin)
 }
 
 // Up to this many rows a group (on average) the kernel that reads weights 128 features at a time wins over pairs of CTAs: in us,
-// pairs second, fp8 1 x 6144 x 4096 8.1 / 17.0, 64 x 6144 x 4096 10.1 / 17.5; 128 groups of 1536 x 2048, 32 rows each 71 / 100, bf16 48 rows
-// each 133 / 134.  Beyond 64 rows it reads the weights more than once: 128 x 24576 x 4096 fp8 41 / 35.
+// pairs second, fp8 1 x 6144 x 4096 8.4 / 17.0, 64 x 6144 x 4096 10.5 / 17.5; 128 groups of 1536 x 2048, 32 rows each 71 / 100, bf16 48 rows
+// each 133 / 134.  Beyond 64 rows it reads the weights more than once: 128 x 24576 x 4096 fp8 41 / 35.  All of equal groups: the
+// offsets are on the device, so a skewed batch goes by its average as well.
 constexpr uint64_t kSmallRows = 64;
 
 int launch(const LinearCall& c)

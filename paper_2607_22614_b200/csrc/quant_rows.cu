@@ -9,8 +9,9 @@
 // over sixteen values.  A CTA covers 8 * RPW rows of 512 columns: a warp starts the loads of its RPW rows before it reduces any
 // of them, and the scales of a column block, side by side in memory, leave as one contiguous store per CTA instead
 // of one 4-byte store per row.  The exact division is quantise8_corrected's.
-// Measured, 8192 x 12288, twenty calls in a graph: from bf16 54 us = 5.6 TB/s, from fp32 73 us = 6.9 TB/s, through SwiGLU from bf16 107 us = 4.7 TB/s: there
-// the arithmetic (an exponential, a reciprocal and some twenty more instructions a value; 81 % of the issue slots) bounds.
+// Measured, 8192 x 12288, calls in a graph: from bf16 54 us = 5.6 TB/s, from fp32 73 us = 6.9 TB/s, through SwiGLU from bf16 105 us =
+// 4.8 TB/s: there the arithmetic (an exponential, a reciprocal and their corrections, two values an instruction where that
+// exists) bounds.  32768 rows of 2048 gathered from 4096: 34 us, 101 MB of reads that L2 serves and 67 MB of codes.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
@@ -22,7 +23,7 @@ namespace dr {
 namespace {
 
 constexpr int kWarps = 8;
-// rows per warp: 128 bytes of raw values a thread (8192 x 12288 through SwiGLU: 2 rows 117 us, 4 rows 131, 1 row 126)
+// rows per warp: 128 bytes of raw values a thread (8192 x 12288 through SwiGLU, when 2 rows took 117 us: 4 rows 131, 1 row 126)
 template <bool F32, bool SWIGLU> constexpr int kManyRows = F32 || SWIGLU ? 2 : 4;
 
 struct RowsArgs {
