@@ -631,6 +631,127 @@ int dr_diag_linear_wait_failures(uint64_t* count);
 int dr_diag_linear_waits(uint32_t limit_us, uint32_t starve);
 
 /*
+ * The attention path of a rollout GPU, between a layer's fused qkv product and its o product: norms and rotation of the query
+ * and key heads, a key and value cache in 8 bits, and attention over it (the paper has no counterpart; its rollout engine has).
+ *
+ * The cache.  n_blocks blocks of block_tokens tokens (16, 32, 64 or 128) for each of kv_heads heads: codes e4m3 at
+ * k and v [n_blocks, kv_heads, block_tokens, head_dim] (64 or 128), contiguous, and one fp32 scale for each block and head at k_scale
+ * and v_scale [n_blocks, kv_heads]; a value is its code times its block's scale.  dr_qk_append writes scales that are
+ * powers of two, the smallest 2^e >= 2^-100 with every finite magnitude of the block within 448 * 2^e: when a later token makes
+ * the scale grow, the codes that the block holds are shifted to it (rounded once more only below 2^-6 of the new scale).
+ * A token with an infinity or a NaN in its key or value of a head is kept as one: the NaN code 0x7F in the first place of its key,
+ * zeros in the places that were not finite; queries that see it get NaN, others nothing of it.  Codes of values that attention
+ * may see hold no NaN code.
+ * Requests find their blocks through a table [requests, width] of block numbers, int32, row r at table + r * ld_table: token t of
+ * request r lies in block table[r][t / block_tokens].  An entry outside [0, n_blocks) stands for a block that is not held.
+ * The handle keeps pointers and owns no memory.  Errors of dr_kv_cache_create: DR_ERR_INVALID (NULL, struct_size, a dimension of
+ * zero), DR_ERR_UNSUPPORTED (block_tokens, head_dim, more than 2^31 - 1 rows of codes), DR_ERR_ALIGN (codes off 16 bytes, scales off
+ * 4), DR_ERR_NOMEM, DR_ERR_CUDA.
+ */
+typedef struct dr_kv_cache_desc {
+    uint32_t struct_size, n_blocks, kv_heads, block_tokens, head_dim, pad;
+    void* k_dev;
+    void* v_dev;
+    float* k_scale_dev;
+    float* v_scale_dev;
+} dr_kv_cache_desc;
+typedef struct dr_kv_cache dr_kv_cache;
+
+int dr_kv_cache_create(const dr_kv_cache_desc* desc, dr_kv_cache** out);
+int dr_kv_cache_destroy(dr_kv_cache* cache); /* NULL is accepted; launches already enqueued may still run */
+
+/*
+ * dr_kv_extend -- block tables and slot maps of one step, from the requests' lengths on the device.
+ *   added     : per request, int32: tokens that arrive (0: none); negative: the request ends, its length becomes 0 and its
+ *               blocks go back to the free list (its row of the table is left as it is)
+ *   lengths   : tokens held before; lengths_out: after (may be the same array)
+ *   free_list : n_blocks int32, of which the first state[0] are the free blocks, taken from the end; state_out[0] = free blocks
+ *               left, state_out[1] = requests refused (state_out may be state).  Blocks that come back are listed before any are taken.
+ * Requests are served in their order.  The rows of the step are the arriving tokens of all requests, one after another:
+ *   offsets   : requests + 1 int32, request r has rows [offsets[r], offsets[r + 1]); held at `rows`, the rows that the step has
+ *   positions : rows int32, each row's position in its request; -1 for rows of refused requests and behind the last request
+ *   runs      : n_runs x 4 int32 {block, first slot in it, first row, rows}: where the new rows go, run by run, in the order of the
+ *               rows; unused entries are {-1, 0, 0, 0}.  n_runs >= min(rows, rows / block_tokens + 2 * requests), or DR_ERR_SIZE.
+ * A request is refused (its length and table stay, its rows get position -1, no run holds them) when the blocks do not suffice
+ * for it and all requests before it, or when its tokens do not fit the table's width or the step's rows.  One launch; nothing is read on
+ * the host, so the step can be captured.  Lengths, counts and states out of range are held inside it.  Arrays other than those
+ * named may not overlap.  Errors: DR_ERR_INVALID, DR_ERR_UNSUPPORTED (2^24 requests, 2^30 rows, 2^24 blocks a
+ * request), DR_ERR_SIZE, DR_ERR_ALIGN (a pointer off 4 bytes, runs off 16), DR_ERR_STATE (another current device), DR_ERR_CUDA.
+ */
+int dr_kv_extend(const dr_kv_cache* cache, const int32_t* added, const int32_t* lengths, int32_t* lengths_out, uint64_t requests,
+                 int32_t* table, uint64_t ld_table, uint64_t width, int32_t* free_list, const int32_t* state, int32_t* state_out,
+                 uint64_t rows, int32_t* offsets, int32_t* positions, int32_t* runs, uint64_t n_runs, void* cuda_stream);
+
+/*
+ * Norms of the query and key heads with the rotation, in one pass.  A row of x is a row of the fused qkv product: n_q_heads query
+ * heads, n_kv_heads key heads, n_kv_heads value heads of head_dim (64 or 128) each.  For query and key heads
+ *   n = x / sqrt(mean(x^2) + eps) * w      (w: q_norm or k_norm; both NULL: n = x)
+ *   y[i] = n[i] cos a - n[i + d/2] sin a,  y[i + d/2] = n[i + d/2] cos a + n[i] sin a,  a = position * base^(-2 i / d), i < d/2
+ * in fp32, angles exact to 2^-32 of a turn at any position.  Rows of negative position are left as they were.
+ * The handle keeps the norms' pointers (norm_dtype DR_BF16 or DR_F32).
+ */
+typedef struct dr_qk_desc {
+    uint32_t struct_size, n_q_heads, n_kv_heads, head_dim, norm_dtype;
+    float eps;
+    double base;
+    const void* q_norm_dev;
+    const void* k_norm_dev;
+} dr_qk_desc;
+typedef struct dr_qk dr_qk;
+
+/* DR_ERR_INVALID (NULL, struct_size, no heads, one norm without the other, eps negative or not finite, base not finite or below 1),
+ * DR_ERR_UNSUPPORTED (head_dim, norm_dtype, more than 2^16 heads), DR_ERR_ALIGN (a norm off its element size), DR_ERR_NOMEM, DR_ERR_CUDA. */
+int dr_qk_create(const dr_qk_desc* desc, dr_qk** out);
+int dr_qk_destroy(dr_qk* qk);
+
+/*
+ * dr_qk_forward -- y [rows, (n_q_heads + n_kv_heads) * head_dim] in x's type (DR_BF16 or DR_F32), one rounding; y may be x
+ *               itself with the same leading dimension.
+ * dr_qk_append -- the same for the query heads alone (y [rows, n_q_heads * head_dim]; may lie in x's query columns); keys, normed and
+ *               rotated, and values go into the cache at the runs of dr_kv_extend, from fp32 to codes in one rounding.  A run is
+ *               skipped where its block, slots or rows lie outside the cache or the step.  Two runs of one call must not share a block.
+ *               Slots before the run's first one keep their values; those behind its last one are left as they were.
+ * dr_qk_grad    -- dy: gradients of dr_qk_forward's y, x its input; dx in the same layout (may be dy itself), and where the
+ *               handle has norms their gradients dq_norm, dk_norm (head_dim fp32 each; accumulate = 1 adds).  The sums are taken in a
+ *               fixed order.  work: dr_qk_grad_work's bytes of device memory that no other call uses meanwhile, 16-byte aligned.
+ * All enqueue on cuda_stream, allocate nothing, read nothing on the host, may be captured.  rows = 0 does nothing (dr_qk_grad without
+ * accumulate: writes zeros).  16-byte aligned bases and rows take vector accesses, others element-wise ones, same result.
+ * Errors (before launch): DR_ERR_INVALID (NULL, leading dimensions as in dr_linear_create, a cache of other heads),
+ * DR_ERR_UNSUPPORTED (dtype, 2^31 rows or runs), DR_ERR_SIZE (work), DR_ERR_ALIGN, DR_ERR_STATE (another current device), DR_ERR_CUDA.
+ */
+int dr_qk_forward(const dr_qk* qk, const void* x_dev, uint32_t dtype, uint64_t ldx, const int32_t* positions_dev, uint64_t rows,
+                  void* y_dev, uint64_t ldy, void* cuda_stream);
+int dr_qk_append(const dr_qk* qk, const void* x_dev, uint32_t dtype, uint64_t ldx, const int32_t* positions_dev, uint64_t rows,
+                 const int32_t* runs_dev, uint64_t n_runs, const dr_kv_cache* cache, void* y_dev, uint64_t ldy, void* cuda_stream);
+int dr_qk_grad_work(const dr_qk* qk, uint64_t* bytes);
+int dr_qk_grad(const dr_qk* qk, const void* x_dev, uint32_t dtype, uint64_t ldx, const int32_t* positions_dev, const void* dy_dev,
+               uint64_t lddy, uint64_t rows, void* dx_dev, uint64_t lddx, float* dq_norm_dev, float* dk_norm_dev, uint32_t accumulate,
+               void* work_dev, uint64_t work_bytes, void* cuda_stream);
+
+/*
+ * dr_attend -- attention of the step's rows over the cache: for row j of request r, n_q_heads heads (head h reads the cache's head
+ * h * kv_heads / n_q_heads), position p = lengths[r] - (rows of r) + j,
+ *   out = sum over visible t of softmax_t(scale * q . k_t) v_t,  t visible: 0 <= t <= p, its block held, and, with window > 0,
+ *         t > p - window or t < sinks.
+ *   q   : bf16, row i at q + i * ldq, heads side by side (the query columns of a qkv row, say); out: bf16 [rows, n_q_heads * head_dim]
+ *   offsets : requests + 1 int32, ascending, as dr_kv_extend gives them; NULL: one row a request (rows = requests)
+ *   lengths : tokens of each request that the cache holds, the step's own among them
+ *   work    : dr_attend_work's bytes of device memory that no other call uses meanwhile, 16-byte aligned
+ * A row that sees nothing gets zeros, one that is not finite NaN.  Rows that no request owns are left as they were.  Lengths beyond the table's width and
+ * offsets beyond the rows are held inside.  Sums are fp32; which tokens are summed together depends on all lengths of the call, in a
+ * fixed order: the same call gives the same bits.
+ * Enqueues on cuda_stream, allocates nothing, reads nothing on the host, may be captured.  The waits inside are bounded as the linear
+ * layers' are, and counted by dr_diag_linear_wait_failures.
+ * Errors: DR_ERR_INVALID (NULL, leading dimensions, n_q_heads no multiple of kv_heads, window below 0, scale not finite),
+ * DR_ERR_UNSUPPORTED (2^30 rows, 2^24 requests, 2^24 blocks a request, 2^31 tokens, more than 64 query heads for a head of the
+ * cache), DR_ERR_SIZE (work), DR_ERR_ALIGN, DR_ERR_STATE, DR_ERR_CUDA.
+ */
+int dr_attend_work(const dr_kv_cache* cache, uint64_t n_q_heads, uint64_t requests, uint64_t rows, uint64_t* bytes);
+int dr_attend(const dr_kv_cache* cache, const void* q_dev, uint64_t ldq, uint64_t n_q_heads, uint64_t rows, const int32_t* offsets_dev,
+              const int32_t* lengths_dev, uint64_t requests, const int32_t* table_dev, uint64_t ld_table, uint64_t width, float scale,
+              uint64_t window, uint64_t sinks, void* out_dev, uint64_t ldo, void* work_dev, uint64_t work_bytes, void* cuda_stream);
+
+/*
  * Hysteresis-guided reconfiguration (Sec. 3.4; host only, no CUDA).  The controller only decides WHEN to
  * move between pre-specified topologies, listed from most-Training to most-Rollout (e.g. 6:2, 5:3, 4:4).
  * Per step: imbalance = (t_rollout - t_train) / max(t_rollout, t_train).  A step signals "towards

@@ -23,7 +23,9 @@ DR_STAGE_DIR_OUT, DR_STAGE_DIR_IN = 0, 1
 EXPORTS = ["dr_plan_create", "dr_plan_create_host", "dr_plan_window_host", "dr_plan_query", "dr_plan_tensor", "dr_plan_segment",
            "dr_reshard", "dr_reshard_inverse", "dr_plan_group", "dr_reshard_groups", "dr_reshard_static", "dr_plan_ranges", "dr_reshard_push", "dr_reshard_stream", "dr_shard_range", "dr_stage_out", "dr_stage_in", "dr_stage_begin", "dr_stage_wait_buffer", "dr_stage_poll", "dr_stage_end", "dr_plan_destroy", "dr_strerror",
            "dr_last_error", "dr_probe_stream", "dr_host_copy", "dr_diag_bulk_wait_failures", "dr_diag_bulk_starve", "dr_ctl_create", "dr_ctl_observe", "dr_ctl_break_even", "dr_ctl_destroy",
-           "dr_quant_rows", "dr_linear_create", "dr_linear_destroy", "dr_linear_forward", "dr_linear_dgrad", "dr_linear_wgrad", "dr_diag_linear_wait_failures", "dr_diag_linear_waits"]
+           "dr_quant_rows", "dr_linear_create", "dr_linear_destroy", "dr_linear_forward", "dr_linear_dgrad", "dr_linear_wgrad", "dr_diag_linear_wait_failures", "dr_diag_linear_waits",
+           "dr_kv_cache_create", "dr_kv_cache_destroy", "dr_kv_extend", "dr_qk_create", "dr_qk_destroy", "dr_qk_forward", "dr_qk_append",
+           "dr_qk_grad_work", "dr_qk_grad", "dr_attend_work", "dr_attend"]
 
 u8, u32, u64, i64, vp = C.c_uint8, C.c_uint32, C.c_uint64, C.c_int64, C.c_void_p
 
@@ -106,6 +108,16 @@ class dr_linear_desc(C.Structure):
                 ("scale_bytes", u64), ("scale_ld", u64)]
 
 
+class dr_kv_cache_desc(C.Structure):
+    _fields_ = [("struct_size", u32), ("n_blocks", u32), ("kv_heads", u32), ("block_tokens", u32), ("head_dim", u32), ("pad", u32),
+                ("k_dev", vp), ("v_dev", vp), ("k_scale_dev", vp), ("v_scale_dev", vp)]
+
+
+class dr_qk_desc(C.Structure):
+    _fields_ = [("struct_size", u32), ("n_q_heads", u32), ("n_kv_heads", u32), ("head_dim", u32), ("norm_dtype", u32), ("eps", C.c_float),
+                ("base", C.c_double), ("q_norm_dev", vp), ("k_norm_dev", vp)]
+
+
 class DrError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -162,6 +174,17 @@ def lib() -> C.CDLL:
         L.dr_linear_wgrad.argtypes = [vp, vp, u64, vp, u64, u64, vp, vp, u64, u32, vp]
         L.dr_diag_linear_wait_failures.argtypes = [P(u64)]
         L.dr_diag_linear_waits.argtypes = [u32, u32]
+        L.dr_kv_cache_create.argtypes = [P(dr_kv_cache_desc), P(vp)]
+        L.dr_kv_cache_destroy.argtypes = [vp]
+        L.dr_kv_extend.argtypes = [vp, vp, vp, vp, u64, vp, u64, u64, vp, vp, vp, u64, vp, vp, vp, u64, vp]
+        L.dr_qk_create.argtypes = [P(dr_qk_desc), P(vp)]
+        L.dr_qk_destroy.argtypes = [vp]
+        L.dr_qk_forward.argtypes = [vp, vp, u32, u64, vp, u64, vp, u64, vp]
+        L.dr_qk_append.argtypes = [vp, vp, u32, u64, vp, u64, vp, u64, vp, vp, u64, vp]
+        L.dr_qk_grad_work.argtypes = [vp, P(u64)]
+        L.dr_qk_grad.argtypes = [vp, vp, u32, u64, vp, vp, u64, u64, vp, u64, vp, vp, u32, vp, u64, vp]
+        L.dr_attend_work.argtypes = [vp, u64, u64, u64, P(u64)]
+        L.dr_attend.argtypes = [vp, vp, u64, u64, u64, vp, vp, u64, vp, u64, u64, C.c_float, u64, u64, vp, u64, vp, u64, vp]
         for n in EXPORTS:
             getattr(L, n).restype = C.c_int
         L.dr_strerror.argtypes = [C.c_int]
@@ -379,6 +402,60 @@ def dr_diag_linear_waits(limit_us, starve):
     return lib().dr_diag_linear_waits(limit_us, starve)
 
 
+def dr_kv_cache_create(desc):
+    h = vp()
+    return lib().dr_kv_cache_create(C.byref(desc), C.byref(h)), h
+
+
+def dr_kv_cache_destroy(cache):
+    return lib().dr_kv_cache_destroy(cache)
+
+
+def dr_kv_extend(cache, added, lengths, lengths_out, requests, table, ld_table, width, free_list, state, state_out, rows, offsets,
+                 positions, runs, n_runs, cuda_stream):
+    return lib().dr_kv_extend(cache, added, lengths, lengths_out, requests, table, ld_table, width, free_list, state, state_out, rows,
+                              offsets, positions, runs, n_runs, cuda_stream)
+
+
+def dr_qk_create(desc):
+    h = vp()
+    return lib().dr_qk_create(C.byref(desc), C.byref(h)), h
+
+
+def dr_qk_destroy(qk):
+    return lib().dr_qk_destroy(qk)
+
+
+def dr_qk_forward(qk, x_dev, dtype, ldx, positions_dev, rows, y_dev, ldy, cuda_stream):
+    return lib().dr_qk_forward(qk, x_dev, dtype, ldx, positions_dev, rows, y_dev, ldy, cuda_stream)
+
+
+def dr_qk_append(qk, x_dev, dtype, ldx, positions_dev, rows, runs_dev, n_runs, cache, y_dev, ldy, cuda_stream):
+    return lib().dr_qk_append(qk, x_dev, dtype, ldx, positions_dev, rows, runs_dev, n_runs, cache, y_dev, ldy, cuda_stream)
+
+
+def dr_qk_grad_work(qk):
+    n = u64()
+    return lib().dr_qk_grad_work(qk, C.byref(n)), n.value
+
+
+def dr_qk_grad(qk, x_dev, dtype, ldx, positions_dev, dy_dev, lddy, rows, dx_dev, lddx, dq_norm_dev, dk_norm_dev, accumulate, work_dev,
+               work_bytes, cuda_stream):
+    return lib().dr_qk_grad(qk, x_dev, dtype, ldx, positions_dev, dy_dev, lddy, rows, dx_dev, lddx, dq_norm_dev, dk_norm_dev, accumulate,
+                            work_dev, work_bytes, cuda_stream)
+
+
+def dr_attend_work(cache, n_q_heads, requests, rows):
+    n = u64()
+    return lib().dr_attend_work(cache, n_q_heads, requests, rows, C.byref(n)), n.value
+
+
+def dr_attend(cache, q_dev, ldq, n_q_heads, rows, offsets_dev, lengths_dev, requests, table_dev, ld_table, width, scale, window, sinks,
+              out_dev, ldo, work_dev, work_bytes, cuda_stream):
+    return lib().dr_attend(cache, q_dev, ldq, n_q_heads, rows, offsets_dev, lengths_dev, requests, table_dev, ld_table, width, scale,
+                           window, sinks, out_dev, ldo, work_dev, work_bytes, cuda_stream)
+
+
 def dr_diag_bulk_starve(on):
     return lib().dr_diag_bulk_starve(int(on))
 
@@ -506,6 +583,7 @@ class Plan:
         if rc:
             raise DrError(rc, "dr_plan_query")
         self.experts = spec.get("n_experts", 0) // max(1, moe_ep)  # held by this rank
+        self.heads_spec = dict(n_q_heads=spec["n_q_heads"], head_dim=spec["head_dim"], qk_norm=int(spec.get("qk_norm", 1)), tp=tp)
 
     def window(self, src_elem_lo, src_elem_hi):
         """Host-only plan for the source window [lo, hi) (what one chunk of the streamed repack covers)."""
@@ -515,6 +593,7 @@ class Plan:
         w = Plan.__new__(Plan)
         w.handle = h
         w.experts = self.experts
+        w.heads_spec = self.heads_spec
         rc, w.info = dr_plan_query(h)
         return w
 
@@ -569,6 +648,18 @@ class Plan:
         if n_groups is None:
             n_groups = max(1, self.experts) if name.rsplit(".", 1)[-1] in ("w13", "w2") else 1
         return Linear(weight, scale, n_groups=n_groups)
+
+    def qk_heads(self, arena, layer, base=1e6, eps=1e-6):
+        """The norms and rotation of `layer`'s query and key heads ("layers.0") over the norms that `arena` holds (a model without
+        qk_norm: the rotation alone); heads as this rank's qkv rows have them."""
+        from .attention import QKHeads
+        rows = next((t.rows for t in self.tensors() if t.name.decode() == layer + ".qkv"), None)
+        if rows is None:
+            raise KeyError(f"the plan has no rollout tensor {layer + '.qkv'!r}")
+        spec, dim = self.heads_spec, self.heads_spec["head_dim"]
+        n_q = spec["n_q_heads"] // spec["tp"]
+        norms = [self.view(arena, f"{layer}.{n}")[0].view(-1) for n in ("q_norm", "k_norm")] if spec["qk_norm"] else [None, None]
+        return QKHeads(n_q, (rows // dim - n_q) // 2, dim, *norms, base=base, eps=eps)
 
     def reshard(self, src, dst, stream=None):
         """src: CUDA tensor holding the flat fp32 buffer; dst: CUDA tensor holding the rollout arena."""

@@ -1,0 +1,632 @@
+// Attention over the 8-bit cache for many rows of a request: prompts, on the tensor cores (sm_100a).
+//
+// A CTA takes 256 rows of one request and cache head (the query heads that share the head, times 256 / group tokens), as two halves of 128,
+// and walks the tokens that they may see in tiles of 128.  For each half and tile
+//   S = Q K^T      tcgen05, fp8: the keys' codes as the cache holds them, brought in by tensor maps and never converted; a query row,
+//                  scaled by a power of two, is the sum of two rows of codes (bf16 has eight significant bits, e4m3 four), both
+//                  products into the same fp32 accumulator.  Exact but for bits below 2^-17 of the row's maximum.
+//   P = exp2(...)  a thread a row, the row's 128 logits in registers: no shuffles, one pass with the running maximum and sum
+//   O += P V       tcgen05, fp16: P goes back to tensor memory, over S, and is the product's first operand from there; the values'
+//                  codes become fp16, exactly, in four warps of their own
+// The halves alternate: while one's exponentials are computed the other's products run.  The exponentials (256 x 128 a tile at 16 a cycle)
+// take as long as the products (4 x 512 cycles), so what bounds it is how well the two overlap.
+//
+// As in the few-row kernel the running maximum is that of log2(p) + log2(value scale); O is multiplied anew only when it grows by more than
+// 2^4, so that p scale in fp16 is at most 2^15 and normal down to 2^-25 of the largest.
+//
+// Warps: 0-3 and 4-7 the exponentials of the two halves, 8-11 the values' codes, 12 the copies, 13 the products.  Tensor memory: S and P of
+// each half 128 columns, O of each half head_dim.  CTAs are started in the order of their number: a request's last rows, which see
+// the most tokens, first.
+// Measured: PLACEHOLDER
+#include "attend.h"
+#include "linear.h"
+#include "tc_ptx.cuh"
+
+namespace dr {
+namespace {
+
+using namespace tc;
+
+__device__ unsigned long long g_wait_failures;  // read by dr_diag_linear_wait_failures
+
+constexpr uint32_t kThreads = 512, kHalf = 128, kRowsCta = 2 * kHalf, kTile = 128;
+constexpr uint32_t kKeyStages = 3, kCodeStages = 2, kValueStages = 2, kMetas = 4;
+constexpr uint32_t kGroups = kTile / 16;  // of sixteen tokens, which share a block
+constexpr float kTop = 11.0f, kLag = 4.0f;
+constexpr float kLeastScale = 7.8886091e-31f;  // 2^-100
+
+struct Meta {
+    float k_scale[kGroups], v_log[kGroups], v_inv[kGroups];
+    uint32_t held;   // a bit for each group
+    uint32_t token;  // first of the tile
+};
+
+template <int D>
+struct Shared {
+    alignas(1024) uint8_t q[2][2][kHalf * D];  // [half][codes, codes of the rest]
+    alignas(1024) uint8_t k[kKeyStages][kTile * D];
+    alignas(1024) uint8_t codes[kCodeStages][kTile * D];
+    alignas(1024) uint8_t v[kValueStages][kTile * D * 2];
+    Meta meta[kMetas];
+    uint64_t q_full, k_full[kKeyStages], k_empty[kKeyStages], c_full[kCodeStages], c_empty[kCodeStages], v_full[kValueStages],
+        v_empty[kValueStages], s_full[2], p_full[2], o_done[2];
+    uint32_t tmem;
+    Limit limit;
+    uint32_t sums[kThreads / 32];
+    uint32_t request, item;
+};
+static_assert(sizeof(Shared<128>) <= 227 * 1024, "shared memory of a CTA");
+
+// What a CTA works on.
+struct Item {
+    Request q;
+    uint32_t r, head, rows0, rows;  // rows0: first of its rows among the request's n * group
+    Tiles tiles;
+};
+
+__device__ __forceinline__ uint32_t tiles_of_rows(const AttendArgs& a, uint32_t r)
+{
+    if (r >= a.requests) return 0;
+    const uint32_t rows = request_of(a, r).n * a.group;
+    return rows > kFewRows ? (rows + kRowsCta - 1) / kRowsCta : 0;
+}
+
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t shape, uint32_t add)
+{
+    asm volatile("{\n.reg .pred p;\nsetp.ne.u32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}"
+                 ::"r"(d), "r"(a), "l"(b), "r"(shape), "r"(add) : "memory");
+}
+// 16 columns of the thread's own lane times f, and back.
+__device__ __forceinline__ void tmem_scale(uint32_t addr, float f)
+{
+    float v[16];
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];\n"
+                 "tcgen05.wait::ld.sync.aligned;"
+                 : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]), "=f"(v[8]), "=f"(v[9]), "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15])
+                 : "r"(addr)
+                 : "memory");
+#pragma unroll
+    for (int k = 0; k < 16; ++k) v[k] *= f;
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
+                 ::"r"(addr), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]), "f"(v[8]), "f"(v[9]), "f"(v[10]), "f"(v[11]), "f"(v[12]), "f"(v[13]), "f"(v[14]), "f"(v[15])
+                 : "memory");
+}
+// 16 columns of the thread's own lane; complete after tmem_stored().
+__device__ __forceinline__ void tmem_store(uint32_t addr, const uint32_t (&v)[16])
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
+                 ::"r"(addr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15])
+                 : "memory");
+}
+__device__ __forceinline__ void tmem_stored() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ float exp2_of(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ uint32_t half2_of(float lo, float hi)
+{
+    uint32_t d;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
+    return d;
+}
+__device__ __forceinline__ uint32_t e4m3x2_of(float lo, float hi)
+{
+    uint16_t d;
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(d) : "f"(hi), "f"(lo));
+    return d;
+}
+__device__ __forceinline__ void e4m3x4_to_half(uint32_t codes, uint32_t& lo, uint32_t& hi)
+{
+    asm("{\n.reg .b16 a, b;\nmov.b32 {a, b}, %2;\ncvt.rn.f16x2.e4m3x2 %0, a;\ncvt.rn.f16x2.e4m3x2 %1, b;\n}" : "=r"(lo), "=r"(hi) : "r"(codes));
+}
+// Rows of D codes, swizzled over their own length as the tensor maps do: where chunk `c` of sixteen bytes of a row lies.
+template <int D>
+__device__ __forceinline__ uint32_t swizzled(uint32_t row, uint32_t c)
+{
+    return row * D + ((D == 128 ? c ^ (row & 7) : c ^ (row >> 1 & 3)) << 4);
+}
+// Descriptor of codes whose rows of 64 or 128 bytes run along the contraction.
+template <int D>
+__device__ __forceinline__ uint64_t codes_operand(uint32_t addr)
+{
+    return (uint64_t)((addr & 0x3FFFF) >> 4) | 1ull << 16 | (uint64_t)(8 * D >> 4) << 32 | 1ull << 46 | (D == 128 ? 2ull : 4ull) << 61;
+}
+
+// Finds blocks and scales four tiles at a time (a lane for each sixteen tokens) and starts the copies of keys and values.
+template <int D>
+__device__ __forceinline__ void produce(const AttendArgs& a, Shared<D>& s, const Item& it, const CUtensorMap* k_map, const CUtensorMap* v_map)
+{
+    const uint32_t lane = threadIdx.x & 31, box = min(1u << a.block_log2, kBoxTokens);
+    const uint32_t k_full = smem_u32(s.k_full), k_empty = smem_u32(s.k_empty), c_full = smem_u32(s.c_full), c_empty = smem_u32(s.c_empty);
+    Turn<kKeyStages> keys;
+    Turn<kCodeStages> codes;
+    uint32_t used = 0;
+    bool ok = true;
+    for (uint32_t i0 = 0; ok && i0 < it.tiles.count; i0 += 4) {
+        const uint32_t i = i0 + lane / 8, token = it.tiles.at(i) * kTile + (lane & 7) * 16;
+        uint32_t id = 0xFFFFFFFFu;
+        float ks = 0.0f, vs = 1.0f;
+        if (i < it.tiles.count && token < it.q.len) id = (uint32_t)a.table[(uint64_t)it.r * a.ld_table + (token >> a.block_log2)];
+        const bool held = id < a.n_blocks;
+        if (held) {
+            ks = a.k_scale[(uint64_t)id * a.n_kv + it.head];
+            vs = fmaxf(a.v_scale[(uint64_t)id * a.n_kv + it.head], kLeastScale);
+        }
+        const float v_log = log2f(vs), v_inv = 1.0f / vs;
+        const uint32_t all = __ballot_sync(0xFFFFFFFFu, held), pieces = __ballot_sync(0xFFFFFFFFu, held && (lane & 7) * 16 % box == 0);
+        const int row = (int)((id * a.n_kv + it.head << a.block_log2) + (token & (1u << a.block_log2) - 1));
+        for (uint32_t b = 0; b < 4 && i0 + b < it.tiles.count; ++b) {
+            const uint32_t mine = pieces >> (8 * b) & 255, bytes = (uint32_t)__popc(mine) * box * D;
+            ok = warp_wait(k_empty + 8 * keys.slot, keys.round ^ 1, &s.limit, &g_wait_failures);
+            if (!ok) break;
+            // (the softmax of the tile that the slot was for has read it: its products came before those that freed the key stage)
+            Meta& m = s.meta[(i0 + b) % kMetas];
+            if (lane / 8 == b) {
+                m.k_scale[lane & 7] = ks;
+                m.v_log[lane & 7] = v_log;
+                m.v_inv[lane & 7] = v_inv;
+                if ((lane & 7) == 0) {
+                    m.held = all >> (8 * b) & 255;
+                    m.token = token;
+                }
+            }
+            __syncwarp();
+            const bool copy = lane / 8 == b && (mine >> (lane & 7) & 1);
+            if (!a.starve) {
+                if (lane == 0) bar_expect(k_full + 8 * keys.slot, bytes);
+                __syncwarp();
+                if (copy) load_2d<false>(smem_u32(s.k[keys.slot]) + (lane & 7) * 16 * D, k_map, k_full + 8 * keys.slot, 0, row);
+            }
+            __syncwarp();
+            keys.next();
+            used = min(used + 1, kKeyStages);
+            ok = warp_wait(c_empty + 8 * codes.slot, codes.round ^ 1, &s.limit, &g_wait_failures);
+            if (!ok) break;
+            if (!a.starve) {
+                if (lane == 0) bar_expect(c_full + 8 * codes.slot, bytes);
+                __syncwarp();
+                if (copy) load_2d<false>(smem_u32(s.codes[codes.slot]) + (lane & 7) * 16 * D, v_map, c_full + 8 * codes.slot, 0, row);
+            }
+            __syncwarp();
+            codes.next();
+        }
+    }
+    if (ok) drain(keys, used, k_empty, &s.limit, &g_wait_failures);
+}
+
+template <int D>
+__device__ __forceinline__ void multiply(const AttendArgs& a, Shared<D>& s, const Item& it)
+{
+    const uint32_t k_full = smem_u32(s.k_full), k_empty = smem_u32(s.k_empty), v_full = smem_u32(s.v_full), v_empty = smem_u32(s.v_empty);
+    const uint32_t halves = it.rows > kHalf ? 2 : 1, n = it.tiles.count;
+    const uint32_t shape_s = shape_of(true, false, false, kHalf, kTile), shape_o = shape_of(true, false, true, kHalf, D);  // (format 0: e4m3, fp16)
+    const uint64_t q0 = codes_operand<D>(smem_u32(s.q)), k0 = codes_operand<D>(smem_u32(s.k)), v0 = operand(smem_u32(s.v), kTile * 128);
+    Turn<kKeyStages> keys;
+    Turn<kValueStages> values;
+    if (!warp_wait(smem_u32(&s.q_full), 0, &s.limit, &g_wait_failures)) return;
+    // S of half h for tile i
+    auto logits = [&](uint32_t h, uint32_t i) {
+        if (h == 0 && !warp_wait(k_full + 8 * keys.slot, keys.round, &s.limit, &g_wait_failures)) return false;
+        // S lies over the P of the tile before, which its product must have read
+        if (i && !warp_wait(smem_u32(&s.o_done[h]), (i - 1) & 1, &s.limit, &g_wait_failures)) return false;
+        fence_after();
+        const uint64_t dk = k0 + keys.slot * (kTile * D >> 4);
+        if (elect()) {
+#pragma unroll
+            for (uint32_t rest = 0; rest < 2; ++rest)
+#pragma unroll
+                for (uint32_t c = 0; c < D / 32; ++c)
+                    mma<1, true>(s.tmem + h * kTile, q0 + (h * 2 + rest) * (kHalf * D >> 4) + c * 2, dk + c * 2, shape_s, rest | c);
+            commit<1>(smem_u32(&s.s_full[h]));
+            if (h + 1 == halves) commit<1>(k_empty + 8 * keys.slot);
+        }
+        __syncwarp();
+        if (h + 1 == halves) keys.next();
+        return true;
+    };
+    for (uint32_t h = 0; h < halves; ++h)
+        if (!logits(h, 0)) return;
+    for (uint32_t i = 0; i < n; ++i) {
+        for (uint32_t h = 0; h < halves; ++h) {
+            if (h == 0 && !warp_wait(v_full + 8 * values.slot, values.round, &s.limit, &g_wait_failures)) return;
+            if (!warp_wait(smem_u32(&s.p_full[h]), i & 1, &s.limit, &g_wait_failures)) return;
+            fence_after();
+            const uint64_t dv = v0 + values.slot * (kTile * D * 2 >> 4);
+            if (elect()) {
+#pragma unroll
+                for (uint32_t c = 0; c < kTile / 16; ++c)
+                    mma_ts(s.tmem + 2 * kTile + h * D, s.tmem + h * kTile + c * 8, dv + c * (2048 >> 4), shape_o, i | c);
+                commit<1>(smem_u32(&s.o_done[h]));
+                if (h + 1 == halves) commit<1>(v_empty + 8 * values.slot);
+            }
+            __syncwarp();
+            if (i + 1 < n && !logits(h, i + 1)) return;
+        }
+        values.next();
+    }
+}
+
+// The values' codes to fp16, a thread a token: rows of 64 dimensions, swizzled, 128 tokens behind one another; the next 64 dimensions behind
+// them.  Tokens that are not held become zeros, whatever the bytes are.
+template <int D>
+__device__ __forceinline__ void convert(const AttendArgs& a, Shared<D>& s, const Item& it)
+{
+    const uint32_t t = threadIdx.x & 127, lane = threadIdx.x & 31;
+    const uint32_t c_full = smem_u32(s.c_full), c_empty = smem_u32(s.c_empty), v_full = smem_u32(s.v_full), v_empty = smem_u32(s.v_empty);
+    Turn<kCodeStages> codes;
+    Turn<kValueStages> values;
+    uint32_t used = 0;
+    for (uint32_t i = 0; i < it.tiles.count; ++i) {
+        if (!warp_wait(c_full + 8 * codes.slot, codes.round, &s.limit, &g_wait_failures)) return;
+        if (!warp_wait(v_empty + 8 * values.slot, values.round ^ 1, &s.limit, &g_wait_failures)) return;
+        const Meta& m = s.meta[i % kMetas];
+        const bool live = (m.held >> (t / 16) & 1) && m.token + t < it.q.len;
+        const uint8_t* from = s.codes[codes.slot];
+        const uint32_t to = smem_u32(s.v[values.slot]) + t * 128;
+#pragma unroll
+        for (uint32_t c = 0; c < D / 16; ++c) {
+            uint4 w = *(const uint4*)(from + swizzled<D>(t, c));
+            if (!live) w = make_uint4(0, 0, 0, 0);
+            uint32_t h[8];
+            e4m3x4_to_half(w.x, h[0], h[1]);
+            e4m3x4_to_half(w.y, h[2], h[3]);
+            e4m3x4_to_half(w.z, h[4], h[5]);
+            e4m3x4_to_half(w.w, h[6], h[7]);
+            const uint32_t panel = to + c / 4 * (kTile * 128);
+            store_shared(panel + ((c % 4 * 2 ^ (t & 7)) << 4), h[0], h[1], h[2], h[3]);
+            store_shared(panel + (((c % 4 * 2 + 1) ^ (t & 7)) << 4), h[4], h[5], h[6], h[7]);
+        }
+        fence_async();
+        __syncwarp();
+        if (lane == 0) {
+            bar_arrive(c_empty + 8 * codes.slot);
+            bar_arrive(v_full + 8 * values.slot);
+        }
+        codes.next();
+        values.next();
+        used = min(used + 1, kValueStages);
+    }
+    drain(values, used, v_empty, &s.limit, &g_wait_failures);
+}
+
+// A half's rows, a thread a row.
+template <int D>
+__device__ __forceinline__ void softmax(const AttendArgs& a, Shared<D>& s, const Item& it, uint32_t half)
+{
+    const uint32_t lane = threadIdx.x & 31, i_row = threadIdx.x & 127, x = it.rows0 + half * kHalf + i_row;
+    const uint32_t last = it.q.n * a.group - 1, y = min(x, last), j = y / a.group;
+    const bool real = x <= last;
+    const int p = (int)it.q.len - (int)it.q.n + (int)j;
+    const uint64_t index = it.q.row0 + j;
+    const uint32_t head = it.head * a.group + y % a.group;
+    // the row as the sum of two rows of codes
+    float back;
+    {
+        const char* q = (const char*)a.q + (index * a.ldq + (uint64_t)head * D) * 2;
+        uint32_t most = 0;
+        // sixteen values; read twice, for the maximum and for the codes, rather than held
+        auto load16 = [&](uint32_t c, uint32_t (&w)[8]) {
+            const char* at = q + 32 * c;
+#pragma unroll
+            for (int k = 0; k < 8; k += 4) {
+                if (a.vec_q == 2) {
+                    asm volatile("ld.global.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(w[k]), "=r"(w[k + 1]), "=r"(w[k + 2]), "=r"(w[k + 3]) : "l"(at + 4 * k) : "memory");
+                } else {
+#pragma unroll
+                    for (int u = k; u < k + 4; ++u)
+                        w[u] = ((const volatile uint16_t*)at)[2 * u] | (uint32_t)((const volatile uint16_t*)at)[2 * u + 1] << 16;
+                }
+            }
+        };
+#pragma unroll 4
+        for (uint32_t c = 0; c < D / 16; ++c) {
+            uint32_t w[8];
+            load16(c, w);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) most = max(most, max(w[k] & 0x7FFFu, w[k] >> 16 & 0x7FFFu));
+        }
+        // times 2^up the maximum lies in (224, 448]; a row that is not finite becomes NaN codes, below
+        const int e = (int)(most >> 7);
+        const int up = e == 255 || most == 0 ? 0 : 8 - (e - 127) - ((most & 127) > 96);  // 448 = 1.75 * 2^8
+        const float x1 = __uint_as_float((uint32_t)(127 + up / 2) << 23), x2 = __uint_as_float((uint32_t)(127 + up - up / 2) << 23);
+        const float sign = a.scale < 0.0f ? -1.0f : 1.0f;
+        back = fabsf(a.scale) * __uint_as_float((uint32_t)(127 - up / 2) << 23) * __uint_as_float((uint32_t)(127 - (up - up / 2)) << 23);
+#pragma unroll 1
+        for (uint32_t c = 0; c < D / 16; ++c) {
+            uint32_t w[8], hi[4], rest[4];
+            load16(c, w);
+#pragma unroll
+            for (int k = 0; k < 8; k += 2) {
+                uint32_t h2[2], r2[2];
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    const uint32_t v = w[k + u];
+                    float f0 = __uint_as_float(v << 16) * x1 * x2 * sign, f1 = __uint_as_float(v & 0xFFFF0000u) * x1 * x2 * sign;
+                    if (e == 255) f0 = f1 = __uint_as_float(0x7FC00000u);
+                    if (!real) f0 = f1 = 0.0f;
+                    h2[u] = e4m3x2_of(f0, f1);
+                    uint32_t wide;
+                    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(wide) : "h"((uint16_t)h2[u]));
+                    float g0, g1;
+                    asm("{\n.reg .b16 a, b;\nmov.b32 {a, b}, %2;\ncvt.f32.f16 %0, a;\ncvt.f32.f16 %1, b;\n}" : "=f"(g0), "=f"(g1) : "r"(wide));
+                    r2[u] = e4m3x2_of(f0 - g0, f1 - g1);
+                }
+                hi[k / 2] = h2[0] | h2[1] << 16;
+                rest[k / 2] = r2[0] | r2[1] << 16;
+            }
+            const uint32_t o = swizzled<D>(i_row, c);
+            store_shared(smem_u32(s.q[half][0]) + o, hi[0], hi[1], hi[2], hi[3]);
+            store_shared(smem_u32(s.q[half][1]) + o, rest[0], rest[1], rest[2], rest[3]);
+        }
+    }
+    fence_async();
+    __syncwarp();
+    if (lane == 0) bar_arrive(smem_u32(&s.q_full));
+    const uint32_t quarter = (threadIdx.x >> 5 & 3) * 32 << 16;
+    const uint32_t s_at = s.tmem + quarter + half * kTile, o_at = s.tmem + quarter + 2 * kTile + half * D;
+    const uint32_t s_full = smem_u32(&s.s_full[half]), p_full = smem_u32(&s.p_full[half]), o_done = smem_u32(&s.o_done[half]);
+    const int p_lo = __shfl_sync(0xFFFFFFFFu, p, 0), p_hi = __shfl_sync(0xFFFFFFFFu, p, 31);  // rows ascend
+    float m = -INFINITY, l = 0.0f;
+    for (uint32_t i = 0; i < it.tiles.count; ++i) {
+        if (!__all_sync(0xFFFFFFFFu, bar_wait(s_full, i & 1, &s.limit, &g_wait_failures))) return;
+        fence_after();
+        float v[4][32];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) tmem_start(s_at + 32 * c, v[c]);
+        const Meta& meta = s.meta[i % kMetas];
+        const int t0 = (int)meta.token;
+        const uint32_t held = meta.held;
+        const bool all = held == 255 && t0 + (int)kTile - 1 <= p_lo && (!a.window || t0 > p_hi - (int)a.window || t0 + (int)kTile - 1 < (int)a.sinks);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) tmem_arrived(v[c]);
+        if (!all) {
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+#pragma unroll
+                for (int k = 0; k < 32; ++k) {
+                    const int t = t0 + 32 * c + k;
+                    const bool hide = !(held >> (2 * c + k / 16) & 1) || t > p || (a.window && t <= p - (int)a.window && t >= (int)a.sinks);
+                    if (hide) v[c][k] = -INFINITY;
+                }
+        }
+        float f[kGroups], top = -INFINITY;
+#pragma unroll
+        for (int g = 0; g < (int)kGroups; ++g) {
+            // (never zero: a hidden logit stays hidden)
+            f[g] = fmaxf(back * meta.k_scale[g], 1.2e-38f);
+            float most = v[g / 2][g % 2 * 16];
+#pragma unroll
+            for (int k = 1; k < 16; ++k) most = fmaxf(most, v[g / 2][g % 2 * 16 + k]);
+            top = fmaxf(top, fmaf(most, f[g], meta.v_log[g]));
+        }
+        if (__any_sync(0xFFFFFFFFu, i == 0 || top > m + kLag || (m == -INFINITY && top > m))) {
+            const float now = fmaxf(m, top), shrink = now == -INFINITY ? 1.0f : exp2_of(m - now);
+            m = now;
+            l *= shrink;
+            if (i) {  // the product before has ended: this S was computed behind it
+#pragma unroll 1
+                for (int c = 0; c < D / 16; ++c) tmem_scale(o_at + 16 * c, shrink);
+            }
+        }
+        const float base = kTop - (m == -INFINITY ? 0.0f : m);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            uint32_t w[16];
+#pragma unroll
+            for (int g = 2 * c; g < 2 * c + 2; ++g) {
+                const float from = meta.v_log[g] + base;
+                float sum = 0.0f;
+#pragma unroll
+                for (int k = 0; k < 16; k += 2) {
+                    const float y0 = exp2_of(fmaf(v[g / 2][g % 2 * 16 + k], f[g], from)), y1 = exp2_of(fmaf(v[g / 2][g % 2 * 16 + k + 1], f[g], from));
+                    sum += y0 + y1;
+                    w[(g - 2 * c) * 8 + k / 2] = half2_of(y0, y1);
+                }
+                l = fmaf(sum, meta.v_inv[g], l);
+            }
+            tmem_store(s_at + 16 * c, w);
+        }
+        tmem_stored();
+        fence_before();
+        __syncwarp();
+        if (lane == 0) bar_arrive(p_full);
+    }
+    if (!__all_sync(0xFFFFFFFFu, bar_wait(o_done, (it.tiles.count - 1) & 1, &s.limit, &g_wait_failures))) return;
+    fence_after();
+    const float norm = l == 0.0f ? 0.0f : 1.0f / l;
+    uint16_t* out = (uint16_t*)a.out + index * a.ldo + (uint64_t)head * D;
+#pragma unroll
+    for (int c = 0; c < D / 32; ++c) {
+        float o[32];
+        tmem_start(o_at + 32 * c, o);
+        tmem_arrived(o);
+        if (real) {
+#pragma unroll
+            for (int k = 0; k < 32; k += 8) {
+                uint32_t w[4];
+#pragma unroll
+                for (int u = 0; u < 4; ++u) w[u] = pack_bf16(o[k + 2 * u] * norm, o[k + 2 * u + 1] * norm);
+                if (a.vec_out == 2) {
+                    *(uint4*)(out + 32 * c + k) = make_uint4(w[0], w[1], w[2], w[3]);
+                } else {
+#pragma unroll
+                    for (int u = 0; u < 8; ++u) out[32 * c + k + u] = (uint16_t)(w[u / 2] >> (u & 1 ? 16 : 0));
+                }
+            }
+        }
+        __syncwarp();
+    }
+}
+
+template <int D>
+__global__ void __launch_bounds__(kThreads, 1)
+    many_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map, const __grid_constant__ AttendArgs a)
+{
+    extern __shared__ __align__(1024) uint8_t raw[];
+    Shared<D>& s = *(Shared<D>*)raw;
+    if (smem_u32(raw) & 1023) {  // the swizzled tiles need the alignment asked for; nothing has been started yet
+        if (threadIdx.x == 0) atomicAdd(&g_wait_failures, 1ull);
+        return;
+    }
+    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    after_previous();
+    // the request, rows and head of this CTA
+    {
+        const uint32_t want = blockIdx.x / a.n_kv;
+        uint32_t base = 0;
+        bool found = false;
+        for (uint32_t r0 = 0; r0 < a.requests && base <= want; r0 += kThreads) {
+            const uint32_t mine = tiles_of_rows(a, r0 + threadIdx.x);
+            uint32_t sum = mine;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const uint32_t up = __shfl_up_sync(0xFFFFFFFFu, sum, o);
+                if (lane >= (uint32_t)o) sum += up;
+            }
+            __syncthreads();
+            if (lane == 31) s.sums[warp] = sum;
+            __syncthreads();
+            uint32_t before = base, total = 0;
+#pragma unroll
+            for (uint32_t w = 0; w < kThreads / 32; ++w) {
+                if (w < warp) before += s.sums[w];
+                total += s.sums[w];
+            }
+            before += sum - mine;
+            if (before <= want && want < before + mine) {
+                s.request = r0 + threadIdx.x;
+                s.item = mine - 1 - (want - before);  // a request's last rows first
+            }
+            base += total;
+            found = base > want;
+        }
+        if (!found) return;  // (by all threads, before anything was set up)
+    }
+    if (threadIdx.x == 0) {
+        prefetch_map(&k_map);
+        prefetch_map(&v_map);
+    }
+    __syncthreads();
+    Item it;
+    it.r = s.request;
+    it.q = request_of(a, it.r);
+    it.head = blockIdx.x % a.n_kv;
+    it.rows0 = s.item * kRowsCta;
+    it.rows = min(kRowsCta, it.q.n * a.group - it.rows0);
+    const int before = (int)it.q.len - (int)it.q.n;
+    it.tiles = tiles_of<kTile>(a, before + (int)(it.rows0 / a.group), before + (int)((it.rows0 + it.rows - 1) / a.group));
+    if (it.tiles.count == 0) it.tiles = Tiles{0, 0, 1};  // rows that see nothing still have to be written
+    const uint32_t halves = it.rows > kHalf ? 2 : 1;
+    if (threadIdx.x == 0) {
+        bar_init(smem_u32(&s.q_full), 4 * halves);
+        for (uint32_t i = 0; i < kKeyStages; ++i) {
+            bar_init(smem_u32(&s.k_full[i]), 1);
+            bar_init(smem_u32(&s.k_empty[i]), 1);
+        }
+        for (uint32_t i = 0; i < kCodeStages; ++i) {
+            bar_init(smem_u32(&s.c_full[i]), 1);
+            bar_init(smem_u32(&s.c_empty[i]), 4);
+        }
+        for (uint32_t i = 0; i < kValueStages; ++i) {
+            bar_init(smem_u32(&s.v_full[i]), 4);
+            bar_init(smem_u32(&s.v_empty[i]), 1);
+        }
+        for (uint32_t h = 0; h < 2; ++h) {
+            bar_init(smem_u32(&s.s_full[h]), 1);
+            bar_init(smem_u32(&s.p_full[h]), 4);
+            bar_init(smem_u32(&s.o_done[h]), 1);
+        }
+        s.limit.stop = 0;
+        s.limit.us = a.limit_us;
+        bar_init_fence();
+    }
+    if (warp == 13) tmem_alloc<1>(smem_u32(&s.tmem), 512);
+    fence_before();
+    __syncthreads();
+    fence_after();
+
+    if (warp < 8) {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 192;");
+        if (warp < 4 * halves) softmax<D>(a, s, it, warp >> 2);
+    } else if (warp < 12) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+        convert<D>(a, s, it);
+    } else {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+        if (warp == 12) produce<D>(a, s, it, &k_map, &v_map);
+        if (warp == 13) multiply<D>(a, s, it);
+    }
+    __syncwarp();
+    let_copies_end(&s.limit);
+    fence_before();
+    __syncthreads();
+    fence_after();
+    if (warp == 13) tmem_free<1>(s.tmem, 512);
+}
+
+template <int D>
+int prepare_many()
+{
+    cudaFuncAttributes at;
+    DR_CUDA(cudaFuncGetAttributes(&at, many_kernel<D>));
+    // the split of the registers draws on what the CTA was launched with
+    if (at.numRegs * (int)kThreads < 256 * 192 + 128 * 64 + 128 * 64) {
+        set_error("the attention kernel was built with %d registers a thread", at.numRegs);
+        return DR_ERR_CUDA;
+    }
+    DR_CUDA(cudaFuncSetAttribute(many_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Shared<D>)));
+    return DR_OK;
+}
+
+template <int D>
+int launch_many(const dr_kv_cache* cache, const AttendArgs& a, uint64_t ctas, cudaStream_t stream)
+{
+    cudaLaunchAttribute attr = overlap_attribute();
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)ctas);
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = sizeof(Shared<D>);
+    cfg.stream = stream;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, many_kernel<D>, cache->k_map, cache->v_map, a);
+    if (e != cudaSuccess) {
+        cudaGetLastError();
+        set_error("attention launch: %s", cudaGetErrorString(e));
+        return DR_ERR_CUDA;
+    }
+    return DR_OK;
+}
+
+}  // namespace
+
+int prepare_attend_many()
+{
+    const int rc = prepare_many<64>();
+    return rc ? rc : prepare_many<128>();
+}
+
+int launch_attend_many(const dr_kv_cache* cache, const AttendArgs& a, cudaStream_t stream)
+{
+    // no more tiles than this have rows: a full one for every 256 of all rows, and a last one for each request that has any
+    const uint64_t by_rows = (uint64_t)a.rows * a.group, most = by_rows / (kFewRows + 1);
+    const uint64_t tiles = by_rows / kRowsCta + (a.requests < most ? a.requests : most);
+    if (tiles * a.n_kv > 0x7FFFFFFFull) {
+        set_error("too many rows for one launch");
+        return DR_ERR_UNSUPPORTED;
+    }
+    if (tiles == 0) return DR_OK;
+    return cache->d.head_dim == 64 ? launch_many<64>(cache, a, tiles * a.n_kv, stream) : launch_many<128>(cache, a, tiles * a.n_kv, stream);
+}
+
+int attend_many_wait_failures(uint64_t* out)
+{
+    unsigned long long n = 0;
+    DR_CUDA(cudaMemcpyFromSymbol(&n, g_wait_failures, sizeof n));
+    *out = n;
+    return DR_OK;
+}
+
+}  // namespace dr

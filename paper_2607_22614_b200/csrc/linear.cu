@@ -1,5 +1,6 @@
 // Entry points of the linear layers: argument checks, the handle, choice of kernel.
 #include "linear.h"
+#include "attend.h"
 
 #include <atomic>
 #include <cstring>
@@ -201,10 +202,12 @@ int dr_diag_linear_wait_failures(uint64_t* count)
     }
     // calls may run on streams that the default stream, which the counters are read on, does not wait for
     DR_CUDA(cudaDeviceSynchronize());
-    uint64_t small = 0;
+    uint64_t small = 0, few = 0, many = 0;
     int rc = linear_wait_failures(count);
     if (rc == DR_OK) rc = linear_small_wait_failures(&small);
-    *count += small;
+    if (rc == DR_OK) rc = attend_few_wait_failures(&few);
+    if (rc == DR_OK) rc = attend_many_wait_failures(&many);
+    *count += small + few + many;
     return rc;
 }
 

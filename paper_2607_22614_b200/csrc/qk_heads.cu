@@ -1,0 +1,783 @@
+// Norms of query and key heads with the position rotation, forward, into the 8-bit cache, and back (sm_100a).
+//
+// A head of 64 or 128 values is spread over 4 or 8 lanes, sixteen values each: eight of its first half and the eight of its second half that
+// the rotation pairs them with, so the rotation stays inside a lane, a sum over a head takes two or three shuffles, and every access is
+// 16 bytes a lane.  A warp takes eight or four heads of one token at a time; the angles belong to the token, so a warp that goes on to the
+// token's next heads keeps their sines.  Every value is read once and written once: HBM bounds it.
+//
+// Angles: base^(-2 i / d) / 2 pi is held as a fraction of a turn in 64 bits, so that position * fraction, taken modulo 2^64, is the
+// angle modulo a turn, exact to 2^-64 * position; its upper 32 bits go to sincospi.  No reduction, no table over positions, and the far end
+// of a long context is as exact as its start.
+//
+// Into the cache: a CTA owns one run (the new tokens of one block) for one head, keys and values both, so that the block's two
+// scales are reductions inside the CTA and nobody else touches the block.  Scales are powers of two: the code of v is e4m3(v 2^-e), one
+// rounding from fp32, and a scale that grows shifts the codes the block holds already.
+//
+// Back: with r = 1 / sqrt(mean x^2 + eps), n = x r, g = the rotation back of dy, h = g w:  dx = r (h - n mean(h n)),
+// dw = sum of g n over all rows and heads.  A warp keeps the sums of dw for its lanes' sixteen values over all the tokens it takes, a CTA adds its
+// warps' in a fixed order, and a second launch adds the CTAs'.
+// Measured: PLACEHOLDER
+#include <cmath>
+#include <new>
+
+#include "fp8_codes.cuh"
+#include "kv_cache.h"
+
+struct dr_qk {
+    dr_qk_desc d{};
+    int device = -1;
+    int sms = 0;
+    uint64_t turns[64] = {};  // base^(-2 i / d) / 2 pi, in units of 2^-64 of a turn
+};
+
+namespace dr {
+namespace {
+
+constexpr int kWarps = 8, kThreads = 32 * kWarps;
+
+struct HeadsArgs {
+    const void* x;
+    void* y;
+    const void* dy;
+    const int32_t* positions;
+    const void* q_norm;
+    const void* k_norm;
+    float* work;
+    uint64_t ldx, ldy, lddy;
+    uint32_t rows, n_q, n_kv;
+    uint32_t heads;      // heads that are normed and rotated from x to y
+    uint32_t parts;      // warps a token's heads are dealt to
+    uint32_t norm_f32, vec, vec_y;
+    float eps;
+    // into the cache
+    uint32_t cache_ctas;
+    const int4* runs;
+    uint8_t* k;
+    uint8_t* v;
+    float* k_scale;
+    float* v_scale;
+    uint32_t n_blocks, block_tokens;
+    uint64_t turns[64];
+};
+
+template <bool F32> constexpr uint64_t kSize = F32 ? 4 : 2;
+
+// Eight values from p on.  Coherent loads that stay behind after_previous().
+template <bool F32>
+__device__ __forceinline__ void load8(const char* p, bool vec, float (&v)[8])
+{
+    if (F32) {
+        if (vec) {
+#pragma unroll
+            for (int k = 0; k < 8; k += 4)
+                asm volatile("ld.global.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v[k]), "=f"(v[k + 1]), "=f"(v[k + 2]), "=f"(v[k + 3]) : "l"(p + 4 * k) : "memory");
+        } else {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] = ((const volatile float*)p)[k];
+        }
+    } else {
+        uint32_t w[4];
+        if (vec) {
+            asm volatile("ld.global.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "l"(p) : "memory");
+        } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) w[k] = ((const volatile uint16_t*)p)[2 * k] | (uint32_t)((const volatile uint16_t*)p)[2 * k + 1] << 16;
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            v[2 * k] = __uint_as_float(w[k] << 16);
+            v[2 * k + 1] = __uint_as_float(w[k] & 0xFFFF0000u);
+        }
+    }
+}
+__device__ __forceinline__ uint32_t bf16x2(float lo, float hi)
+{
+    uint32_t d;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
+    return d;
+}
+template <bool F32>
+__device__ __forceinline__ void store8(char* p, bool vec, const float (&v)[8])
+{
+    if (F32) {
+        if (vec) {
+            ((float4*)p)[0] = make_float4(v[0], v[1], v[2], v[3]);
+            ((float4*)p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+        } else {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) ((float*)p)[k] = v[k];
+        }
+    } else {
+        uint32_t w[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) w[k] = bf16x2(v[2 * k], v[2 * k + 1]);
+        if (vec) {
+            *(uint4*)p = make_uint4(w[0], w[1], w[2], w[3]);
+        } else {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) ((uint16_t*)p)[k] = (uint16_t)(w[k / 2] >> (k & 1 ? 16 : 0));
+        }
+    }
+}
+
+// What a CTA keeps of the handle: the turns, and the norms in fp32.
+template <int D>
+struct HeadsShared {
+    uint64_t turns[D / 2];
+    float4 norm[2][D / 4];
+};
+template <int D>
+__device__ __forceinline__ void fill_turns(HeadsShared<D>& s, const HeadsArgs& a)
+{
+    if (threadIdx.x < D / 2) s.turns[threadIdx.x] = a.turns[threadIdx.x];
+}
+template <int D>
+__device__ __forceinline__ void fill_norms(HeadsShared<D>& s, const HeadsArgs& a)
+{
+    if (a.q_norm && threadIdx.x < 2 * D) {
+        const void* w = threadIdx.x < D ? a.q_norm : a.k_norm;
+        const uint32_t i = threadIdx.x & (D - 1);
+        ((float*)s.norm)[threadIdx.x] = a.norm_f32 ? ((const volatile float*)w)[i] : __uint_as_float((uint32_t)((const volatile uint16_t*)w)[i] << 16);
+    }
+}
+template <int D>
+__device__ __forceinline__ void load_norm(const HeadsShared<D>& s, uint32_t key, uint32_t i0, float (&w)[16])
+{
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int k = 0; k < 8; k += 4) {
+            const float4 f = s.norm[key][(h * D / 2 + i0 + k) / 4];
+            w[8 * h + k] = f.x;
+            w[8 * h + k + 1] = f.y;
+            w[8 * h + k + 2] = f.z;
+            w[8 * h + k + 3] = f.w;
+        }
+}
+
+// Cosines and sines of the lane's eight angles at a position.
+template <int D>
+__device__ __forceinline__ void angles(const HeadsShared<D>& s, uint32_t i0, int32_t position, float (&c)[8], float (&sn)[8])
+{
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        const int32_t turn = (int32_t)((uint64_t)position * s.turns[i0 + k] >> 32);  // of 2^32
+        sincospif((float)turn * 4.656612873077393e-10f, &sn[k], &c[k]);
+    }
+}
+template <int D>
+__device__ __forceinline__ float head_sum(float v)
+{
+#pragma unroll
+    for (int o = 1; o < D / 16; o <<= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
+    return v;
+}
+// x -> normed and rotated, in place: the lane's eight of the first half, then of the second
+template <int D>
+__device__ __forceinline__ void norm_rotate(const HeadsShared<D>& s, const HeadsArgs& a, uint32_t key, uint32_t i0, const float (&c)[8],
+                                            const float (&sn)[8], float (&lo)[8], float (&hi)[8])
+{
+    if (a.q_norm) {
+        float sum = 0.0f, w[16];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) sum = fmaf(lo[k], lo[k], fmaf(hi[k], hi[k], sum));
+        const float r = rsqrtf(head_sum<D>(sum) * (1.0f / D) + a.eps);
+        load_norm<D>(s, key, i0, w);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            lo[k] *= r * w[k];
+            hi[k] *= r * w[8 + k];
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        const float l = lo[k], h = hi[k];
+        lo[k] = fmaf(l, c[k], -h * sn[k]);
+        hi[k] = fmaf(h, c[k], l * sn[k]);
+    }
+}
+
+// Heads [0, a.heads) of the CTA's tokens.
+template <int D, bool F32>
+__device__ __forceinline__ void rotate_heads(const HeadsArgs& a, const HeadsShared<D>& s, uint32_t cta)
+{
+    constexpr uint32_t kLanes = D / 16, kHeads = 32 / kLanes;  // of a head; heads of a warp
+    const uint32_t lane = threadIdx.x & 31, i0 = (lane % kLanes) * 8;
+    const uint64_t w = (uint64_t)cta * kWarps + (threadIdx.x >> 5);
+    const uint32_t row = (uint32_t)(w / a.parts), part = (uint32_t)(w % a.parts);
+    if (row >= a.rows) return;
+    const int32_t position = ((const volatile int32_t*)a.positions)[row];
+    if (position < 0) return;
+    const uint32_t groups = (a.heads + kHeads - 1) / kHeads, per = (groups + a.parts - 1) / a.parts;
+    const char* x = (const char*)a.x + (uint64_t)row * a.ldx * kSize<F32>;
+    char* y = (char*)a.y + (uint64_t)row * a.ldy * kSize<F32>;
+    float c[8], sn[8];
+    bool have = false;
+    const uint32_t end = min(groups, (part + 1) * per);
+    for (uint32_t g = part * per; g < end; ++g) {
+        const uint32_t head = g * kHeads + lane / kLanes;
+        const bool mine = head < a.heads;
+        const uint64_t at = ((uint64_t)min(head, a.heads - 1) * D + i0) * kSize<F32>;
+        float lo[8], hi[8];
+        load8<F32>(x + at, a.vec, lo);
+        load8<F32>(x + at + D / 2 * kSize<F32>, a.vec, hi);
+        if (!have) angles<D>(s, i0, position, c, sn);
+        have = true;
+        norm_rotate<D>(s, a, head >= a.n_q, i0, c, sn, lo, hi);
+        if (mine) {
+            store8<F32>(y + at, a.vec_y, lo);
+            store8<F32>(y + at + D / 2 * kSize<F32>, a.vec_y, hi);
+        }
+    }
+}
+
+// The exponent e of the smallest scale 2^e >= 2^-100 with m <= 448 * 2^e (448 = 1.75 * 2^8); m is finite.
+__device__ __forceinline__ float scale_above(float m)
+{
+    const uint32_t bits = __float_as_uint(m);
+    const int e = (int)(bits >> 23) - 127 - 8 + ((bits & 0x7FFFFFu) > 0x600000u);
+    return __uint_as_float((uint32_t)(max(e, -100) + 127) << 23);
+}
+__device__ __forceinline__ bool finite(float v) { return (__float_as_uint(v) & 0x7F800000u) != 0x7F800000u; }
+
+// Codes of the block's first `bytes` bytes, held at a scale `ratio` times the new one.
+__device__ __forceinline__ void shift_codes(uint8_t* codes, uint32_t bytes, float ratio)
+{
+    for (uint32_t o = threadIdx.x * 8; o < bytes; o += kThreads * 8) {
+        uint32_t w[2];
+        asm volatile("ld.global.v2.b32 {%0,%1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "l"(codes + o) : "memory");
+        float f[8];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const uint16_t two = (uint16_t)(w[k / 2] >> (k & 1 ? 16 : 0));
+            uint32_t h;
+            asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"(two));
+            float lo, hi;
+            asm("{\n.reg .b16 a, b;\nmov.b32 {a, b}, %2;\ncvt.f32.f16 %0, a;\ncvt.f32.f16 %1, b;\n}" : "=f"(lo), "=f"(hi) : "r"(h));
+            f[2 * k] = lo * ratio;
+            f[2 * k + 1] = hi * ratio;
+        }
+        *(uint2*)(codes + o) = pack8(f);
+    }
+}
+
+// One run of one head: keys normed and rotated, values as they are, both to codes.  TURNS: tokens a group of lanes takes.
+template <int D, bool F32, int TURNS>
+__device__ __forceinline__ void append_run(const HeadsArgs& a, const HeadsShared<D>& s, uint32_t cta)
+{
+    constexpr uint32_t kLanes = D / 16, kGroups = kThreads / kLanes;
+    __shared__ float s_most[2][kWarps];
+    const uint32_t head = cta % a.n_kv;
+    int4 run;
+    asm volatile("ld.global.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(run.x), "=r"(run.y), "=r"(run.z), "=r"(run.w) : "l"(a.runs + cta / a.n_kv) : "memory");
+    const uint32_t block = (uint32_t)run.x, start = (uint32_t)run.y, row0 = (uint32_t)run.z, count = (uint32_t)run.w;
+    if (count == 0 || block >= a.n_blocks || start >= a.block_tokens || count > a.block_tokens - start || row0 >= a.rows || count > a.rows - row0)
+        return;
+    const uint32_t lane = threadIdx.x & 31, i0 = (threadIdx.x % kLanes) * 8, group = threadIdx.x / kLanes;
+    const uint64_t tile = (uint64_t)block * a.n_kv + head;
+    float k_lo[TURNS][8], k_hi[TURNS][8], v_lo[TURNS][8], v_hi[TURNS][8];
+    float k_most = 0.0f, v_most = 0.0f;
+    uint32_t poisoned = 0;
+#pragma unroll
+    for (int t = 0; t < TURNS; ++t) {
+        // (all lanes take part in the head's sums; those without a token take the run's last one)
+        const uint32_t j = min(group + t * kGroups, count - 1), row = row0 + j;
+        const char* x = (const char*)a.x + ((uint64_t)row * a.ldx + (uint64_t)(a.n_q + head) * D + i0) * kSize<F32>;
+        load8<F32>(x, a.vec, k_lo[t]);
+        load8<F32>(x + D / 2 * kSize<F32>, a.vec, k_hi[t]);
+        const uint64_t to_v = (uint64_t)a.n_kv * D * kSize<F32>;
+        load8<F32>(x + to_v, a.vec, v_lo[t]);
+        load8<F32>(x + to_v + D / 2 * kSize<F32>, a.vec, v_hi[t]);
+    }
+#pragma unroll
+    for (int t = 0; t < TURNS; ++t) {
+        const uint32_t row = row0 + min(group + t * kGroups, count - 1);
+        float c[8], sn[8];
+        angles<D>(s, i0, ((const volatile int32_t*)a.positions)[row], c, sn);
+        norm_rotate<D>(s, a, 1, i0, c, sn, k_lo[t], k_hi[t]);
+        bool all = true;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            float* const four[4] = {&k_lo[t][k], &k_hi[t][k], &v_lo[t][k], &v_hi[t][k]};
+#pragma unroll
+            for (int f = 0; f < 4; ++f) {
+                if (!finite(*four[f])) {
+                    all = false;
+                    *four[f] = 0.0f;
+                }
+            }
+            k_most = fmaxf(k_most, fmaxf(fabsf(k_lo[t][k]), fabsf(k_hi[t][k])));
+            v_most = fmaxf(v_most, fmaxf(fabsf(v_lo[t][k]), fabsf(v_hi[t][k])));
+        }
+        const uint32_t bad = __ballot_sync(0xFFFFFFFFu, !all);
+        if (bad >> (lane / kLanes * kLanes) & ((1u << kLanes) - 1)) poisoned |= 1u << t;
+    }
+#pragma unroll
+    for (int o = 16; o; o >>= 1) {
+        k_most = fmaxf(k_most, __shfl_xor_sync(0xFFFFFFFFu, k_most, o));
+        v_most = fmaxf(v_most, __shfl_xor_sync(0xFFFFFFFFu, v_most, o));
+    }
+    if (lane == 0) {
+        s_most[0][threadIdx.x >> 5] = k_most;
+        s_most[1][threadIdx.x >> 5] = v_most;
+    }
+    float k_was = 0.0f, v_was = 0.0f;
+    if (start) {
+        k_was = *(const volatile float*)(a.k_scale + tile);
+        v_was = *(const volatile float*)(a.v_scale + tile);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) {
+        k_most = fmaxf(k_most, s_most[0][w]);
+        v_most = fmaxf(v_most, s_most[1][w]);
+    }
+    const float k_scale = fmaxf(scale_above(k_most), k_was), v_scale = fmaxf(scale_above(v_most), v_was);
+    const float k_inv = __frcp_rn(k_scale), v_inv = __frcp_rn(v_scale);
+    if (threadIdx.x == 0) {  // (read by all before the barrier)
+        a.k_scale[tile] = k_scale;
+        a.v_scale[tile] = v_scale;
+    }
+    uint8_t* const k = a.k + tile * a.block_tokens * D;
+    uint8_t* const v = a.v + tile * a.block_tokens * D;
+    if (start && k_was != k_scale) shift_codes(k, start * D, k_was * k_inv);
+    if (start && v_was != v_scale) shift_codes(v, start * D, v_was * v_inv);
+#pragma unroll
+    for (int t = 0; t < TURNS; ++t) {
+        const uint32_t j = group + t * kGroups;
+        if (j >= count) break;
+        const uint32_t o = (start + j) * D + i0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            k_lo[t][i] *= k_inv;
+            k_hi[t][i] *= k_inv;
+            v_lo[t][i] *= v_inv;
+            v_hi[t][i] *= v_inv;
+        }
+        uint2 first = pack8(k_lo[t]);
+        if ((poisoned >> t & 1) && i0 == 0) first.x = (first.x & ~0xFFu) | 0x7Fu;
+        *(uint2*)(k + o) = first;
+        *(uint2*)(k + o + D / 2) = pack8(k_hi[t]);
+        *(uint2*)(v + o) = pack8(v_lo[t]);
+        *(uint2*)(v + o + D / 2) = pack8(v_hi[t]);
+    }
+}
+
+template <int D, bool F32, int TURNS>
+__global__ void __launch_bounds__(kThreads) heads_kernel(const __grid_constant__ HeadsArgs a)
+{
+    __shared__ HeadsShared<D> s;
+    fill_turns<D>(s, a);
+    after_previous();
+    fill_norms<D>(s, a);
+    __syncthreads();
+    if (TURNS && blockIdx.x < a.cache_ctas) {
+        if constexpr (TURNS > 0) append_run<D, F32, TURNS>(a, s, blockIdx.x);
+    } else {
+        rotate_heads<D, F32>(a, s, blockIdx.x - a.cache_ctas);
+    }
+}
+
+// Back through rotation and norm.  CTAs stride over the tokens; a warp takes one token's query heads, then its key heads.
+template <int D, bool F32>
+__global__ void __launch_bounds__(kThreads, 2) grad_kernel(const __grid_constant__ HeadsArgs a)
+{
+    constexpr uint32_t kLanes = D / 16, kHeads = 32 / kLanes;
+    __shared__ HeadsShared<D> s;
+    __shared__ float s_sum[kWarps][2][D];
+    fill_turns<D>(s, a);
+    after_previous();
+    fill_norms<D>(s, a);
+    __syncthreads();
+    const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5, i0 = (lane % kLanes) * 8;
+    float dw[2][16];
+#pragma unroll
+    for (int k = 0; k < 16; ++k) dw[0][k] = dw[1][k] = 0.0f;
+    for (uint64_t row = (uint64_t)blockIdx.x * kWarps + warp; row < a.rows; row += (uint64_t)gridDim.x * kWarps) {
+        const int32_t position = ((const volatile int32_t*)a.positions)[row];
+        if (position < 0) continue;
+        const char* x = (const char*)a.x + row * a.ldx * kSize<F32>;
+        const char* dy = (const char*)a.dy + row * a.lddy * kSize<F32>;
+        char* dx = (char*)a.y + row * a.ldy * kSize<F32>;
+        float c[8], sn[8];
+        angles<D>(s, i0, position, c, sn);
+#pragma unroll
+        for (int key = 0; key < 2; ++key) {
+            const uint32_t first = key ? a.n_q : 0, heads = key ? a.n_kv : a.n_q;
+            float w[16];
+            if (a.q_norm) load_norm<D>(s, key, i0, w);
+            for (uint32_t h0 = 0; h0 < heads; h0 += kHeads) {
+                const uint32_t h = h0 + lane / kLanes;
+                const bool mine = h < heads;
+                const uint64_t at = ((uint64_t)(first + min(h, heads - 1)) * D + i0) * kSize<F32>;
+                float v[2][8], g[2][8];
+                load8<F32>(dy + at, a.vec, g[0]);
+                load8<F32>(dy + at + D / 2 * kSize<F32>, a.vec, g[1]);
+                if (a.q_norm) {
+                    load8<F32>(x + at, a.vec, v[0]);
+                    load8<F32>(x + at + D / 2 * kSize<F32>, a.vec, v[1]);
+                }
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    const float l = g[0][k], u = g[1][k];
+                    g[0][k] = fmaf(l, c[k], u * sn[k]);
+                    g[1][k] = fmaf(u, c[k], -l * sn[k]);
+                }
+                if (a.q_norm) {
+                    float sum = 0.0f, dot = 0.0f;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const float f = v[i / 8][i % 8];
+                        sum = fmaf(f, f, sum);
+                        dot = fmaf(g[i / 8][i % 8] * w[i], f, dot);
+                    }
+                    sum = head_sum<D>(sum);
+                    dot = head_sum<D>(dot);
+                    const float r = rsqrtf(sum * (1.0f / D) + a.eps), back = dot * (1.0f / D) * r * r;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const float f = v[i / 8][i % 8], gi = g[i / 8][i % 8];
+                        if (mine) dw[key][i] = fmaf(gi, f * r, dw[key][i]);
+                        g[i / 8][i % 8] = r * fmaf(-f, back, gi * w[i]);
+                    }
+                }
+                if (mine) {
+                    store8<F32>(dx + at, a.vec_y, g[0]);
+                    store8<F32>(dx + at + D / 2 * kSize<F32>, a.vec_y, g[1]);
+                }
+            }
+        }
+    }
+    if (!a.q_norm) return;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+        float v = dw[i / 16][i % 16];
+#pragma unroll
+        for (int o = kLanes; o < 32; o <<= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
+        if (lane < kLanes) s_sum[warp][i / 16][(i % 16 / 8) * (D / 2) + i0 + i % 8] = v;
+    }
+    __syncthreads();
+    if (threadIdx.x < 2 * D) {
+        float v = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) v += ((const float*)s_sum[w])[threadIdx.x];
+        a.work[(uint64_t)blockIdx.x * 2 * D + threadIdx.x] = v;
+    }
+}
+
+// The CTAs' sums of dw, added in their order: 32 columns a CTA, 32 threads a column.
+__global__ void __launch_bounds__(1024) norm_sum_kernel(const float* work, uint32_t n, uint32_t d, float* dq, float* dk, uint32_t accumulate)
+{
+    __shared__ float s[32][33];
+    const uint32_t lane = threadIdx.x & 31, part = threadIdx.x >> 5, col = blockIdx.x * 32 + lane;
+    after_previous();
+    float v = 0.0f;
+    for (uint32_t i = part; i < n; i += 32) v += *(const volatile float*)(work + (uint64_t)i * 2 * d + col);
+    s[part][lane] = v;
+    __syncthreads();
+    v = s[lane][part];
+#pragma unroll
+    for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
+    if (lane == 0) {
+        const uint32_t c = blockIdx.x * 32 + part;
+        float* to = c < d ? dq + c : dk + (c - d);
+        *to = accumulate ? *to + v : v;
+    }
+}
+
+template <class K, class... A>
+int launch(const char* what, K kernel, uint64_t ctas, int threads, cudaStream_t stream, const A&... args)
+{
+    if (ctas > 0x7FFFFFFFull) {
+        set_error("too many rows for one launch");
+        return DR_ERR_UNSUPPORTED;
+    }
+    cudaLaunchAttribute attr = overlap_attribute();
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)ctas);
+    cfg.blockDim = dim3(threads);
+    cfg.stream = stream;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, args...);
+    if (e != cudaSuccess) {
+        cudaGetLastError();
+        set_error("%s launch: %s", what, cudaGetErrorString(e));
+        return DR_ERR_CUDA;
+    }
+    return DR_OK;
+}
+
+template <int TURNS>
+int launch_heads(const dr_qk* qk, bool f32, const HeadsArgs& a, uint64_t ctas, cudaStream_t s)
+{
+    if (qk->d.head_dim == 64) {
+        if constexpr (TURNS <= 2)
+            return f32 ? launch("heads", heads_kernel<64, true, TURNS>, ctas, kThreads, s, a) : launch("heads", heads_kernel<64, false, TURNS>, ctas, kThreads, s, a);
+        return DR_ERR_UNSUPPORTED;  // (a block of 128 tokens is two turns of 64)
+    }
+    return f32 ? launch("heads", heads_kernel<128, true, TURNS>, ctas, kThreads, s, a) : launch("heads", heads_kernel<128, false, TURNS>, ctas, kThreads, s, a);
+}
+
+int check_qk(const dr_qk* qk)
+{
+    if (!qk) {
+        set_error("NULL heads");
+        return DR_ERR_INVALID;
+    }
+    int dev = -1;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev != qk->device) {
+        set_error("current device differs from the heads' device");
+        return DR_ERR_STATE;
+    }
+    return DR_OK;
+}
+
+// x, positions and one more matrix of rows.
+int check_rows(uint32_t dtype, uint64_t rows, const void* x, uint64_t ldx, uint64_t x_cols, const int32_t* positions, const void* y,
+               uint64_t ldy, uint64_t y_cols)
+{
+    if (dtype != DR_BF16 && dtype != DR_F32) {
+        set_error("rows must be DR_BF16 or DR_F32");
+        return DR_ERR_UNSUPPORTED;
+    }
+    if (rows > 0x7FFFFFFFull) {
+        set_error("more than 2^31 - 1 rows");
+        return DR_ERR_UNSUPPORTED;
+    }
+    if (rows && (!x || !y || !positions)) {
+        set_error("NULL buffer");
+        return DR_ERR_INVALID;
+    }
+    if (!pitch_ok(rows, x_cols, ldx) || !pitch_ok(rows, y_cols, ldy)) {
+        set_error("leading dimension below the row's length or out of range");
+        return DR_ERR_INVALID;
+    }
+    const uint32_t es = dtype == DR_F32 ? 4 : 2;
+    if (((uintptr_t)x | (uintptr_t)y) % es || (uintptr_t)positions % 4) {
+        set_error("a pointer is not aligned to its element size");
+        return DR_ERR_ALIGN;
+    }
+    return DR_OK;
+}
+
+HeadsArgs heads_args(const dr_qk* qk, const void* x, uint32_t dtype, uint64_t ldx, const int32_t* positions, uint64_t rows, void* y, uint64_t ldy)
+{
+    HeadsArgs a{};
+    const uint32_t es = dtype == DR_F32 ? 4 : 2;
+    a.x = x;
+    a.y = y;
+    a.positions = positions;
+    a.q_norm = qk->d.q_norm_dev;
+    a.k_norm = qk->d.k_norm_dev;
+    a.norm_f32 = qk->d.norm_dtype == DR_F32;
+    a.ldx = ldx;
+    a.ldy = ldy;
+    a.rows = (uint32_t)rows;
+    a.n_q = qk->d.n_q_heads;
+    a.n_kv = qk->d.n_kv_heads;
+    a.eps = qk->d.eps;
+    a.vec = ((uintptr_t)x | ldx * es) % 16 == 0;
+    a.vec_y = ((uintptr_t)y | ldy * es) % 16 == 0;
+    for (int i = 0; i < 64; ++i) a.turns[i] = qk->turns[i];
+    return a;
+}
+
+// How many warps a token's head groups are dealt to: one while the tokens alone fill the machine, so that it works out the angles once;
+// with few tokens every group has a warp of its own.
+void deal(HeadsArgs& a, int sms, uint32_t dim)
+{
+    const uint32_t per_warp = 512 / dim, groups = (a.heads + per_warp - 1) / per_warp;
+    a.parts = 1;
+    while (a.parts < groups && (uint64_t)a.rows * a.parts < (uint64_t)sms * 32) a.parts *= 2;
+    if (a.parts > groups) a.parts = groups;
+}
+
+constexpr uint32_t kGradCtas = 2;  // for each SM
+
+}  // namespace
+}  // namespace dr
+
+using namespace dr;
+
+extern "C" {
+
+int dr_qk_create(const dr_qk_desc* desc, dr_qk** out)
+{
+    if (!out) {
+        set_error("NULL out");
+        return DR_ERR_INVALID;
+    }
+    *out = nullptr;
+    if (!desc || desc->struct_size != sizeof(dr_qk_desc)) {
+        set_error("NULL descriptor or struct_size mismatch");
+        return DR_ERR_INVALID;
+    }
+    const dr_qk_desc& d = *desc;
+    if (!d.n_q_heads || !d.n_kv_heads || !d.q_norm_dev != !d.k_norm_dev) {
+        set_error("no heads, or one norm without the other");
+        return DR_ERR_INVALID;
+    }
+    if (!std::isfinite(d.eps) || d.eps < 0.0f || !std::isfinite(d.base) || d.base < 1.0) {
+        set_error("eps must be finite and not negative, base finite and at least 1");
+        return DR_ERR_INVALID;
+    }
+    if (d.head_dim != 64 && d.head_dim != 128) {
+        set_error("heads have 64 or 128 dimensions");
+        return DR_ERR_UNSUPPORTED;
+    }
+    if (d.n_q_heads > 65536 || d.n_kv_heads > 65536 || (d.q_norm_dev && d.norm_dtype != DR_BF16 && d.norm_dtype != DR_F32)) {
+        set_error("norms must be DR_BF16 or DR_F32, heads at most 2^16");
+        return DR_ERR_UNSUPPORTED;
+    }
+    if (((uintptr_t)d.q_norm_dev | (uintptr_t)d.k_norm_dev) % (d.norm_dtype == DR_F32 ? 4 : 2)) {
+        set_error("a norm is not aligned to its element size");
+        return DR_ERR_ALIGN;
+    }
+    dr_qk* qk = new (std::nothrow) dr_qk();
+    if (!qk) return DR_ERR_NOMEM;
+    qk->d = d;
+    const long double two_pi = 6.283185307179586476925286766559L;
+    for (uint32_t i = 0; i < d.head_dim / 2; ++i) {
+        const long double f = powl((long double)d.base, -2.0L * i / d.head_dim) / two_pi;  // below 1 / 6
+        qk->turns[i] = (uint64_t)roundl(ldexpl(f, 64));
+    }
+    const int rc = [&]() -> int {
+        DR_CUDA(cudaGetDevice(&qk->device));
+        DR_CUDA(cudaDeviceGetAttribute(&qk->sms, cudaDevAttrMultiProcessorCount, qk->device));
+        return DR_OK;
+    }();
+    if (rc) {
+        delete qk;
+        return rc;
+    }
+    *out = qk;
+    return DR_OK;
+}
+
+int dr_qk_destroy(dr_qk* qk)
+{
+    delete qk;
+    return DR_OK;
+}
+
+int dr_qk_forward(const dr_qk* qk, const void* x_dev, uint32_t dtype, uint64_t ldx, const int32_t* positions_dev, uint64_t rows,
+                  void* y_dev, uint64_t ldy, void* cuda_stream)
+{
+    int rc = check_qk(qk);
+    if (rc) return rc;
+    const uint64_t cols = (uint64_t)(qk->d.n_q_heads + qk->d.n_kv_heads) * qk->d.head_dim;
+    rc = check_rows(dtype, rows, x_dev, ldx, cols, positions_dev, y_dev, ldy, cols);
+    if (rc || rows == 0) return rc;
+    HeadsArgs a = heads_args(qk, x_dev, dtype, ldx, positions_dev, rows, y_dev, ldy);
+    a.heads = a.n_q + a.n_kv;
+    deal(a, qk->sms, qk->d.head_dim);
+    return launch_heads<0>(qk, dtype == DR_F32, a, (rows * a.parts + kWarps - 1) / kWarps, (cudaStream_t)cuda_stream);
+}
+
+int dr_qk_append(const dr_qk* qk, const void* x_dev, uint32_t dtype, uint64_t ldx, const int32_t* positions_dev, uint64_t rows,
+                 const int32_t* runs_dev, uint64_t n_runs, const dr_kv_cache* cache, void* y_dev, uint64_t ldy, void* cuda_stream)
+{
+    int rc = check_qk(qk);
+    if (rc == DR_OK) rc = check_cache(cache);
+    if (rc) return rc;
+    const dr_qk_desc& d = qk->d;
+    if (cache->d.kv_heads != d.n_kv_heads || cache->d.head_dim != d.head_dim) {
+        set_error("the cache has %u heads of %u dimensions, the rows have %u of %u", cache->d.kv_heads, cache->d.head_dim, d.n_kv_heads, d.head_dim);
+        return DR_ERR_INVALID;
+    }
+    rc = check_rows(dtype, rows, x_dev, ldx, (uint64_t)(d.n_q_heads + 2 * d.n_kv_heads) * d.head_dim, positions_dev, y_dev, ldy,
+                    (uint64_t)d.n_q_heads * d.head_dim);
+    if (rc) return rc;
+    if (n_runs > 0x7FFFFFFFull) {
+        set_error("more than 2^31 - 1 runs");
+        return DR_ERR_UNSUPPORTED;
+    }
+    if (n_runs && !runs_dev) {
+        set_error("NULL buffer");
+        return DR_ERR_INVALID;
+    }
+    if ((uintptr_t)runs_dev % 16) {
+        set_error("runs off 16 bytes");
+        return DR_ERR_ALIGN;
+    }
+    if (rows == 0) return DR_OK;
+    HeadsArgs a = heads_args(qk, x_dev, dtype, ldx, positions_dev, rows, y_dev, ldy);
+    a.heads = a.n_q;
+    deal(a, qk->sms, d.head_dim);
+    a.runs = (const int4*)runs_dev;
+    a.k = (uint8_t*)cache->d.k_dev;
+    a.v = (uint8_t*)cache->d.v_dev;
+    a.k_scale = cache->d.k_scale_dev;
+    a.v_scale = cache->d.v_scale_dev;
+    a.n_blocks = cache->d.n_blocks;
+    a.block_tokens = cache->d.block_tokens;
+    const uint64_t cache_ctas = n_runs * d.n_kv_heads, ctas = cache_ctas + (rows * a.parts + kWarps - 1) / kWarps;
+    if (ctas > 0x7FFFFFFFull) {
+        set_error("too many rows and runs for one launch");
+        return DR_ERR_UNSUPPORTED;
+    }
+    a.cache_ctas = (uint32_t)cache_ctas;
+    const uint32_t turns = (a.block_tokens * (d.head_dim / 16) + kThreads - 1) / kThreads;
+    cudaStream_t s = (cudaStream_t)cuda_stream;
+    if (turns == 1) return launch_heads<1>(qk, dtype == DR_F32, a, ctas, s);
+    return turns == 2 ? launch_heads<2>(qk, dtype == DR_F32, a, ctas, s) : launch_heads<4>(qk, dtype == DR_F32, a, ctas, s);
+}
+
+int dr_qk_grad_work(const dr_qk* qk, uint64_t* bytes)
+{
+    if (!qk || !bytes) {
+        set_error("NULL argument");
+        return DR_ERR_INVALID;
+    }
+    *bytes = qk->d.q_norm_dev ? (uint64_t)kGradCtas * qk->sms * 2 * qk->d.head_dim * 4 : 0;
+    return DR_OK;
+}
+
+int dr_qk_grad(const dr_qk* qk, const void* x_dev, uint32_t dtype, uint64_t ldx, const int32_t* positions_dev, const void* dy_dev,
+               uint64_t lddy, uint64_t rows, void* dx_dev, uint64_t lddx, float* dq_norm_dev, float* dk_norm_dev, uint32_t accumulate,
+               void* work_dev, uint64_t work_bytes, void* cuda_stream)
+{
+    int rc = check_qk(qk);
+    if (rc) return rc;
+    const bool norms = qk->d.q_norm_dev != nullptr;
+    const uint64_t cols = (uint64_t)(qk->d.n_q_heads + qk->d.n_kv_heads) * qk->d.head_dim;
+    rc = check_rows(dtype, rows, norms ? x_dev : dy_dev, norms ? ldx : lddy, cols, positions_dev, dx_dev, lddx, cols);
+    if (rc == DR_OK) rc = check_rows(dtype, rows, dy_dev, lddy, cols, positions_dev, dx_dev, lddx, cols);
+    if (rc) return rc;
+    if (accumulate > 1 || (norms && (!dq_norm_dev || !dk_norm_dev))) {
+        set_error("NULL gradient of a norm, or accumulate not 0 / 1");
+        return DR_ERR_INVALID;
+    }
+    uint64_t need = 0;
+    dr_qk_grad_work(qk, &need);
+    if (norms && (!work_dev || work_bytes < need)) {
+        set_error("work holds %llu bytes, %llu are needed", (unsigned long long)(work_dev ? work_bytes : 0), (unsigned long long)need);
+        return DR_ERR_SIZE;
+    }
+    if (((uintptr_t)dq_norm_dev | (uintptr_t)dk_norm_dev) % 4 || (norms && (uintptr_t)work_dev % 16)) {
+        set_error("a gradient off 4 bytes or work off 16");
+        return DR_ERR_ALIGN;
+    }
+    if (rows == 0 && (!norms || accumulate)) return DR_OK;
+    HeadsArgs a = heads_args(qk, x_dev, dtype, ldx, positions_dev, rows, dx_dev, lddx);
+    const uint32_t es = dtype == DR_F32 ? 4 : 2;
+    a.dy = dy_dev;
+    a.lddy = lddy;
+    a.vec = ((norms ? (uintptr_t)x_dev | ldx * es : 0) | (uintptr_t)dy_dev | lddy * es) % 16 == 0;
+    a.work = (float*)work_dev;
+    const uint64_t most = (uint64_t)kGradCtas * qk->sms, wanted = (rows + kWarps - 1) / kWarps, ctas = wanted < most ? wanted : most;
+    cudaStream_t s = (cudaStream_t)cuda_stream;
+    if (ctas) {
+        if (qk->d.head_dim == 64)
+            rc = dtype == DR_F32 ? launch("heads", grad_kernel<64, true>, ctas, kThreads, s, a) : launch("heads", grad_kernel<64, false>, ctas, kThreads, s, a);
+        else
+            rc = dtype == DR_F32 ? launch("heads", grad_kernel<128, true>, ctas, kThreads, s, a) : launch("heads", grad_kernel<128, false>, ctas, kThreads, s, a);
+        if (rc) return rc;
+    }
+    if (!norms) return DR_OK;
+    return launch("norm sums", norm_sum_kernel, 2 * qk->d.head_dim / 32, 1024, s, (const float*)work_dev, (uint32_t)ctas, qk->d.head_dim,
+                  dq_norm_dev, dk_norm_dev, accumulate);
+}
+
+}  // extern "C"
