@@ -33,7 +33,8 @@ struct dr_qk {
 namespace dr {
 namespace {
 
-constexpr int kWarps = 8, kThreads = 32 * kWarps;
+constexpr int kWarps = 8, kThreads = 32 * kWarps;  // of a CTA from x to y, and back
+constexpr int kAppendThreads = 512;                // of a CTA into the cache: a run of 64 tokens of a head of 128
 
 struct HeadsArgs {
     const void* x;
@@ -62,31 +63,42 @@ struct HeadsArgs {
 
 template <bool F32> constexpr uint64_t kSize = F32 ? 4 : 2;
 
-// Eight values from p on.  Coherent loads that stay behind after_previous().
+// Sixteen values of a head as they lie in memory: eight from p on, eight from half a head further.  Coherent loads that stay behind
+// after_previous(), and in their order: a load written before the work on the values before it is on its way meanwhile.
 template <bool F32>
-__device__ __forceinline__ void load8(const char* p, bool vec, float (&v)[8])
+struct Raw {
+    uint32_t w[F32 ? 16 : 8];
+    __device__ __forceinline__ float value(int half, int k) const
+    {
+        if (F32) return __uint_as_float(w[F32 ? 8 * half + k : 0]);
+        const uint32_t v = w[4 * half + k / 2];
+        return __uint_as_float(k & 1 ? v & 0xFFFF0000u : v << 16);
+    }
+    __device__ __forceinline__ void get(float (&lo)[8], float (&hi)[8]) const
+    {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            lo[k] = value(0, k);
+            hi[k] = value(1, k);
+        }
+    }
+};
+template <int D, bool F32>
+__device__ __forceinline__ void load16(const char* p, bool vec, Raw<F32>& r)
 {
-    if (F32) {
+    constexpr int n = F32 ? 8 : 4;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const char* at = p + h * (D / 2) * kSize<F32>;
         if (vec) {
 #pragma unroll
-            for (int k = 0; k < 8; k += 4)
-                asm volatile("ld.global.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v[k]), "=f"(v[k + 1]), "=f"(v[k + 2]), "=f"(v[k + 3]) : "l"(p + 4 * k) : "memory");
+            for (int k = h * n; k < h * n + n; k += 4, at += 16)
+                asm volatile("ld.global.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(r.w[k]), "=r"(r.w[k + 1]), "=r"(r.w[k + 2]), "=r"(r.w[k + 3]) : "l"(at) : "memory");
         } else {
 #pragma unroll
-            for (int k = 0; k < 8; ++k) v[k] = ((const volatile float*)p)[k];
-        }
-    } else {
-        uint32_t w[4];
-        if (vec) {
-            asm volatile("ld.global.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "l"(p) : "memory");
-        } else {
-#pragma unroll
-            for (int k = 0; k < 4; ++k) w[k] = ((const volatile uint16_t*)p)[2 * k] | (uint32_t)((const volatile uint16_t*)p)[2 * k + 1] << 16;
-        }
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            v[2 * k] = __uint_as_float(w[k] << 16);
-            v[2 * k + 1] = __uint_as_float(w[k] & 0xFFFF0000u);
+            for (int k = 0; k < n; ++k)
+                r.w[h * n + k] = F32 ? ((const volatile uint32_t*)at)[k]
+                                     : ((const volatile uint16_t*)at)[2 * k] | (uint32_t)((const volatile uint16_t*)at)[2 * k + 1] << 16;
         }
     }
 }
@@ -203,7 +215,7 @@ __device__ __forceinline__ void rotate_heads(const HeadsArgs& a, const HeadsShar
 {
     constexpr uint32_t kLanes = D / 16, kHeads = 32 / kLanes;  // of a head; heads of a warp
     const uint32_t lane = threadIdx.x & 31, i0 = (lane % kLanes) * 8;
-    const uint64_t w = (uint64_t)cta * kWarps + (threadIdx.x >> 5);
+    const uint64_t w = (uint64_t)cta * (blockDim.x / 32) + (threadIdx.x >> 5);
     const uint32_t row = (uint32_t)(w / a.parts), part = (uint32_t)(w % a.parts);
     if (row >= a.rows) return;
     const int32_t position = ((const volatile int32_t*)a.positions)[row];
@@ -211,22 +223,22 @@ __device__ __forceinline__ void rotate_heads(const HeadsArgs& a, const HeadsShar
     const uint32_t groups = (a.heads + kHeads - 1) / kHeads, per = (groups + a.parts - 1) / a.parts;
     const char* x = (const char*)a.x + (uint64_t)row * a.ldx * kSize<F32>;
     char* y = (char*)a.y + (uint64_t)row * a.ldy * kSize<F32>;
+    const uint32_t first = part * per, end = min(groups, first + per), sub = lane / kLanes;
+    if (first >= end) return;
+    auto at = [&](uint32_t g) { return ((uint64_t)min(g * kHeads + sub, a.heads - 1) * D + i0) * kSize<F32>; };
+    Raw<F32> next;
+    load16<D, F32>(x + at(first), a.vec, next);
     float c[8], sn[8];
-    bool have = false;
-    const uint32_t end = min(groups, (part + 1) * per);
-    for (uint32_t g = part * per; g < end; ++g) {
-        const uint32_t head = g * kHeads + lane / kLanes;
-        const bool mine = head < a.heads;
-        const uint64_t at = ((uint64_t)min(head, a.heads - 1) * D + i0) * kSize<F32>;
+    angles<D>(s, i0, position, c, sn);
+    for (uint32_t g = first; g < end; ++g) {
         float lo[8], hi[8];
-        load8<F32>(x + at, a.vec, lo);
-        load8<F32>(x + at + D / 2 * kSize<F32>, a.vec, hi);
-        if (!have) angles<D>(s, i0, position, c, sn);
-        have = true;
+        next.get(lo, hi);
+        if (g + 1 < end) load16<D, F32>(x + at(g + 1), a.vec, next);
+        const uint32_t head = g * kHeads + sub;
         norm_rotate<D>(s, a, head >= a.n_q, i0, c, sn, lo, hi);
-        if (mine) {
-            store8<F32>(y + at, a.vec_y, lo);
-            store8<F32>(y + at + D / 2 * kSize<F32>, a.vec_y, hi);
+        if (head < a.heads) {
+            store8<F32>(y + at(g), a.vec_y, lo);
+            store8<F32>(y + at(g) + D / 2 * kSize<F32>, a.vec_y, hi);
         }
     }
 }
@@ -243,7 +255,7 @@ __device__ __forceinline__ bool finite(float v) { return (__float_as_uint(v) & 0
 // Codes of the block's first `bytes` bytes, held at a scale `ratio` times the new one.
 __device__ __forceinline__ void shift_codes(uint8_t* codes, uint32_t bytes, float ratio)
 {
-    for (uint32_t o = threadIdx.x * 8; o < bytes; o += kThreads * 8) {
+    for (uint32_t o = threadIdx.x * 8; o < bytes; o += kAppendThreads * 8) {
         uint32_t w[2];
         asm volatile("ld.global.v2.b32 {%0,%1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "l"(codes + o) : "memory");
         float f[8];
@@ -261,12 +273,13 @@ __device__ __forceinline__ void shift_codes(uint8_t* codes, uint32_t bytes, floa
     }
 }
 
-// One run of one head: keys normed and rotated, values as they are, both to codes.  TURNS: tokens a group of lanes takes.
+// One run of one head: keys normed and rotated, values as they are, both to codes.  TURNS: tokens a group of lanes takes; its one token's values
+// stay in registers until the scales are known, of several they are made twice (with two in registers the kernel takes twice as many).
 template <int D, bool F32, int TURNS>
 __device__ __forceinline__ void append_run(const HeadsArgs& a, const HeadsShared<D>& s, uint32_t cta)
 {
-    constexpr uint32_t kLanes = D / 16, kGroups = kThreads / kLanes;
-    __shared__ float s_most[2][kWarps];
+    constexpr uint32_t kLanes = D / 16, kGroups = kAppendThreads / kLanes;
+    __shared__ float s_most[2][kAppendThreads / 32];
     const uint32_t head = cta % a.n_kv;
     int4 run;
     asm volatile("ld.global.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(run.x), "=r"(run.y), "=r"(run.z), "=r"(run.w) : "l"(a.runs + cta / a.n_kv) : "memory");
@@ -275,42 +288,51 @@ __device__ __forceinline__ void append_run(const HeadsArgs& a, const HeadsShared
         return;
     const uint32_t lane = threadIdx.x & 31, i0 = (threadIdx.x % kLanes) * 8, group = threadIdx.x / kLanes;
     const uint64_t tile = (uint64_t)block * a.n_kv + head;
-    float k_lo[TURNS][8], k_hi[TURNS][8], v_lo[TURNS][8], v_hi[TURNS][8];
-    float k_most = 0.0f, v_most = 0.0f;
-    uint32_t poisoned = 0;
-#pragma unroll
-    for (int t = 0; t < TURNS; ++t) {
-        // (all lanes take part in the head's sums; those without a token take the run's last one)
-        const uint32_t j = min(group + t * kGroups, count - 1), row = row0 + j;
-        const char* x = (const char*)a.x + ((uint64_t)row * a.ldx + (uint64_t)(a.n_q + head) * D + i0) * kSize<F32>;
-        load8<F32>(x, a.vec, k_lo[t]);
-        load8<F32>(x + D / 2 * kSize<F32>, a.vec, k_hi[t]);
-        const uint64_t to_v = (uint64_t)a.n_kv * D * kSize<F32>;
-        load8<F32>(x + to_v, a.vec, v_lo[t]);
-        load8<F32>(x + to_v + D / 2 * kSize<F32>, a.vec, v_hi[t]);
+    float k_was = 0.0f, v_was = 0.0f;
+    if (start) {
+        k_was = *(const volatile float*)(a.k_scale + tile);
+        v_was = *(const volatile float*)(a.v_scale + tile);
     }
-#pragma unroll
-    for (int t = 0; t < TURNS; ++t) {
+    float k_lo[8], k_hi[8], v_lo[8], v_hi[8];
+    bool poisoned;
+    auto token = [&](int t) {
+        // (all lanes take part in the head's sums; those without a token take the run's last one)
         const uint32_t row = row0 + min(group + t * kGroups, count - 1);
+        const char* x = (const char*)a.x + ((uint64_t)row * a.ldx + (uint64_t)(a.n_q + head) * D + i0) * kSize<F32>;
+        Raw<F32> rk, rv;
+        load16<D, F32>(x, a.vec, rk);
+        load16<D, F32>(x + (uint64_t)a.n_kv * D * kSize<F32>, a.vec, rv);
         float c[8], sn[8];
         angles<D>(s, i0, ((const volatile int32_t*)a.positions)[row], c, sn);
-        norm_rotate<D>(s, a, 1, i0, c, sn, k_lo[t], k_hi[t]);
+        rk.get(k_lo, k_hi);
+        rv.get(v_lo, v_hi);
+        norm_rotate<D>(s, a, 1, i0, c, sn, k_lo, k_hi);
         bool all = true;
+        auto keep = [&](float& f) {
+            if (!finite(f)) {
+                all = false;
+                f = 0.0f;
+            }
+        };
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
-            float* const four[4] = {&k_lo[t][k], &k_hi[t][k], &v_lo[t][k], &v_hi[t][k]};
-#pragma unroll
-            for (int f = 0; f < 4; ++f) {
-                if (!finite(*four[f])) {
-                    all = false;
-                    *four[f] = 0.0f;
-                }
-            }
-            k_most = fmaxf(k_most, fmaxf(fabsf(k_lo[t][k]), fabsf(k_hi[t][k])));
-            v_most = fmaxf(v_most, fmaxf(fabsf(v_lo[t][k]), fabsf(v_hi[t][k])));
+            keep(k_lo[k]);
+            keep(k_hi[k]);
+            keep(v_lo[k]);
+            keep(v_hi[k]);
         }
         const uint32_t bad = __ballot_sync(0xFFFFFFFFu, !all);
-        if (bad >> (lane / kLanes * kLanes) & ((1u << kLanes) - 1)) poisoned |= 1u << t;
+        poisoned = bad >> (lane / kLanes * kLanes) & ((1u << kLanes) - 1);
+    };
+    float k_most = 0.0f, v_most = 0.0f;
+#pragma unroll 1
+    for (int t = 0; t < TURNS; ++t) {
+        token(t);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            k_most = fmaxf(k_most, fmaxf(fabsf(k_lo[k]), fabsf(k_hi[k])));
+            v_most = fmaxf(v_most, fmaxf(fabsf(v_lo[k]), fabsf(v_hi[k])));
+        }
     }
 #pragma unroll
     for (int o = 16; o; o >>= 1) {
@@ -321,14 +343,9 @@ __device__ __forceinline__ void append_run(const HeadsArgs& a, const HeadsShared
         s_most[0][threadIdx.x >> 5] = k_most;
         s_most[1][threadIdx.x >> 5] = v_most;
     }
-    float k_was = 0.0f, v_was = 0.0f;
-    if (start) {
-        k_was = *(const volatile float*)(a.k_scale + tile);
-        v_was = *(const volatile float*)(a.v_scale + tile);
-    }
     __syncthreads();
 #pragma unroll
-    for (int w = 0; w < kWarps; ++w) {
+    for (int w = 0; w < kAppendThreads / 32; ++w) {
         k_most = fmaxf(k_most, s_most[0][w]);
         v_most = fmaxf(v_most, s_most[1][w]);
     }
@@ -342,29 +359,32 @@ __device__ __forceinline__ void append_run(const HeadsArgs& a, const HeadsShared
     uint8_t* const v = a.v + tile * a.block_tokens * D;
     if (start && k_was != k_scale) shift_codes(k, start * D, k_was * k_inv);
     if (start && v_was != v_scale) shift_codes(v, start * D, v_was * v_inv);
-#pragma unroll
+#pragma unroll 1
     for (int t = 0; t < TURNS; ++t) {
+        if (TURNS > 1) token(t);
         const uint32_t j = group + t * kGroups;
-        if (j >= count) break;
-        const uint32_t o = (start + j) * D + i0;
+        if (j < count) {
+            const uint32_t o = (start + j) * D + i0;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            k_lo[t][i] *= k_inv;
-            k_hi[t][i] *= k_inv;
-            v_lo[t][i] *= v_inv;
-            v_hi[t][i] *= v_inv;
+            for (int i = 0; i < 8; ++i) {
+                k_lo[i] *= k_inv;
+                k_hi[i] *= k_inv;
+                v_lo[i] *= v_inv;
+                v_hi[i] *= v_inv;
+            }
+            uint2 first = pack8(k_lo);
+            if (poisoned && i0 == 0) first.x = (first.x & ~0xFFu) | 0x7Fu;
+            *(uint2*)(k + o) = first;
+            *(uint2*)(k + o + D / 2) = pack8(k_hi);
+            *(uint2*)(v + o) = pack8(v_lo);
+            *(uint2*)(v + o + D / 2) = pack8(v_hi);
         }
-        uint2 first = pack8(k_lo[t]);
-        if ((poisoned >> t & 1) && i0 == 0) first.x = (first.x & ~0xFFu) | 0x7Fu;
-        *(uint2*)(k + o) = first;
-        *(uint2*)(k + o + D / 2) = pack8(k_hi[t]);
-        *(uint2*)(v + o) = pack8(v_lo[t]);
-        *(uint2*)(v + o + D / 2) = pack8(v_hi[t]);
     }
 }
 
+// TURNS 0: x to y alone.  Otherwise the first CTAs take the runs, the others x to y.
 template <int D, bool F32, int TURNS>
-__global__ void __launch_bounds__(kThreads) heads_kernel(const __grid_constant__ HeadsArgs a)
+__global__ void __launch_bounds__(TURNS ? kAppendThreads : kThreads, TURNS ? 2 : 4) heads_kernel(const __grid_constant__ HeadsArgs a)
 {
     __shared__ HeadsShared<D> s;
     fill_turns<D>(s, a);
@@ -404,18 +424,19 @@ __global__ void __launch_bounds__(kThreads, 2) grad_kernel(const __grid_constant
 #pragma unroll
         for (int key = 0; key < 2; ++key) {
             const uint32_t first = key ? a.n_q : 0, heads = key ? a.n_kv : a.n_q;
-            float w[16];
-            if (a.q_norm) load_norm<D>(s, key, i0, w);
+            auto at_of = [&](uint32_t h0) { return ((uint64_t)(first + min(h0 + lane / kLanes, heads - 1)) * D + i0) * kSize<F32>; };
+            Raw<F32> next_dy, next_x;
+            load16<D, F32>(dy + at_of(0), a.vec, next_dy);
+            if (a.q_norm) load16<D, F32>(x + at_of(0), a.vec, next_x);
             for (uint32_t h0 = 0; h0 < heads; h0 += kHeads) {
-                const uint32_t h = h0 + lane / kLanes;
-                const bool mine = h < heads;
-                const uint64_t at = ((uint64_t)(first + min(h, heads - 1)) * D + i0) * kSize<F32>;
+                const bool mine = h0 + lane / kLanes < heads;
+                const uint64_t at = at_of(h0);
                 float v[2][8], g[2][8];
-                load8<F32>(dy + at, a.vec, g[0]);
-                load8<F32>(dy + at + D / 2 * kSize<F32>, a.vec, g[1]);
-                if (a.q_norm) {
-                    load8<F32>(x + at, a.vec, v[0]);
-                    load8<F32>(x + at + D / 2 * kSize<F32>, a.vec, v[1]);
+                next_dy.get(g[0], g[1]);
+                if (a.q_norm) next_x.get(v[0], v[1]);
+                if (h0 + kHeads < heads) {
+                    load16<D, F32>(dy + at_of(h0 + kHeads), a.vec, next_dy);
+                    if (a.q_norm) load16<D, F32>(x + at_of(h0 + kHeads), a.vec, next_x);
                 }
 #pragma unroll
                 for (int k = 0; k < 8; ++k) {
@@ -424,7 +445,8 @@ __global__ void __launch_bounds__(kThreads, 2) grad_kernel(const __grid_constant
                     g[1][k] = fmaf(u, c[k], -l * sn[k]);
                 }
                 if (a.q_norm) {
-                    float sum = 0.0f, dot = 0.0f;
+                    float sum = 0.0f, dot = 0.0f, w[16];
+                    load_norm<D>(s, key, i0, w);
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
                         const float f = v[i / 8][i % 8];
@@ -508,15 +530,11 @@ int launch(const char* what, K kernel, uint64_t ctas, int threads, cudaStream_t 
     return DR_OK;
 }
 
-template <int TURNS>
-int launch_heads(const dr_qk* qk, bool f32, const HeadsArgs& a, uint64_t ctas, cudaStream_t s)
+template <int D, int TURNS>
+int launch_heads(bool f32, const HeadsArgs& a, uint64_t ctas, cudaStream_t s)
 {
-    if (qk->d.head_dim == 64) {
-        if constexpr (TURNS <= 2)
-            return f32 ? launch("heads", heads_kernel<64, true, TURNS>, ctas, kThreads, s, a) : launch("heads", heads_kernel<64, false, TURNS>, ctas, kThreads, s, a);
-        return DR_ERR_UNSUPPORTED;  // (a block of 128 tokens is two turns of 64)
-    }
-    return f32 ? launch("heads", heads_kernel<128, true, TURNS>, ctas, kThreads, s, a) : launch("heads", heads_kernel<128, false, TURNS>, ctas, kThreads, s, a);
+    constexpr int threads = TURNS ? kAppendThreads : kThreads;
+    return f32 ? launch("heads", heads_kernel<D, true, TURNS>, ctas, threads, s, a) : launch("heads", heads_kernel<D, false, TURNS>, ctas, threads, s, a);
 }
 
 int check_qk(const dr_qk* qk)
@@ -583,13 +601,15 @@ HeadsArgs heads_args(const dr_qk* qk, const void* x, uint32_t dtype, uint64_t ld
     return a;
 }
 
-// How many warps a token's head groups are dealt to: one while the tokens alone fill the machine, so that it works out the angles once;
-// with few tokens every group has a warp of its own.
+constexpr uint32_t kWarpsWanted = 96;  // for each SM: three rounds of the 32 that run at a time
+
+// How many warps a token's head groups are dealt to: one while the tokens alone fill the machine some times over, so that it works out the
+// angles once; with few tokens every group has a warp of its own.
 void deal(HeadsArgs& a, int sms, uint32_t dim)
 {
     const uint32_t per_warp = 512 / dim, groups = (a.heads + per_warp - 1) / per_warp;
     a.parts = 1;
-    while (a.parts < groups && (uint64_t)a.rows * a.parts < (uint64_t)sms * 32) a.parts *= 2;
+    while (a.parts < groups && (uint64_t)a.rows * a.parts < (uint64_t)sms * kWarpsWanted) a.parts *= 2;
     if (a.parts > groups) a.parts = groups;
 }
 
@@ -672,7 +692,9 @@ int dr_qk_forward(const dr_qk* qk, const void* x_dev, uint32_t dtype, uint64_t l
     HeadsArgs a = heads_args(qk, x_dev, dtype, ldx, positions_dev, rows, y_dev, ldy);
     a.heads = a.n_q + a.n_kv;
     deal(a, qk->sms, qk->d.head_dim);
-    return launch_heads<0>(qk, dtype == DR_F32, a, (rows * a.parts + kWarps - 1) / kWarps, (cudaStream_t)cuda_stream);
+    const uint64_t ctas = (rows * a.parts + kWarps - 1) / kWarps;
+    cudaStream_t s = (cudaStream_t)cuda_stream;
+    return qk->d.head_dim == 64 ? launch_heads<64, 0>(dtype == DR_F32, a, ctas, s) : launch_heads<128, 0>(dtype == DR_F32, a, ctas, s);
 }
 
 int dr_qk_append(const dr_qk* qk, const void* x_dev, uint32_t dtype, uint64_t ldx, const int32_t* positions_dev, uint64_t rows,
@@ -712,16 +734,15 @@ int dr_qk_append(const dr_qk* qk, const void* x_dev, uint32_t dtype, uint64_t ld
     a.v_scale = cache->d.v_scale_dev;
     a.n_blocks = cache->d.n_blocks;
     a.block_tokens = cache->d.block_tokens;
-    const uint64_t cache_ctas = n_runs * d.n_kv_heads, ctas = cache_ctas + (rows * a.parts + kWarps - 1) / kWarps;
+    const uint64_t cache_ctas = n_runs * d.n_kv_heads, ctas = cache_ctas + (rows * a.parts + kAppendThreads / 32 - 1) / (kAppendThreads / 32);
     if (ctas > 0x7FFFFFFFull) {
         set_error("too many rows and runs for one launch");
         return DR_ERR_UNSUPPORTED;
     }
     a.cache_ctas = (uint32_t)cache_ctas;
-    const uint32_t turns = (a.block_tokens * (d.head_dim / 16) + kThreads - 1) / kThreads;
     cudaStream_t s = (cudaStream_t)cuda_stream;
-    if (turns == 1) return launch_heads<1>(qk, dtype == DR_F32, a, ctas, s);
-    return turns == 2 ? launch_heads<2>(qk, dtype == DR_F32, a, ctas, s) : launch_heads<4>(qk, dtype == DR_F32, a, ctas, s);
+    if (d.head_dim == 64) return launch_heads<64, 1>(dtype == DR_F32, a, ctas, s);  // (a block of 128 tokens is one turn)
+    return a.block_tokens <= 64 ? launch_heads<128, 1>(dtype == DR_F32, a, ctas, s) : launch_heads<128, 2>(dtype == DR_F32, a, ctas, s);
 }
 
 int dr_qk_grad_work(const dr_qk* qk, uint64_t* bytes)
