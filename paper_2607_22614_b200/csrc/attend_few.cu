@@ -64,6 +64,7 @@ struct Shared {
     alignas(1024) uint8_t v[kStages<SETS>][kTileTokens * D];
     float o[kConsumers][kRows<SETS>][D + 4];
     float m[kConsumers][kRows<SETS>], l[kConsumers][kRows<SETS>];
+    uint2 q[SETS < 3 ? 1 : SETS][D / 16][32];  // the rows' fragments, where registers do not hold them
     Meta meta[kStages<SETS>];
     uint64_t full[kStages<SETS>], empty[kStages<SETS>];
     Limit limit;
@@ -371,7 +372,8 @@ __device__ __forceinline__ void consume(const AttendArgs& a, Shared<D, SETS>& s,
 #pragma unroll
     for (int c = 0; c < kChunks / 2; ++c) addr[c] = swizzled<D>(my_row, 2 * c + my_chunk);
     // rows 2 tig and 2 tig + 1 of each set: [.][row][.]; o: dimensions 16 c + 2 g + {0, 1} at e = row + 2 dimension
-    uint32_t qf[SETS][kChunks][2];
+    constexpr bool kHeld = SETS < 3;  // the rows' fragments in registers: with three sets 400 bytes a thread would be spilled
+    uint32_t qf[kHeld ? SETS : 1][kChunks][2];
     float o[SETS][kChunks][4], m[SETS][2], l[SETS][2], back[SETS][2];
     int p[SETS][2];
     Turn<kStages<SETS>> ring;
@@ -384,7 +386,11 @@ __device__ __forceinline__ void consume(const AttendArgs& a, Shared<D, SETS>& s,
 #pragma unroll
             for (int n = 0; n < SETS; ++n) {
                 const Row row = row_of(a, meta, 8 * n + g);
-                const float undo = load_row<D>(a, row, qf[n]);
+                const float undo = load_row<D>(a, row, qf[kHeld ? n : 0]);
+                if (!kHeld && warp == n) {
+#pragma unroll
+                    for (int c = 0; c < kChunks; ++c) s.q[kHeld ? 0 : n][c][lane] = make_uint2(qf[0][c][0], qf[0][c][1]);
+                }
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     back[n][h] = __shfl_sync(0xFFFFFFFFu, undo, (2 * tig + h) * 4);
@@ -397,17 +403,16 @@ __device__ __forceinline__ void consume(const AttendArgs& a, Shared<D, SETS>& s,
 #pragma unroll
                     for (int e = 0; e < 4; ++e) o[n][c][e] = 0.0f;
             }
+            if (!kHeld) sync_consumers();  // (everybody has read the rows of the group before: the barriers at its end)
         }
         const int t0 = (int)(meta.token + warp * 16);
         if (meta.ok[warp] && t0 < (int)meta.len) {
             const uint32_t k_at = smem_u32(s.k[ring.slot]), v_at = smem_u32(s.v[ring.slot]);
-            // two chains of products, where there are registers for them
-            constexpr int kChains = SETS < 3 ? 2 : 1;
-            float x[SETS][4], odd[kChains == 2 ? SETS : 1][4];
+            float x[SETS][4], odd[SETS][4];  // two chains of products
 #pragma unroll
             for (int n = 0; n < SETS; ++n)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) x[n][e] = odd[kChains == 2 ? n : 0][e] = 0.0f;
+                for (int e = 0; e < 4; ++e) x[n][e] = odd[n][e] = 0.0f;
 #pragma unroll
             for (int c = 0; c < kChunks / 2; ++c) {
                 uint32_t r[4], f[2][4];
@@ -416,8 +421,14 @@ __device__ __forceinline__ void consume(const AttendArgs& a, Shared<D, SETS>& s,
                 for (int i = 0; i < 4; ++i) wide(r[i], f[i >> 1][i & 1], f[i >> 1][2 + (i & 1)]);
 #pragma unroll
                 for (int n = 0; n < SETS; ++n) {
-                    mma(x[n], f[0], qf[n][2 * c][0], qf[n][2 * c][1]);
-                    mma(kChains == 2 ? odd[kChains == 2 ? n : 0] : x[n], f[1], qf[n][2 * c + 1][0], qf[n][2 * c + 1][1]);
+                    if (kHeld) {
+                        mma(x[n], f[0], qf[kHeld ? n : 0][2 * c][0], qf[kHeld ? n : 0][2 * c][1]);
+                        mma(odd[n], f[1], qf[kHeld ? n : 0][2 * c + 1][0], qf[kHeld ? n : 0][2 * c + 1][1]);
+                    } else {
+                        const uint2 q0 = s.q[kHeld ? 0 : n][2 * c][lane], q1 = s.q[kHeld ? 0 : n][2 * c + 1][lane];
+                        mma(x[n], f[0], q0.x, q0.y);
+                        mma(odd[n], f[1], q1.x, q1.y);
+                    }
                 }
             }
             const float ks = meta.k_scale[warp], v_log = meta.v_log[warp];
@@ -429,7 +440,7 @@ __device__ __forceinline__ void consume(const AttendArgs& a, Shared<D, SETS>& s,
 #pragma unroll
             for (int n = 0; n < SETS; ++n)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) x[n][e] = fmaf(x[n][e] + odd[kChains == 2 ? n : 0][e], back[n][e & 1] * ks, v_log);
+                for (int e = 0; e < 4; ++e) x[n][e] = fmaf(x[n][e] + odd[n][e], back[n][e & 1] * ks, v_log);
             if (!all) {
 #pragma unroll
                 for (int n = 0; n < SETS; ++n)
