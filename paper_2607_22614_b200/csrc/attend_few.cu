@@ -31,10 +31,13 @@ using namespace tc;
 
 __device__ unsigned long long g_wait_failures;  // read by dr_diag_linear_wait_failures
 
-constexpr uint32_t kConsumers = 4, kThreads = 32 * (kConsumers + 1), kCtasPerSm = 2;
+constexpr uint32_t kConsumers = 4, kThreads = 32 * (kConsumers + 1);
 constexpr int kMaxSets = 3;                    // of eight rows in a group
 template <int SETS> constexpr uint32_t kRows = 8 * SETS;
-template <int SETS> constexpr uint32_t kStages = 6 - SETS;  // the rest of two CTAs' shared memory goes to the warps' outputs
+// CTAs on an SM and their stages, the rest of whose shared memory goes to the warps' outputs: three hide the products' latency better than
+// two (WHAT), for which more rows leave no registers
+template <int SETS> constexpr uint32_t kCtasPerSm = SETS == 1 ? 3 : 2;
+template <int SETS> constexpr uint32_t kStages = SETS == 1 ? 3 : 6 - SETS;
 constexpr float kTop = 11.0f, kLag = 4.0f;     // log2 of p at the running maximum in fp16, and how far a p may be above it
 constexpr float kLeastScale = 7.8886091e-31f;  // 2^-100
 
@@ -65,6 +68,8 @@ struct Shared {
     float o[kConsumers][kRows<SETS>][D + 4];
     float m[kConsumers][kRows<SETS>], l[kConsumers][kRows<SETS>];
     uint2 q[SETS < 3 ? 1 : SETS][D / 16][32];  // the rows' fragments, where registers do not hold them
+    float back[kRows<SETS>];
+    int p[kRows<SETS>];
     Meta meta[kStages<SETS>];
     uint64_t full[kStages<SETS>], empty[kStages<SETS>];
     Limit limit;
@@ -72,9 +77,8 @@ struct Shared {
     uint64_t offset;
     uint32_t request;
 };
-static_assert(kCtasPerSm * (sizeof(Shared<128, 1>) + 1024) <= 228 * 1024 && kCtasPerSm * (sizeof(Shared<128, 2>) + 1024) <= 228 * 1024 &&
-                  kCtasPerSm * (sizeof(Shared<128, 3>) + 1024) <= 228 * 1024,
-              "shared memory of an SM");
+template <int SETS> constexpr bool kFits = kCtasPerSm<SETS> * (sizeof(Shared<128, SETS>) + 1024) <= 228 * 1024;
+static_assert(kFits<1> && kFits<2> && kFits<3>, "shared memory of an SM");
 
 template <int SETS>
 __device__ __forceinline__ uint32_t groups_of(const AttendArgs& a, uint32_t n)
@@ -146,7 +150,7 @@ __device__ __forceinline__ uint32_t half2_of(float lo, float hi)
 }
 __device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
 {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
@@ -160,7 +164,7 @@ __device__ __forceinline__ float exp2_of(float x)
 __device__ __forceinline__ uint32_t transposed(uint32_t v)
 {
     uint32_t d;
-    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(v));
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(v));
     return d;
 }
 __device__ __forceinline__ void sync_consumers() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
@@ -374,8 +378,7 @@ __device__ __forceinline__ void consume(const AttendArgs& a, Shared<D, SETS>& s,
     // rows 2 tig and 2 tig + 1 of each set: [.][row][.]; o: dimensions 16 c + 2 g + {0, 1} at e = row + 2 dimension
     constexpr bool kHeld = SETS < 3;  // the rows' fragments in registers: with three sets 400 bytes a thread would be spilled
     uint32_t qf[kHeld ? SETS : 1][kChunks][2];
-    float o[SETS][kChunks][4], m[SETS][2], l[SETS][2], back[SETS][2];
-    int p[SETS][2];
+    float o[SETS][kChunks][4], m[SETS][2], l[SETS][2];
     Turn<kStages<SETS>> ring;
     for (;;) {
         if (!__all_sync(0xFFFFFFFFu, bar_wait(full + 8 * ring.slot, ring.round, &s.limit, &g_wait_failures))) return;
@@ -387,14 +390,16 @@ __device__ __forceinline__ void consume(const AttendArgs& a, Shared<D, SETS>& s,
             for (int n = 0; n < SETS; ++n) {
                 const Row row = row_of(a, meta, 8 * n + g);
                 const float undo = load_row<D>(a, row, qf[kHeld ? n : 0]);
+                if (warp == 0 && tig == 0) {
+                    s.back[8 * n + g] = undo;
+                    s.p[8 * n + g] = row.p;
+                }
                 if (!kHeld && warp == n) {
 #pragma unroll
                     for (int c = 0; c < kChunks; ++c) s.q[kHeld ? 0 : n][c][lane] = make_uint2(qf[0][c][0], qf[0][c][1]);
                 }
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    back[n][h] = __shfl_sync(0xFFFFFFFFu, undo, (2 * tig + h) * 4);
-                    p[n][h] = __shfl_sync(0xFFFFFFFFu, row.p, (2 * tig + h) * 4);
                     m[n][h] = -INFINITY;
                     l[n][h] = 0.0f;
                 }
@@ -403,7 +408,7 @@ __device__ __forceinline__ void consume(const AttendArgs& a, Shared<D, SETS>& s,
 #pragma unroll
                     for (int e = 0; e < 4; ++e) o[n][c][e] = 0.0f;
             }
-            if (!kHeld) sync_consumers();  // (everybody has read the rows of the group before: the barriers at its end)
+            sync_consumers();  // (everybody has read the rows of the group before: the barriers at its end)
         }
         const int t0 = (int)(meta.token + warp * 16);
         if (meta.ok[warp] && t0 < (int)meta.len) {
@@ -413,12 +418,19 @@ __device__ __forceinline__ void consume(const AttendArgs& a, Shared<D, SETS>& s,
             for (int n = 0; n < SETS; ++n)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) x[n][e] = odd[n][e] = 0.0f;
+            // all of the keys' loads, and where there are registers the values', are on their way before the first product
+            uint32_t kr[kChunks / 2][4], vr[kChunks / 2][4];
+#pragma unroll
+            for (int c = 0; c < kChunks / 2; ++c) ldmatrix(k_at + addr[c], kr[c]);
+            if (kHeld) {
+#pragma unroll
+                for (int c = 0; c < kChunks / 2; ++c) ldmatrix_t(v_at + addr[c], vr[c]);
+            }
 #pragma unroll
             for (int c = 0; c < kChunks / 2; ++c) {
-                uint32_t r[4], f[2][4];
-                ldmatrix(k_at + addr[c], r);
+                uint32_t f[2][4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) wide(r[i], f[i >> 1][i & 1], f[i >> 1][2 + (i & 1)]);
+                for (int i = 0; i < 4; ++i) wide(kr[c][i], f[i >> 1][i & 1], f[i >> 1][2 + (i & 1)]);
 #pragma unroll
                 for (int n = 0; n < SETS; ++n) {
                     if (kHeld) {
@@ -431,6 +443,10 @@ __device__ __forceinline__ void consume(const AttendArgs& a, Shared<D, SETS>& s,
                     }
                 }
             }
+            if (!kHeld) {
+#pragma unroll
+                for (int c = 0; c < kChunks / 2; ++c) ldmatrix_t(v_at + addr[c], vr[c]);
+            }
             const float ks = meta.k_scale[warp], v_log = meta.v_log[warp];
             bool grows = false;
             // whether every row sees all sixteen tokens: rows ascend in position, and the last one's is at most len - 1
@@ -440,13 +456,17 @@ __device__ __forceinline__ void consume(const AttendArgs& a, Shared<D, SETS>& s,
 #pragma unroll
             for (int n = 0; n < SETS; ++n)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) x[n][e] = fmaf(x[n][e] + odd[n][e], back[n][e & 1] * ks, v_log);
+                for (int h = 0; h < 2; ++h) {
+                    const float f = s.back[8 * n + 2 * tig + h] * ks;
+                    x[n][h] = fmaf(x[n][h] + odd[n][h], f, v_log);
+                    x[n][h + 2] = fmaf(x[n][h + 2] + odd[n][h + 2], f, v_log);
+                }
             if (!all) {
 #pragma unroll
                 for (int n = 0; n < SETS; ++n)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        const int t = t0 + (int)g + 8 * (e >> 1), at = p[n][e & 1];
+                        const int t = t0 + (int)g + 8 * (e >> 1), at = s.p[8 * n + 2 * tig + (e & 1)];
                         if (t > at || (a.window && t <= at - (int)a.window && t >= (int)a.sinks)) x[n][e] = -INFINITY;
                     }
 #pragma unroll
@@ -490,10 +510,9 @@ __device__ __forceinline__ void consume(const AttendArgs& a, Shared<D, SETS>& s,
             }
 #pragma unroll
             for (int c = 0; c < kChunks / 2; ++c) {
-                uint32_t r[4], f[2][4];
-                ldmatrix_t(v_at + addr[c], r);
+                uint32_t f[2][4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) wide(__byte_perm(r[i] & keep[i & 1], 0, 0x3120), f[i >> 1][2 * (i & 1)], f[i >> 1][2 * (i & 1) + 1]);
+                for (int i = 0; i < 4; ++i) wide(__byte_perm(vr[c][i] & keep[i & 1], 0, 0x3120), f[i >> 1][2 * (i & 1)], f[i >> 1][2 * (i & 1) + 1]);
 #pragma unroll
                 for (int n = 0; n < SETS; ++n) {
                     mma(o[n][2 * c], f[0], pf[n][0], pf[n][1]);
@@ -527,7 +546,7 @@ __device__ __forceinline__ void consume(const AttendArgs& a, Shared<D, SETS>& s,
 }
 
 template <int D, int SETS>
-__global__ void __launch_bounds__(kThreads, kCtasPerSm)
+__global__ void __launch_bounds__(kThreads, kCtasPerSm<SETS>)
     few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map, const __grid_constant__ AttendArgs a,
                Part<D, SETS>* parts, Join* joins)
 {
@@ -682,12 +701,13 @@ __global__ void __launch_bounds__(32 * kJoinRows * kJoinWarps) join_kernel(const
     for (int d = 0; d < kOwn; ++d) out[d] = (uint16_t)pack_bf16(o[d] * norm, 0.0f);
 }
 
-uint32_t ctas_of(const dr_kv_cache* cache) { return kCtasPerSm * (uint32_t)cache->sms; }
+template <int SETS>
+uint64_t ctas_of(const dr_kv_cache* cache) { return kCtasPerSm<SETS> * (uint64_t)cache->sms; }
 
 template <int D, int SETS>
 int launch_few(const dr_kv_cache* cache, const AttendArgs& a, void* work, cudaStream_t stream)
 {
-    const uint32_t ctas = ctas_of(cache);
+    const uint32_t ctas = (uint32_t)ctas_of<SETS>(cache);
     Part<D, SETS>* parts = (Part<D, SETS>*)work;
     Join* joins = (Join*)(parts + 2 * (uint64_t)ctas);
     cudaLaunchAttribute attr = overlap_attribute();
@@ -743,11 +763,14 @@ int prepare_attend_few()
     return rc;
 }
 
-uint64_t attend_few_work(const dr_kv_cache* cache)
+template <int D>
+uint64_t few_work(const dr_kv_cache* cache)
 {
-    const uint64_t ctas = ctas_of(cache);
-    return ctas * (2 * (cache->d.head_dim == 64 ? sizeof(Part<64, kMaxSets>) : sizeof(Part<128, kMaxSets>)) + sizeof(Join));
+    const uint64_t one = ctas_of<1>(cache) * (2 * sizeof(Part<D, 1>) + sizeof(Join)), two = ctas_of<2>(cache) * (2 * sizeof(Part<D, 2>) + sizeof(Join)),
+                   three = ctas_of<3>(cache) * (2 * sizeof(Part<D, 3>) + sizeof(Join));
+    return one > two ? (one > three ? one : three) : two > three ? two : three;
 }
+uint64_t attend_few_work(const dr_kv_cache* cache) { return cache->d.head_dim == 64 ? few_work<64>(cache) : few_work<128>(cache); }
 
 int launch_attend_few(const dr_kv_cache* cache, const AttendArgs& a, void* work, cudaStream_t stream)
 {
