@@ -11,10 +11,18 @@ import math
 from . import binding as B
 
 
-def _ints(t, what, n, device):
-    """The address of a contiguous int32 vector of n on GPU `device`."""
+_int32 = _bfloat16 = _uint8 = None  # torch's, from the first object on: an import in a call takes 0.2 us
+
+
+def _types():
+    global _int32, _bfloat16, _uint8
     import torch
-    if t.dtype != torch.int32 or t.dim() != 1 or t.shape[0] != n or not t.is_contiguous():
+    _int32, _bfloat16, _uint8 = torch.int32, torch.bfloat16, torch.uint8
+
+
+def _ints(t, what, n, device):
+    """The address of n contiguous int32 on GPU `device`."""
+    if t.dtype is not _int32 or t.numel() != n or not t.is_contiguous():
         raise ValueError(f"{what} must be {n} contiguous int32")
     if t.get_device() != device:
         raise B._elsewhere(t, what, device)
@@ -29,9 +37,8 @@ def _check_device(t, what):
 
 
 def _table(table, requests, device):
-    import torch
     rows, width, ld = B._matrix(table, "table", device)
-    if table.dtype != torch.int32 or rows != requests:
+    if table.dtype is not _int32 or rows != requests:
         raise ValueError(f"table must be int32 with {requests} rows")
     return width, ld
 
@@ -42,6 +49,7 @@ class KVCache:
 
     def __init__(self, k, v, k_scale, v_scale):
         import torch
+        _types()
         self.device = _check_device(k, "k")
         for t, what in ((k, "k"), (v, "v")):
             if t.get_device() != self.device:
@@ -92,11 +100,10 @@ class KVCache:
         [requests], table [requests, width], free [blocks], state [2] (free blocks, requests refused) are int32; lengths and state are
         updated in place unless lengths_out and state_out are given; rows: the step's rows.  Returns (offsets [requests + 1],
         positions [rows], runs [runs_for(requests, rows), 4])."""
-        import torch
         device = self.device
         if device != B._current_device():
             raise B._not_current(self.k, "the cache")
-        n = lengths.shape[0] if lengths.dim() == 1 else -1
+        n = lengths.numel()
         p_added, p_lengths = _ints(added, "added", n, device), _ints(lengths, "lengths", n, device)
         p_out = p_lengths if lengths_out is None else _ints(lengths_out, "lengths_out", n, device)
         p_free, p_state = _ints(free, "free", self.n_blocks, device), _ints(state, "state", 2, device)
@@ -104,13 +111,12 @@ class KVCache:
         width, ld = _table(table, n, device)
         if rows < 0:
             raise ValueError("rows must not be negative")
-        n_runs = self.runs_for(n, rows)
         if offsets is None:
-            offsets = B._empty(1, n + 1, torch.int32, lengths.device, stream).view(-1)
+            offsets = B._empty(1, n + 1, _int32, lengths.device, stream).view(-1)
         if positions is None:
-            positions = B._empty(1, rows, torch.int32, lengths.device, stream).view(-1)
+            positions = B._empty(1, rows, _int32, lengths.device, stream).view(-1)
         if runs is None:
-            runs = B._empty(n_runs, 4, torch.int32, lengths.device, stream)
+            runs = B._empty(self.runs_for(n, rows), 4, _int32, lengths.device, stream)
         p_runs, n_runs = self._runs(runs)
         rc = B._fn("dr_kv_extend")(self.handle, p_added, p_lengths, p_out, n, table.data_ptr(), ld, width, p_free, p_state, p_state_out,
                                    rows, _ints(offsets, "offsets", n + 1, device), _ints(positions, "positions", rows, device), p_runs, n_runs,
@@ -120,12 +126,12 @@ class KVCache:
         return offsets, positions, runs
 
     def _runs(self, runs):
-        import torch
-        if runs.dtype != torch.int32 or runs.dim() != 2 or runs.shape[1] != 4 or not runs.is_contiguous():
+        n, four = runs.shape
+        if runs.dtype is not _int32 or four != 4 or not runs.is_contiguous():
             raise ValueError("runs must be contiguous int32 of four columns")
         if runs.get_device() != self.device:
             raise B._elsewhere(runs, "runs", self.device)
-        return runs.data_ptr(), runs.shape[0]
+        return runs.data_ptr(), n
 
     def attend(self, q, lengths, table, offsets=None, *, window=0, sinks=0, scale=None, out=None, stream=None):
         """dr_attend: q [rows, query heads * head dim] (bf16; any number of rows apart, so the query columns of a qkv product will do),
@@ -133,42 +139,38 @@ class KVCache:
         request) -> out [rows, query heads * head dim] bf16.  A token sees those before it and itself; window > 0: the last `window` of
         them and the first `sinks`.  scale: head_dim ** -0.5 by default.  Rows of an allocated output that no request owns are not
         initialised."""
-        import torch
         device = q.get_device()
         if device != self.device or device != B._current_device():
             raise B._elsewhere(q, "q", self.device) if device != self.device else B._not_current(q, "q")
         if q.requires_grad:
             _refuse("q")
         rows, cols, ldq = B._matrix(q, "q", device)
-        if q.dtype != torch.bfloat16:
+        if q.dtype is not _bfloat16:
             raise TypeError(f"q must be bfloat16, not {q.dtype}")
         n_q = cols // self.head_dim
         if cols % self.head_dim or n_q < 1 or n_q % self.kv_heads:
             raise ValueError(f"q must hold heads of {self.head_dim}, a multiple of the cache's {self.kv_heads}")
         if window < 0 or sinks < 0:
             raise ValueError("window and sinks must not be negative")
-        n = lengths.shape[0] if lengths.dim() == 1 else -1
+        n = lengths.numel()
         p_lengths = _ints(lengths, "lengths", n, device)
         p_offsets = None if offsets is None else _ints(offsets, "offsets", n + 1, device)
         if offsets is None and rows != n:
             raise ValueError("without offsets q has one row for each request")
         width, ld = _table(table, n, device)
         if out is None:
-            out, ldo = B._empty(rows, cols, torch.bfloat16, q.device, stream), cols
+            out, ldo = B._empty(rows, cols, _bfloat16, q.device, stream), cols
         else:
             got_rows, got_cols, ldo = B._matrix(out, "out", device)
-            if got_rows != rows or got_cols != cols or out.dtype != torch.bfloat16:
+            if got_rows != rows or got_cols != cols or out.dtype is not _bfloat16:
                 raise ValueError(f"out must be bfloat16, {rows} x {cols}")
-        key = (n_q, n, rows)
-        need = self._work.get(key)
+        need = self._work.get(n_q)  # (the library checks the other sizes, and that this is enough)
         if need is None:
             rc, need = B.dr_attend_work(self.handle, n_q, n, rows)
             if rc:
                 raise B.DrError(rc, "dr_attend_work")
-            if len(self._work) > 1000:
-                self._work.clear()
-            self._work[key] = need
-        work = B._empty(1, need, torch.uint8, q.device, stream)
+            self._work[n_q] = need
+        work = B._empty(1, need, _uint8, q.device, stream)
         rc = B._fn("dr_attend")(self.handle, q.data_ptr(), ldq, n_q, rows, p_offsets, p_lengths, n, table.data_ptr(), ld, width,
                                 1.0 / math.sqrt(self.head_dim) if scale is None else scale, window, sinks, out.data_ptr(), ldo,
                                 work.data_ptr(), need, B._stream_of(device, stream))
@@ -189,6 +191,7 @@ class QKHeads:
     None: no norm) and the rotation by position, base^(-2 i / head_dim) for pair (i, i + head_dim / 2).  Keeps references to the norms."""
 
     def __init__(self, n_q_heads, n_kv_heads, head_dim, q_norm=None, k_norm=None, *, base=1e6, eps=1e-6):
+        _types()
         self.n_q_heads, self.n_kv_heads, self.head_dim, self.q_norm, self.k_norm = n_q_heads, n_kv_heads, head_dim, q_norm, k_norm
         self.device = None
         if q_norm is not None or k_norm is not None:
@@ -211,6 +214,7 @@ class QKHeads:
             self.handle = None
             raise B.DrError(rc, "dr_qk_create")
         self._work = None
+        self._norms = () if q_norm is None else (q_norm, k_norm)
 
     def close(self):
         if getattr(self, "handle", None):
@@ -225,7 +229,8 @@ class QKHeads:
         device = x.get_device()
         if device != self.device or device != B._current_device():
             raise B._elsewhere(x, what, self.device) if device != self.device else B._not_current(x, what)
-        if record and (x.requires_grad or (self.q_norm is not None and (self.q_norm.requires_grad or self.k_norm.requires_grad))):
+        norms = self._norms
+        if record and (x.requires_grad or (norms and (norms[0].requires_grad or norms[1].requires_grad))):
             _refuse(f"{what} or a norm")
         rows, cols, ld = B._matrix(x, what, device)
         if cols < heads * self.head_dim:

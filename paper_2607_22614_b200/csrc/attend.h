@@ -18,6 +18,7 @@ struct AttendArgs {
     float scale;             // of the logits, times log2(e)
     uint32_t vec_q, vec_out;  // rows of q and out start on 16 bytes: 2, on 8: 1, neither: 0
     uint32_t limit_us, starve;
+    uint32_t whole;  // few rows: groups are not divided between CTAs
 };
 
 constexpr uint32_t kTileTokens = 64;  // of the cache that a step of the few-row kernel takes

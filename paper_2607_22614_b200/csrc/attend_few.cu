@@ -32,7 +32,6 @@ using namespace tc;
 __device__ unsigned long long g_wait_failures;  // read by dr_diag_linear_wait_failures
 
 constexpr uint32_t kConsumers = 4, kThreads = 32 * (kConsumers + 1);
-constexpr int kMaxSets = 3;                    // of eight rows in a group
 template <int SETS> constexpr uint32_t kRows = 8 * SETS;
 // CTAs on an SM and their stages, the rest of whose shared memory goes to the warps' outputs: three hide the products' latency better than
 // two (WHAT), for which more rows leave no registers
@@ -71,7 +70,7 @@ struct Shared {
     float back[kRows<SETS>];
     int p[kRows<SETS>];
     Meta meta[kStages<SETS>];
-    uint64_t full[kStages<SETS>], empty[kStages<SETS>];
+    uint64_t full[kStages<SETS>], empty[kStages<SETS>], met;
     Limit limit;
     uint64_t sums[kThreads / 32];
     uint64_t offset;
@@ -97,7 +96,7 @@ __device__ __forceinline__ uint64_t cost_of(const AttendArgs& a, uint32_t r)
     if (r >= a.requests) return 0;
     const Request q = request_of(a, r);
     if (q.n * a.group > kFewRows) return 0;
-    return (uint64_t)a.n_kv * groups_of<SETS>(a, q.n) * tiles_of_request(a, q).count;
+    return (uint64_t)a.n_kv * groups_of<SETS>(a, q.n) * (a.whole ? 1 : tiles_of_request(a, q).count);
 }
 
 // Exclusive sum over the CTA's threads and the total.
@@ -167,7 +166,16 @@ __device__ __forceinline__ uint32_t transposed(uint32_t v)
     asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(v));
     return d;
 }
-__device__ __forceinline__ void sync_consumers() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
+// The four consuming warps meet; false where one of them has given up.
+template <class S>
+__device__ __forceinline__ bool meet(S& s, uint32_t& round)
+{
+    __syncwarp();
+    if ((threadIdx.x & 31) == 0) bar_arrive(smem_u32(&s.met));
+    const bool ok = __all_sync(0xFFFFFFFFu, bar_wait(smem_u32(&s.met), round, &s.limit, &g_wait_failures));
+    round ^= 1;
+    return ok;
+}
 
 // Walks the CTA's tiles: finds blocks and scales eight tiles at a time (a lane for each sixteen tokens) and starts the copies.
 template <int D, int SETS>
@@ -185,10 +193,11 @@ __device__ __forceinline__ void produce(const AttendArgs& a, Shared<D, SETS>& s,
         const Tiles tiles = tiles_of_request(a, q);
         const uint64_t cost = cost_of<SETS>(a, r);
         while (at < end && offset < cost) {
-            const uint64_t segment = offset / tiles.count;
-            const uint32_t tile0 = (uint32_t)(offset - segment * tiles.count);
+            const uint32_t per = a.whole ? 1 : tiles.count;
+            const uint64_t segment = offset / per;
+            const uint32_t tile0 = (uint32_t)(offset - segment * per);
             const uint32_t head = (uint32_t)(segment / groups), rows0 = (uint32_t)(segment % groups) * kRows<SETS>;
-            const uint32_t count = (uint32_t)min((uint64_t)(tiles.count - tile0), end - at);
+            const uint32_t count = a.whole ? tiles.count : (uint32_t)min((uint64_t)(tiles.count - tile0), end - at);
             const uint32_t have = tile0 ? kTail : count < tiles.count ? kHead : kWhole;
             for (uint32_t t0 = 0; t0 < count; t0 += 8) {
                 const uint32_t i = tile0 + t0 + lane / 4, token = tiles.at(i) * kTileTokens + (lane & 3) * 16;
@@ -237,8 +246,8 @@ __device__ __forceinline__ void produce(const AttendArgs& a, Shared<D, SETS>& s,
                     ring.next();
                 }
             }
-            at += count;
-            offset += count;
+            at += a.whole ? 1 : count;
+            offset += a.whole ? 1 : count;
         }
         ++r;
         offset = 0;
@@ -380,6 +389,7 @@ __device__ __forceinline__ void consume(const AttendArgs& a, Shared<D, SETS>& s,
     uint32_t qf[kHeld ? SETS : 1][kChunks][2];
     float o[SETS][kChunks][4], m[SETS][2], l[SETS][2];
     Turn<kStages<SETS>> ring;
+    uint32_t met = 0;
     for (;;) {
         if (!__all_sync(0xFFFFFFFFu, bar_wait(full + 8 * ring.slot, ring.round, &s.limit, &g_wait_failures))) return;
         const Meta& meta = s.meta[ring.slot];
@@ -408,7 +418,7 @@ __device__ __forceinline__ void consume(const AttendArgs& a, Shared<D, SETS>& s,
 #pragma unroll
                     for (int e = 0; e < 4; ++e) o[n][c][e] = 0.0f;
             }
-            sync_consumers();  // (everybody has read the rows of the group before: the barriers at its end)
+            if (!meet(s, met)) return;  // (everybody has read the rows of the group before: they met at its end)
         }
         const int t0 = (int)(meta.token + warp * 16);
         if (meta.ok[warp] && t0 < (int)meta.len) {
@@ -535,9 +545,9 @@ __device__ __forceinline__ void consume(const AttendArgs& a, Shared<D, SETS>& s,
 #pragma unroll
                     for (int c = 0; c < kChunks; ++c) *(float2*)&s.o[warp][row][16 * c + 2 * g] = make_float2(o[n][c][h], o[n][c][h + 2]);
                 }
-            sync_consumers();
+            if (!meet(s, met)) return;
             write_group<D, SETS>(a, s, meta, parts);
-            sync_consumers();
+            if (!meet(s, met)) return;
         }
         __syncwarp();
         if (lane == 0) bar_arrive(empty + 8 * ring.slot);
@@ -564,33 +574,44 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm<SETS>)
             bar_init(smem_u32(&s.full[i]), 1);
             bar_init(smem_u32(&s.empty[i]), kConsumers);
         }
+        bar_init(smem_u32(&s.met), kConsumers);
         s.limit.stop = 0;
         s.limit.us = a.limit_us;
         bar_init_fence();
     }
     after_previous();
     // all tiles of the call, the CTA's share of them, and the request that it begins in
-    uint64_t mine = 0, total, unused;
-    for (uint32_t r = threadIdx.x; r < a.requests; r += kThreads) mine += cost_of<SETS>(a, r);
-    scan(s, mine, total);
+    const uint64_t own = cost_of<SETS>(a, threadIdx.x);
+    uint64_t all, total = 0;
+    const uint64_t first = scan(s, own, all);
+    total = all;
+    if (a.requests > kThreads) {
+        uint64_t mine = 0, rest;
+        for (uint32_t r = kThreads + threadIdx.x; r < a.requests; r += kThreads) mine += cost_of<SETS>(a, r);
+        scan(s, mine, rest);
+        total += rest;
+    }
     const uint64_t ctas = min((uint64_t)gridDim.x, total), cta = blockIdx.x;
     const uint64_t begin = cta < ctas ? total * cta / ctas : total, end = cta < ctas ? total * (cta + 1) / ctas : total;
     if (begin < end) {
-        uint64_t base = 0;
-        for (uint32_t r0 = 0; base <= begin; r0 += kThreads) {
-            const uint64_t c = cost_of<SETS>(a, r0 + threadIdx.x), before = base + scan(s, c, unused);
+        uint64_t c = own, before = first, base = all;  // base: of all up to and with the chunk at hand
+        for (uint32_t r0 = 0;;) {
             if (before <= begin && begin < before + c) {
                 s.request = r0 + threadIdx.x;
                 s.offset = begin - before;
             }
-            base += unused;
+            if (base > begin) break;
+            r0 += kThreads;
+            c = cost_of<SETS>(a, r0 + threadIdx.x);
+            before = base + scan(s, c, all);
+            base += all;
         }
     }
     __syncthreads();
     if (threadIdx.x == 0) {
         // a group that an earlier CTA has begun: the CTA behind the one that began it has it joined
         Join j{};
-        if (begin < end && s.offset) {
+        if (begin < end && s.offset && !a.whole) {
             const Request q = request_of(a, s.request);
             const uint32_t groups = groups_of<SETS>(a, q.n), tiles = tiles_of_request(a, q).count;
             const uint64_t segment = s.offset / tiles, inside = s.offset - segment * tiles, first = begin - inside, last = first + tiles;
@@ -602,7 +623,7 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm<SETS>)
                 j.rows0 = (uint32_t)(segment % groups) * kRows<SETS>;
             }
         }
-        joins[cta] = j;
+        if (!a.whole) joins[cta] = j;
     }
     if (begin < end) {
         if (warp == kConsumers)
@@ -614,17 +635,18 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm<SETS>)
     let_copies_end(&s.limit);
 }
 
-// The parts of a group that several CTAs have, added in an order of their own: four rows a CTA, a row by four warps that take a quarter
-// of the parts each, with the loads of eight parts on their way (74 parts one after another took 30 us).
-constexpr uint32_t kJoinRows = 4, kJoinWarps = 4;
-template <int D, int SETS>
-__global__ void __launch_bounds__(32 * kJoinRows * kJoinWarps) join_kernel(const __grid_constant__ AttendArgs a, const Part<D, SETS>* parts, const Join* joins)
+// The parts of a group that several CTAs have, added in an order of their own: eight rows a CTA and a warp for each where a group has few
+// parts, four rows and four warps for each where it has many (74 parts one after another took 30 us); eight parts' loads are on their
+// way together.
+template <int WARPS> constexpr uint32_t kJoinRows = WARPS == 1 ? 8 : 4;
+template <int D, int SETS, int WARPS>
+__global__ void __launch_bounds__(32 * kJoinRows<WARPS> * WARPS) join_kernel(const __grid_constant__ AttendArgs a, const Part<D, SETS>* parts, const Join* joins)
 {
     constexpr int kOwn = D / 32;  // dimensions a lane has, side by side
-    __shared__ float s_m[kJoinRows][kJoinWarps], s_l[kJoinRows][kJoinWarps], s_o[kJoinRows][kJoinWarps][D];
+    __shared__ float s_m[kJoinRows<WARPS>][WARPS], s_l[kJoinRows<WARPS>][WARPS], s_o[kJoinRows<WARPS>][WARPS][D];
     after_previous();
-    const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5, r = warp / kJoinWarps, w = warp % kJoinWarps, cta = blockIdx.x;
-    const uint32_t i = blockIdx.y * kJoinRows + r;
+    const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5, r = warp / WARPS, w = warp % WARPS, cta = blockIdx.x;
+    const uint32_t i = blockIdx.y * kJoinRows<WARPS> + r;
     const uint32_t count = *(const volatile uint32_t*)&joins[cta].count;
     if (count == 0) return;
     Meta m;
@@ -638,11 +660,11 @@ __global__ void __launch_bounds__(32 * kJoinRows * kJoinWarps) join_kernel(const
     auto part = [&](uint32_t k) -> const Part<D, SETS>& { return parts[(cta - 1 + k) * 2 + (k == 0)]; };
     float most = -INFINITY, l = 0.0f, o[kOwn] = {};
     if (row.real) {
-        for (uint32_t k0 = w; k0 < count; k0 += 8 * kJoinWarps) {
+        for (uint32_t k0 = w; k0 < count; k0 += 8 * WARPS) {
             float pm[8], pl[8], po[8][kOwn];
 #pragma unroll
             for (int u = 0; u < 8; ++u) {
-                const uint32_t k = k0 + u * kJoinWarps;
+                const uint32_t k = k0 + u * WARPS;
                 pm[u] = -INFINITY;
                 pl[u] = 0.0f;
                 for (int d = 0; d < kOwn; ++d) po[u][d] = 0.0f;
@@ -683,13 +705,13 @@ __global__ void __launch_bounds__(32 * kJoinRows * kJoinWarps) join_kernel(const
     if (w || !row.real) return;
     most = -INFINITY;
 #pragma unroll
-    for (uint32_t k = 0; k < kJoinWarps; ++k) most = fmaxf(most, s_m[r][k]);
+    for (uint32_t k = 0; k < WARPS; ++k) most = fmaxf(most, s_m[r][k]);
     const float safe = most == -INFINITY ? 0.0f : most;
     l = 0.0f;
 #pragma unroll
     for (int d = 0; d < kOwn; ++d) o[d] = 0.0f;
 #pragma unroll
-    for (uint32_t k = 0; k < kJoinWarps; ++k) {
+    for (uint32_t k = 0; k < WARPS; ++k) {
         const float e = exp2_of(s_m[r][k] - safe);
         l = fmaf(s_l[r][k], e, l);
 #pragma unroll
@@ -719,11 +741,14 @@ int launch_few(const dr_kv_cache* cache, const AttendArgs& a, void* work, cudaSt
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
     cudaError_t e = cudaLaunchKernelEx(&cfg, few_kernel<D, SETS>, cache->k_map, cache->v_map, a, parts, joins);
-    if (e == cudaSuccess) {
-        cfg.gridDim = dim3(ctas, kRows<SETS> / kJoinRows);
-        cfg.blockDim = dim3(32 * kJoinRows * kJoinWarps);
+    if (e == cudaSuccess && !a.whole) {
+        // a dozen parts a group on average divide the two
+        const uint64_t rows = ((uint64_t)a.rows * a.group + a.requests - 1) / a.requests, groups = (uint64_t)a.requests * a.n_kv * ((rows + kRows<SETS> - 1) / kRows<SETS>);
+        const bool few = groups * 12 >= ctas;
+        cfg.gridDim = dim3(ctas, kRows<SETS> / (few ? kJoinRows<1> : kJoinRows<4>));
+        cfg.blockDim = dim3(few ? 32 * kJoinRows<1> : 32 * 4 * kJoinRows<4>);
         cfg.dynamicSmemBytes = 0;
-        e = cudaLaunchKernelEx(&cfg, join_kernel<D, SETS>, a, (const Part<D, SETS>*)parts, (const Join*)joins);
+        e = cudaLaunchKernelEx(&cfg, few ? join_kernel<D, SETS, 1> : join_kernel<D, SETS, 4>, a, (const Part<D, SETS>*)parts, (const Join*)joins);
     }
     if (e != cudaSuccess) {
         cudaGetLastError();
