@@ -1,22 +1,23 @@
 // Attention over the 8-bit cache for many rows of a request: prompts, on the tensor cores (sm_100a).
 //
 // A CTA takes 256 rows of one request and cache head (the query heads that share the head, times 256 / group tokens), as two halves of 128,
-// and walks the tokens that they may see in tiles of 128.  For each half and tile
+// and walks the tokens that they may see, 64 at a time.  For each half and 64 tokens
 //   S = Q K^T      tcgen05, fp8: the keys' codes as the cache holds them, brought in by tensor maps and never converted; a query row,
 //                  scaled by a power of two, is the sum of two rows of codes (bf16 has eight significant bits, e4m3 four), both
 //                  products into the same fp32 accumulator.  Exact but for bits below 2^-17 of the row's maximum.
-//   P = exp2(...)  a thread a row, the row's 128 logits in registers: no shuffles, one pass with the running maximum and sum
+//   P = exp2(...)  a thread a row, the row's 64 logits in registers: no shuffles, one pass with the running maximum and sum
 //   O += P V       tcgen05, fp16: P goes back to tensor memory, over S, and is the product's first operand from there; the values'
 //                  codes become fp16, exactly, in four warps of their own
-// The halves alternate: while one's exponentials are computed the other's products run.  The exponentials (256 x 128 a tile at 16 a cycle)
-// take as long as the products (4 x 512 cycles), so what bounds it is how well the two overlap.
+// Tensor memory holds two S of 64 columns for each half, so the next S is computed while the exponentials of this one are.  (One S of 128 columns, which
+// has to wait for the P over it to be read: a tile took 4600 cycles, 2100 of them exponentials and 1600 waiting for S.)  Exponentials (16 a
+// cycle), products and the shared memory's reads for them would each take some 2100 to 2600 cycles for 128 tokens: what bounds it is how well
+// they overlap.
 //
 // As in the few-row kernel the running maximum is that of log2(p) + log2(value scale); O is multiplied anew only when it grows by more than
 // 2^4, so that p scale in fp16 is at most 2^15 and normal down to 2^-25 of the largest.
 //
-// Warps: 0-3 and 4-7 the exponentials of the two halves, 8-11 the values' codes, 12 the copies, 13 the products.  Tensor memory: S and P of
-// each half 128 columns, O of each half head_dim.  CTAs are started in the order of their number: a request's last rows, which see
-// the most tokens, first.
+// Warps: 0-3 and 4-7 the exponentials of the two halves, 8-11 the values' codes, 12 the copies, 14 and 15 the products of the halves.
+// CTAs are started in the order of their number: a request's last rows, which see the most tokens, first.
 // Measured: PLACEHOLDER
 #include "attend.h"
 #include "linear.h"
@@ -29,9 +30,10 @@ using namespace tc;
 
 __device__ unsigned long long g_wait_failures;  // read by dr_diag_linear_wait_failures
 
-constexpr uint32_t kThreads = 512, kHalf = 128, kRowsCta = 2 * kHalf, kTile = 128;
+constexpr uint32_t kThreads = 512, kHalf = 128, kRowsCta = 2 * kHalf;
+constexpr uint32_t kTile = 128, kStep = 64;  // tokens of a copy, and of a product
 constexpr uint32_t kKeyStages = 3, kCodeStages = 2, kValueStages = 2, kMetas = 4;
-constexpr uint32_t kGroups = kTile / 16;  // of sixteen tokens, which share a block
+constexpr uint32_t kGroups = kTile / 16, kStepGroups = kStep / 16;  // of sixteen tokens, which share a block
 constexpr float kTop = 11.0f, kLag = 4.0f;
 constexpr float kLeastScale = 7.8886091e-31f;  // 2^-100
 
@@ -48,8 +50,8 @@ struct Shared {
     alignas(1024) uint8_t codes[kCodeStages][kTile * D];
     alignas(1024) uint8_t v[kValueStages][kTile * D * 2];
     Meta meta[kMetas];
-    uint64_t q_full, k_full[kKeyStages], k_empty[kKeyStages], c_full[kCodeStages], c_empty[kCodeStages], v_full[kValueStages],
-        v_empty[kValueStages], s_full[2], p_full[2], o_done[2];
+    uint64_t k_full[kKeyStages], k_empty[kKeyStages], c_full[kCodeStages], c_empty[kCodeStages], v_full[kValueStages], v_empty[kValueStages];
+    uint64_t q_full[2], s_full[2][2], p_full[2][2], o_done[2], o_last[2];  // of each half; S and P of even and odd steps
     uint32_t tmem;
     Limit limit;
     uint32_t sums[kThreads / 32];
@@ -121,6 +123,20 @@ __device__ __forceinline__ void e4m3x4_to_half(uint32_t codes, uint32_t& lo, uin
 {
     asm("{\n.reg .b16 a, b;\nmov.b32 {a, b}, %2;\ncvt.rn.f16x2.e4m3x2 %0, a;\ncvt.rn.f16x2.e4m3x2 %1, b;\n}" : "=r"(lo), "=r"(hi) : "r"(codes));
 }
+__device__ __forceinline__ float max3(float a, float b, float c) { return fmaxf(fmaxf(a, b), c); }
+__device__ __forceinline__ uint64_t fma_pair(uint64_t a, uint64_t b, uint64_t c)
+{
+    uint64_t d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+__device__ __forceinline__ uint64_t add_pair(uint64_t a, uint64_t b)
+{
+    uint64_t d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+__device__ __forceinline__ void split(uint64_t v, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
 // Rows of D codes, swizzled over their own length as the tensor maps do: where chunk `c` of sixteen bytes of a row lies.
 template <int D>
 __device__ __forceinline__ uint32_t swizzled(uint32_t row, uint32_t c)
@@ -196,55 +212,54 @@ __device__ __forceinline__ void produce(const AttendArgs& a, Shared<D>& s, const
     if (ok) drain(keys, used, k_empty, &s.limit, &g_wait_failures);
 }
 
+// The products of one half: S of the next step, then this one's part of O.
 template <int D>
-__device__ __forceinline__ void multiply(const AttendArgs& a, Shared<D>& s, const Item& it)
+__device__ __forceinline__ void multiply(const AttendArgs& a, Shared<D>& s, const Item& it, uint32_t half)
 {
     const uint32_t k_full = smem_u32(s.k_full), k_empty = smem_u32(s.k_empty), v_full = smem_u32(s.v_full), v_empty = smem_u32(s.v_empty);
-    const uint32_t halves = it.rows > kHalf ? 2 : 1, n = it.tiles.count;
-    const uint32_t shape_s = shape_of(true, false, false, kHalf, kTile), shape_o = shape_of(true, false, true, kHalf, D);  // (format 0: e4m3, fp16)
-    const uint64_t q0 = codes_operand<D>(smem_u32(s.q)), k0 = codes_operand<D>(smem_u32(s.k)), v0 = operand(smem_u32(s.v), kTile * 128);
+    const uint32_t s_full = smem_u32(s.s_full[half]), p_full = smem_u32(s.p_full[half]), o_done = smem_u32(&s.o_done[half]);
+    const uint32_t shape_s = shape_of(true, false, false, kHalf, kStep), shape_o = shape_of(true, false, true, kHalf, D);  // (format 0: e4m3, fp16)
+    const uint64_t q0 = codes_operand<D>(smem_u32(s.q[half])), k0 = codes_operand<D>(smem_u32(s.k)), v0 = operand(smem_u32(s.v), kTile * 128);
+    const uint32_t s_at = s.tmem + half * 2 * kStep, o_at = s.tmem + 4 * kStep + half * D;
+    const uint32_t steps = it.tiles.count * (kTile / kStep);
     Turn<kKeyStages> keys;
     Turn<kValueStages> values;
-    if (!warp_wait(smem_u32(&s.q_full), 0, &s.limit, &g_wait_failures)) return;
-    // S of half h for tile i
-    auto logits = [&](uint32_t h, uint32_t i) {
-        if (h == 0 && !warp_wait(k_full + 8 * keys.slot, keys.round, &s.limit, &g_wait_failures)) return false;
-        // S lies over the P of the tile before, which its product must have read
-        if (i && !warp_wait(smem_u32(&s.o_done[h]), (i - 1) & 1, &s.limit, &g_wait_failures)) return false;
+    // S of step i lies over the P of step i - 2, which its product must have read
+    auto logits = [&](uint32_t i) {
+        if (!(i & 1) && !warp_wait(k_full + 8 * keys.slot, keys.round, &s.limit, &g_wait_failures)) return false;
+        if (i > 1 && !warp_wait(o_done, i & 1, &s.limit, &g_wait_failures)) return false;
         fence_after();
-        const uint64_t dk = k0 + keys.slot * (kTile * D >> 4);
+        const uint64_t dk = k0 + keys.slot * (kTile * D >> 4) + (i & 1) * (kStep * D >> 4);
         if (elect()) {
 #pragma unroll
             for (uint32_t rest = 0; rest < 2; ++rest)
 #pragma unroll
                 for (uint32_t c = 0; c < D / 32; ++c)
-                    mma<1, true>(s.tmem + h * kTile, q0 + (h * 2 + rest) * (kHalf * D >> 4) + c * 2, dk + c * 2, shape_s, rest | c);
-            commit<1>(smem_u32(&s.s_full[h]));
-            if (h + 1 == halves) commit<1>(k_empty + 8 * keys.slot);
+                    mma<1, true>(s_at + (i & 1) * kStep, q0 + rest * (kHalf * D >> 4) + c * 2, dk + c * 2, shape_s, rest | c);
+            commit<1>(s_full + 8 * (i & 1));
+            if (i & 1) commit<1>(k_empty + 8 * keys.slot);
         }
         __syncwarp();
-        if (h + 1 == halves) keys.next();
+        if (i & 1) keys.next();
         return true;
     };
-    for (uint32_t h = 0; h < halves; ++h)
-        if (!logits(h, 0)) return;
-    for (uint32_t i = 0; i < n; ++i) {
-        for (uint32_t h = 0; h < halves; ++h) {
-            if (h == 0 && !warp_wait(v_full + 8 * values.slot, values.round, &s.limit, &g_wait_failures)) return;
-            if (!warp_wait(smem_u32(&s.p_full[h]), i & 1, &s.limit, &g_wait_failures)) return;
-            fence_after();
-            const uint64_t dv = v0 + values.slot * (kTile * D * 2 >> 4);
-            if (elect()) {
+    if (!warp_wait(smem_u32(&s.q_full[half]), 0, &s.limit, &g_wait_failures) || !logits(0)) return;
+    for (uint32_t i = 0; i < steps; ++i) {
+        if (i + 1 < steps && !logits(i + 1)) return;
+        if (!(i & 1) && !warp_wait(v_full + 8 * values.slot, values.round, &s.limit, &g_wait_failures)) return;
+        if (!warp_wait(p_full + 8 * (i & 1), i >> 1 & 1, &s.limit, &g_wait_failures)) return;
+        fence_after();
+        const uint64_t dv = v0 + values.slot * (kTile * D * 2 >> 4) + (i & 1) * (kStep * 128 >> 4);
+        if (elect()) {
 #pragma unroll
-                for (uint32_t c = 0; c < kTile / 16; ++c)
-                    mma_ts(s.tmem + 2 * kTile + h * D, s.tmem + h * kTile + c * 8, dv + c * (2048 >> 4), shape_o, i | c);
-                commit<1>(smem_u32(&s.o_done[h]));
-                if (h + 1 == halves) commit<1>(v_empty + 8 * values.slot);
-            }
-            __syncwarp();
-            if (i + 1 < n && !logits(h, i + 1)) return;
+            for (uint32_t c = 0; c < kStep / 16; ++c)
+                mma_ts(o_at, s_at + (i & 1) * kStep + c * 8, dv + c * (2048 >> 4), shape_o, i | c);
+            commit<1>(o_done);
+            if (i + 1 == steps) commit<1>(smem_u32(&s.o_last[half]));
+            if (i & 1) commit<1>(v_empty + 8 * values.slot);
         }
-        values.next();
+        __syncwarp();
+        if (i & 1) values.next();
     }
 }
 
@@ -363,77 +378,85 @@ __device__ __forceinline__ void softmax(const AttendArgs& a, Shared<D>& s, const
     }
     fence_async();
     __syncwarp();
-    if (lane == 0) bar_arrive(smem_u32(&s.q_full));
+    if (lane == 0) bar_arrive(smem_u32(&s.q_full[half]));
     const uint32_t quarter = (threadIdx.x >> 5 & 3) * 32 << 16;
-    const uint32_t s_at = s.tmem + quarter + half * kTile, o_at = s.tmem + quarter + 2 * kTile + half * D;
-    const uint32_t s_full = smem_u32(&s.s_full[half]), p_full = smem_u32(&s.p_full[half]), o_done = smem_u32(&s.o_done[half]);
+    const uint32_t s_at = s.tmem + quarter + half * 2 * kStep, o_at = s.tmem + quarter + 4 * kStep + half * D;
+    const uint32_t s_full = smem_u32(s.s_full[half]), p_full = smem_u32(s.p_full[half]), o_done = smem_u32(&s.o_done[half]);
     const int p_lo = __shfl_sync(0xFFFFFFFFu, p, 0), p_hi = __shfl_sync(0xFFFFFFFFu, p, 31);  // rows ascend
+    const uint32_t steps = it.tiles.count * (kTile / kStep);
     float m = -INFINITY, l = 0.0f;
-    for (uint32_t i = 0; i < it.tiles.count; ++i) {
-        if (!__all_sync(0xFFFFFFFFu, bar_wait(s_full, i & 1, &s.limit, &g_wait_failures))) return;
+    for (uint32_t i = 0; i < steps; ++i) {
+        const uint32_t odd = i & 1, at = s_at + odd * kStep;
+        if (!__all_sync(0xFFFFFFFFu, bar_wait(s_full + 8 * odd, i >> 1 & 1, &s.limit, &g_wait_failures))) return;
         fence_after();
-        float v[4][32];
-#pragma unroll
-        for (int c = 0; c < 4; ++c) tmem_start(s_at + 32 * c, v[c]);
-        const Meta& meta = s.meta[i % kMetas];
-        const int t0 = (int)meta.token;
-        const uint32_t held = meta.held;
-        const bool all = held == 255 && t0 + (int)kTile - 1 <= p_lo && (!a.window || t0 > p_hi - (int)a.window || t0 + (int)kTile - 1 < (int)a.sinks);
-#pragma unroll
-        for (int c = 0; c < 4; ++c) tmem_arrived(v[c]);
+        float v[2][32];
+        tmem_start(at, v[0]);
+        tmem_start(at + 32, v[1]);
+        const Meta& meta = s.meta[(i >> 1) % kMetas];
+        const int t0 = (int)(meta.token + odd * kStep), g0 = (int)(odd * kStepGroups);
+        const uint32_t held = meta.held >> g0 & ((1u << kStepGroups) - 1);
+        const bool all = held == (1u << kStepGroups) - 1 && t0 + (int)kStep - 1 <= p_lo &&
+                         (!a.window || t0 > p_hi - (int)a.window || t0 + (int)kStep - 1 < (int)a.sinks);
+        tmem_arrived(v[0]);
+        tmem_arrived(v[1]);
         if (!all) {
 #pragma unroll
-            for (int c = 0; c < 4; ++c)
-#pragma unroll
-                for (int k = 0; k < 32; ++k) {
-                    const int t = t0 + 32 * c + k;
-                    const bool hide = !(held >> (2 * c + k / 16) & 1) || t > p || (a.window && t <= p - (int)a.window && t >= (int)a.sinks);
-                    if (hide) v[c][k] = -INFINITY;
-                }
+            for (int k = 0; k < (int)kStep; ++k) {
+                const int t = t0 + k;
+                if (!(held >> (k / 16) & 1) || t > p || (a.window && t <= p - (int)a.window && t >= (int)a.sinks)) v[k / 32][k % 32] = -INFINITY;
+            }
         }
-        float f[kGroups], top = -INFINITY;
+        float top = -INFINITY, f[kStepGroups];
 #pragma unroll
-        for (int g = 0; g < (int)kGroups; ++g) {
-            // (never zero: a hidden logit stays hidden)
-            f[g] = fmaxf(back * meta.k_scale[g], 1.2e-38f);
-            float most = v[g / 2][g % 2 * 16];
-#pragma unroll
-            for (int k = 1; k < 16; ++k) most = fmaxf(most, v[g / 2][g % 2 * 16 + k]);
-            top = fmaxf(top, fmaf(most, f[g], meta.v_log[g]));
+        for (int g = 0; g < (int)kStepGroups; ++g) {
+            const float* const u = &v[g / 2][g % 2 * 16];
+            const float most = max3(max3(max3(u[0], u[1], u[2]), max3(u[3], u[4], u[5]), max3(u[6], u[7], u[8])), max3(u[9], u[10], u[11]),
+                                    max3(max3(u[12], u[13], u[14]), u[15], u[15]));
+            f[g] = fmaxf(back * meta.k_scale[g0 + g], 1.2e-38f);  // (never zero: a hidden logit stays hidden)
+            top = fmaxf(top, fmaf(most, f[g], meta.v_log[g0 + g]));
         }
         if (__any_sync(0xFFFFFFFFu, i == 0 || top > m + kLag || (m == -INFINITY && top > m))) {
             const float now = fmaxf(m, top), shrink = now == -INFINITY ? 1.0f : exp2_of(m - now);
             m = now;
             l *= shrink;
-            if (i) {  // the product before has ended: this S was computed behind it
+            if (i) {  // once every product so far has ended
+                if (!__all_sync(0xFFFFFFFFu, bar_wait(o_done, (i - 1) & 1, &s.limit, &g_wait_failures))) return;
+                fence_after();
 #pragma unroll 1
                 for (int c = 0; c < D / 16; ++c) tmem_scale(o_at + 16 * c, shrink);
             }
         }
         const float base = kTop - (m == -INFINITY ? 0.0f : m);
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
+        for (int c = 0; c < 2; ++c) {
             uint32_t w[16];
 #pragma unroll
             for (int g = 2 * c; g < 2 * c + 2; ++g) {
-                const float from = meta.v_log[g] + base;
-                float sum = 0.0f;
+                const float from = meta.v_log[g0 + g] + base;
+                const uint64_t f2 = pair_of(f[g], f[g]), from2 = pair_of(from, from);
+                uint64_t sum = 0;
 #pragma unroll
                 for (int k = 0; k < 16; k += 2) {
-                    const float y0 = exp2_of(fmaf(v[g / 2][g % 2 * 16 + k], f[g], from)), y1 = exp2_of(fmaf(v[g / 2][g % 2 * 16 + k + 1], f[g], from));
-                    sum += y0 + y1;
-                    w[(g - 2 * c) * 8 + k / 2] = half2_of(y0, y1);
+                    float x0, x1;
+                    split(fma_pair(pair_of(v[c][g % 2 * 16 + k], v[c][g % 2 * 16 + k + 1]), f2, from2), x0, x1);
+                    x0 = exp2_of(x0);
+                    x1 = exp2_of(x1);
+                    sum = add_pair(sum, pair_of(x0, x1));
+                    w[(g - 2 * c) * 8 + k / 2] = half2_of(x0, x1);
                 }
-                l = fmaf(sum, meta.v_inv[g], l);
+                float lo, hi;
+                split(sum, lo, hi);
+                l = fmaf(lo + hi, meta.v_inv[g0 + g], l);
             }
-            tmem_store(s_at + 16 * c, w);
+            tmem_store(at + 16 * c, w);
         }
         tmem_stored();
         fence_before();
         __syncwarp();
-        if (lane == 0) bar_arrive(p_full);
+        if (lane == 0) bar_arrive(p_full + 8 * odd);
     }
-    if (!__all_sync(0xFFFFFFFFu, bar_wait(o_done, (it.tiles.count - 1) & 1, &s.limit, &g_wait_failures))) return;
+    // (a barrier of its own: o_done may be one or two phases on, which its parity does not tell apart)
+    if (!__all_sync(0xFFFFFFFFu, bar_wait(smem_u32(&s.o_last[half]), 0, &s.limit, &g_wait_failures))) return;
     fence_after();
     const float norm = l == 0.0f ? 0.0f : 1.0f / l;
     uint16_t* out = (uint16_t*)a.out + index * a.ldo + (uint64_t)head * D;
@@ -520,10 +543,9 @@ __global__ void __launch_bounds__(kThreads, 1)
     if (it.tiles.count == 0) it.tiles = Tiles{0, 0, 1};  // rows that see nothing still have to be written
     const uint32_t halves = it.rows > kHalf ? 2 : 1;
     if (threadIdx.x == 0) {
-        bar_init(smem_u32(&s.q_full), 4 * halves);
         for (uint32_t i = 0; i < kKeyStages; ++i) {
             bar_init(smem_u32(&s.k_full[i]), 1);
-            bar_init(smem_u32(&s.k_empty[i]), 1);
+            bar_init(smem_u32(&s.k_empty[i]), halves);
         }
         for (uint32_t i = 0; i < kCodeStages; ++i) {
             bar_init(smem_u32(&s.c_full[i]), 1);
@@ -531,12 +553,16 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         for (uint32_t i = 0; i < kValueStages; ++i) {
             bar_init(smem_u32(&s.v_full[i]), 4);
-            bar_init(smem_u32(&s.v_empty[i]), 1);
+            bar_init(smem_u32(&s.v_empty[i]), halves);
         }
         for (uint32_t h = 0; h < 2; ++h) {
-            bar_init(smem_u32(&s.s_full[h]), 1);
-            bar_init(smem_u32(&s.p_full[h]), 4);
+            bar_init(smem_u32(&s.q_full[h]), 4);
+            for (uint32_t i = 0; i < 2; ++i) {
+                bar_init(smem_u32(&s.s_full[h][i]), 1);
+                bar_init(smem_u32(&s.p_full[h][i]), 4);
+            }
             bar_init(smem_u32(&s.o_done[h]), 1);
+            bar_init(smem_u32(&s.o_last[h]), 1);
         }
         s.limit.stop = 0;
         s.limit.us = a.limit_us;
@@ -556,7 +582,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
         if (warp == 12) produce<D>(a, s, it, &k_map, &v_map);
-        if (warp == 13) multiply<D>(a, s, it);
+        if (warp >= 14 && warp < 14 + halves) multiply<D>(a, s, it, warp - 14);
     }
     __syncwarp();
     let_copies_end(&s.limit);
