@@ -34,6 +34,7 @@ constexpr uint32_t kThreads = 512, kHalf = 128, kRowsCta = 2 * kHalf;
 constexpr uint32_t kTile = 128, kStep = 64;  // tokens of a copy, and of a product
 constexpr uint32_t kKeyStages = 3, kCodeStages = 2, kValueStages = 2, kMetas = 4;
 constexpr uint32_t kGroups = kTile / 16, kStepGroups = kStep / 16;  // of sixteen tokens, which share a block
+constexpr int kByFma = 3;  // pairs of each eight whose exponentials multiply-adds take (a tile: 2.23 us with none, 2.11 with 2 or 3, 2.16 with 4)
 constexpr float kTop = 11.0f, kLag = 4.0f;
 constexpr float kLeastScale = 7.8886091e-31f;  // 2^-100
 
@@ -123,7 +124,13 @@ __device__ __forceinline__ void e4m3x4_to_half(uint32_t codes, uint32_t& lo, uin
 {
     asm("{\n.reg .b16 a, b;\nmov.b32 {a, b}, %2;\ncvt.rn.f16x2.e4m3x2 %0, a;\ncvt.rn.f16x2.e4m3x2 %1, b;\n}" : "=r"(lo), "=r"(hi) : "r"(codes));
 }
-__device__ __forceinline__ float max3(float a, float b, float c) { return fmaxf(fmaxf(a, b), c); }
+// The larger one; NaN where one of them is.
+__device__ __forceinline__ float max_nan(float a, float b)
+{
+    float d;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
+    return d;
+}
 __device__ __forceinline__ uint64_t fma_pair(uint64_t a, uint64_t b, uint64_t c)
 {
     uint64_t d;
@@ -135,6 +142,23 @@ __device__ __forceinline__ uint64_t add_pair(uint64_t a, uint64_t b)
     uint64_t d;
     asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
     return d;
+}
+// 2^x for a pair by multiply-adds, where the exponential unit (16 a cycle) is busy: x = n + f with n a whole number, which the addition of
+// 1.5 * 2^23 leaves in the low bits, |f| <= 1/2, and 2^f by a polynomial of degree 4 whose largest relative error is the least possible
+// (2.6e-6, found by weighted least squares), n added to its exponent.  Below 2^-126: 2^-126.  Not for NaN.
+__device__ __forceinline__ uint64_t exp2_pair(float x0, float x1)
+{
+    const uint64_t big = 0x4B4000004B400000ull, minus_big = 0xCB400000CB400000ull, minus_one = 0xBF800000BF800000ull;
+    const uint64_t x = tc::pair_of(fmaxf(x0, -126.0f), fmaxf(x1, -126.0f)), t = add_pair(x, big);
+    const uint64_t f = fma_pair(add_pair(t, minus_big), minus_one, x);
+    uint64_t y = fma_pair(f, tc::pair_of(0.009570102f, 0.009570102f), tc::pair_of(0.05591786f, 0.05591786f));
+    y = fma_pair(y, f, tc::pair_of(0.24024744f, 0.24024744f));
+    y = fma_pair(y, f, tc::pair_of(0.6931218f, 0.6931218f));
+    y = fma_pair(y, f, tc::pair_of(0.9999993f, 0.9999993f));
+    uint32_t y0, y1, t0, t1;
+    asm("mov.b64 {%0, %1}, %2;" : "=r"(y0), "=r"(y1) : "l"(y));
+    asm("mov.b64 {%0, %1}, %2;" : "=r"(t0), "=r"(t1) : "l"(t));
+    return tc::pair_of(__uint_as_float(y0 + (t0 << 23)), __uint_as_float(y1 + (t1 << 23)));
 }
 __device__ __forceinline__ void split(uint64_t v, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
 // Rows of D codes, swizzled over their own length as the tensor maps do: where chunk `c` of sixteen bytes of a row lies.
@@ -320,44 +344,34 @@ __device__ __forceinline__ void softmax(const AttendArgs& a, Shared<D>& s, const
     float back;
     {
         const char* q = (const char*)a.q + (index * a.ldq + (uint64_t)head * D) * 2;
-        uint32_t most = 0;
-        // sixteen values; read twice, for the maximum and for the codes, rather than held
-        auto load16 = [&](uint32_t c, uint32_t (&w)[8]) {
-            const char* at = q + 32 * c;
+        uint32_t w[D / 2], most = 0;
 #pragma unroll
-            for (int k = 0; k < 8; k += 4) {
-                if (a.vec_q == 2) {
-                    asm volatile("ld.global.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(w[k]), "=r"(w[k + 1]), "=r"(w[k + 2]), "=r"(w[k + 3]) : "l"(at + 4 * k) : "memory");
-                } else {
+        for (int c = 0; c < D / 2; c += 4) {
+            if (a.vec_q == 2) {
+                asm volatile("ld.global.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(w[c]), "=r"(w[c + 1]), "=r"(w[c + 2]), "=r"(w[c + 3]) : "l"(q + 4 * c) : "memory");
+            } else {
 #pragma unroll
-                    for (int u = k; u < k + 4; ++u)
-                        w[u] = ((const volatile uint16_t*)at)[2 * u] | (uint32_t)((const volatile uint16_t*)at)[2 * u + 1] << 16;
-                }
+                for (int k = c; k < c + 4; ++k)
+                    w[k] = ((const volatile uint16_t*)q)[2 * k] | (uint32_t)((const volatile uint16_t*)q)[2 * k + 1] << 16;
             }
-        };
-#pragma unroll 4
-        for (uint32_t c = 0; c < D / 16; ++c) {
-            uint32_t w[8];
-            load16(c, w);
-#pragma unroll
-            for (int k = 0; k < 8; ++k) most = max(most, max(w[k] & 0x7FFFu, w[k] >> 16 & 0x7FFFu));
         }
+#pragma unroll
+        for (int c = 0; c < D / 2; ++c) most = max(most, max(w[c] & 0x7FFFu, w[c] >> 16 & 0x7FFFu));
         // times 2^up the maximum lies in (224, 448]; a row that is not finite becomes NaN codes, below
         const int e = (int)(most >> 7);
         const int up = e == 255 || most == 0 ? 0 : 8 - (e - 127) - ((most & 127) > 96);  // 448 = 1.75 * 2^8
         const float x1 = __uint_as_float((uint32_t)(127 + up / 2) << 23), x2 = __uint_as_float((uint32_t)(127 + up - up / 2) << 23);
         const float sign = a.scale < 0.0f ? -1.0f : 1.0f;
         back = fabsf(a.scale) * __uint_as_float((uint32_t)(127 - up / 2) << 23) * __uint_as_float((uint32_t)(127 - (up - up / 2)) << 23);
-#pragma unroll 1
-        for (uint32_t c = 0; c < D / 16; ++c) {
-            uint32_t w[8], hi[4], rest[4];
-            load16(c, w);
+#pragma unroll
+        for (int c = 0; c < D / 16; ++c) {
+            uint32_t hi[4], rest[4];
 #pragma unroll
             for (int k = 0; k < 8; k += 2) {
                 uint32_t h2[2], r2[2];
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
-                    const uint32_t v = w[k + u];
+                    const uint32_t v = w[8 * c + k + u];
                     float f0 = __uint_as_float(v << 16) * x1 * x2 * sign, f1 = __uint_as_float(v & 0xFFFF0000u) * x1 * x2 * sign;
                     if (e == 255) f0 = f1 = __uint_as_float(0x7FC00000u);
                     if (!real) f0 = f1 = 0.0f;
@@ -410,11 +424,17 @@ __device__ __forceinline__ void softmax(const AttendArgs& a, Shared<D>& s, const
 #pragma unroll
         for (int g = 0; g < (int)kStepGroups; ++g) {
             const float* const u = &v[g / 2][g % 2 * 16];
-            const float most = max3(max3(max3(u[0], u[1], u[2]), max3(u[3], u[4], u[5]), max3(u[6], u[7], u[8])), max3(u[9], u[10], u[11]),
-                                    max3(max3(u[12], u[13], u[14]), u[15], u[15]));
+            float most = u[0], other = u[1];  // (two chains)
+#pragma unroll
+            for (int k = 2; k < 16; k += 2) {
+                most = max_nan(most, u[k]);
+                other = max_nan(other, u[k + 1]);
+            }
+            most = max_nan(most, other);
             f[g] = fmaxf(back * meta.k_scale[g0 + g], 1.2e-38f);  // (never zero: a hidden logit stays hidden)
-            top = fmaxf(top, fmaf(most, f[g], meta.v_log[g0 + g]));
+            top = max_nan(top, fmaf(most, f[g], meta.v_log[g0 + g]));
         }
+        if (top != top) l = top;  // a NaN among the logits: the row's sum, and its result, are NaN
         if (__any_sync(0xFFFFFFFFu, i == 0 || top > m + kLag || (m == -INFINITY && top > m))) {
             const float now = fmaxf(m, top), shrink = now == -INFINITY ? 1.0f : exp2_of(m - now);
             m = now;
@@ -439,9 +459,14 @@ __device__ __forceinline__ void softmax(const AttendArgs& a, Shared<D>& s, const
                 for (int k = 0; k < 16; k += 2) {
                     float x0, x1;
                     split(fma_pair(pair_of(v[c][g % 2 * 16 + k], v[c][g % 2 * 16 + k + 1]), f2, from2), x0, x1);
-                    x0 = exp2_of(x0);
-                    x1 = exp2_of(x1);
-                    sum = add_pair(sum, pair_of(x0, x1));
+                    uint64_t y;
+                    if (k % 16 < 16 - 2 * kByFma) {
+                        y = pair_of(exp2_of(x0), exp2_of(x1));
+                    } else {
+                        y = exp2_pair(x0, x1);
+                    }
+                    split(y, x0, x1);
+                    sum = add_pair(sum, y);
                     w[(g - 2 * c) * 8 + k / 2] = half2_of(x0, x1);
                 }
                 float lo, hi;
@@ -458,7 +483,7 @@ __device__ __forceinline__ void softmax(const AttendArgs& a, Shared<D>& s, const
     // (a barrier of its own: o_done may be one or two phases on, which its parity does not tell apart)
     if (!__all_sync(0xFFFFFFFFu, bar_wait(smem_u32(&s.o_last[half]), 0, &s.limit, &g_wait_failures))) return;
     fence_after();
-    const float norm = l == 0.0f ? 0.0f : 1.0f / l;
+    const float norm = l == 0.0f || (m == -INFINITY && l == l) ? 0.0f : 1.0f / l;  // (a row that has seen nothing: zeros)
     uint16_t* out = (uint16_t*)a.out + index * a.ldo + (uint64_t)head * D;
 #pragma unroll
     for (int c = 0; c < D / 32; ++c) {
