@@ -17,7 +17,7 @@
 // 2^4, so that p scale in fp16 is at most 2^15 and normal down to 2^-25 of the largest.
 //
 // Warps: 0-3 and 4-7 the exponentials of the two halves, 8-11 the values' codes, 12 the copies, 14 and 15 the products of the halves.
-// CTAs are started in the order of their number: a request's last rows, which see the most tokens, first.
+// CTAs are started in the order of their number: the longest request first, and a request's last rows, which see the most tokens, first.
 // Measured: PLACEHOLDER
 #include "attend.h"
 #include "linear.h"
@@ -33,6 +33,7 @@ __device__ unsigned long long g_wait_failures;  // read by dr_diag_linear_wait_f
 constexpr uint32_t kThreads = 512, kHalf = 128, kRowsCta = 2 * kHalf;
 constexpr uint32_t kTile = 128, kStep = 64;  // tokens of a copy, and of a product
 constexpr uint32_t kKeyStages = 3, kCodeStages = 2, kValueStages = 2, kMetas = 4;
+constexpr uint32_t kRanked = 128;  // requests up to which the longest are begun first
 constexpr uint32_t kGroups = kTile / 16, kStepGroups = kStep / 16;  // of sixteen tokens, which share a block
 constexpr int kByFma = 3;  // pairs of each eight whose exponentials multiply-adds take (a tile: 2.23 us with none, 2.11 with 2 or 3, 2.16 with 4)
 constexpr float kTop = 11.0f, kLag = 4.0f;
@@ -57,6 +58,7 @@ struct Shared {
     Limit limit;
     uint32_t sums[kThreads / 32];
     uint32_t request, item;
+    uint32_t lengths[kRanked], tiles[kRanked], ranked[kRanked];
 };
 static_assert(sizeof(Shared<128>) <= 227 * 1024, "shared memory of a CTA");
 
@@ -525,8 +527,21 @@ __global__ void __launch_bounds__(kThreads, 1)
         const uint32_t want = blockIdx.x / a.n_kv;
         uint32_t base = 0;
         bool found = false;
+        const bool ranked = a.requests <= kRanked;
+        if (ranked) {  // by their tokens, so that the last CTAs to start are short ones
+            const uint32_t r = threadIdx.x, len = r < a.requests ? request_of(a, r).len : 0;
+            if (r < a.requests) s.lengths[r] = len;
+            __syncthreads();
+            if (r < a.requests) {
+                uint32_t rank = 0;
+                for (uint32_t i = 0; i < a.requests; ++i) rank += s.lengths[i] > len || (s.lengths[i] == len && i < r);
+                s.ranked[rank] = r;
+                s.tiles[rank] = tiles_of_rows(a, r);
+            }
+            __syncthreads();
+        }
         for (uint32_t r0 = 0; r0 < a.requests && base <= want; r0 += kThreads) {
-            const uint32_t mine = tiles_of_rows(a, r0 + threadIdx.x);
+            const uint32_t mine = !ranked ? tiles_of_rows(a, r0 + threadIdx.x) : threadIdx.x < a.requests ? s.tiles[threadIdx.x] : 0;
             uint32_t sum = mine;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
@@ -544,7 +559,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
             before += sum - mine;
             if (before <= want && want < before + mine) {
-                s.request = r0 + threadIdx.x;
+                s.request = ranked ? s.ranked[threadIdx.x] : r0 + threadIdx.x;
                 s.item = mine - 1 - (want - before);  // a request's last rows first
             }
             base += total;

@@ -6,8 +6,8 @@
 // token's next heads keeps their sines.  Every value is read once and written once: HBM bounds it.
 //
 // Angles: base^(-2 i / d) / 2 pi is held as a fraction of a turn in 64 bits, so that position * fraction, taken modulo 2^64, is the
-// angle modulo a turn, exact to 2^-64 * position; its upper 32 bits go to sincospi.  No reduction, no table over positions, and the far end
-// of a long context is as exact as its start.
+// angle modulo a turn, exact to 2^-64 * position.  No reduction, no table over positions, and the far end of a long context is as
+// exact as its start.  Arithmetic is two values an instruction where that exists.
 //
 // Into the cache: a CTA owns one run (the new tokens of one block) for one head, keys and values both, so that the block's two
 // scales are reductions inside the CTA and nobody else touches the block.  Scales are powers of two: the code of v is e4m3(v 2^-e), one
@@ -68,18 +68,18 @@ template <bool F32> constexpr uint64_t kSize = F32 ? 4 : 2;
 template <bool F32>
 struct Raw {
     uint32_t w[F32 ? 16 : 8];
-    __device__ __forceinline__ float value(int half, int k) const
+    __device__ __forceinline__ uint64_t pair(int half, int k) const
     {
-        if (F32) return __uint_as_float(w[F32 ? 8 * half + k : 0]);
-        const uint32_t v = w[4 * half + k / 2];
-        return __uint_as_float(k & 1 ? v & 0xFFFF0000u : v << 16);
+        if (F32) return two_of(__uint_as_float(w[F32 ? 8 * half + 2 * k : 0]), __uint_as_float(w[F32 ? 8 * half + 2 * k + 1 : 0]));
+        const uint32_t v = w[4 * half + k];
+        return two_of(__uint_as_float(v << 16), __uint_as_float(v & 0xFFFF0000u));
     }
-    __device__ __forceinline__ void get(float (&lo)[8], float (&hi)[8]) const
+    __device__ __forceinline__ void get(uint64_t (&lo)[4], uint64_t (&hi)[4]) const
     {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            lo[k] = value(0, k);
-            hi[k] = value(1, k);
+        for (int k = 0; k < 4; ++k) {
+            lo[k] = pair(0, k);
+            hi[k] = pair(1, k);
         }
     }
 };
@@ -109,8 +109,11 @@ __device__ __forceinline__ uint32_t bf16x2(float lo, float hi)
     return d;
 }
 template <bool F32>
-__device__ __forceinline__ void store8(char* p, bool vec, const float (&v)[8])
+__device__ __forceinline__ void store8(char* p, bool vec, const uint64_t (&two)[4])
 {
+    float v[8];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) asm("mov.b64 {%0, %1}, %2;" : "=f"(v[2 * k]), "=f"(v[2 * k + 1]) : "l"(two[k]));
     if (F32) {
         if (vec) {
             ((float4*)p)[0] = make_float4(v[0], v[1], v[2], v[3]);
@@ -132,11 +135,16 @@ __device__ __forceinline__ void store8(char* p, bool vec, const float (&v)[8])
     }
 }
 
-// What a CTA keeps of the handle: the turns, and the norms in fp32.
+__device__ __forceinline__ uint64_t same_two(float v) { return two_of(v, v); }
+__device__ __forceinline__ void parts_of(uint64_t v, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
+__device__ __forceinline__ uint64_t two_of_bf16(uint32_t w) { return two_of(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u)); }
+
+// What a CTA keeps of the handle: the turns, and the norms in their own type (their reads take as much of the shared memory's
+// time as the rows' do of the L1's: half as much in bf16).
 template <int D>
 struct HeadsShared {
     uint64_t turns[D / 2];
-    float4 norm[2][D / 4];
+    alignas(16) uint32_t norm[2][D];
 };
 template <int D>
 __device__ __forceinline__ void fill_turns(HeadsShared<D>& s, const HeadsArgs& a)
@@ -148,33 +156,71 @@ __device__ __forceinline__ void fill_norms(HeadsShared<D>& s, const HeadsArgs& a
 {
     if (a.q_norm && threadIdx.x < 2 * D) {
         const void* w = threadIdx.x < D ? a.q_norm : a.k_norm;
-        const uint32_t i = threadIdx.x & (D - 1);
-        ((float*)s.norm)[threadIdx.x] = a.norm_f32 ? ((const volatile float*)w)[i] : __uint_as_float((uint32_t)((const volatile uint16_t*)w)[i] << 16);
+        const uint32_t key = threadIdx.x / D, i = threadIdx.x & (D - 1);
+        if (a.norm_f32)
+            s.norm[key][i] = ((const volatile uint32_t*)w)[i];
+        else
+            ((uint16_t*)s.norm[key])[i] = ((const volatile uint16_t*)w)[i];
     }
 }
 template <int D>
-__device__ __forceinline__ void load_norm(const HeadsShared<D>& s, uint32_t key, uint32_t i0, float (&w)[16])
+__device__ __forceinline__ void load_norm(const HeadsShared<D>& s, const HeadsArgs& a, uint32_t key, uint32_t i0, uint64_t (&w)[8])
 {
+    if (a.norm_f32) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int k = 0; k < 8; k += 4) {
-            const float4 f = s.norm[key][(h * D / 2 + i0 + k) / 4];
-            w[8 * h + k] = f.x;
-            w[8 * h + k + 1] = f.y;
-            w[8 * h + k + 2] = f.z;
-            w[8 * h + k + 3] = f.w;
+        for (int k = 0; k < 8; k += 2) {
+            const uint4 f = *(const uint4*)&s.norm[key][k / 4 * (D / 2) + i0 + k % 4 * 2];
+            w[k] = two_of(__uint_as_float(f.x), __uint_as_float(f.y));
+            w[k + 1] = two_of(__uint_as_float(f.z), __uint_as_float(f.w));
         }
+    } else {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const uint4 f = *(const uint4*)((const uint16_t*)s.norm[key] + h * (D / 2) + i0);
+            w[4 * h] = two_of_bf16(f.x);
+            w[4 * h + 1] = two_of_bf16(f.y);
+            w[4 * h + 2] = two_of_bf16(f.z);
+            w[4 * h + 3] = two_of_bf16(f.w);
+        }
+    }
 }
 
-// Cosines and sines of the lane's eight angles at a position.
+// Cosines and sines of the lane's eight angles at a position, in pairs.  A turn is 2^32: the nearest quarter turn comes off, sine and cosine
+// of the rest, within an eighth of a turn, are their Taylor series (the first terms left out are 2e-9 and 3e-8), and the
+// quarter turns swap and negate them.
 template <int D>
-__device__ __forceinline__ void angles(const HeadsShared<D>& s, uint32_t i0, int32_t position, float (&c)[8], float (&sn)[8])
+__device__ __forceinline__ void angles(const HeadsShared<D>& s, uint32_t i0, int32_t position, uint64_t (&c)[4], uint64_t (&sn)[4])
 {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-        const int32_t turn = (int32_t)((uint64_t)position * s.turns[i0 + k] >> 32);  // of 2^32
-        sincospif((float)turn * 4.656612873077393e-10f, &sn[k], &c[k]);
+    for (int k = 0; k < 4; ++k) {
+        uint32_t quarter[2];
+        float z[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const uint32_t turn = (uint32_t)((uint64_t)position * s.turns[i0 + 2 * k + h] >> 32);
+            quarter[h] = turn + 0x20000000u;
+            z[h] = (float)(int32_t)(turn - (quarter[h] & 0xC0000000u)) * 1.4629180792671596e-9f;  // 2 pi / 2^32
+        }
+        const uint64_t x = two_of(z[0], z[1]), x2 = mul_two(x, x);
+        uint64_t a = fma_two(x2, same_two(1.0f / 362880), same_two(-1.0f / 5040)), b = fma_two(x2, same_two(1.0f / 40320), same_two(-1.0f / 720));
+        a = fma_two(a, x2, same_two(1.0f / 120));
+        b = fma_two(b, x2, same_two(1.0f / 24));
+        a = fma_two(a, x2, same_two(-1.0f / 6));
+        b = fma_two(b, x2, same_two(-0.5f));
+        a = fma_two(mul_two(x, x2), a, x);
+        b = fma_two(b, x2, same_two(1.0f));
+        float sine[2], cosine[2];
+        parts_of(a, sine[0], sine[1]);
+        parts_of(b, cosine[0], cosine[1]);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const bool swap = quarter[h] & 0x40000000u;
+            const float u = swap ? cosine[h] : sine[h], v = swap ? sine[h] : cosine[h];
+            sine[h] = __uint_as_float(__float_as_uint(u) ^ (quarter[h] & 0x80000000u));
+            cosine[h] = __uint_as_float(__float_as_uint(v) ^ ((quarter[h] + 0x40000000u) & 0x80000000u));
+        }
+        c[k] = two_of(cosine[0], cosine[1]);
+        sn[k] = two_of(sine[0], sine[1]);
     }
 }
 template <int D>
@@ -184,54 +230,63 @@ __device__ __forceinline__ float head_sum(float v)
     for (int o = 1; o < D / 16; o <<= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
     return v;
 }
-// x -> normed and rotated, in place: the lane's eight of the first half, then of the second
+// x -> normed and rotated, in place: pairs of the lane's eight of the first half, then of the second
 template <int D>
-__device__ __forceinline__ void norm_rotate(const HeadsShared<D>& s, const HeadsArgs& a, uint32_t key, uint32_t i0, const float (&c)[8],
-                                            const float (&sn)[8], float (&lo)[8], float (&hi)[8])
+__device__ __forceinline__ void norm_rotate(const HeadsShared<D>& s, const HeadsArgs& a, uint32_t key, uint32_t i0, const uint64_t (&c)[4],
+                                            const uint64_t (&sn)[4], uint64_t (&lo)[4], uint64_t (&hi)[4])
 {
     if (a.q_norm) {
-        float sum = 0.0f, w[16];
+        uint64_t sum = mul_two(lo[0], lo[0]), other = mul_two(hi[0], hi[0]);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) sum = fmaf(lo[k], lo[k], fmaf(hi[k], hi[k], sum));
-        const float r = rsqrtf(head_sum<D>(sum) * (1.0f / D) + a.eps);
-        load_norm<D>(s, key, i0, w);
+        for (int k = 1; k < 4; ++k) {
+            sum = fma_two(lo[k], lo[k], sum);
+            other = fma_two(hi[k], hi[k], other);
+        }
+        float x, y;
+        parts_of(add_two(sum, other), x, y);
+        const float r = rsqrtf(head_sum<D>(x + y) * (1.0f / D) + a.eps);
+        uint64_t w[8];
+        load_norm<D>(s, a, key, i0, w);
+        const uint64_t r2 = same_two(r);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            lo[k] *= r * w[k];
-            hi[k] *= r * w[8 + k];
+        for (int k = 0; k < 4; ++k) {
+            lo[k] = mul_two(lo[k], mul_two(w[k], r2));
+            hi[k] = mul_two(hi[k], mul_two(w[4 + k], r2));
         }
     }
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-        const float l = lo[k], h = hi[k];
-        lo[k] = fmaf(l, c[k], -h * sn[k]);
-        hi[k] = fmaf(h, c[k], l * sn[k]);
+    for (int k = 0; k < 4; ++k) {
+        const uint64_t l = lo[k], h = hi[k];
+        lo[k] = fma_two(l, c[k], mul_two(h, sn[k] ^ 0x8000000080000000ull));
+        hi[k] = fma_two(h, c[k], mul_two(l, sn[k]));
     }
 }
 
-// Heads [0, a.heads) of the CTA's tokens.
-template <int D, bool F32>
-__device__ __forceinline__ void rotate_heads(const HeadsArgs& a, const HeadsShared<D>& s, uint32_t cta)
+// Heads [0, a.heads) of the CTA's tokens.  `ready` fills the CTA's shared memory and waits for all of it: the first rows are on their way before.
+template <int D, bool F32, class Ready>
+__device__ __forceinline__ void rotate_heads(const HeadsArgs& a, const HeadsShared<D>& s, uint32_t cta, Ready ready)
 {
     constexpr uint32_t kLanes = D / 16, kHeads = 32 / kLanes;  // of a head; heads of a warp
-    const uint32_t lane = threadIdx.x & 31, i0 = (lane % kLanes) * 8;
+    const uint32_t lane = threadIdx.x & 31, i0 = (lane % kLanes) * 8, sub = lane / kLanes;
     const uint64_t w = (uint64_t)cta * (blockDim.x / 32) + (threadIdx.x >> 5);
     const uint32_t row = (uint32_t)(w / a.parts), part = (uint32_t)(w % a.parts);
-    if (row >= a.rows) return;
-    const int32_t position = ((const volatile int32_t*)a.positions)[row];
-    if (position < 0) return;
     const uint32_t groups = (a.heads + kHeads - 1) / kHeads, per = (groups + a.parts - 1) / a.parts;
+    const uint32_t first = part * per, end = row < a.rows ? min(groups, first + per) : 0;
     const char* x = (const char*)a.x + (uint64_t)row * a.ldx * kSize<F32>;
     char* y = (char*)a.y + (uint64_t)row * a.ldy * kSize<F32>;
-    const uint32_t first = part * per, end = min(groups, first + per), sub = lane / kLanes;
-    if (first >= end) return;
     auto at = [&](uint32_t g) { return ((uint64_t)min(g * kHeads + sub, a.heads - 1) * D + i0) * kSize<F32>; };
-    Raw<F32> next;
-    load16<D, F32>(x + at(first), a.vec, next);
-    float c[8], sn[8];
+    Raw<F32> next;  // (loads two groups ahead, with three CTAs an SM for their registers, gain nothing)
+    int32_t position = -1;
+    if (first < end) {
+        position = ((const volatile int32_t*)a.positions)[row];
+        load16<D, F32>(x + at(first), a.vec, next);
+    }
+    ready();
+    if (position < 0) return;
+    uint64_t c[4], sn[4];
     angles<D>(s, i0, position, c, sn);
     for (uint32_t g = first; g < end; ++g) {
-        float lo[8], hi[8];
+        uint64_t lo[4], hi[4];
         next.get(lo, hi);
         if (g + 1 < end) load16<D, F32>(x + at(g + 1), a.vec, next);
         const uint32_t head = g * kHeads + sub;
@@ -250,7 +305,29 @@ __device__ __forceinline__ float scale_above(float m)
     const int e = (int)(bits >> 23) - 127 - 8 + ((bits & 0x7FFFFFu) > 0x600000u);
     return __uint_as_float((uint32_t)(max(e, -100) + 127) << 23);
 }
-__device__ __forceinline__ bool finite(float v) { return (__float_as_uint(v) & 0x7F800000u) != 0x7F800000u; }
+__device__ __forceinline__ uint64_t finite_or_zero(uint64_t two)
+{
+    float v[2];
+    parts_of(two, v[0], v[1]);
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+        if ((__float_as_uint(v[h]) & 0x7F800000u) == 0x7F800000u) v[h] = 0.0f;
+    return two_of(v[0], v[1]);
+}
+__device__ __forceinline__ float most_of(uint64_t two)
+{
+    float lo, hi;
+    parts_of(two, lo, hi);
+    return fmaxf(fabsf(lo), fabsf(hi));
+}
+__device__ __forceinline__ uint2 codes_of(const uint64_t (&two)[4], float inv)
+{
+    float v[8];
+    const uint64_t by = two_of(inv, inv);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) parts_of(mul_two(two[k], by), v[2 * k], v[2 * k + 1]);
+    return pack8(v);
+}
 
 // Codes of the block's first `bytes` bytes, held at a scale `ratio` times the new one.
 __device__ __forceinline__ void shift_codes(uint8_t* codes, uint32_t bytes, float ratio)
@@ -275,14 +352,15 @@ __device__ __forceinline__ void shift_codes(uint8_t* codes, uint32_t bytes, floa
 
 // One run of one head: keys normed and rotated, values as they are, both to codes.  TURNS: tokens a group of lanes takes; its one token's values
 // stay in registers until the scales are known, of several they are made twice (with two in registers the kernel takes twice as many).
-template <int D, bool F32, int TURNS>
-__device__ __forceinline__ void append_run(const HeadsArgs& a, const HeadsShared<D>& s, uint32_t cta)
+template <int D, bool F32, int TURNS, class Ready>
+__device__ __forceinline__ void append_run(const HeadsArgs& a, const HeadsShared<D>& s, uint32_t cta, Ready ready)
 {
     constexpr uint32_t kLanes = D / 16, kGroups = kAppendThreads / kLanes;
-    __shared__ float s_most[2][kAppendThreads / 32];
+    __shared__ uint32_t s_most[2];  // bits of the largest magnitudes
     const uint32_t head = cta % a.n_kv;
     int4 run;
     asm volatile("ld.global.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(run.x), "=r"(run.y), "=r"(run.z), "=r"(run.w) : "l"(a.runs + cta / a.n_kv) : "memory");
+    if (threadIdx.x < 2) s_most[threadIdx.x] = 0;
     const uint32_t block = (uint32_t)run.x, start = (uint32_t)run.y, row0 = (uint32_t)run.z, count = (uint32_t)run.w;
     if (count == 0 || block >= a.n_blocks || start >= a.block_tokens || count > a.block_tokens - start || row0 >= a.rows || count > a.rows - row0)
         return;
@@ -293,45 +371,59 @@ __device__ __forceinline__ void append_run(const HeadsArgs& a, const HeadsShared
         k_was = *(const volatile float*)(a.k_scale + tile);
         v_was = *(const volatile float*)(a.v_scale + tile);
     }
-    float k_lo[8], k_hi[8], v_lo[8], v_hi[8];
-    bool poisoned;
-    auto token = [&](int t) {
-        // (all lanes take part in the head's sums; those without a token take the run's last one)
-        const uint32_t row = row0 + min(group + t * kGroups, count - 1);
+    // (all lanes take part in the head's sums; those without a token take the run's last one)
+    auto row_of = [&](int t) { return row0 + min(group + t * kGroups, count - 1); };
+    Raw<F32> rk, rv;
+    int32_t position;
+    auto load = [&](int t) {
+        const uint32_t row = row_of(t);
         const char* x = (const char*)a.x + ((uint64_t)row * a.ldx + (uint64_t)(a.n_q + head) * D + i0) * kSize<F32>;
-        Raw<F32> rk, rv;
+        position = ((const volatile int32_t*)a.positions)[row];
         load16<D, F32>(x, a.vec, rk);
         load16<D, F32>(x + (uint64_t)a.n_kv * D * kSize<F32>, a.vec, rv);
-        float c[8], sn[8];
-        angles<D>(s, i0, ((const volatile int32_t*)a.positions)[row], c, sn);
+    };
+    uint64_t k_lo[4], k_hi[4], v_lo[4], v_hi[4];
+    bool poisoned;
+    auto token = [&] {
+        uint64_t c[4], sn[4];
+        angles<D>(s, i0, position, c, sn);
         rk.get(k_lo, k_hi);
         rv.get(v_lo, v_hi);
         norm_rotate<D>(s, a, 1, i0, c, sn, k_lo, k_hi);
-        bool all = true;
-        auto keep = [&](float& f) {
-            if (!finite(f)) {
-                all = false;
-                f = 0.0f;
-            }
-        };
+        // zero times a value is zero, unless the value is not finite
+        uint64_t odd = 0;
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            keep(k_lo[k]);
-            keep(k_hi[k]);
-            keep(v_lo[k]);
-            keep(v_hi[k]);
+        for (int k = 0; k < 4; ++k) {
+            odd = fma_two(k_lo[k], 0, odd);
+            odd = fma_two(k_hi[k], 0, odd);
+            odd = fma_two(v_lo[k], 0, odd);
+            odd = fma_two(v_hi[k], 0, odd);
         }
-        const uint32_t bad = __ballot_sync(0xFFFFFFFFu, !all);
+        float p, q;
+        parts_of(odd, p, q);
+        const uint32_t bad = __ballot_sync(0xFFFFFFFFu, p != 0.0f || q != 0.0f);
         poisoned = bad >> (lane / kLanes * kLanes) & ((1u << kLanes) - 1);
+        if (poisoned) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                k_lo[k] = finite_or_zero(k_lo[k]);
+                k_hi[k] = finite_or_zero(k_hi[k]);
+                v_lo[k] = finite_or_zero(v_lo[k]);
+                v_hi[k] = finite_or_zero(v_hi[k]);
+            }
+        }
     };
+    load(0);
+    ready();
     float k_most = 0.0f, v_most = 0.0f;
 #pragma unroll 1
     for (int t = 0; t < TURNS; ++t) {
-        token(t);
+        if (t) load(t);
+        token();
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            k_most = fmaxf(k_most, fmaxf(fabsf(k_lo[k]), fabsf(k_hi[k])));
-            v_most = fmaxf(v_most, fmaxf(fabsf(v_lo[k]), fabsf(v_hi[k])));
+        for (int k = 0; k < 4; ++k) {
+            k_most = fmaxf(k_most, fmaxf(most_of(k_lo[k]), most_of(k_hi[k])));
+            v_most = fmaxf(v_most, fmaxf(most_of(v_lo[k]), most_of(v_hi[k])));
         }
     }
 #pragma unroll
@@ -339,17 +431,9 @@ __device__ __forceinline__ void append_run(const HeadsArgs& a, const HeadsShared
         k_most = fmaxf(k_most, __shfl_xor_sync(0xFFFFFFFFu, k_most, o));
         v_most = fmaxf(v_most, __shfl_xor_sync(0xFFFFFFFFu, v_most, o));
     }
-    if (lane == 0) {
-        s_most[0][threadIdx.x >> 5] = k_most;
-        s_most[1][threadIdx.x >> 5] = v_most;
-    }
+    if (lane < 2) atomicMax(&s_most[lane], __float_as_uint(lane ? v_most : k_most));
     __syncthreads();
-#pragma unroll
-    for (int w = 0; w < kAppendThreads / 32; ++w) {
-        k_most = fmaxf(k_most, s_most[0][w]);
-        v_most = fmaxf(v_most, s_most[1][w]);
-    }
-    const float k_scale = fmaxf(scale_above(k_most), k_was), v_scale = fmaxf(scale_above(v_most), v_was);
+    const float k_scale = fmaxf(scale_above(__uint_as_float(s_most[0])), k_was), v_scale = fmaxf(scale_above(__uint_as_float(s_most[1])), v_was);
     const float k_inv = __frcp_rn(k_scale), v_inv = __frcp_rn(v_scale);
     if (threadIdx.x == 0) {  // (read by all before the barrier)
         a.k_scale[tile] = k_scale;
@@ -361,23 +445,19 @@ __device__ __forceinline__ void append_run(const HeadsArgs& a, const HeadsShared
     if (start && v_was != v_scale) shift_codes(v, start * D, v_was * v_inv);
 #pragma unroll 1
     for (int t = 0; t < TURNS; ++t) {
-        if (TURNS > 1) token(t);
+        if (TURNS > 1) {
+            load(t);
+            token();
+        }
         const uint32_t j = group + t * kGroups;
         if (j < count) {
             const uint32_t o = (start + j) * D + i0;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                k_lo[i] *= k_inv;
-                k_hi[i] *= k_inv;
-                v_lo[i] *= v_inv;
-                v_hi[i] *= v_inv;
-            }
-            uint2 first = pack8(k_lo);
+            uint2 first = codes_of(k_lo, k_inv);
             if (poisoned && i0 == 0) first.x = (first.x & ~0xFFu) | 0x7Fu;
             *(uint2*)(k + o) = first;
-            *(uint2*)(k + o + D / 2) = pack8(k_hi);
-            *(uint2*)(v + o) = pack8(v_lo);
-            *(uint2*)(v + o + D / 2) = pack8(v_hi);
+            *(uint2*)(k + o + D / 2) = codes_of(k_hi, k_inv);
+            *(uint2*)(v + o) = codes_of(v_lo, v_inv);
+            *(uint2*)(v + o + D / 2) = codes_of(v_hi, v_inv);
         }
     }
 }
@@ -389,16 +469,18 @@ __global__ void __launch_bounds__(TURNS ? kAppendThreads : kThreads, TURNS ? 2 :
     __shared__ HeadsShared<D> s;
     fill_turns<D>(s, a);
     after_previous();
-    fill_norms<D>(s, a);
-    __syncthreads();
-    if (TURNS && blockIdx.x < a.cache_ctas) {
-        if constexpr (TURNS > 0) append_run<D, F32, TURNS>(a, s, blockIdx.x);
+    auto ready = [&] {
+        fill_norms<D>(s, a);
+        __syncthreads();
+    };
+    if (TURNS && blockIdx.x < a.cache_ctas) {  // (the two kinds of CTA in turn: 51 us where this takes 49)
+        if constexpr (TURNS > 0) append_run<D, F32, TURNS>(a, s, blockIdx.x, ready);
     } else {
-        rotate_heads<D, F32>(a, s, blockIdx.x - a.cache_ctas);
+        rotate_heads<D, F32>(a, s, blockIdx.x - a.cache_ctas, ready);
     }
 }
 
-// Back through rotation and norm.  CTAs stride over the tokens; a warp takes one token's query heads, then its key heads.
+// Back through rotation and norm.  Warps stride over tokens, or parts of their heads: groups of query heads, then of key heads.
 template <int D, bool F32>
 __global__ void __launch_bounds__(kThreads, 2) grad_kernel(const __grid_constant__ HeadsArgs a)
 {
@@ -410,70 +492,85 @@ __global__ void __launch_bounds__(kThreads, 2) grad_kernel(const __grid_constant
     fill_norms<D>(s, a);
     __syncthreads();
     const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5, i0 = (lane % kLanes) * 8;
-    float dw[2][16];
+    uint64_t dw[2][8];
 #pragma unroll
-    for (int k = 0; k < 16; ++k) dw[0][k] = dw[1][k] = 0.0f;
-    for (uint64_t row = (uint64_t)blockIdx.x * kWarps + warp; row < a.rows; row += (uint64_t)gridDim.x * kWarps) {
+    for (int k = 0; k < 8; ++k) dw[0][k] = dw[1][k] = 0;
+    const uint32_t q_groups = (a.n_q + kHeads - 1) / kHeads, groups = q_groups + (a.n_kv + kHeads - 1) / kHeads;
+    for (uint64_t u = (uint64_t)blockIdx.x * kWarps + warp; u < (uint64_t)a.rows * a.parts; u += (uint64_t)gridDim.x * kWarps) {
+        const uint64_t row = u / a.parts;
+        const uint32_t part = (uint32_t)(u - row * a.parts), begin = groups * part / a.parts, end = groups * (part + 1) / a.parts;
         const int32_t position = ((const volatile int32_t*)a.positions)[row];
         if (position < 0) continue;
         const char* x = (const char*)a.x + row * a.ldx * kSize<F32>;
         const char* dy = (const char*)a.dy + row * a.lddy * kSize<F32>;
         char* dx = (char*)a.y + row * a.ldy * kSize<F32>;
-        float c[8], sn[8];
+        // groups of query heads, then of key heads: the lane's head of group g, and where its values are
+        auto head_of = [&](uint32_t g) { return (g < q_groups ? g : g - q_groups) * kHeads + lane / kLanes; };
+        auto at_of = [&](uint32_t g) {
+            const uint32_t h = g < q_groups ? min(head_of(g), a.n_q - 1) : a.n_q + min(head_of(g), a.n_kv - 1);
+            return ((uint64_t)h * D + i0) * kSize<F32>;
+        };
+        Raw<F32> next_dy, next_x;
+        if (begin < end) {
+            load16<D, F32>(dy + at_of(begin), a.vec, next_dy);
+            if (a.q_norm) load16<D, F32>(x + at_of(begin), a.vec, next_x);
+        }
+        uint64_t c[4], sn[4];
         angles<D>(s, i0, position, c, sn);
+        for (uint32_t gr = begin; gr < end; ++gr) {
+            const bool key = gr >= q_groups, mine = head_of(gr) < (key ? a.n_kv : a.n_q);
+            const uint64_t at = at_of(gr);
+            uint64_t v[2][4], g[2][4];
+            next_dy.get(g[0], g[1]);
+            if (a.q_norm) next_x.get(v[0], v[1]);
+            if (gr + 1 < end) {
+                load16<D, F32>(dy + at_of(gr + 1), a.vec, next_dy);
+                if (a.q_norm) load16<D, F32>(x + at_of(gr + 1), a.vec, next_x);
+            }
 #pragma unroll
-        for (int key = 0; key < 2; ++key) {
-            const uint32_t first = key ? a.n_q : 0, heads = key ? a.n_kv : a.n_q;
-            auto at_of = [&](uint32_t h0) { return ((uint64_t)(first + min(h0 + lane / kLanes, heads - 1)) * D + i0) * kSize<F32>; };
-            Raw<F32> next_dy, next_x;
-            load16<D, F32>(dy + at_of(0), a.vec, next_dy);
-            if (a.q_norm) load16<D, F32>(x + at_of(0), a.vec, next_x);
-            for (uint32_t h0 = 0; h0 < heads; h0 += kHeads) {
-                const bool mine = h0 + lane / kLanes < heads;
-                const uint64_t at = at_of(h0);
-                float v[2][8], g[2][8];
-                next_dy.get(g[0], g[1]);
-                if (a.q_norm) next_x.get(v[0], v[1]);
-                if (h0 + kHeads < heads) {
-                    load16<D, F32>(dy + at_of(h0 + kHeads), a.vec, next_dy);
-                    if (a.q_norm) load16<D, F32>(x + at_of(h0 + kHeads), a.vec, next_x);
+            for (int k = 0; k < 4; ++k) {
+                const uint64_t l = g[0][k], up = g[1][k];
+                g[0][k] = fma_two(l, c[k], mul_two(up, sn[k]));
+                g[1][k] = fma_two(up, c[k], mul_two(l, sn[k] ^ 0x8000000080000000ull));
+            }
+            if (a.q_norm) {
+                uint64_t sum2 = 0, dot2 = 0, w[8];
+                load_norm<D>(s, a, key, i0, w);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const uint64_t f = v[i / 4][i % 4];
+                    sum2 = fma_two(f, f, sum2);
+                    w[i] = mul_two(g[i / 4][i % 4], w[i]);
+                    dot2 = fma_two(w[i], f, dot2);
+                }
+                float lo, hi;
+                parts_of(sum2, lo, hi);
+                const float sum = head_sum<D>(lo + hi);
+                parts_of(dot2, lo, hi);
+                const float dot = head_sum<D>(lo + hi);
+                const float r = rsqrtf(sum * (1.0f / D) + a.eps);
+                const uint64_t r2 = same_two(r), back = same_two(-dot * (1.0f / D) * r * r), mine2 = same_two(mine ? r : 0.0f);
+                if (key) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) dw[1][i] = fma_two(g[i / 4][i % 4], mul_two(v[i / 4][i % 4], mine2), dw[1][i]);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) dw[0][i] = fma_two(g[i / 4][i % 4], mul_two(v[i / 4][i % 4], mine2), dw[0][i]);
                 }
 #pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    const float l = g[0][k], u = g[1][k];
-                    g[0][k] = fmaf(l, c[k], u * sn[k]);
-                    g[1][k] = fmaf(u, c[k], -l * sn[k]);
-                }
-                if (a.q_norm) {
-                    float sum = 0.0f, dot = 0.0f, w[16];
-                    load_norm<D>(s, key, i0, w);
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const float f = v[i / 8][i % 8];
-                        sum = fmaf(f, f, sum);
-                        dot = fmaf(g[i / 8][i % 8] * w[i], f, dot);
-                    }
-                    sum = head_sum<D>(sum);
-                    dot = head_sum<D>(dot);
-                    const float r = rsqrtf(sum * (1.0f / D) + a.eps), back = dot * (1.0f / D) * r * r;
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const float f = v[i / 8][i % 8], gi = g[i / 8][i % 8];
-                        if (mine) dw[key][i] = fmaf(gi, f * r, dw[key][i]);
-                        g[i / 8][i % 8] = r * fmaf(-f, back, gi * w[i]);
-                    }
-                }
-                if (mine) {
-                    store8<F32>(dx + at, a.vec_y, g[0]);
-                    store8<F32>(dx + at + D / 2 * kSize<F32>, a.vec_y, g[1]);
-                }
+                for (int i = 0; i < 8; ++i) g[i / 4][i % 4] = mul_two(r2, fma_two(v[i / 4][i % 4], back, w[i]));
+            }
+            if (mine) {
+                store8<F32>(dx + at, a.vec_y, g[0]);
+                store8<F32>(dx + at + D / 2 * kSize<F32>, a.vec_y, g[1]);
             }
         }
     }
     if (!a.q_norm) return;
 #pragma unroll
     for (int i = 0; i < 32; ++i) {
-        float v = dw[i / 16][i % 16];
+        float v, other;
+        parts_of(dw[i / 16][i % 16 / 2], i & 1 ? other : v, i & 1 ? v : other);
 #pragma unroll
         for (int o = kLanes; o < 32; o <<= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
         if (lane < kLanes) s_sum[warp][i / 16][(i % 16 / 8) * (D / 2) + i0 + i % 8] = v;
@@ -601,7 +698,7 @@ HeadsArgs heads_args(const dr_qk* qk, const void* x, uint32_t dtype, uint64_t ld
     return a;
 }
 
-constexpr uint32_t kWarpsWanted = 96;  // for each SM: three rounds of the 32 that run at a time
+constexpr uint32_t kWarpsWanted = 40;  // for each SM, of which 32 run at a time (8192 tokens of 40 heads: 34 us; three times as many 35, six times 44)
 
 // How many warps a token's head groups are dealt to: one while the tokens alone fill the machine some times over, so that it works out the
 // angles once; with few tokens every group has a warp of its own.
@@ -614,6 +711,7 @@ void deal(HeadsArgs& a, int sms, uint32_t dim)
 }
 
 constexpr uint32_t kGradCtas = 2;  // for each SM
+constexpr uint32_t kGradParts = 2;  // 8192 tokens of 40 heads: 55.7 us; undivided 57.7, in three 59.9
 
 }  // namespace
 }  // namespace dr
@@ -787,7 +885,11 @@ int dr_qk_grad(const dr_qk* qk, const void* x_dev, uint32_t dtype, uint64_t ldx,
     a.lddy = lddy;
     a.vec = ((norms ? (uintptr_t)x_dev | ldx * es : 0) | (uintptr_t)dy_dev | lddy * es) % 16 == 0;
     a.work = (float*)work_dev;
-    const uint64_t most = (uint64_t)kGradCtas * qk->sms, wanted = (rows + kWarps - 1) / kWarps, ctas = wanted < most ? wanted : most;
+    // parts of a token's heads, so that the warps' shares differ by little
+    const uint64_t most = (uint64_t)kGradCtas * qk->sms;
+    const uint32_t per_warp = 512 / qk->d.head_dim, groups = (a.n_q + per_warp - 1) / per_warp + (a.n_kv + per_warp - 1) / per_warp;
+    a.parts = groups < kGradParts ? groups : kGradParts;
+    const uint64_t wanted = (rows * a.parts + kWarps - 1) / kWarps, ctas = wanted < most ? wanted : most;
     cudaStream_t s = (cudaStream_t)cuda_stream;
     if (ctas) {
         if (qk->d.head_dim == 64)
