@@ -209,16 +209,22 @@ __device__ __forceinline__ void produce(const AttendArgs& a, Shared<D, SETS>& s,
                     ks = a.k_scale[(uint64_t)id * a.n_kv + head];
                     vs = fmaxf(a.v_scale[(uint64_t)id * a.n_kv + head], kLeastScale);
                 }
-                const float v_log = log2f(vs), v_inv = 1.0f / vs;
                 const uint32_t pieces = __ballot_sync(0xFFFFFFFFu, ok && (lane & 3) * 16 % box == 0);
                 const int row = (int)((id * a.n_kv + head << a.block_log2) + (token & (1u << a.block_log2) - 1));
                 for (uint32_t b = 0; b < 8 && t0 + b < count; ++b) {
                     if (!warp_wait(empty + 8 * ring.slot, ring.round ^ 1, &s.limit, &g_wait_failures)) return;
+                    // the copies first: they need no scales, which may still be on their way
+                    const uint32_t mine = pieces >> (4 * b) & 15, bar = full + 8 * ring.slot;
+                    if (!a.starve && lane / 4 == b && (mine >> (lane & 3) & 1)) {
+                        const uint32_t to = (lane & 3) * 16 * D;
+                        load_2d<false>(smem_u32(s.k[ring.slot]) + to, k_map, bar, 0, row);
+                        load_2d<false>(smem_u32(s.v[ring.slot]) + to, v_map, bar, 0, row);
+                    }
                     Meta& m = s.meta[ring.slot];
                     if (lane / 4 == b) {
                         m.k_scale[lane & 3] = ks;
-                        m.v_log[lane & 3] = v_log;
-                        m.v_inv[lane & 3] = v_inv;
+                        m.v_log[lane & 3] = log2f(vs);
+                        m.v_inv[lane & 3] = 1.0f / vs;
                         m.ok[lane & 3] = ok;
                         if ((lane & 3) == 0) {
                             m.flags = (t0 + b == 0 ? kFirst : 0) | (t0 + b + 1 == count ? kLast : 0);
@@ -232,16 +238,8 @@ __device__ __forceinline__ void produce(const AttendArgs& a, Shared<D, SETS>& s,
                         }
                     }
                     __syncwarp();
-                    const uint32_t mine = pieces >> (4 * b) & 15, bar = full + 8 * ring.slot;
-                    if (!a.starve) {
-                        if (lane == 0) bar_expect(bar, (uint32_t)__popc(mine) * box * D * 2);
-                        __syncwarp();
-                        if (lane / 4 == b && (mine >> (lane & 3) & 1)) {
-                            const uint32_t to = (lane & 3) * 16 * D;
-                            load_2d<false>(smem_u32(s.k[ring.slot]) + to, k_map, bar, 0, row);
-                            load_2d<false>(smem_u32(s.v[ring.slot]) + to, v_map, bar, 0, row);
-                        }
-                    }
+                    // (the stage cannot be full before this arrival, whatever has landed)
+                    if (!a.starve && lane == 0) bar_expect(bar, (uint32_t)__popc(mine) * box * D * 2);
                     __syncwarp();
                     ring.next();
                 }
@@ -390,24 +388,47 @@ __device__ __forceinline__ void consume(const AttendArgs& a, Shared<D, SETS>& s,
     float o[SETS][kChunks][4], m[SETS][2], l[SETS][2];
     Turn<kStages<SETS>> ring;
     uint32_t met = 0;
+    // a group's rows (everybody has read those of the group before: the warps met at its end)
+    auto load_rows = [&](const Meta& g_) {
+#pragma unroll
+        for (int n = 0; n < SETS; ++n) {
+            const Row row = row_of(a, g_, 8 * n + g);
+            const float undo = load_row<D>(a, row, qf[kHeld ? n : 0]);
+            if (warp == 0 && tig == 0) {
+                s.back[8 * n + g] = undo;
+                s.p[8 * n + g] = row.p;
+            }
+            if (!kHeld && warp == n) {
+#pragma unroll
+                for (int c = 0; c < kChunks; ++c) s.q[kHeld ? 0 : n][c][lane] = make_uint2(qf[0][c][0], qf[0][c][1]);
+            }
+        }
+        return meet(s, met);
+    };
+    // the first group's while its tiles are on their way
+    {
+        const Request q = request_of(a, s.request);
+        const uint32_t groups = groups_of<SETS>(a, q.n);
+        const uint64_t segment = s.offset / (a.whole ? 1 : tiles_of_request(a, q).count);
+        Meta first;
+        first.row0 = q.row0;
+        first.n = q.n;
+        first.len = q.len;
+        first.head = (uint32_t)(segment / groups);
+        first.rows0 = (uint32_t)(segment % groups) * kRows<SETS>;
+        if (!load_rows(first)) return;
+    }
+    bool loaded = true;
     for (;;) {
         if (!__all_sync(0xFFFFFFFFu, bar_wait(full + 8 * ring.slot, ring.round, &s.limit, &g_wait_failures))) return;
         const Meta& meta = s.meta[ring.slot];
         const uint32_t flags = meta.flags;
         if (flags & kEnd) return;
         if (flags & kFirst) {
+            if (!loaded && !load_rows(meta)) return;
+            loaded = false;
 #pragma unroll
             for (int n = 0; n < SETS; ++n) {
-                const Row row = row_of(a, meta, 8 * n + g);
-                const float undo = load_row<D>(a, row, qf[kHeld ? n : 0]);
-                if (warp == 0 && tig == 0) {
-                    s.back[8 * n + g] = undo;
-                    s.p[8 * n + g] = row.p;
-                }
-                if (!kHeld && warp == n) {
-#pragma unroll
-                    for (int c = 0; c < kChunks; ++c) s.q[kHeld ? 0 : n][c][lane] = make_uint2(qf[0][c][0], qf[0][c][1]);
-                }
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     m[n][h] = -INFINITY;
@@ -418,7 +439,6 @@ __device__ __forceinline__ void consume(const AttendArgs& a, Shared<D, SETS>& s,
 #pragma unroll
                     for (int e = 0; e < 4; ++e) o[n][c][e] = 0.0f;
             }
-            if (!meet(s, met)) return;  // (everybody has read the rows of the group before: they met at its end)
         }
         const int t0 = (int)(meta.token + warp * 16);
         if (meta.ok[warp] && t0 < (int)meta.len) {
@@ -636,9 +656,9 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm<SETS>)
 }
 
 // The parts of a group that several CTAs have, added in an order of their own: eight rows a CTA and a warp for each where a group has few
-// parts, four rows and four warps for each where it has many (74 parts one after another took 30 us); eight parts' loads are on their
+// parts, two rows and eight warps for each where it has many (111 parts one after another took 30 us); eight parts' loads are on their
 // way together.
-template <int WARPS> constexpr uint32_t kJoinRows = WARPS == 1 ? 8 : 4;
+template <int WARPS> constexpr uint32_t kJoinRows = WARPS == 1 ? 8 : 2;
 template <int D, int SETS, int WARPS>
 __global__ void __launch_bounds__(32 * kJoinRows<WARPS> * WARPS) join_kernel(const __grid_constant__ AttendArgs a, const Part<D, SETS>* parts, const Join* joins)
 {
@@ -745,10 +765,10 @@ int launch_few(const dr_kv_cache* cache, const AttendArgs& a, void* work, cudaSt
         // a dozen parts a group on average divide the two
         const uint64_t rows = ((uint64_t)a.rows * a.group + a.requests - 1) / a.requests, groups = (uint64_t)a.requests * a.n_kv * ((rows + kRows<SETS> - 1) / kRows<SETS>);
         const bool few = groups * 12 >= ctas;
-        cfg.gridDim = dim3(ctas, kRows<SETS> / (few ? kJoinRows<1> : kJoinRows<4>));
-        cfg.blockDim = dim3(few ? 32 * kJoinRows<1> : 32 * 4 * kJoinRows<4>);
+        cfg.gridDim = dim3(ctas, kRows<SETS> / (few ? kJoinRows<1> : kJoinRows<8>));
+        cfg.blockDim = dim3(few ? 32 * kJoinRows<1> : 32 * 8 * kJoinRows<8>);
         cfg.dynamicSmemBytes = 0;
-        e = cudaLaunchKernelEx(&cfg, few ? join_kernel<D, SETS, 1> : join_kernel<D, SETS, 4>, a, (const Part<D, SETS>*)parts, (const Join*)joins);
+        e = cudaLaunchKernelEx(&cfg, few ? join_kernel<D, SETS, 1> : join_kernel<D, SETS, 8>, a, (const Part<D, SETS>*)parts, (const Join*)joins);
     }
     if (e != cudaSuccess) {
         cudaGetLastError();
