@@ -615,8 +615,8 @@ int dr_linear_wgrad(const dr_linear* lin, const void* x_dev, uint64_t ldx, const
                     const int32_t* offsets_dev, float* dw_dev, uint64_t lddw, uint32_t accumulate, void* cuda_stream);
 
 /*
- * dr_diag_linear_wait_failures -- diagnostic: the tensor-core kernels of the linear layers wait for their copies and products
- * with a limit (2 s, and 10 us for every 64 of the contraction); a wait that runs out ends the kernel with its output incomplete and counts here.  *count = such waiting
+ * dr_diag_linear_wait_failures -- diagnostic: the tensor-core kernels of the linear layers and of dr_attend wait for their copies and products
+ * with a limit (2 s, and 10 us for every 64 of a linear layer's contraction); a wait that runs out ends the kernel with its output incomplete and counts here.  *count = such waiting
  * threads on the current device since the library was loaded; expected 0.  Waits for all work that the device
  * has been given, on every stream (so it cannot be captured).  DR_ERR_INVALID, DR_ERR_CUDA.
  */
@@ -737,7 +737,7 @@ int dr_qk_grad(const dr_qk* qk, const void* x_dev, uint32_t dtype, uint64_t ldx,
  *   offsets : requests + 1 int32, ascending, as dr_kv_extend gives them; NULL: one row a request (rows = requests)
  *   lengths : tokens of each request that the cache holds, the step's own among them
  *   work    : dr_attend_work's bytes of device memory that no other call uses meanwhile, 16-byte aligned
- * A row that sees nothing gets zeros, one that is not finite NaN.  Rows that no request owns are left as they were.  Lengths beyond the table's width and
+ * out must not overlap q.  A row that sees nothing gets zeros, one that is not finite NaN.  Rows that no request owns are left as they were.  Lengths beyond the table's width and
  * offsets beyond the rows are held inside.  Sums are fp32; which tokens are summed together depends on all lengths of the call, in a
  * fixed order: the same call gives the same bits.
  * Enqueues on cuda_stream, allocates nothing, reads nothing on the host, may be captured.  The waits inside are bounded as the linear

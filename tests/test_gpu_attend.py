@@ -206,3 +206,47 @@ def test_lengths_and_offsets_out_of_range_stay_inside():
     torch.cuda.synchronize()
     rc, failed = dr.dr_diag_linear_wait_failures()
     assert rc == 0 and failed == 0
+
+
+@pytest.mark.parametrize("added", [[1, 1], [6, 2], [140, 90]])
+@pytest.mark.parametrize("what", [float("nan"), float("inf"), -float("inf")])
+def test_query_rows_that_are_not_finite_give_nan_and_spoil_no_others(added, what):
+    lengths = [300, 100]
+    q, cache, table, offsets = setup(31, lengths, added, 8, 2, 128, 32)
+    want = dr.KVCache(*cache).attend(q, ints(lengths), table, ints(offsets))
+    bad = added[0] // 2
+    q[bad, 5 * 128 + 17] = what
+    got = dr.KVCache(*cache).attend(q, ints(lengths), table, ints(offsets))
+    nan = torch.zeros_like(want, dtype=torch.bool)
+    nan[bad, 5 * 128:6 * 128] = True
+    assert torch.equal(torch.isnan(got), nan) and torch.equal(got[~nan], want[~nan])
+
+
+@pytest.mark.parametrize("added", [[1, 1], [70, 3]])
+def test_codes_as_bytes_and_a_table_that_shares_blocks(added):
+    """uint8 codes are e4m3 codes; two requests may share the blocks of a common prefix."""
+    lengths = [200, 170]
+    q, cache, table, offsets = setup(37, lengths, added, 8, 2, 64, 32, garbage=False)
+    table[1, :3] = table[0, :3]
+    want = check(q, cache, table, lengths, offsets, 8)
+    k, v, ks, vs = cache
+    got = dr.KVCache(k.view(torch.uint8), v.view(torch.uint8), ks, vs).attend(q, ints(lengths), table, ints(offsets))
+    assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("added", [[1], [90]])
+def test_a_cache_beyond_four_gigabytes(added):
+    """Blocks whose codes lie past 2^32 bytes, written by append and read by attend."""
+    n_blocks, kv, block, dim, n = 300000, 2, 64, 128, 150
+    assert n_blocks * kv * block * dim > 1 << 32
+    c = dr.KVCache.empty(n_blocks, kv, block, dim)
+    table = ints([[n_blocks - 1, n_blocks - 7, 3]])
+    heads = dr.QKHeads(8, kv, dim)
+    x = torch.randn(n, 12 * dim, device=DEV, generator=gen(41)).bfloat16()
+    runs = ints([[n_blocks - 1, 0, 0, 64], [n_blocks - 7, 0, 64, 64], [3, 0, 128, 22]])
+    q = heads.append(x, torch.arange(n, device=DEV).int(), runs, c)[n - added[0]:]
+    got = c.attend(q, ints([n]), table, ints([0, added[0]]))
+    held = table[0].long()
+    near = torch.tensor([[0, 1, 2]], dtype=torch.int32, device=DEV)
+    want, tol = attention(q, c.k[held], c.v[held], c.k_scale[held], c.v_scale[held], [n], [0, added[0]], near, 8)
+    assert ((got.double() - want).abs() <= tol).all()
