@@ -752,6 +752,14 @@ int dr_attend(const dr_kv_cache* cache, const void* q_dev, uint64_t ldq, uint64_
               uint64_t window, uint64_t sinks, void* out_dev, uint64_t ldo, void* work_dev, uint64_t work_bytes, void* cuda_stream);
 
 /*
+ * dr_call -- for bindings whose calls cost by the argument: the entry point `what` with its arguments as 64-bit words in their order
+ * (integers and pointers as they are, a float as a double's bits, 32-bit ones in the low half), with the same checks and status.  DR_ERR_INVALID
+ * (NULL, unknown `what`).
+ */
+enum { DR_CALL_KV_EXTEND = 0, DR_CALL_QK_FORWARD = 1, DR_CALL_QK_APPEND = 2, DR_CALL_QK_GRAD = 3, DR_CALL_ATTEND = 4 };
+int dr_call(uint32_t what, const uint64_t* words);
+
+/*
  * Hysteresis-guided reconfiguration (Sec. 3.4; host only, no CUDA).  The controller only decides WHEN to
  * move between pre-specified topologies, listed from most-Training to most-Rollout (e.g. 6:2, 5:3, 4:4).
  * Per step: imbalance = (t_rollout - t_train) / max(t_rollout, t_train).  A step signals "towards

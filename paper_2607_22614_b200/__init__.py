@@ -14,6 +14,6 @@ from .binding import (  # noqa: F401
     Linear, quant_rows, dr_linear_desc, dr_linear_create, dr_linear_destroy, dr_linear_forward, dr_linear_dgrad, dr_linear_wgrad,
     dr_diag_linear_wait_failures, dr_diag_linear_waits, dr_quant_rows, DR_ROWS_PLAIN, DR_ROWS_SWIGLU,
     dr_kv_cache_desc, dr_kv_cache_create, dr_kv_cache_destroy, dr_kv_extend, dr_qk_desc, dr_qk_create, dr_qk_destroy, dr_qk_forward,
-    dr_qk_append, dr_qk_grad_work, dr_qk_grad, dr_attend_work, dr_attend,
+    dr_qk_append, dr_qk_grad_work, dr_qk_grad, dr_attend_work, dr_attend, dr_call,
 )
 from .attention import KVCache, QKHeads  # noqa: F401

@@ -70,7 +70,7 @@ class KVCache:
         if rc:
             self.handle = None
             raise B.DrError(rc, "dr_kv_cache_create")
-        self._work = {}
+        self._word, self._work = self.handle.value or 0, {}
 
     @classmethod
     def empty(cls, n_blocks, kv_heads, block_tokens, head_dim, device=None):
@@ -84,7 +84,7 @@ class KVCache:
     def close(self):
         if getattr(self, "handle", None):
             B.dr_kv_cache_destroy(self.handle)
-            self.handle = None
+            self.handle, self._word = None, 0
 
     def __del__(self):
         if B is not None and B.lib is not None:  # at the interpreter's end the module may be gone before its objects
@@ -118,7 +118,7 @@ class KVCache:
         if runs is None:
             runs = B._empty(self.runs_for(n, rows), 4, _int32, lengths.device, stream)
         p_runs, n_runs = self._runs(runs)
-        rc = B._fn("dr_kv_extend")(self.handle, p_added, p_lengths, p_out, n, table.data_ptr(), ld, width, p_free, p_state, p_state_out,
+        rc = B._fn("dr_kv_extend")(self._word, p_added, p_lengths, p_out, n, table.data_ptr(), ld, width, p_free, p_state, p_state_out,
                                    rows, _ints(offsets, "offsets", n + 1, device), _ints(positions, "positions", rows, device), p_runs, n_runs,
                                    B._stream_of(device, stream))
         if rc:
@@ -154,7 +154,7 @@ class KVCache:
             raise ValueError("window and sinks must not be negative")
         n = lengths.numel()
         p_lengths = _ints(lengths, "lengths", n, device)
-        p_offsets = None if offsets is None else _ints(offsets, "offsets", n + 1, device)
+        p_offsets = 0 if offsets is None else _ints(offsets, "offsets", n + 1, device)
         if offsets is None and rows != n:
             raise ValueError("without offsets q has one row for each request")
         width, ld = _table(table, n, device)
@@ -171,7 +171,7 @@ class KVCache:
                 raise B.DrError(rc, "dr_attend_work")
             self._work[n_q] = need
         work = B._empty(1, need, _uint8, q.device, stream)
-        rc = B._fn("dr_attend")(self.handle, q.data_ptr(), ldq, n_q, rows, p_offsets, p_lengths, n, table.data_ptr(), ld, width,
+        rc = B._fn("dr_attend")(self._word, q.data_ptr(), ldq, n_q, rows, p_offsets, p_lengths, n, table.data_ptr(), ld, width,
                                 1.0 / math.sqrt(self.head_dim) if scale is None else scale, window, sinks, out.data_ptr(), ldo,
                                 work.data_ptr(), need, B._stream_of(device, stream))
         if rc:
@@ -213,13 +213,13 @@ class QKHeads:
         if rc:
             self.handle = None
             raise B.DrError(rc, "dr_qk_create")
-        self._work = None
+        self._word, self._work = self.handle.value or 0, None
         self._norms = () if q_norm is None else (q_norm, k_norm)
 
     def close(self):
         if getattr(self, "handle", None):
             B.dr_qk_destroy(self.handle)
-            self.handle = None
+            self.handle, self._word = None, 0
 
     def __del__(self):
         if B is not None and B.lib is not None:
@@ -252,7 +252,7 @@ class QKHeads:
         they are (of an allocated output: not initialised)."""
         rows, ldx, code = self._rows(x, self.n_q_heads + self.n_kv_heads, "x")
         y, ldy = self._out(out, rows, self.n_q_heads + self.n_kv_heads, x, "out", stream)
-        rc = B._fn("dr_qk_forward")(self.handle, x.data_ptr(), code, ldx, _ints(positions, "positions", rows, self.device), rows,
+        rc = B._fn("dr_qk_forward")(self._word, x.data_ptr(), code, ldx, _ints(positions, "positions", rows, self.device), rows,
                                     y.data_ptr(), ldy, B._stream_of(self.device, stream))
         if rc:
             raise B.DrError(rc, "dr_qk_forward")
@@ -268,8 +268,8 @@ class QKHeads:
         if cache.device != self.device:
             raise B._elsewhere(cache.k, "cache", self.device)
         p_runs, n_runs = cache._runs(runs)
-        rc = B._fn("dr_qk_append")(self.handle, x.data_ptr(), code, ldx, _ints(positions, "positions", rows, self.device), rows, p_runs,
-                                   n_runs, cache.handle, y.data_ptr(), ldy, B._stream_of(self.device, stream))
+        rc = B._fn("dr_qk_append")(self._word, x.data_ptr(), code, ldx, _ints(positions, "positions", rows, self.device), rows, p_runs,
+                                   n_runs, cache._word, y.data_ptr(), ldy, B._stream_of(self.device, stream))
         if rc:
             raise B.DrError(rc, "dr_qk_append")
         return y
@@ -284,7 +284,7 @@ class QKHeads:
         if dy_rows != rows or dy_code != code or dy.shape[1] != heads * self.head_dim:
             raise ValueError(f"dy must be {rows} x {heads * self.head_dim} of x's type")
         dx, lddx = self._out(dx, rows, heads, x, "dx", stream)
-        need, p_work, p_dq, p_dk = 0, None, None, None
+        need, p_work, p_dq, p_dk = 0, 0, 0, 0
         if self.q_norm is not None:
             if accumulate and (dq_norm is None or dk_norm is None):
                 raise ValueError("accumulate adds to dq_norm and dk_norm: give both")
@@ -308,7 +308,7 @@ class QKHeads:
             p_work = work.data_ptr()
         elif dq_norm is not None or dk_norm is not None:
             raise ValueError("without norms there are no gradients of them")
-        rc = B._fn("dr_qk_grad")(self.handle, x.data_ptr(), code, ldx, _ints(positions, "positions", rows, self.device), dy.data_ptr(), lddy,
+        rc = B._fn("dr_qk_grad")(self._word, x.data_ptr(), code, ldx, _ints(positions, "positions", rows, self.device), dy.data_ptr(), lddy,
                                  rows, dx.data_ptr(), lddx, p_dq, p_dk, int(accumulate), p_work, need, B._stream_of(self.device, stream))
         if rc:
             raise B.DrError(rc, "dr_qk_grad")

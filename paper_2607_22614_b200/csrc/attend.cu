@@ -2,6 +2,7 @@
 #include "attend.h"
 
 #include <cmath>
+#include <cstring>
 
 #include "linear.h"
 
@@ -108,6 +109,29 @@ int dr_attend(const dr_kv_cache* cache, const void* q_dev, uint64_t ldq, uint64_
     // each request's rows on the device decide which of the two takes it; without offsets every request has few
     if (offsets_dev) rc = launch_attend_many(cache, a, (cudaStream_t)cuda_stream);
     return rc ? rc : launch_attend_few(cache, a, work_dev, (cudaStream_t)cuda_stream);
+}
+
+int dr_call(uint32_t what, const uint64_t* w)
+{
+    if (!w || what > DR_CALL_ATTEND) {
+        set_error("NULL words or an unknown entry point");
+        return DR_ERR_INVALID;
+    }
+    if (what == DR_CALL_KV_EXTEND)
+        return dr_kv_extend((const dr_kv_cache*)w[0], (const int32_t*)w[1], (const int32_t*)w[2], (int32_t*)w[3], w[4], (int32_t*)w[5], w[6], w[7],
+                            (int32_t*)w[8], (const int32_t*)w[9], (int32_t*)w[10], w[11], (int32_t*)w[12], (int32_t*)w[13], (int32_t*)w[14], w[15], (void*)w[16]);
+    if (what == DR_CALL_QK_FORWARD)
+        return dr_qk_forward((const dr_qk*)w[0], (const void*)w[1], (uint32_t)w[2], w[3], (const int32_t*)w[4], w[5], (void*)w[6], w[7], (void*)w[8]);
+    if (what == DR_CALL_QK_APPEND)
+        return dr_qk_append((const dr_qk*)w[0], (const void*)w[1], (uint32_t)w[2], w[3], (const int32_t*)w[4], w[5], (const int32_t*)w[6], w[7],
+                            (const dr_kv_cache*)w[8], (void*)w[9], w[10], (void*)w[11]);
+    if (what == DR_CALL_QK_GRAD)
+        return dr_qk_grad((const dr_qk*)w[0], (const void*)w[1], (uint32_t)w[2], w[3], (const int32_t*)w[4], (const void*)w[5], w[6], w[7], (void*)w[8], w[9],
+                          (float*)w[10], (float*)w[11], (uint32_t)w[12], (void*)w[13], w[14], (void*)w[15]);
+    double scale;
+    memcpy(&scale, w + 11, sizeof scale);
+    return dr_attend((const dr_kv_cache*)w[0], (const void*)w[1], w[2], w[3], w[4], (const int32_t*)w[5], (const int32_t*)w[6], w[7], (const int32_t*)w[8],
+                     w[9], w[10], (float)scale, w[12], w[13], (void*)w[14], w[15], (void*)w[16], w[17], (void*)w[18]);
 }
 
 }  // extern "C"

@@ -200,3 +200,14 @@ def test_null_handles():
     assert B.dr_kv_extend(None, *[None] * 3, 0, None, 0, 0, None, None, None, 0, None, None, None, 0, None) == B.DR_ERR_INVALID
     assert B.dr_qk_forward(None, None, B.DR_BF16, 0, None, 0, None, 0, None) == B.DR_ERR_INVALID
     assert B.dr_attend(None, None, 0, 8, 0, None, None, 0, None, 0, 0, 1.0, 0, 0, None, 0, None, 0, None) == B.DR_ERR_INVALID
+
+
+def test_calls_by_words():
+    """dr_call has the entry points' own checks, and every packed form has as many words as its entry point has arguments."""
+    import struct
+    assert B.dr_call(0, None) == B.DR_ERR_INVALID and B.dr_call(5, bytes(200)) == B.DR_ERR_INVALID
+    for name, (what, form) in B._PACKED.items():
+        args = getattr(dr.lib(), name).argtypes
+        assert struct.calcsize(form) == 8 * len(args), name
+        assert B.dr_call(what, bytes(8 * len(args))) == B.DR_ERR_INVALID  # no handle
+        assert B._fn(name)(*[0] * len(args)) == B.DR_ERR_INVALID
