@@ -736,7 +736,8 @@ int dr_qk_grad(const dr_qk* qk, const void* x_dev, uint32_t dtype, uint64_t ldx,
  *   q   : bf16, row i at q + i * ldq, heads side by side (the query columns of a qkv row, say); out: bf16 [rows, n_q_heads * head_dim]
  *   offsets : requests + 1 int32, ascending, as dr_kv_extend gives them; NULL: one row a request (rows = requests)
  *   lengths : tokens of each request that the cache holds, the step's own among them
- *   work    : dr_attend_work's bytes of device memory that no other call uses meanwhile, 16-byte aligned
+ *   work    : dr_attend_work's bytes of device memory that no other call uses meanwhile, 16-byte aligned; none is needed (NULL, 0) where the
+ *             table's width holds at most 512 tokens
  * out must not overlap q.  A row that sees nothing gets zeros, one that is not finite NaN.  Rows that no request owns are left as they were.  Lengths beyond the table's width and
  * offsets beyond the rows are held inside.  Sums are fp32; which tokens are summed together depends on all lengths of the call, in a
  * fixed order: the same call gives the same bits.

@@ -164,16 +164,21 @@ class KVCache:
             got_rows, got_cols, ldo = B._matrix(out, "out", device)
             if got_rows != rows or got_cols != cols or out.dtype is not _bfloat16:
                 raise ValueError(f"out must be bfloat16, {rows} x {cols}")
-        need = self._work.get(n_q)  # (the library checks the other sizes, and that this is enough)
+        # (the library checks the sizes, and that this is enough: none for tables of 512 tokens at most)
+        need, p_work = 0, 0
+        if width * self.block_tokens > 512:
+            need = self._work.get(n_q)
         if need is None:
             rc, need = B.dr_attend_work(self.handle, n_q, n, rows)
             if rc:
                 raise B.DrError(rc, "dr_attend_work")
             self._work[n_q] = need
-        work = B._empty(1, need, _uint8, q.device, stream)
+        if need:
+            work = B._empty(1, need, _uint8, q.device, stream)
+            p_work = work.data_ptr()
         rc = B._fn("dr_attend")(self._word, q.data_ptr(), ldq, n_q, rows, p_offsets, p_lengths, n, table.data_ptr(), ld, width,
                                 1.0 / math.sqrt(self.head_dim) if scale is None else scale, window, sinks, out.data_ptr(), ldo,
-                                work.data_ptr(), need, B._stream_of(device, stream))
+                                p_work, need, B._stream_of(device, stream))
         if rc:
             raise B.DrError(rc, "dr_attend")
         return out

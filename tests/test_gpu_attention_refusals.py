@@ -66,12 +66,12 @@ def test_attend(live):
     rc, need = dr.dr_attend_work(cache.handle, 8, 3, 7)
     assert rc == 0 and need > 0
     work = torch.zeros(need, dtype=torch.uint8, device=DEV)
-    good = dict(cache=cache.handle, q=p, ldq=512, n_q_heads=8, rows=7, offsets=p, lengths=p, requests=3, table=p, ld_table=5, width=5, scale=0.1, window=0,
+    good = dict(cache=cache.handle, q=p, ldq=512, n_q_heads=8, rows=7, offsets=p, lengths=p, requests=3, table=p, ld_table=500, width=500, scale=0.1, window=0,
                 sinks=0, out=p, ldo=512, work=work.data_ptr(), work_bytes=need, stream=None)
     refused(dr.dr_attend, good, [({k: None}, B.DR_ERR_INVALID) for k in ("q", "lengths", "table", "out")] + [
         (dict(n_q_heads=7), B.DR_ERR_INVALID), (dict(n_q_heads=0), B.DR_ERR_INVALID), (dict(n_q_heads=130, ldq=9000, ldo=9000), B.DR_ERR_UNSUPPORTED),
         (dict(offsets=None), B.DR_ERR_INVALID), (dict(scale=float("nan")), B.DR_ERR_INVALID), (dict(scale=float("inf")), B.DR_ERR_INVALID),
-        (dict(ldq=511), B.DR_ERR_INVALID), (dict(ldo=511), B.DR_ERR_INVALID), (dict(ld_table=4), B.DR_ERR_INVALID), (dict(width=0), B.DR_ERR_INVALID),
+        (dict(ldq=511), B.DR_ERR_INVALID), (dict(ldo=511), B.DR_ERR_INVALID), (dict(ld_table=499), B.DR_ERR_INVALID), (dict(width=0), B.DR_ERR_INVALID),
         (dict(work=None), B.DR_ERR_SIZE), (dict(work_bytes=need - 1), B.DR_ERR_SIZE), (dict(work=work.data_ptr() + 8), B.DR_ERR_ALIGN), (dict(q=p + 1), B.DR_ERR_ALIGN),
         (dict(lengths=p + 2), B.DR_ERR_ALIGN), (dict(requests=1 << 25), B.DR_ERR_UNSUPPORTED), (dict(rows=1 << 31), B.DR_ERR_UNSUPPORTED),
         (dict(width=1 << 25, ld_table=1 << 25), B.DR_ERR_UNSUPPORTED)])
