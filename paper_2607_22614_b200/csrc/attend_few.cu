@@ -209,7 +209,7 @@ __device__ __forceinline__ void produce(const AttendArgs& a, Shared<D, SETS>& s,
                 const bool ok = id < a.n_blocks;
                 if (ok) {
                     ks = a.k_scale[(uint64_t)id * a.n_kv + head];
-                    vs = fmaxf(a.v_scale[(uint64_t)id * a.n_kv + head], kLeastScale);
+                    vs = a.v_scale[(uint64_t)id * a.n_kv + head];
                 }
                 const uint32_t pieces = __ballot_sync(0xFFFFFFFFu, ok && (lane & 3) * 16 % box == 0);
                 const int row = (int)((id * a.n_kv + head << a.block_log2) + (token & (1u << a.block_log2) - 1));
@@ -225,8 +225,8 @@ __device__ __forceinline__ void produce(const AttendArgs& a, Shared<D, SETS>& s,
                     Meta& m = s.meta[ring.slot];
                     if (lane / 4 == b) {
                         m.k_scale[lane & 3] = ks;
-                        m.v_log[lane & 3] = log2f(vs);
-                        m.v_inv[lane & 3] = 1.0f / vs;
+                        m.v_log[lane & 3] = log2f(fmaxf(vs, kLeastScale));
+                        m.v_inv[lane & 3] = 1.0f / fmaxf(vs, kLeastScale);
                         m.ok[lane & 3] = ok;
                         if ((lane & 3) == 0) {
                             m.flags = (t0 + b == 0 ? kFirst : 0) | (t0 + b + 1 == count ? kLast : 0);

@@ -195,33 +195,31 @@ __device__ __forceinline__ void produce(const AttendArgs& a, Shared<D>& s, const
         const bool held = id < a.n_blocks;
         if (held) {
             ks = a.k_scale[(uint64_t)id * a.n_kv + it.head];
-            vs = fmaxf(a.v_scale[(uint64_t)id * a.n_kv + it.head], kLeastScale);
+            vs = a.v_scale[(uint64_t)id * a.n_kv + it.head];
         }
-        const float v_log = log2f(vs), v_inv = 1.0f / vs;
         const uint32_t all = __ballot_sync(0xFFFFFFFFu, held), pieces = __ballot_sync(0xFFFFFFFFu, held && (lane & 7) * 16 % box == 0);
         const int row = (int)((id * a.n_kv + it.head << a.block_log2) + (token & (1u << a.block_log2) - 1));
         for (uint32_t b = 0; b < 4 && i0 + b < it.tiles.count; ++b) {
             const uint32_t mine = pieces >> (8 * b) & 255, bytes = (uint32_t)__popc(mine) * box * D;
             ok = warp_wait(k_empty + 8 * keys.slot, keys.round ^ 1, &s.limit, &g_wait_failures);
             if (!ok) break;
+            // the copy first: it needs no scales, which may still be on their way
+            const bool copy = !a.starve && lane / 8 == b && (mine >> (lane & 7) & 1);
+            if (copy) load_2d<false>(smem_u32(s.k[keys.slot]) + (lane & 7) * 16 * D, k_map, k_full + 8 * keys.slot, 0, row);
             // (the softmax of the tile that the slot was for has read it: its products came before those that freed the key stage)
             Meta& m = s.meta[(i0 + b) % kMetas];
             if (lane / 8 == b) {
                 m.k_scale[lane & 7] = ks;
-                m.v_log[lane & 7] = v_log;
-                m.v_inv[lane & 7] = v_inv;
+                m.v_log[lane & 7] = log2f(fmaxf(vs, kLeastScale));
+                m.v_inv[lane & 7] = 1.0f / fmaxf(vs, kLeastScale);
                 if ((lane & 7) == 0) {
                     m.held = all >> (8 * b) & 255;
                     m.token = token;
                 }
             }
             __syncwarp();
-            const bool copy = lane / 8 == b && (mine >> (lane & 7) & 1);
-            if (!a.starve) {
-                if (lane == 0) bar_expect(k_full + 8 * keys.slot, bytes);
-                __syncwarp();
-                if (copy) load_2d<false>(smem_u32(s.k[keys.slot]) + (lane & 7) * 16 * D, k_map, k_full + 8 * keys.slot, 0, row);
-            }
+            // (the stage cannot be full before this arrival, whatever has landed)
+            if (!a.starve && lane == 0) bar_expect(k_full + 8 * keys.slot, bytes);
             __syncwarp();
             keys.next();
             used = min(used + 1, kKeyStages);
