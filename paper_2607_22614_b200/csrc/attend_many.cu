@@ -18,8 +18,8 @@
 //
 // Warps: 0-3 and 4-7 the exponentials of the two halves, 8-11 the values' codes, 12 the copies, 14 and 15 the products of the halves.
 // CTAs are started in the order of their number: the longest request first, and a request's last rows, which see the most tokens, first.
-// Measured: a tile 2.11 us, a CTA's start and end some 6; a prompt of 8192 tokens, 32 query over 8 cache heads of 128: 558 us = 986 TFLOP/s (a
-// library product of 8192^3: 1694); 3501 and 4500 tokens, these behind 4501 others: 667 us = 897.
+// Measured: a tile 2.11 us, a CTA's start and end some 6; a prompt of 8192 tokens, 32 query over 8 cache heads of 128: 560 us = 980 TFLOP/s (a
+// library product of 8192^3: 1694); 3501 and 4500 tokens, these behind 4501 others: 646 us in a graph, 676 a pass (926 and 885).
 #include "attend.h"
 #include "linear.h"
 #include "tc_ptx.cuh"
