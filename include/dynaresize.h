@@ -639,6 +639,7 @@ int dr_diag_linear_waits(uint32_t limit_us, uint32_t starve);
  * and v_scale [n_blocks, kv_heads]; a value is its code times its block's scale.  dr_qk_append writes scales that are
  * powers of two, the smallest 2^e >= 2^-100 with every finite magnitude of the block within 448 * 2^e: when a later token makes
  * the scale grow, the codes that the block holds are shifted to it (rounded once more only below 2^-6 of the new scale).
+ * Scales that a caller brings may be any finite ones that are not negative.
  * A token with an infinity or a NaN in its key or value of a head is kept as one: the NaN code 0x7F in the first place of its key,
  * zeros in the places that were not finite; queries that see it get NaN, others nothing of it.  Codes of values that attention
  * may see hold no NaN code.

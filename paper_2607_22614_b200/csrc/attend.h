@@ -21,6 +21,16 @@ struct AttendArgs {
     uint32_t whole;  // few rows: groups are not divided between CTAs
 };
 
+// A block's value scale goes into p: the kernels' running maximum is that of log2(p) + log2(scale), and the sum of p takes the scale out again by
+// its reciprocal.  That is sound while the scales of a request differ by no more than an exponential's range: from 2^-40 to 2^40 what an
+// exponential flushes to nothing, or keeps of a hidden token (2^-126), is below 2^-86 where the sum is above 2^-29.  From the first scale on that is
+// not among those (the 2^-100 of a block without values, say) a row's sum has exponentials of its own, relative to a maximum of the logits alone.
+constexpr float kLeastNear = 9.0949470e-13f, kMostNear = 1.0995116e12f;  // 2^-40, 2^40
+constexpr float kLeastScale = 1.4e-45f;                                  // 2^-149, for the logarithm of 0
+__device__ __forceinline__ float log2_scale(float scale) { return log2f(fmaxf(scale, kLeastScale)); }
+// 0: the sum needs exponentials of its own.
+__device__ __forceinline__ float reciprocal_near(float scale) { return scale >= kLeastNear && scale <= kMostNear ? 1.0f / scale : 0.0f; }
+
 constexpr uint32_t kTileTokens = 64;  // of the cache that a step of the few-row kernel takes
 
 // A request's rows and tokens, held inside the call's buffers whatever the arrays say.

@@ -40,7 +40,6 @@ template <int SETS> constexpr uint32_t kRows = 8 * SETS;
 template <int SETS> constexpr uint32_t kCtasPerSm = SETS == 1 ? 3 : 2;
 template <int SETS> constexpr uint32_t kStages = SETS == 1 ? 3 : 6 - SETS;
 constexpr float kTop = 11.0f, kLag = 4.0f;     // log2 of p at the running maximum in fp16, and how far a p may be above it
-constexpr float kLeastScale = 7.8886091e-31f;  // 2^-100
 
 // What the consumers have to know of a stage.
 enum : uint32_t { kFirst = 1, kLast = 2, kEnd = 4 };
@@ -49,13 +48,14 @@ struct Meta {
     uint32_t flags, have;
     uint32_t row0, n, len, head, rows0;  // rows0: first of the group's rows among the request's n * group
     uint32_t token;                      // first of the tile
-    float k_scale[4], v_log[4], v_inv[4];  // of each sixteen tokens: the keys' scale, log2 of the values' and its reciprocal
+    float k_scale[4], v_log[4], v_inv[4];  // of each sixteen tokens: the keys' scale, log2 of the values' and reciprocal_near of it
     uint32_t ok[4];                        // whether they are held
 };
-// A part of a group that other CTAs have parts of, too: output and sum of p relative to 2^m.
+// A part of a group that other CTAs have parts of, too: output and sum of p relative to 2^m; a sum below zero is one that has had exponentials of
+// its own, negated, relative to 2^r.
 template <int D, int SETS>
 struct Part {
-    float m[kRows<SETS>], l[kRows<SETS>], o[kRows<SETS>][D];
+    float m[kRows<SETS>], r[kRows<SETS>], l[kRows<SETS>], o[kRows<SETS>][D];
 };
 // What the second launch joins: parts of CTAs first .. first + count - 1.
 struct Join {
@@ -67,7 +67,7 @@ struct Shared {
     alignas(1024) uint8_t k[kStages<SETS>][kTileTokens * D];
     alignas(1024) uint8_t v[kStages<SETS>][kTileTokens * D];
     float o[kConsumers][kRows<SETS>][D + 4];
-    float m[kConsumers][kRows<SETS>], l[kConsumers][kRows<SETS>];
+    float m[kConsumers][kRows<SETS>], r[kConsumers][kRows<SETS>], l[kConsumers][kRows<SETS>];  // (as in Part)
     uint2 q[SETS < 3 ? 1 : SETS][D / 16][32];  // the rows' fragments, where registers do not hold them
     float back[kRows<SETS>];
     int p[kRows<SETS>];
@@ -161,6 +161,8 @@ __device__ __forceinline__ float exp2_of(float x)
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
+// The square root of what an output relative to 2^m is multiplied with over a sum relative to 2^r: twice it reaches where one float does not.
+__device__ __forceinline__ float half_lift(float m, float r) { return exp2_of((m - r) * 0.5f); }
 // An 8 x 8 block of 16-bit values, transposed between the lanes.
 __device__ __forceinline__ uint32_t transposed(uint32_t v)
 {
@@ -225,8 +227,8 @@ __device__ __forceinline__ void produce(const AttendArgs& a, Shared<D, SETS>& s,
                     Meta& m = s.meta[ring.slot];
                     if (lane / 4 == b) {
                         m.k_scale[lane & 3] = ks;
-                        m.v_log[lane & 3] = log2f(fmaxf(vs, kLeastScale));
-                        m.v_inv[lane & 3] = 1.0f / fmaxf(vs, kLeastScale);
+                        m.v_log[lane & 3] = log2_scale(vs);
+                        m.v_inv[lane & 3] = reciprocal_near(vs);
                         m.ok[lane & 3] = ok;
                         if ((lane & 3) == 0) {
                             m.flags = (t0 + b == 0 ? kFirst : 0) | (t0 + b + 1 == count ? kLast : 0);
@@ -348,11 +350,31 @@ __device__ __forceinline__ void write_group(const AttendArgs& a, Shared<D, SETS>
             weight[w] = exp2_of(s.m[w][i] - safe);
             l = fmaf(s.l[w][i], weight[w], l);
         }
-        const float norm = l == 0.0f ? 0.0f : 1.0f / l;
         Part<D, SETS>& part = parts[blockIdx.x * 2 + (m.have == kHead)];
+        float lift = 1.0f, sign = 1.0f;
+        if (fminf(fminf(s.l[0][i], s.l[1][i]), fminf(s.l[2][i], s.l[3][i])) < 0.0f) {
+            float most_r = -INFINITY, r[kConsumers];
+#pragma unroll
+            for (uint32_t w = 0; w < kConsumers; ++w) {
+                r[w] = s.l[w][i] < 0.0f ? s.r[w][i] : s.m[w][i];
+                most_r = fmaxf(most_r, r[w]);
+            }
+            l = 0.0f;
+#pragma unroll
+            for (uint32_t w = 0; w < kConsumers; ++w) l = fmaf(fabsf(s.l[w][i]), exp2_of(r[w] - most_r), l);
+            if (m.have == kWhole) {
+                lift = half_lift(most, most_r);
+#pragma unroll
+                for (uint32_t w = 0; w < kConsumers; ++w) weight[w] *= lift;
+            } else {
+                part.r[i] = most_r;
+                sign = -1.0f;
+            }
+        }
+        const float norm = l == 0.0f ? 0.0f : lift / l;
         if (m.have != kWhole && piece == 0) {
             part.m[i] = most;
-            part.l[i] = l;
+            part.l[i] = sign * l;
         }
 #pragma unroll
         for (uint32_t d = piece * 4; d < D; d += 32) {
@@ -373,6 +395,24 @@ __device__ __forceinline__ void write_group(const AttendArgs& a, Shared<D, SETS>
     }
 }
 
+// A row's sixteen logits (log2 of p, plus v_log) into its sum of p with exponentials of its own, held negated relative to 2^r; the first time behind eight
+// sums so far, relative to 2^x[24].
+__device__ __noinline__ void sum_apart(const float* x, float v_log, bool apart, float& r, float& l)
+{
+    float sum = 0.0f, was = 0.0f;
+    const float from = apart ? r : x[24];
+    float now = from;
+#pragma unroll 1
+    for (int k = 0; k < 16; ++k) now = fmaxf(now, x[k] - v_log);
+    const float base = kTop - (now == -INFINITY ? 0.0f : now);
+#pragma unroll 1
+    for (int k = 0; k < 16; ++k) sum += exp2_of(x[k] - v_log + base);
+#pragma unroll 1
+    for (int k = 16; k < 24; ++k) was += x[k];
+    l = -fmaf(apart ? -l : was, now == -INFINITY ? 1.0f : exp2_of(from - now), sum);
+    r = now;
+}
+
 template <int D, int SETS>
 __device__ __forceinline__ void consume(const AttendArgs& a, Shared<D, SETS>& s, Part<D, SETS>* parts)
 {
@@ -388,6 +428,7 @@ __device__ __forceinline__ void consume(const AttendArgs& a, Shared<D, SETS>& s,
     constexpr bool kHeld = SETS < 3;  // the rows' fragments in registers: with three sets 400 bytes a thread would be spilled
     uint32_t qf[kHeld ? SETS : 1][kChunks][2];
     float o[SETS][kChunks][4], m[SETS][2], l[SETS][2];
+    bool apart = false;  // the sums have exponentials of their own: the rows' are in s.l, negated, relative to 2^s.r
     Turn<kStages<SETS>> ring;
     uint32_t met = 0;
     // a group's rows (everybody has read those of the group before: the warps met at its end)
@@ -429,6 +470,7 @@ __device__ __forceinline__ void consume(const AttendArgs& a, Shared<D, SETS>& s,
         if (flags & kFirst) {
             if (!loaded && !load_rows(meta)) return;
             loaded = false;
+            apart = false;
 #pragma unroll
             for (int n = 0; n < SETS; ++n) {
 #pragma unroll
@@ -480,7 +522,9 @@ __device__ __forceinline__ void consume(const AttendArgs& a, Shared<D, SETS>& s,
                 for (int c = 0; c < kChunks / 2; ++c) ldmatrix_t(v_at + addr[c], vr[c]);
             }
             const float ks = meta.k_scale[warp], v_log = meta.v_log[warp];
-            bool grows = false;
+            const float v_inv = meta.v_inv[warp];
+            // (sums that have exponentials of their own are made where a maximum grows: a branch for them here costs 300 tokens 0.3 us a call)
+            bool grows = apart || v_inv == 0.0f;
             // whether every row sees all sixteen tokens: rows ascend in position, and the last one's is at most len - 1
             const int p_lo = (int)meta.len - (int)meta.n + (int)(meta.rows0 / a.group);
             const bool all = t0 + 15 <= p_lo && (!a.window || t0 > (int)meta.len - 1 - (int)a.window || t0 + 15 < (int)a.sinks);
@@ -510,6 +554,24 @@ __device__ __forceinline__ void consume(const AttendArgs& a, Shared<D, SETS>& s,
 #pragma unroll
                 for (int e = 0; e < 4; ++e) grows |= x[n][e] > m[n][e & 1] + kLag;
             if (__any_sync(0xFFFFFFFFu, grows)) {
+                if (apart || v_inv == 0.0f) {
+                    // the logits, and the sums so far, go through the warp's part of s.o, so that little code stands here
+#pragma unroll
+                    for (int n = 0; n < SETS; ++n)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            float* const row = s.o[warp][8 * n + 2 * tig + (e & 1)];
+                            row[g + (e & 2) * 4] = x[n][e];
+                            if (e < 2) {
+                                row[16 + g] = l[n][e];
+                                row[24] = m[n][e];
+                            }
+                        }
+                    __syncwarp();
+                    if (lane < kRows<SETS>) sum_apart(s.o[warp][lane], v_log, apart, s.r[warp][lane], s.l[warp][lane]);
+                    apart = true;
+                    __syncwarp();
+                }
 #pragma unroll
                 for (int n = 0; n < SETS; ++n) {
                     float f[2];
@@ -528,7 +590,6 @@ __device__ __forceinline__ void consume(const AttendArgs& a, Shared<D, SETS>& s,
                         for (int e = 0; e < 4; ++e) o[n][c][e] *= f[e & 1];
                 }
             }
-            const float v_inv = meta.v_inv[warp];
             uint32_t pf[SETS][2];
 #pragma unroll
             for (int n = 0; n < SETS; ++n) {
@@ -562,7 +623,7 @@ __device__ __forceinline__ void consume(const AttendArgs& a, Shared<D, SETS>& s,
                     for (int b = 4; b < 32; b <<= 1) l[n][h] += __shfl_xor_sync(0xFFFFFFFFu, l[n][h], b);
                     if (g == 0) {
                         s.m[warp][row] = m[n][h];
-                        s.l[warp][row] = l[n][h];
+                        if (!apart) s.l[warp][row] = l[n][h];
                     }
 #pragma unroll
                     for (int c = 0; c < kChunks; ++c) *(float2*)&s.o[warp][row][16 * c + 2 * g] = make_float2(o[n][c][h], o[n][c][h + 2]);
@@ -662,7 +723,7 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm<SETS>)
 // way together.
 template <int WARPS> constexpr uint32_t kJoinRows = WARPS == 1 ? 8 : 2;
 template <int D, int SETS, int WARPS>
-__global__ void __launch_bounds__(32 * kJoinRows<WARPS> * WARPS) join_kernel(const __grid_constant__ AttendArgs a, const Part<D, SETS>* parts, const Join* joins)
+__global__ void __launch_bounds__(32 * kJoinRows<WARPS> * WARPS, 1024 / (32 * kJoinRows<WARPS> * WARPS)) join_kernel(const __grid_constant__ AttendArgs a, const Part<D, SETS>* parts, const Join* joins)
 {
     constexpr int kOwn = D / 32;  // dimensions a lane has, side by side
     __shared__ float s_m[kJoinRows<WARPS>][WARPS], s_l[kJoinRows<WARPS>][WARPS], s_o[kJoinRows<WARPS>][WARPS][D];
@@ -680,7 +741,7 @@ __global__ void __launch_bounds__(32 * kJoinRows<WARPS> * WARPS) join_kernel(con
     const Row row = row_of(a, m, i);
     // part 0 is the group's beginning in CTA cta - 1, the others the ends that the CTAs behind it met first
     auto part = [&](uint32_t k) -> const Part<D, SETS>& { return parts[(cta - 1 + k) * 2 + (k == 0)]; };
-    float most = -INFINITY, l = 0.0f, o[kOwn] = {};
+    float most = -INFINITY, l = 0.0f, least = 0.0f, o[kOwn] = {};  // least: below zero where a part has a sum relative to 2^r
     if (row.real) {
         for (uint32_t k0 = w; k0 < count; k0 += 8 * WARPS) {
             float pm[8], pl[8], po[8][kOwn];
@@ -702,7 +763,10 @@ __global__ void __launch_bounds__(32 * kJoinRows<WARPS> * WARPS) join_kernel(con
             }
             float now = most;
 #pragma unroll
-            for (int u = 0; u < 8; ++u) now = fmaxf(now, pm[u]);
+            for (int u = 0; u < 8; ++u) {
+                now = fmaxf(now, pm[u]);
+                least = fminf(least, pl[u]);
+            }
             const float safe = now == -INFINITY ? 0.0f : now, old = exp2_of(most - safe);
             l *= old;
 #pragma unroll
@@ -718,7 +782,7 @@ __global__ void __launch_bounds__(32 * kJoinRows<WARPS> * WARPS) join_kernel(con
         }
         if (lane == 0) {
             s_m[r][w] = most;
-            s_l[r][w] = l;
+            s_l[r][w] = least < 0.0f ? least : l;
         }
 #pragma unroll
         for (int d = 0; d < kOwn; ++d) s_o[r][w][lane * kOwn + d] = o[d];
@@ -736,10 +800,36 @@ __global__ void __launch_bounds__(32 * kJoinRows<WARPS> * WARPS) join_kernel(con
     for (uint32_t k = 0; k < WARPS; ++k) {
         const float e = exp2_of(s_m[r][k] - safe);
         l = fmaf(s_l[r][k], e, l);
+        least = fminf(least, s_l[r][k]);
 #pragma unroll
         for (int d = 0; d < kOwn; ++d) o[d] = fmaf(s_o[r][k][lane * kOwn + d], e, o[d]);
     }
-    const float norm = l == 0.0f ? 0.0f : 1.0f / l;
+    float norm = l == 0.0f ? 0.0f : 1.0f / l;
+    if (least < 0.0f) {  // the sum anew, a lane a part (l is of no account)
+        float most_r = -INFINITY;
+        l = 0.0f;
+        for (uint32_t k0 = 0; k0 < count; k0 += 32) {
+            float pr = -INFINITY, pl = 0.0f;
+            if (k0 + lane < count) {
+                const Part<D, SETS>& q = part(k0 + lane);
+                pl = *(const volatile float*)&q.l[i];
+                pr = pl < 0.0f ? *(const volatile float*)&q.r[i] : *(const volatile float*)&q.m[i];
+            }
+            const float now = fmaxf(most_r, pr), safe_r = now == -INFINITY ? 0.0f : now;
+            l = fmaf(fabsf(pl), exp2_of(pr - safe_r), l * exp2_of(most_r - safe_r));
+            most_r = now;
+        }
+        float all_r = most_r;
+#pragma unroll
+        for (int b = 16; b; b >>= 1) all_r = fmaxf(all_r, __shfl_xor_sync(0xFFFFFFFFu, all_r, b));
+        l *= exp2_of(most_r - all_r);  // (a part with a sum has a finite r)
+#pragma unroll
+        for (int b = 16; b; b >>= 1) l += __shfl_xor_sync(0xFFFFFFFFu, l, b);
+        const float lift = half_lift(most, all_r);
+        norm = lift / l;
+#pragma unroll
+        for (int d = 0; d < kOwn; ++d) o[d] *= lift;
+    }
     uint16_t* out = (uint16_t*)a.out + row.index * a.ldo + (uint64_t)row.head * D + lane * kOwn;
 #pragma unroll
     for (int d = 0; d < kOwn; ++d) out[d] = (uint16_t)pack_bf16(o[d] * norm, 0.0f);

@@ -38,11 +38,11 @@ constexpr uint32_t kRanked = 128;  // requests up to which the longest are begun
 constexpr uint32_t kGroups = kTile / 16, kStepGroups = kStep / 16;  // of sixteen tokens, which share a block
 constexpr int kByFma = 3;  // pairs of each eight whose exponentials multiply-adds take (a tile: 2.23 us with none, 2.11 with 2 or 3, 2.16 with 4)
 constexpr float kTop = 11.0f, kLag = 4.0f;
-constexpr float kLeastScale = 7.8886091e-31f;  // 2^-100
 
 struct Meta {
     float k_scale[kGroups], v_log[kGroups], v_inv[kGroups];
     uint32_t held;   // a bit for each group
+    uint32_t apart;  // and one where the value scale is not near
     uint32_t token;  // first of the tile
 };
 
@@ -59,6 +59,7 @@ struct Shared {
     Limit limit;
     uint32_t sums[kThreads / 32];
     uint32_t request, item;
+    float apart_r[kRowsCta], apart_l[kRowsCta];  // the rows' sums of p that have exponentials of their own, relative to 2^r
     uint32_t lengths[kRanked], tiles[kRanked], ranked[kRanked];
 };
 static_assert(sizeof(Shared<128>) <= 227 * 1024, "shared memory of a CTA");
@@ -197,7 +198,8 @@ __device__ __forceinline__ void produce(const AttendArgs& a, Shared<D>& s, const
             ks = a.k_scale[(uint64_t)id * a.n_kv + it.head];
             vs = a.v_scale[(uint64_t)id * a.n_kv + it.head];
         }
-        const uint32_t all = __ballot_sync(0xFFFFFFFFu, held), pieces = __ballot_sync(0xFFFFFFFFu, held && (lane & 7) * 16 % box == 0);
+        const uint32_t all = __ballot_sync(0xFFFFFFFFu, held), apart = __ballot_sync(0xFFFFFFFFu, reciprocal_near(vs) == 0.0f),
+                       pieces = __ballot_sync(0xFFFFFFFFu, held && (lane & 7) * 16 % box == 0);
         const int row = (int)((id * a.n_kv + it.head << a.block_log2) + (token & (1u << a.block_log2) - 1));
         for (uint32_t b = 0; b < 4 && i0 + b < it.tiles.count; ++b) {
             const uint32_t mine = pieces >> (8 * b) & 255, bytes = (uint32_t)__popc(mine) * box * D;
@@ -210,10 +212,11 @@ __device__ __forceinline__ void produce(const AttendArgs& a, Shared<D>& s, const
             Meta& m = s.meta[(i0 + b) % kMetas];
             if (lane / 8 == b) {
                 m.k_scale[lane & 7] = ks;
-                m.v_log[lane & 7] = log2f(fmaxf(vs, kLeastScale));
-                m.v_inv[lane & 7] = 1.0f / fmaxf(vs, kLeastScale);
+                m.v_log[lane & 7] = log2_scale(vs);
+                m.v_inv[lane & 7] = reciprocal_near(vs);
                 if ((lane & 7) == 0) {
                     m.held = all >> (8 * b) & 255;
+                    m.apart = apart >> (8 * b) & 255;
                     m.token = token;
                 }
             }
@@ -331,6 +334,41 @@ __device__ __forceinline__ void convert(const AttendArgs& a, Shared<D>& s, const
     drain(values, used, v_empty, &s.limit, &g_wait_failures);
 }
 
+// One step's part of a row's sum of p with exponentials of its own: r is the largest logit so far, l the sum relative to 2^r.  (The logits are read
+// from tensor memory anew, sixteen at a time, before the step needs its registers: with the 64 that it has loaded a prompt that
+// never comes here takes 6 % longer.)
+__device__ __forceinline__ void sum_apart(const AttendArgs& a, const Meta& meta, uint32_t at, int odd, float back, int p, float& r, float& l)
+{
+    float now = r, sum = 0.0f;
+#pragma unroll 1
+    for (int pass = 0; pass < 2; ++pass) {
+        const float base = kTop - (now == -INFINITY ? 0.0f : now);
+#pragma unroll 1
+        for (int g = 0; g < (int)kStepGroups; ++g) {
+            float v[16];
+            asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];\n"
+                         "tcgen05.wait::ld.sync.aligned;"
+                         : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]), "=f"(v[8]), "=f"(v[9]), "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15])
+                         : "r"(at + 16 * g)
+                         : "memory");
+            const int of = odd * (int)kStepGroups + g, t0 = (int)meta.token + 16 * of;
+            const bool held = meta.held >> of & 1;
+            const float f = fmaxf(back * meta.k_scale[of], 1.2e-38f);
+#pragma unroll
+            for (int k = 0; k < 16; ++k) {
+                const int t = t0 + k;
+                if (!held || t > p || (a.window && t <= p - (int)a.window && t >= (int)a.sinks)) continue;
+                if (pass)
+                    sum += exp2_of(fmaf(v[k], f, base));
+                else
+                    now = fmaxf(now, v[k] * f);
+            }
+        }
+    }
+    l = fmaf(l, now == -INFINITY ? 1.0f : exp2_of(r - now), sum);
+    r = now;
+}
+
 // A half's rows, a thread a row.
 template <int D>
 __device__ __forceinline__ void softmax(const AttendArgs& a, Shared<D>& s, const Item& it, uint32_t half)
@@ -400,14 +438,25 @@ __device__ __forceinline__ void softmax(const AttendArgs& a, Shared<D>& s, const
     const int p_lo = __shfl_sync(0xFFFFFFFFu, p, 0), p_hi = __shfl_sync(0xFFFFFFFFu, p, 31);  // rows ascend
     const uint32_t steps = it.tiles.count * (kTile / kStep);
     float m = -INFINITY, l = 0.0f;
+    bool apart = false;  // the row's sum is in s.apart_l
     for (uint32_t i = 0; i < steps; ++i) {
         const uint32_t odd = i & 1, at = s_at + odd * kStep;
         if (!__all_sync(0xFFFFFFFFu, bar_wait(s_full + 8 * odd, i >> 1 & 1, &s.limit, &g_wait_failures))) return;
         fence_after();
+        const Meta& meta = s.meta[(i >> 1) % kMetas];
+        if (apart || (!odd && meta.apart)) {
+            float& r_row = s.apart_r[half * kHalf + i_row];
+            float& l_row = s.apart_l[half * kHalf + i_row];
+            if (!apart) {
+                r_row = m;
+                l_row = l;
+            }
+            apart = true;
+            sum_apart(a, meta, at, (int)odd, back, p, r_row, l_row);
+        }
         float v[2][32];
         tmem_start(at, v[0]);
         tmem_start(at + 32, v[1]);
-        const Meta& meta = s.meta[(i >> 1) % kMetas];
         const int t0 = (int)(meta.token + odd * kStep), g0 = (int)(odd * kStepGroups);
         const uint32_t held = meta.held >> g0 & ((1u << kStepGroups) - 1);
         const bool all = held == (1u << kStepGroups) - 1 && t0 + (int)kStep - 1 <= p_lo &&
@@ -484,7 +533,15 @@ __device__ __forceinline__ void softmax(const AttendArgs& a, Shared<D>& s, const
     // (a barrier of its own: o_done may be one or two phases on, which its parity does not tell apart)
     if (!__all_sync(0xFFFFFFFFu, bar_wait(smem_u32(&s.o_last[half]), 0, &s.limit, &g_wait_failures))) return;
     fence_after();
-    const float norm = l == 0.0f || (m == -INFINITY && l == l) ? 0.0f : 1.0f / l;  // (a row that has seen nothing: zeros)
+    float lift = 1.0f;
+    if (apart) {  // (in two steps, whose product need not be a float)
+        l = s.apart_l[half * kHalf + i_row];
+        lift = m == -INFINITY ? 1.0f : exp2_of((m - s.apart_r[half * kHalf + i_row]) * 0.5f);
+#pragma unroll 1
+        for (int c = 0; c < D / 16; ++c) tmem_scale(o_at + 16 * c, lift);
+        tmem_stored();
+    }
+    const float norm = l == 0.0f || (m == -INFINITY && l == l) ? 0.0f : 1.0f / l * lift;  // (a row that has seen nothing: zeros)
     uint16_t* out = (uint16_t*)a.out + index * a.ldo + (uint64_t)head * D;
 #pragma unroll
     for (int c = 0; c < D / 32; ++c) {
