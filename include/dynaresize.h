@@ -739,14 +739,14 @@ int dr_qk_grad(const dr_qk* qk, const void* x_dev, uint32_t dtype, uint64_t ldx,
  *   lengths : tokens of each request that the cache holds, the step's own among them
  *   work    : dr_attend_work's bytes of device memory that no other call uses meanwhile, 16-byte aligned; none is needed (NULL, 0) where the
  *             table's width holds at most 512 tokens
- * out must not overlap q.  A row that sees nothing gets zeros, one that is not finite NaN.  Rows that no request owns are left as they were.  Lengths beyond the table's width and
- * offsets beyond the rows are held inside.  Sums are fp32; which tokens are summed together depends on all lengths of the call, in a
+ * out must not overlap q.  A row that sees nothing gets zeros, one that is not finite NaN.  Rows that no request owns are left as they were.  Lengths beyond the table's width or
+ * 2^31 - 1 and offsets beyond the rows are held inside.  Sums are fp32; which tokens are summed together depends on all lengths of the call, in a
  * fixed order: the same call gives the same bits.
  * Enqueues on cuda_stream, allocates nothing, reads nothing on the host, may be captured.  The waits inside are bounded as the linear
  * layers' are, and counted by dr_diag_linear_wait_failures.
  * Errors: DR_ERR_INVALID (NULL, leading dimensions, n_q_heads no multiple of kv_heads, window below 0, scale not finite),
- * DR_ERR_UNSUPPORTED (2^30 rows, 2^24 requests, 2^24 blocks a request, 2^31 tokens, more than 64 query heads for a head of the
- * cache), DR_ERR_SIZE (work), DR_ERR_ALIGN, DR_ERR_STATE, DR_ERR_CUDA.
+ * DR_ERR_UNSUPPORTED (2^30 rows, 2^31 rows times the query heads of a cache head, 2^24 requests, 2^24 blocks a request, more than
+ * 64 query heads for a head of the cache), DR_ERR_SIZE (work), DR_ERR_ALIGN, DR_ERR_STATE, DR_ERR_CUDA.
  */
 int dr_attend_work(const dr_kv_cache* cache, uint64_t n_q_heads, uint64_t requests, uint64_t rows, uint64_t* bytes);
 int dr_attend(const dr_kv_cache* cache, const void* q_dev, uint64_t ldq, uint64_t n_q_heads, uint64_t rows, const int32_t* offsets_dev,

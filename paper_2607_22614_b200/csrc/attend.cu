@@ -97,9 +97,9 @@ int dr_attend(const dr_kv_cache* cache, const void* q_dev, uint64_t ldq, uint64_
     a.group = a.n_q / a.n_kv;
     a.n_blocks = d.n_blocks;
     a.block_log2 = cache->block_log2;
-    // a window that no token lies outside of is none
-    a.window = window <= 0x3FFFFFFFull ? (uint32_t)window : 0;
-    a.sinks = (uint32_t)(sinks <= 0x3FFFFFFFull ? sinks : 0x3FFFFFFFull);
+    // a window that no token lies outside of is none: positions end at 2^31 - 2
+    a.window = window < 0x7FFFFFFFull ? (uint32_t)window : 0;
+    a.sinks = (uint32_t)(sinks < 0x7FFFFFFFull ? sinks : 0x7FFFFFFFull);
     a.scale = scale * 1.4426950408889634f;
     auto vec = [](const void* p, uint64_t ld) { const uint64_t bits = (uintptr_t)p | ld * 2; return bits % 16 == 0 ? 2u : bits % 8 == 0 ? 1u : 0u; };
     a.vec_q = vec(q_dev, ldq);

@@ -51,6 +51,7 @@ __device__ __forceinline__ Request request_of(const AttendArgs& a, uint32_t r)
     q.len = (uint32_t)min((uint64_t)(uint32_t)max(a.lengths[r], 0), min((uint64_t)a.width << a.block_log2, (uint64_t)0x7FFFFFFFu));
     return q;
 }
+// (Rows before a request's first token see nothing, whatever their position: -1 stands for all of them, from which any window can be taken.)
 // The tiles of TILE tokens that rows at positions p_lo .. p_hi may see: [0, sinks) and [first, first + count - sinks).
 struct Tiles {
     uint32_t sinks, first, count;
@@ -62,7 +63,7 @@ __device__ __forceinline__ Tiles tiles_of(const AttendArgs& a, int p_lo, int p_h
     Tiles t{0, 0, p_hi >= 0 ? (uint32_t)p_hi / TILE + 1 : 0};
     if (a.window) {
         const uint32_t end = t.count;
-        const int lo = max(0, p_lo - (int)a.window + 1);
+        const int lo = max(0, max(p_lo, -1) - (int)a.window + 1);
         t.sinks = min((a.sinks + TILE - 1) / TILE, end);
         t.first = max(t.sinks, (uint32_t)lo / TILE);
         t.count = t.sinks + (end > t.first ? end - t.first : 0);

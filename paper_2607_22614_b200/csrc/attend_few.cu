@@ -274,7 +274,7 @@ __device__ __forceinline__ Row row_of(const AttendArgs& a, const Meta& m, uint32
     const uint32_t x = m.rows0 + i;
     r.real = x < m.n * a.group;
     const uint32_t y = min(x, m.n * a.group - 1), j = y / a.group;
-    r.p = (int)m.len - (int)m.n + (int)j;
+    r.p = max((int)m.len - (int)m.n + (int)j, -1);
     r.index = m.row0 + j;
     r.head = m.head * a.group + y % a.group;
     return r;

@@ -376,7 +376,7 @@ __device__ __forceinline__ void softmax(const AttendArgs& a, Shared<D>& s, const
     const uint32_t lane = threadIdx.x & 31, i_row = threadIdx.x & 127, x = it.rows0 + half * kHalf + i_row;
     const uint32_t last = it.q.n * a.group - 1, y = min(x, last), j = y / a.group;
     const bool real = x <= last;
-    const int p = (int)it.q.len - (int)it.q.n + (int)j;
+    const int p = max((int)it.q.len - (int)it.q.n + (int)j, -1);
     const uint64_t index = it.q.row0 + j;
     const uint32_t head = it.head * a.group + y % a.group;
     // the row as the sum of two rows of codes
