@@ -667,7 +667,8 @@ int dr_kv_cache_destroy(dr_kv_cache* cache); /* NULL is accepted; launches alrea
  *               blocks go back to the free list (its row of the table is left as it is)
  *   lengths   : tokens held before; lengths_out: after (may be the same array)
  *   free_list : n_blocks int32, of which the first state[0] are the free blocks, taken from the end; state_out[0] = free blocks
- *               left, state_out[1] = requests refused (state_out may be state).  Blocks that come back are listed before any are taken.
+ *               left, state_out[1] = requests refused (state_out may be state).  Blocks that come back are listed before any are taken; entries
+ *               of the table that stand for no block do not come back.
  * Requests are served in their order.  The rows of the step are the arriving tokens of all requests, one after another:
  *   offsets   : requests + 1 int32, request r has rows [offsets[r], offsets[r + 1]); held at `rows`, the rows that the step has
  *   positions : rows int32, each row's position in its request; -1 for rows of refused requests and behind the last request

@@ -8,7 +8,7 @@
 // A few KB in and out: the launch and two passes over memory bound it, so one CTA does a decode step, and a cluster of
 // up to eight CTAs, each with the sums of all requests, shares the entries of a large one.  Between phases that read what another CTA
 // may write (arrays that may be updated in place) stands the cluster's barrier.
-// Measured, calls in a graph: 64 requests of one token 5.9 us, 200 prompts of 10 600 rows 7.5 (the calls' host time: 7.3).
+// Measured, calls in a graph: 64 requests of one token, two of them ending, 6.4 us, 200 prompts of 10 600 rows 7.9 (the calls' host time: 7.3).
 #include <new>
 
 #include "attend.h"
@@ -93,11 +93,68 @@ __device__ __forceinline__ void sync_all()
     }
 }
 
+// Lists the blocks that a chunk's ending requests hold behind the first `from` entries of the free list, and returns how many they are: `total` entries of the
+// table, request r0 + o's from begin[o] on, of which those that stand for no block are skipped.  A warp has a stretch of them: it counts the
+// blocks in it, adds the counts of the warps before it, which may be in other CTAs, and lists its own.  (A call, as most steps have none.)
+template <bool CLUSTER>
+__device__ __noinline__ uint32_t come_back(const ExtendArgs& a, uint32_t r0, uint32_t total, uint64_t from, uint32_t ctas, uint32_t cta, const uint32_t* begin,
+                                              uint32_t (&counts)[kThreads / 32])
+{
+    constexpr uint32_t kOf = kThreads / 32;  // warps of a CTA
+    const uint32_t lane = threadIdx.x & 31, me = cta * kOf + (threadIdx.x >> 5), warps = ctas * kOf;
+    const uint32_t per = (uint32_t)(((uint64_t)total + 32 * warps - 1) / (32 * warps)) * 32, lo = min((uint64_t)me * per, (uint64_t)total),
+                   hi = min((uint64_t)lo + per, (uint64_t)total);
+    uint32_t o = 0, end = 0;  // of the request that a lane's last entry belongs to; the entries ascend, but for the second time round
+    auto entry = [&](uint32_t i) {
+        if (i >= hi) return -1;
+        if (i >= end) {
+            o = owner(begin, kThreads, i);
+            end = o + 1 < kThreads ? begin[o + 1] : total;
+        }
+        return a.table[(uint64_t)(r0 + o) * a.ld_table + (i - begin[o])];
+    };
+    auto held = [&](int32_t id) { return __ballot_sync(0xFFFFFFFFu, (uint32_t)id < a.n_blocks); };
+    int32_t id = entry(lo + lane);
+    uint32_t n = __popc(held(id));
+#pragma unroll 4
+    for (uint32_t i = lo + 32; i < hi; i += 32) n += __popc(held(entry(i + lane)));
+    if (lane == 0) counts[threadIdx.x >> 5] = n;
+    sync_all<CLUSTER>();
+    uint32_t before = 0, sum = 0;
+    for (uint32_t w = lane; w < warps; w += 32) {
+        uint32_t v;
+        if (CLUSTER) {
+            uint32_t at = (uint32_t)__cvta_generic_to_shared(&counts[w % kOf]);
+            asm volatile("mapa.shared::cluster.u32 %0, %0, %1;" : "+r"(at) : "r"(w / kOf));
+            asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
+        } else {
+            v = counts[w];
+        }
+        sum += v;
+        if (w < me) before += v;
+    }
+#pragma unroll
+    for (int o = 16; o; o >>= 1) {
+        before += __shfl_xor_sync(0xFFFFFFFFu, before, o);
+        sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
+    }
+    uint64_t to = from + before;
+    end = 0;
+    for (uint32_t i = lo; i < hi; i += 32) {
+        if (i > lo) id = entry(i + lane);
+        const uint32_t bits = held(id);
+        const uint64_t at = to + __popc(bits & ((1u << lane) - 1));
+        if ((uint32_t)id < a.n_blocks && at < a.n_blocks) a.free_list[at] = id;
+        to += __popc(bits);
+    }
+    return sum;
+}
+
 template <bool CLUSTER>
 __global__ void __launch_bounds__(kThreads) extend_kernel(const ExtendArgs a)
 {
     __shared__ uint2 scratch[kThreads / 32];
-    __shared__ uint32_t s_row[kThreads], s_take[kThreads], s_run[kThreads], s_len[kThreads], s_flag[kThreads];
+    __shared__ uint32_t s_row[kThreads], s_take[kThreads], s_run[kThreads], s_len[kThreads], s_flag[kThreads], s_back[2][kThreads / 32];
     const uint32_t ctas = CLUSTER ? gridDim.x : 1, cta = CLUSTER ? blockIdx.x : 0;
     const uint32_t tid = threadIdx.x, me = cta * kThreads + tid, all = ctas * kThreads;
     const uint32_t block = 1u << a.block_log2, most = min((uint64_t)a.width << a.block_log2, (uint64_t)kMost);
@@ -115,7 +172,7 @@ __global__ void __launch_bounds__(kThreads) extend_kernel(const ExtendArgs a)
     auto blocks_of = [&](uint32_t tokens) { return (tokens + block - 1) >> a.block_log2; };
 
     // what comes back
-    uint32_t back = 0;
+    uint32_t back = 0, turn = 0;
     for (uint32_t r0 = 0; r0 < a.requests; r0 += kThreads) {
         uint32_t len;
         int32_t add;
@@ -125,12 +182,8 @@ __global__ void __launch_bounds__(kThreads) extend_kernel(const ExtendArgs a)
         if (total == 0) continue;
         s_take[tid] = mine;
         __syncthreads();
-        for (uint32_t i = me; i < total; i += all) {
-            const uint32_t o = owner(s_take, kThreads, i);
-            const uint64_t at = (uint64_t)count + back + i;
-            if (at < a.n_blocks) a.free_list[at] = a.table[(uint64_t)(r0 + o) * a.ld_table + (i - s_take[o])];
-        }
-        back = sat(back, total);
+        back = sat(back, come_back<CLUSTER>(a, r0, total, (uint64_t)count + back, ctas, cta, s_take, s_back[turn]));
+        turn ^= 1;  // (a CTA may be a chunk ahead of one that still reads its counts)
         __syncthreads();
     }
     const uint32_t available = min(sat(count, back), a.n_blocks);
