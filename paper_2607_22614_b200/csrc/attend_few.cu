@@ -646,7 +646,11 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm<SETS>)
     extern __shared__ __align__(1024) uint8_t raw[];
     Shared<D, SETS>& s = *(Shared<D, SETS>*)raw;
     if (smem_u32(raw) & 1023) {  // the swizzled tiles need the alignment asked for; nothing has been started yet
-        if (threadIdx.x == 0) atomicAdd(&g_wait_failures, 1ull);
+        after_previous();
+        if (threadIdx.x == 0) {
+            atomicAdd(&g_wait_failures, 1ull);
+            if (!a.whole) joins[blockIdx.x] = Join{};  // (the second launch reads it)
+        }
         return;
     }
     const uint32_t warp = threadIdx.x >> 5;
