@@ -5,8 +5,8 @@
 // its way.
 //
 // Work is counted in tiles of 64 tokens of one request, cache head and group of rows, one behind another, and every CTA takes the
-// same share of them, wherever a request ends: two CTAs on each SM, whatever the lengths.  A CTA that ends inside a group
-// leaves its part (running maximum, sum, unnormalised output) in the work buffer, and a second launch adds the parts in order.
+// same share of them, wherever a request ends: three CTAs on each SM for groups of eight rows and two for larger ones, whatever the
+// lengths.  A CTA that ends inside a group leaves its part (running maximum, sum, unnormalised output) in the work buffer, and a second launch adds the parts in order.
 //
 // A CTA's fifth warp looks blocks up and brings tiles in through tensor maps, some stages ahead; the other four take sixteen
 // tokens of a tile each: codes leave shared memory through ldmatrix (keys as they lie, values transposed two dimensions at a time),
@@ -18,7 +18,7 @@
 // Roundings: a query row is scaled by a power of two to 2^14 before it becomes fp16 (no bits of bf16 are lost above 2^-28 of the row's
 // maximum).  A block's value scale goes into p: the running maximum is that of log2(p) + log2(scale), raised only when it grows by more
 // than 2^4, and p scale enters the second product in fp16, eleven bits, at most 2^15, so that it stays normal down to 2^-25 of the
-// largest; the sum of p takes the scale out again.
+// largest; the sum of p takes the scale out again (attend.h says how far that goes).
 // Measured, calls in a graph: 64 sequences of 700 to 32768 tokens, 32 query over 8 cache heads of 128 (1.1 GB) 184 us = 6.0 TB/s; one of 131000
 // tokens over 4 cache heads 35 us = 3.8 TB/s (start, and 111 parts a group to join); 16 sequences with five rows each, 20 rows a cache head, 65 us =
 // 1.8 TB/s: there the products, in eight warps an SM, bound it.  32 sequences that see 1000 tokens each: 13.7 us, start and join.
@@ -402,12 +402,12 @@ __device__ __noinline__ void sum_apart(const float* x, float v_log, bool apart, 
     float sum = 0.0f, was = 0.0f;
     const float from = apart ? r : x[24];
     float now = from;
-#pragma unroll 1
+#pragma unroll
     for (int k = 0; k < 16; ++k) now = fmaxf(now, x[k] - v_log);
     const float base = kTop - (now == -INFINITY ? 0.0f : now);
-#pragma unroll 1
+#pragma unroll
     for (int k = 0; k < 16; ++k) sum += exp2_of(x[k] - v_log + base);
-#pragma unroll 1
+#pragma unroll
     for (int k = 16; k < 24; ++k) was += x[k];
     l = -fmaf(apart ? -l : was, now == -INFINITY ? 1.0f : exp2_of(from - now), sum);
     r = now;

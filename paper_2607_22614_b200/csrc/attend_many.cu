@@ -334,38 +334,41 @@ __device__ __forceinline__ void convert(const AttendArgs& a, Shared<D>& s, const
     drain(values, used, v_empty, &s.limit, &g_wait_failures);
 }
 
+// The lowest n of sixteen bits; none for n <= 0.
+__device__ __forceinline__ uint32_t low_bits(int n) { return (1u << min(max(n, 0), 16)) - 1; }
 // One step's part of a row's sum of p with exponentials of its own: r is the largest logit so far, l the sum relative to 2^r.  (The logits are read
 // from tensor memory anew, sixteen at a time, before the step needs its registers: with the 64 that it has loaded a prompt that
 // never comes here takes 6 % longer.)
 __device__ __forceinline__ void sum_apart(const AttendArgs& a, const Meta& meta, uint32_t at, int odd, float back, int p, float& r, float& l)
 {
-    float now = r, sum = 0.0f;
+    float now = r, all = l;
 #pragma unroll 1
-    for (int pass = 0; pass < 2; ++pass) {
-        const float base = kTop - (now == -INFINITY ? 0.0f : now);
-#pragma unroll 1
-        for (int g = 0; g < (int)kStepGroups; ++g) {
-            float v[16];
-            asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];\n"
-                         "tcgen05.wait::ld.sync.aligned;"
-                         : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]), "=f"(v[8]), "=f"(v[9]), "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15])
-                         : "r"(at + 16 * g)
-                         : "memory");
-            const int of = odd * (int)kStepGroups + g, t0 = (int)meta.token + 16 * of;
-            const bool held = meta.held >> of & 1;
-            const float f = fmaxf(back * meta.k_scale[of], 1.2e-38f);
+    for (int g = 0; g < (int)kStepGroups; ++g) {
+        float v[16];
+        asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];\n"
+                     "tcgen05.wait::ld.sync.aligned;"
+                     : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]), "=f"(v[8]), "=f"(v[9]), "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15])
+                     : "r"(at + 16 * g)
+                     : "memory");
+        const int of = odd * (int)kStepGroups + g, t0 = (int)meta.token + 16 * of;
+        const float f = fmaxf(back * meta.k_scale[of], 1.2e-38f);
+        const int far = p - (int)a.window;  // (from 1 - 2^31 on)
+        uint32_t seen = meta.held >> of & 1 ? low_bits(p - t0 + 1) : 0;
+        if (a.window && far >= t0) seen &= ~low_bits(far - t0 + 1) | low_bits((int)a.sinks - t0);
+        float top[2] = {-INFINITY, -INFINITY}, sum[2] = {0.0f, 0.0f};
 #pragma unroll
-            for (int k = 0; k < 16; ++k) {
-                const int t = t0 + k;
-                if (!held || t > p || (a.window && t <= p - (int)a.window && t >= (int)a.sinks)) continue;
-                if (pass)
-                    sum += exp2_of(fmaf(v[k], f, base));
-                else
-                    now = fmaxf(now, v[k] * f);
-            }
+        for (int k = 0; k < 16; ++k) {
+            if (!(seen >> k & 1)) v[k] = -INFINITY;
+            top[k & 1] = fmaxf(top[k & 1], v[k]);
         }
+        const float was = now;
+        now = fmaxf(now, fmaxf(top[0], top[1]) * f);
+        const float base = kTop - (now == -INFINITY ? 0.0f : now);
+#pragma unroll
+        for (int k = 0; k < 16; ++k) sum[k & 1] += exp2_of(fmaf(v[k], f, base));
+        all = fmaf(all, now == -INFINITY ? 1.0f : exp2_of(was - now), sum[0] + sum[1]);
     }
-    l = fmaf(l, now == -INFINITY ? 1.0f : exp2_of(r - now), sum);
+    l = all;
     r = now;
 }
 

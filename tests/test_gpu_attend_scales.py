@@ -89,6 +89,20 @@ def test_scales_over_their_whole_range(added, dim):
         check(q, cache, table, lengths, offsets)
 
 
+@pytest.mark.parametrize("rows", [1, 3, 6, 14])
+def test_parts_of_many_groups(rows):
+    """Groups of eight, sixteen and 24 rows of which several CTAs have parts, some with sums of their own and some without."""
+    lengths = [600 + 17 * i for i in range(60)]
+    added = [rows] * 60
+    q, cache, table, offsets = setup(11, lengths, added, 32)
+    for r in range(60):
+        if r % 3:
+            without_values(cache, table[r, r % 7:-(-lengths[r] // 32):1 + r % 5].long())
+    cache[3][table[::4, 2].long()] = 2.0 ** 60
+    check(q, cache, table, lengths, offsets)
+    check(q, cache, table, lengths, offsets, window=300, sinks=40)
+
+
 @pytest.mark.parametrize("added", [[1], [6], [150]])
 def test_scales_that_are_no_powers_of_two(added):
     q, cache, table, offsets = setup(4, [400], added, 32)
