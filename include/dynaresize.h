@@ -639,7 +639,8 @@ int dr_diag_linear_waits(uint32_t limit_us, uint32_t starve);
  * and v_scale [n_blocks, kv_heads]; a value is its code times its block's scale.  dr_qk_append writes scales that are
  * powers of two, the smallest 2^e >= 2^-100 with every finite magnitude of the block within 448 * 2^e: when a later token makes
  * the scale grow, the codes that the block holds are shifted to it (rounded once more only below 2^-6 of the new scale).
- * Scales that a caller brings may be any finite ones that are not negative.
+ * Scales that a caller brings may be any finite ones that are not negative; dr_qk_append into a block that has one which is no power of two keeps it, or
+ * rounds the codes that the block holds once more.
  * A token with an infinity or a NaN in its key or value of a head is kept as one: the NaN code 0x7F in the first place of its key,
  * zeros in the places that were not finite; queries that see it get NaN, others nothing of it.  Codes of values that attention
  * may see hold no NaN code.
@@ -674,9 +675,12 @@ int dr_kv_cache_destroy(dr_kv_cache* cache); /* NULL is accepted; launches alrea
  *   positions : rows int32, each row's position in its request; -1 for rows of refused requests and behind the last request
  *   runs      : n_runs x 4 int32 {block, first slot in it, first row, rows}: where the new rows go, run by run, in the order of the
  *               rows; unused entries are {-1, 0, 0, 0}.  n_runs >= min(rows, rows / block_tokens + 2 * requests), or DR_ERR_SIZE.
- * A request is refused (its length and table stay, its rows get position -1, no run holds them) when the blocks do not suffice
+ * A request is refused (its length and table stay, its rows get position -1, no run holds them; dr_qk_append leaves their queries as they were,
+ * and dr_attend, which is given no positions, makes rows without meaning of them) when the blocks do not suffice
  * for it and all requests before it, or when its tokens do not fit the table's width or the step's rows.  One launch; nothing is read on
- * the host, so the step can be captured.  Lengths, counts and states out of range are held inside it.  Arrays other than those
+ * the host, so the step can be captured.  Every block belongs to one
+ * request: one that two rows of the table share comes back twice.  Lengths shrink only where requests end; a caller that lowers one (drafts that were
+ * rejected) itself puts the blocks behind its new last token on the free list, or keeps as many, or else they are lost.  Lengths, counts and states out of range are held inside it.  Arrays other than those
  * named may not overlap.  Errors: DR_ERR_INVALID, DR_ERR_UNSUPPORTED (2^24 requests, 2^30 rows, 2^24 blocks a
  * request), DR_ERR_SIZE, DR_ERR_ALIGN (a pointer off 4 bytes, runs off 16), DR_ERR_STATE (another current device), DR_ERR_CUDA.
  */
@@ -689,7 +693,8 @@ int dr_kv_extend(const dr_kv_cache* cache, const int32_t* added, const int32_t* 
  * heads, n_kv_heads key heads, n_kv_heads value heads of head_dim (64 or 128) each.  For query and key heads
  *   n = x / sqrt(mean(x^2) + eps) * w      (w: q_norm or k_norm; both NULL: n = x)
  *   y[i] = n[i] cos a - n[i + d/2] sin a,  y[i + d/2] = n[i + d/2] cos a + n[i] sin a,  a = position * base^(-2 i / d), i < d/2
- * in fp32, angles exact to 2^-32 of a turn at any position.  Rows of negative position are left as they were.
+ * in fp32, angles exact to 2^-32 of a turn at any position and then rounded to fp32 (2^-28 of a turn at most).  Rows of negative position are
+ * left as they were, in y as in dx.
  * The handle keeps the norms' pointers (norm_dtype DR_BF16 or DR_F32).
  */
 typedef struct dr_qk_desc {
@@ -714,7 +719,7 @@ int dr_qk_destroy(dr_qk* qk);
  *               skipped where its block, slots or rows lie outside the cache or the step.  Two runs of one call must not share a block.
  *               Slots before the run's first one keep their values; those behind its last one are left as they were.
  * dr_qk_grad    -- dy: gradients of dr_qk_forward's y, x its input; dx in the same layout (may be dy itself), and where the
- *               handle has norms their gradients dq_norm, dk_norm (head_dim fp32 each; accumulate = 1 adds).  The sums are taken in a
+ *               handle has norms their gradients dq_norm, dk_norm (head_dim fp32 each; accumulate = 1 adds).  The sums are fp32, in a
  *               fixed order.  work: dr_qk_grad_work's bytes of device memory that no other call uses meanwhile, 16-byte aligned.
  * All enqueue on cuda_stream, allocate nothing, read nothing on the host, may be captured.  rows = 0 does nothing (dr_qk_grad without
  * accumulate: writes zeros).  16-byte aligned bases and rows take vector accesses, others element-wise ones, same result.
@@ -741,8 +746,11 @@ int dr_qk_grad(const dr_qk* qk, const void* x_dev, uint32_t dtype, uint64_t ldx,
  *   work    : dr_attend_work's bytes of device memory that no other call uses meanwhile, 16-byte aligned; none is needed (NULL, 0) where the
  *             table's width holds at most 512 tokens
  * out must not overlap q.  A row that sees nothing gets zeros, one that is not finite NaN.  Rows that no request owns are left as they were.  Lengths beyond the table's width or
- * 2^31 - 1 and offsets beyond the rows are held inside.  Sums are fp32; which tokens are summed together depends on all lengths of the call, in a
- * fixed order: the same call gives the same bits.
+ * 2^31 - 1 and offsets beyond the rows are held inside.  Logits, maxima and sums are fp32; which tokens are summed together depends on all lengths of
+ * the call, in a fixed order: the same call gives the same bits.  Held in fewer bits on the way: p times its block's value scale in the second product, as
+ * fp16 relative to the row's largest such product (eleven bits, and 2^-36 of the largest below 2^-25 of it; the sum of p is of values before that); a query, for
+ * requests of more than 64 rows times query heads of a cache head as the sum of two e4m3 codes (exact above 2^-17 of the row's largest value), for
+ * others as fp16 (2^-28); exponentials are off by up to 2^-18.5.  out is rounded once.
  * Enqueues on cuda_stream, allocates nothing, reads nothing on the host, may be captured.  The waits inside are bounded as the linear
  * layers' are, and counted by dr_diag_linear_wait_failures.
  * Errors: DR_ERR_INVALID (NULL, leading dimensions, n_q_heads no multiple of kv_heads, window below 0, scale not finite),

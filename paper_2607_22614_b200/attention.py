@@ -98,7 +98,8 @@ class KVCache:
                runs=None, stream=None):
         """dr_kv_extend: one step's block table, positions and runs of slots from the requests' lengths, all on the GPU.  added, lengths
         [requests], table [requests, width], free [blocks], state [2] (free blocks, requests refused) are int32; lengths and state are
-        updated in place unless lengths_out and state_out are given; rows: the step's rows.  Returns (offsets [requests + 1],
+        updated in place unless lengths_out and state_out are given; rows: the step's rows.  Rows of refused requests have position -1, and
+        what attend makes of them has no meaning.  A length lowered by hand loses blocks, unless they are put on the free list.  Returns (offsets [requests + 1],
         positions [rows], runs [runs_for(requests, rows), 4])."""
         device = self.device
         if device != B._current_device():
@@ -267,7 +268,8 @@ class QKHeads:
 
     def append(self, x, positions, runs, cache, out=None, stream=None):
         """dr_qk_append: x [rows, (query + 2 key-value heads) * head_dim] -> the query heads, normed and rotated ([rows, query heads *
-        head_dim], `out` may be x's own columns); keys, normed and rotated, and values go into `cache` at `runs` (KVCache.extend)."""
+        head_dim], `out` may be x's own columns); keys, normed and rotated, and values go into `cache` at `runs` (KVCache.extend).  Rows of
+        negative position are left as they are (of an allocated output: not initialised)."""
         rows, ldx, code = self._rows(x, self.n_q_heads + 2 * self.n_kv_heads, "x")
         y, ldy = self._out(out, rows, self.n_q_heads, x, "out", stream)
         if cache.device != self.device:
@@ -281,7 +283,8 @@ class QKHeads:
 
     def grad(self, x, positions, dy, dx=None, dq_norm=None, dk_norm=None, accumulate=False, stream=None):
         """dr_qk_grad: gradients of forward at x for dy [rows, (query + key heads) * head_dim] of x's type: (dx, dq_norm, dk_norm), the norms'
-        in fp32 (None without norms; accumulate adds them to the ones given).  `dx` may be dy."""
+        in fp32 (None without norms; accumulate adds them to the ones given).  `dx` may be dy.  Rows of negative position add nothing to the
+        norms' gradients and are left as they are in dx (allocated: not initialised)."""
         import torch
         heads = self.n_q_heads + self.n_kv_heads
         rows, ldx, code = self._rows(x, heads, "x", record=False)

@@ -72,7 +72,7 @@ __device__ __forceinline__ Tiles tiles_of(const AttendArgs& a, int p_lo, int p_h
 }
 
 // Requests of up to this many rows (tokens times query heads of a cache head) go to the few-row kernel, which reads the cache once for
-// each sixteen of them; the others to the tensor cores, 256 rows a CTA.
+// each eight, sixteen or twenty-four of them; the others to the tensor cores, 256 rows a CTA.
 constexpr uint32_t kFewRows = 64;
 
 int launch_attend_many(const dr_kv_cache* cache, const AttendArgs& a, cudaStream_t stream);

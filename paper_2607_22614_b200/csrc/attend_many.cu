@@ -13,13 +13,14 @@
 // cycle), products and the shared memory's reads for them would each take some 2100 to 2600 cycles for 128 tokens: what bounds it is how well
 // they overlap.
 //
-// As in the few-row kernel the running maximum is that of log2(p) + log2(value scale); O is multiplied anew only when it grows by more than
+// As in the few-row kernel the running maximum is that of log2(p) + log2(value scale) (attend.h); O is multiplied anew only when it grows by more than
 // 2^4, so that p scale in fp16 is at most 2^15 and normal down to 2^-25 of the largest.
 //
 // Warps: 0-3 and 4-7 the exponentials of the two halves, 8-11 the values' codes, 12 the copies, 14 and 15 the products of the halves.
 // CTAs are started in the order of their number: the longest request first, and a request's last rows, which see the most tokens, first.
-// Measured: a tile 2.11 us, a CTA's start and end some 6; a prompt of 8192 tokens, 32 query over 8 cache heads of 128: 560 us = 980 TFLOP/s (a
-// library product of 8192^3: 1694); 3501 and 4500 tokens, these behind 4501 others: 646 us in a graph, 676 a pass (926 and 885).
+// Measured: a tile 2.11 us, a CTA's start and end some 6; a prompt of 8192 tokens, 32 query over 8 cache heads of 128: 571 us = 960 TFLOP/s (a
+// library product of 8192^3: 1694; with half of the blocks without values 949 us); 3501 and 4500 tokens, these behind 4501 others: 619 to 655 us
+// in a graph, 690 a pass among other inputs (966 to 913 and 867).
 #include "attend.h"
 #include "linear.h"
 #include "tc_ptx.cuh"
